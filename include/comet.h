@@ -298,6 +298,99 @@ const char *comet_status_string(comet_status s);
  * For testing and measurement; results are the same up to summation order. */
 comet_status comet_tensor_set_variant(comet_tensor *t, int variant);
 
+/* ---------------------------------------------------------------------------------------------------
+ * Dense rows over a vocabulary and their sparse top part: what a model's output layer is trained and
+ * read with.  The sparse side is the level storage above -- a row's kept logits are a compressed level,
+ * pos / crd / vals -- but it changes with every call, so these operations take the arrays themselves
+ * instead of a handle and plan nothing.
+ *
+ *   Z      device, N rows of V elements of `type`, row r at element r * ldz (ldz >= V); an element's
+ *          neighbours in a row are its neighbours in memory.  Z is aligned to its element; rows may start
+ *          anywhere (16-byte loads are used inside of a row, whatever its start).
+ *   work   device scratch of at least the bytes that the matching _work call states, 16-byte aligned, in
+ *          use until the call's work on `stream` is done (NULL where that is 0).  Nothing in it has to be
+ *          cleared or kept.
+ * Sums and logarithms of sums are held in 32 bits or more.  No call allocates or synchronises, and all can be captured into a
+ * HIP graph.  Coordinates, positions and lengths beyond 2^31 bytes or elements are computed in 64 bits; V < 2^31, N <= 2^23.
+ * Errors of all of them: COMET_ERR_INVALID_ARG (null pointer, negative size, misaligned pointer, flag, scale not finite and
+ * positive, work too small), COMET_ERR_SHAPE (ldz < V), COMET_ERR_UNSUPPORTED (a size beyond the stated limits). */
+typedef enum { COMET_F32 = 0, COMET_BF16 = 1, COMET_F16 = 2 } comet_type_t;
+
+/* The K largest elements of every row: a dense row as the compressed level of its largest elements.
+ *   crd, vals  device, [N x K]: coordinates and values (as 32 bits) of the kept elements, largest first; of equal ones the lower
+ *              coordinate comes first and is kept first (-0 equals 0).  With COMET_BY_COORDINATE a row's entries are in the order of
+ *              their coordinates, so that crd and vals with pos = {0, K, 2K, ..} are a [D,CU] matrix.  An element that is -inf
+ *              (a masked place) or NaN is no entry; where a row has fewer than K, the places at its end hold -1 and -inf.
+ *   lse        device, [N], may be NULL: log sum_j exp(scale z_rj) over the whole row; -inf for a row without an element
+ *              over -inf, +inf with a +inf in it, NaN with a NaN.
+ *   K          1 <= K <= COMET_MAX_TOP. */
+#define COMET_BY_COORDINATE 1u
+#define COMET_MAX_TOP 1024
+comet_status comet_rows_topk_work(comet_type_t type, int64_t N, int64_t V, int64_t K, int64_t *bytes /* host */);
+comet_status comet_rows_topk(const void *Z, comet_type_t type, int64_t N, int64_t V, int64_t ldz, double scale, int64_t K,
+                             unsigned flags, int32_t *crd, float *vals, float *lse, void *work, int64_t work_bytes,
+                             void *stream);
+
+/* Distillation: how far the distribution that dense logits give is from a teacher's, of which the top logits are known.
+ * With x = scale z_r, q = softmax(x), the row's entries (c, t) and a = scale t:
+ *     without tlse   p_c = exp(a) / sum exp(a) over the row's entries,   rest = 0
+ *     with tlse      p_c = exp(a - tlse_r),   rest = 1 - sum p (0 if that is below 2^-20, which 32-bit inputs do not resolve):
+ *                    the teacher's mass outside of what it kept counts as one more outcome, with the student's mass there
+ *     loss_r = weight_r (sum_c p_c (log p_c - log q_c) + rest (log rest - log sum of q outside of the entries))
+ *   pos        device, [N + 1], or NULL: entries of row r are pos[r] .. pos[r+1]-1.  NULL: K entries each, row r from r * K.
+ *   crd, tvals device: coordinates (distinct in a row, in any order) and teacher logits.  An entry whose coordinate is outside
+ *              of [0, V) is skipped (comet_rows_topk marks missing ones with -1).
+ *   tlse       device, [N], or NULL: log sum exp(scale t) over the teacher's whole row (comet_rows_topk's lse, of its scale).
+ *   scale      1 / temperature, the same for both sides.
+ *   weight     device, [N], or NULL (all 1).  A row of weight 0 is not read: its loss is 0 and its gradient 0 whatever it holds.
+ *   loss       device, [N].
+ *   stat       device, [N x COMET_DISTILL_STAT]: what the backward call needs of the forward call with the same arguments.
+ *   dloss      device, [N], or NULL (all 1): the derivative by each row's loss.
+ *   dZ         device, of Z's type, rows at r * lddz (lddz >= V): sum of dloss_r loss_r by every z, rounded to the type once.
+ *              dZ may be Z itself (lddz == ldz), which is then overwritten; otherwise the two must not overlap.
+ * comet_distill_step is the forward and the backward call (dloss all 1) in one, without a stat.
+ * Where the row's distribution is empty: no entry with a probability and no rest gives loss 0 and gradient 0.  A place of Z that
+ * is -inf has q = 0; where the teacher gives it mass the loss is +inf, and the gradient still finite (q - p).  NaN and +inf
+ * in a row of Z, a row's tvals, tlse or weight make that row's loss and gradient NaN, and no other row's. */
+#define COMET_DISTILL_STAT 7
+comet_status comet_distill_work(comet_type_t type, int64_t N, int64_t V, int64_t *bytes /* host */);
+comet_status comet_distill_forward(const void *Z, comet_type_t type, int64_t N, int64_t V, int64_t ldz, const int32_t *pos, int64_t K,
+                                   const int32_t *crd, const float *tvals, const float *tlse, double scale, const float *weight,
+                                   float *loss, double *stat, void *work, int64_t work_bytes, void *stream);
+comet_status comet_distill_backward(const void *Z, comet_type_t type, int64_t N, int64_t V, int64_t ldz, const int32_t *pos, int64_t K,
+                                    const int32_t *crd, const float *tvals, const float *tlse, double scale, const float *weight,
+                                    const double *stat, const float *dloss, void *dZ, int64_t lddz, void *stream);
+comet_status comet_distill_step(const void *Z, comet_type_t type, int64_t N, int64_t V, int64_t ldz, const int32_t *pos, int64_t K,
+                                const int32_t *crd, const float *tvals, const float *tlse, double scale, const float *weight,
+                                float *loss, void *dZ, int64_t lddz, void *work, int64_t work_bytes, void *stream);
+
+/* Beam search's selection.  Batch b has W beams; beam w has the score c_bw (log probability so far) and the logits in row
+ * b * W + w of Z.  A candidate (w, v) has the score c_bw + z_v - log sum_j exp(z_j).  The n candidates with the largest scores
+ * of a batch are returned, largest first; of equal ones the lower beam comes first, then the larger logit (two logits of a beam
+ * can round to one score), then the lower token.  Scores are compared in 64 bits and rounded to 32 when they are stored.
+ *   score      device, [B x W].
+ *   finished   device, [B x W] bytes, or NULL: a beam with a byte that is not 0 has ended; its row is not read, and it
+ *              has one candidate, `eos` with the score c_bw.
+ *   out_score, out_parent, out_token   device, [B x n]: score, beam and token of each selected candidate.
+ *              A candidate whose score is -inf or NaN is none (masked tokens, beams that are not in use); where a batch has fewer than
+ *              n, the places at its end hold -inf, -1 and -1.
+ *   1 <= W <= COMET_MAX_BEAMS, 1 <= n <= COMET_MAX_TOP, W * n <= 8192, V < 2^24. */
+#define COMET_MAX_BEAMS 256
+comet_status comet_beam_select_work(comet_type_t type, int64_t B, int64_t W, int64_t V, int64_t n, int64_t *bytes /* host */);
+comet_status comet_beam_select(const void *Z, comet_type_t type, int64_t B, int64_t W, int64_t V, int64_t ldz, const float *score,
+                               const uint8_t *finished, int32_t eos, int64_t n, float *out_score, int32_t *out_parent,
+                               int32_t *out_token, void *work, int64_t work_bytes, void *stream);
+
+/* The beams' states follow the selection: state (b, w) becomes what state (b, parent[b, w]) was, in place, for every listed
+ * array.  Beams that are their own parent are neither read for themselves nor written.
+ *   states     host array of nstates device pointers to arrays of one layout: the part of beam (b, w) that moves is
+ *              `outer` pieces of `inner` bytes, piece o at byte b * batch_stride + w * beam_stride + o * outer_stride.
+ *              No two pieces may overlap (COMET_ERR_INVALID_ARG where the strides say so).
+ *   parent     device, [B x W]; a value outside of [0, W) leaves the beam as it is (comet_beam_select's -1).
+ *   1 <= W <= COMET_MAX_BEAMS. */
+comet_status comet_beam_reorder(void *const *states, int64_t nstates, int64_t B, int64_t W, int64_t batch_stride, int64_t beam_stride,
+                                int64_t outer, int64_t outer_stride, int64_t inner, const int32_t *parent, void *stream);
+
 /* Calibration of the device's memory system, for the benchmark (no tensor involved): the two access
  * patterns the operations are made of, timed by the caller.
  *   comet_calibrate_read    streams n doubles (n >= 2, data 16-byte aligned) once through the device.

@@ -21,6 +21,9 @@ COMET_D, COMET_CU, COMET_CN, COMET_S = 0, 1, 2, 3
 COMET_BORROW, COMET_COPY, COMET_VALIDATE, COMET_LEAN = 0, 1, 2, 4
 COMET_OK = 0
 COMET_MAX_ORDER = 4
+COMET_F32, COMET_BF16, COMET_F16 = 0, 1, 2
+COMET_BY_COORDINATE = 1
+COMET_MAX_TOP, COMET_MAX_BEAMS, COMET_DISTILL_STAT = 1024, 256, 7
 
 _STATUS_NAMES = {0: "COMET_OK", 1: "COMET_ERR_INVALID_ARG", 2: "COMET_ERR_BAD_FORMAT", 3: "COMET_ERR_SHAPE",
                  4: "COMET_ERR_UNSUPPORTED", 5: "COMET_ERR_ALLOC", 6: "COMET_ERR_DEVICE"}
@@ -29,7 +32,8 @@ EXPORTS = ["comet_tensor_create", "comet_tensor_destroy", "comet_tensor_info", "
            "comet_ttv", "comet_ttm", "comet_mttkrp", "comet_status_string", "comet_tensor_set_variant",
            "comet_tensor_reorder", "comet_tensor_convert", "comet_tensor_reserve", "comet_spmv_static",
            "comet_calibrate_read", "comet_calibrate_gather", "comet_spmv_axpby", "comet_spmm_axpby",
-           "comet_mttkrp_axpby"]
+           "comet_mttkrp_axpby", "comet_rows_topk_work", "comet_rows_topk", "comet_distill_work", "comet_distill_forward",
+           "comet_distill_backward", "comet_distill_step", "comet_beam_select_work", "comet_beam_select", "comet_beam_reorder"]
 
 
 class CometError(RuntimeError):
@@ -85,6 +89,17 @@ def _lib():
         lib.comet_tensor_set_variant.argtypes = [vp, ci]
         lib.comet_tensor_reorder.argtypes = [vp, vp, ctypes.POINTER(vp), vp]
         lib.comet_tensor_convert.argtypes = [vp, vp, vp, ctypes.POINTER(vp), vp]
+        pi64 = ctypes.POINTER(i64)
+        lib.comet_rows_topk_work.argtypes = [ci, i64, i64, i64, pi64]
+        lib.comet_rows_topk.argtypes = [vp, ci, i64, i64, i64, f64, i64, ctypes.c_uint, vp, vp, vp, vp, i64, vp]
+        lib.comet_distill_work.argtypes = [ci, i64, i64, pi64]
+        rows = [vp, ci, i64, i64, i64, vp, i64, vp, vp, vp, f64, vp]
+        lib.comet_distill_forward.argtypes = rows + [vp, vp, vp, i64, vp]
+        lib.comet_distill_backward.argtypes = rows + [vp, vp, vp, i64, vp]
+        lib.comet_distill_step.argtypes = rows + [vp, vp, i64, vp, i64, vp]
+        lib.comet_beam_select_work.argtypes = [ci, i64, i64, i64, i64, pi64]
+        lib.comet_beam_select.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ctypes.c_int32, i64, vp, vp, vp, vp, i64, vp]
+        lib.comet_beam_reorder.argtypes = [vp, i64, i64, i64, i64, i64, i64, i64, i64, vp, vp]
         lib.comet_status_string.argtypes = [ci]
         lib.comet_status_string.restype = ctypes.c_char_p
         for n in EXPORTS:
@@ -446,3 +461,203 @@ def comet_mttkrp_axpby(X: Tensor, mode: int, alpha: float, factors: Sequence[Opt
 def from_levels(T, flags: int = COMET_VALIDATE, stream=None) -> Tensor:
     """Create a handle from a synth.LevelTensor-like object (dims, tags, pos, crd, vals on the GPU)."""
     return comet_tensor_create(T.dims, T.tags, T.pos, T.crd, T.vals, flags, stream)
+
+
+# ---- dense rows over a vocabulary and their sparse top part -------------------------------------------------------------
+_TYPES = {torch.float32: COMET_F32, torch.bfloat16: COMET_BF16, torch.float16: COMET_F16}
+
+
+def _rows(Z: torch.Tensor, what: str = "Z"):
+    """(pointer, type, rows, columns, distance of rows) of a matrix whose rows may lie apart but not its columns."""
+    if not isinstance(Z, torch.Tensor) or not Z.is_cuda:
+        raise TypeError("%s must be a torch tensor in device memory" % what)
+    if Z.dtype not in _TYPES:
+        raise TypeError("%s must have dtype float32, bfloat16 or float16, got %s" % (what, Z.dtype))
+    if Z.dim() != 2:
+        raise ValueError("%s must have two dimensions" % what)
+    (N, V), (ld, step) = Z.shape, Z.stride()
+    if (step != 1 and V > 1) or (ld < V and N > 1):
+        raise ValueError("%s must have its columns next to each other and rows that do not overlap" % what)
+    return Z.data_ptr(), _TYPES[Z.dtype], N, V, ld if N > 1 else V
+
+
+def _given(t: Optional[torch.Tensor], dtype, shape, what: str, device) -> Optional[torch.Tensor]:
+    """An operand of a stated shape on the same device as the others."""
+    if t is None:
+        return None
+    _dev(t, dtype, what)
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must have shape %s, got %s" % (what, shape, tuple(t.shape)))
+    if t.device != device:
+        raise ValueError("%s must be on %s" % (what, device))
+    return t
+
+
+def _new(t: Optional[torch.Tensor], dtype, shape, what: str, device, stream) -> torch.Tensor:
+    """A result: the caller's tensor, or a new one, which other streams than the current one are told about."""
+    if t is not None:
+        return _given(t, dtype, shape, what, device)
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _work(need: int, device, stream):
+    """(tensor, pointer) of scratch for one call: its memory goes back to torch's allocator, which keeps it for the stream."""
+    if need == 0:
+        return None, None
+    t = _new(None, torch.uint8, (need,), "work", device, stream)
+    return t, t.data_ptr()
+
+
+def comet_rows_topk(Z: torch.Tensor, K: int, scale: float = 1.0, by_coordinate: bool = False, crd: Optional[torch.Tensor] = None,
+                    vals: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None):
+    """(crd, vals, lse): the K largest elements of every row of Z and log sum exp(scale * row)."""
+    ptr, kind, N, V, ld = _rows(Z)
+    K, dev = int(K), Z.device
+    need = ctypes.c_int64(0)
+    _check(_lib().comet_rows_topk_work(kind, N, V, K, ctypes.byref(need)), "comet_rows_topk")
+    crd = _new(crd, torch.int32, (N, K), "crd", dev, stream)
+    vals = _new(vals, torch.float32, (N, K), "vals", dev, stream)
+    lse = _new(lse, torch.float32, (N,), "lse", dev, stream)
+    work, wptr = _work(need.value, dev, stream)
+    _check(_lib().comet_rows_topk(ptr, kind, N, V, ld, float(scale), K, COMET_BY_COORDINATE if by_coordinate else 0, crd.data_ptr(),
+                                  vals.data_ptr(), lse.data_ptr(), wptr, need.value, _stream(stream)), "comet_rows_topk")
+    return crd, vals, lse
+
+
+def _teacher(Z, crd, tvals, pos, tlse, scale, weight):
+    """The arguments that the three distillation calls share."""
+    ptr, kind, N, V, ld = _rows(Z)
+    dev = Z.device
+    if pos is None:
+        if not isinstance(crd, torch.Tensor) or crd.dim() != 2:
+            raise ValueError("crd must be an [N, K] matrix where there is no pos")
+        K, shape = crd.shape[1], (N, crd.shape[1])
+    else:
+        _given(pos, torch.int32, (N + 1,), "pos", dev)
+        if not isinstance(crd, torch.Tensor) or crd.dim() != 1:
+            raise ValueError("crd must have one dimension where there is a pos")
+        K, shape = 0, tuple(crd.shape)
+    _given(crd, torch.int32, shape, "crd", dev)
+    _given(tvals, torch.float32, shape, "tvals", dev)
+    _given(tlse, torch.float32, (N,), "tlse", dev)
+    _given(weight, torch.float32, (N,), "weight", dev)
+    return N, V, kind, dev, (ptr, kind, N, V, ld, _ptr(pos), K, _ptr(crd), _ptr(tvals), _ptr(tlse), float(scale), _ptr(weight))
+
+
+def comet_distill_forward(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                          tlse: Optional[torch.Tensor] = None, scale: float = 1.0, weight: Optional[torch.Tensor] = None,
+                          loss: Optional[torch.Tensor] = None, stat: Optional[torch.Tensor] = None, stream=None):
+    """(loss, stat): the loss of every row, and what comet_distill_backward needs of it."""
+    N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
+    need = ctypes.c_int64(0)
+    _check(_lib().comet_distill_work(kind, N, V, ctypes.byref(need)), "comet_distill_forward")
+    loss = _new(loss, torch.float32, (N,), "loss", dev, stream)
+    stat = _new(stat, torch.float64, (N, COMET_DISTILL_STAT), "stat", dev, stream)
+    work, wptr = _work(need.value, dev, stream)
+    _check(_lib().comet_distill_forward(*args, loss.data_ptr(), stat.data_ptr(), wptr, need.value, _stream(stream)), "comet_distill_forward")
+    return loss, stat
+
+
+def _gradient(Z, dZ, stream):
+    if dZ is None:
+        dZ = _new(None, Z.dtype, tuple(Z.shape), "dZ", Z.device, stream)
+    elif dZ.dtype != Z.dtype or dZ.shape != Z.shape or dZ.device != Z.device:
+        raise ValueError("dZ must have Z's shape, dtype and device")
+    ptr, _, _, _, ld = _rows(dZ, "dZ")
+    return dZ, ptr, ld
+
+
+def comet_distill_backward(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tensor, stat: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                           tlse: Optional[torch.Tensor] = None, scale: float = 1.0, weight: Optional[torch.Tensor] = None,
+                           dloss: Optional[torch.Tensor] = None, dZ: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """dZ, which may be Z itself: the gradient of sum(dloss * loss) by Z, from the stat of the forward call with the same arguments."""
+    N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
+    _given(stat, torch.float64, (N, COMET_DISTILL_STAT), "stat", dev)
+    _given(dloss, torch.float32, (N,), "dloss", dev)
+    dZ, out, ldo = _gradient(Z, dZ, stream)
+    _check(_lib().comet_distill_backward(*args, _ptr(stat), _ptr(dloss), out, ldo, _stream(stream)), "comet_distill_backward")
+    return dZ
+
+
+def comet_distill_step(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tensor, pos: Optional[torch.Tensor] = None,
+                       tlse: Optional[torch.Tensor] = None, scale: float = 1.0, weight: Optional[torch.Tensor] = None,
+                       loss: Optional[torch.Tensor] = None, dZ: Optional[torch.Tensor] = None, stream=None):
+    """(loss, dZ): both at once, for a training step that knows its rows' weights; dZ may be Z itself."""
+    N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
+    need = ctypes.c_int64(0)
+    _check(_lib().comet_distill_work(kind, N, V, ctypes.byref(need)), "comet_distill_step")
+    loss = _new(loss, torch.float32, (N,), "loss", dev, stream)
+    dZ, out, ldo = _gradient(Z, dZ, stream)
+    work, wptr = _work(need.value, dev, stream)
+    _check(_lib().comet_distill_step(*args, loss.data_ptr(), out, ldo, wptr, need.value, _stream(stream)), "comet_distill_step")
+    return loss, dZ
+
+
+def comet_beam_select(Z: torch.Tensor, score: torch.Tensor, n: int, finished: Optional[torch.Tensor] = None, eos: int = 0, stream=None):
+    """(score, parent, token), each [B, n]: the best continuations of every batch's beams.  Z: [B, W, V] logits."""
+    if not isinstance(Z, torch.Tensor) or Z.dim() != 3:
+        raise ValueError("Z must have three dimensions")
+    B, W, V = Z.shape
+    if B > 1 and W > 1 and Z.stride(0) != W * Z.stride(1):
+        raise ValueError("Z must have its batches' rows at one distance")
+    ptr, kind, _, _, ld = _rows(Z.flatten(0, 1))
+    n, dev = int(n), Z.device
+    _given(score, torch.float32, (B, W), "score", dev)
+    if finished is not None:
+        if isinstance(finished, torch.Tensor) and finished.dtype == torch.bool:
+            finished = finished.view(torch.uint8)
+        _given(finished, torch.uint8, (B, W), "finished", dev)
+    need = ctypes.c_int64(0)
+    _check(_lib().comet_beam_select_work(kind, B, W, V, n, ctypes.byref(need)), "comet_beam_select")
+    best = _new(None, torch.float32, (B, n), "score", dev, stream)
+    parent = _new(None, torch.int32, (B, n), "parent", dev, stream)
+    token = _new(None, torch.int32, (B, n), "token", dev, stream)
+    work, wptr = _work(need.value, dev, stream)
+    _check(_lib().comet_beam_select(ptr, kind, B, W, V, ld, score.data_ptr(), _ptr(finished), int(eos), n, best.data_ptr(), parent.data_ptr(),
+                                    token.data_ptr(), wptr, need.value, _stream(stream)), "comet_beam_select")
+    return best, parent, token
+
+
+def _pieces(t: torch.Tensor):
+    """(outer, outer_stride, inner) in bytes of what a beam holds: the dimensions behind the first two as equal pieces."""
+    size, dims = t.element_size(), [(n, s) for n, s in zip(t.shape[2:], t.stride()[2:]) if n != 1]
+    inner = 1
+    while dims and dims[-1][1] == inner:
+        inner *= dims.pop()[0]
+    if not dims:
+        return 1, 0, inner * size
+    outer, stride = dims.pop()
+    while dims and dims[-1][1] == outer * stride:
+        outer *= dims.pop()[0]
+    if dims:
+        raise ValueError("a state's beam must be pieces of one length at one distance")
+    return outer, stride * size, inner * size
+
+
+def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, stream=None) -> None:
+    """states[i][b, w] = old states[i][b, parent[b, w]], in place; the states are [B, W, ...] tensors, of one layout or several."""
+    if not isinstance(parent, torch.Tensor) or parent.dim() != 2:
+        raise ValueError("parent must have two dimensions")
+    B, W = parent.shape
+    _dev(parent, torch.int32, "parent")
+    groups = {}
+    for t in states:
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError("states must be torch tensors in device memory")
+        if t.dim() < 2 or t.shape[0] != B or t.shape[1] != W:
+            raise ValueError("a state must have shape [%d, %d, ...], got %s" % (B, W, tuple(t.shape)))
+        if t.device != parent.device:
+            raise ValueError("states must be on %s" % parent.device)
+        groups.setdefault((t.dtype, t.shape, t.stride()), []).append(t)
+    for group in groups.values():
+        t = group[0]
+        if t.numel() == 0:
+            continue
+        size = t.element_size()
+        outer, outer_stride, inner = _pieces(t)
+        ptrs = (ctypes.c_void_p * len(group))(*[x.data_ptr() for x in group])
+        _check(_lib().comet_beam_reorder(ptrs, len(group), B, W, t.stride(0) * size, t.stride(1) * size, outer, outer_stride, inner,
+                                         parent.data_ptr(), _stream(stream)), "comet_beam_reorder")

@@ -1,0 +1,211 @@
+// What the kernels over dense rows share: element types, 16-byte vectors of a row that starts anywhere, the running
+// maximum and sum of a softmax, and reductions over a workgroup.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+#include "../../include/comet.h"
+
+namespace comet {
+
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr double kNegInfD = -__builtin_huge_val();
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWave = 64;
+
+// ---- element types ------------------------------------------------------------------------------------
+template <int TYPE> struct Elem;
+template <> struct Elem<COMET_F32> {
+    using T = uint32_t;
+    static constexpr int kPer = 4;                          // elements of a 16-byte vector
+    static __device__ __forceinline__ float one(uint32_t x) { return __uint_as_float(x); }
+    static __device__ __forceinline__ void widen(const uint4 &v, float *f) {
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    }
+    static __device__ __forceinline__ uint32_t bits(float f) { return __float_as_uint(f); }
+    static __device__ __forceinline__ uint4 narrow(const float *f) {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+};
+template <> struct Elem<COMET_BF16> {
+    using T = uint16_t;
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ float one(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+    static __device__ __forceinline__ void widen(const uint4 &v, float *f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    // to the nearest, ties to even; a NaN stays one
+    static __device__ __forceinline__ uint16_t bits(float f) {
+        const __bf16 b = (__bf16)f;
+        return __builtin_bit_cast(uint16_t, b);
+    }
+    static __device__ __forceinline__ uint4 narrow(const float *f) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)bits(f[2 * i]) | (uint32_t)bits(f[2 * i + 1]) << 16;
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <> struct Elem<COMET_F16> {
+    using T = uint16_t;
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ float one(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
+    static __device__ __forceinline__ void widen(const uint4 &v, float *f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = one((uint16_t)(w[i] & 0xffffu));
+            f[2 * i + 1] = one((uint16_t)(w[i] >> 16));
+        }
+    }
+    static __device__ __forceinline__ uint16_t bits(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
+    static __device__ __forceinline__ uint4 narrow(const float *f) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)bits(f[2 * i]) | (uint32_t)bits(f[2 * i + 1]) << 16;
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+// ---- a row as 16-byte vectors ---------------------------------------------------------------------------
+// Vector i holds the elements i * kPer .. of the row wherever the row starts, so that what is computed from a row does not
+// depend on its address.  The device loads and stores 16 bytes at any address: at multiples of 4 as fast as at multiples of
+// 16 (6.6 TB/s over rows of 256 KB), at odd multiples of 2 a fifth slower (5.2 TB/s).
+typedef uint32_t V4At4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t V4At2 __attribute__((ext_vector_type(4), aligned(2)));
+template <int ALIGN> struct Wide { using type = V4At4; };
+template <> struct Wide<2> { using type = V4At2; };
+
+template <int TYPE> struct Row {
+    using E = Elem<TYPE>;
+    using T = typename E::T;
+    using V4 = typename Wide<sizeof(T)>::type;
+    const T *p;              // the row's first element
+    int64_t n;               // its length
+    __device__ __forceinline__ Row(const void *base, int64_t row, int64_t ld, int64_t len) : p((const T *)base + row * ld), n(len) {}
+    __device__ __forceinline__ int64_t nvec() const { return (n + E::kPer - 1) / E::kPer; }
+    __device__ __forceinline__ int64_t first(int64_t i) const { return i * E::kPer; }           // column of the vector's first element
+    __device__ __forceinline__ bool whole(int64_t i) const { return first(i) + E::kPer <= n; }
+    __device__ __forceinline__ uint4 raw(int64_t i) const {
+        const V4 v = *(const V4 *)(p + first(i));
+        return make_uint4(v.x, v.y, v.z, v.w);
+    }
+    // elements of vector i as floats, -inf behind the row's end
+    __device__ __forceinline__ void load(int64_t i, float *f) const {
+        if (whole(i)) { E::widen(raw(i), f); return; }
+        const int64_t c = first(i);
+#pragma unroll
+        for (int k = 0; k < E::kPer; ++k) f[k] = c + k < n ? E::one(p[c + k]) : kNegInf;
+    }
+};
+
+// ---- running maximum and sum ------------------------------------------------------------------------------
+// s = sum of exp2(c (z - m)) over what was taken in, m its largest element.  An element that is -inf adds nothing, a NaN makes s a NaN.
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+struct MaxSum {
+    float m = kNegInf, s = 0.f;
+    template <int N> __device__ __forceinline__ void take(const float *f, float c) {
+        float b = f[0];
+#pragma unroll
+        for (int k = 1; k < N; ++k) b = fmaxf(b, f[k]);
+        if (b > m) { s *= exp2_fast((m - b) * c); m = b; }
+        if (m > kNegInf) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) s += exp2_fast((f[k] - m) * c);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) if (f[k] != f[k]) s = f[k];
+        }
+    }
+    __device__ __forceinline__ void join(float m2, float s2, float c) {
+        const float M = fmaxf(m, m2);
+        s = s * (m == M ? 1.f : exp2_fast((m - M) * c)) + s2 * (m2 == M ? 1.f : exp2_fast((m2 - M) * c));
+        m = M;
+    }
+};
+
+// A logarithm of a sum in two parts, big + log(sum of exp(. - big)): where all terms are the lowest value of their type, or near it,
+// the second part would be lost in one number.
+struct Log {
+    double big, rest;
+    __device__ __forceinline__ double value() const { return big + rest; }
+    __device__ __forceinline__ bool none() const { return big == kNegInfD; }                      // of nothing
+};
+__device__ __forceinline__ Log make_log(double big, double sum) {
+    Log l;
+    l.big = big;
+    l.rest = big == kNegInfD && !(sum != sum) ? 0.0 : log(sum);
+    if (sum != sum) l.big = sum;
+    return l;
+}
+// x - l and exp(x - l); what is -inf stays so, and has the probability 0
+__device__ __forceinline__ double minus(double x, const Log &l) { return x == kNegInfD ? x : (x - l.big) - l.rest; }
+__device__ __forceinline__ double prob(double x, const Log &l) { return x == kNegInfD ? 0.0 : exp((x - l.big) - l.rest); }
+// log sum exp(scale z) from the running maximum and sum.  With +inf among the z the differences are NaN, and so is the result.
+__device__ __forceinline__ Log log_sum(const MaxSum &a, double scale) { return make_log((double)a.m * scale, (double)a.s); }
+
+// ---- reductions ---------------------------------------------------------------------------------------------
+template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) {
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
+    return v;
+}
+template <class F> __device__ __forceinline__ double wave_reduce(double v, F f) {
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
+    return v;
+}
+__device__ __forceinline__ void wave_join(MaxSum &a, float c) {
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d >>= 1) {
+        const float m2 = __shfl_xor(a.m, d), s2 = __shfl_xor(a.s, d);
+        a.join(m2, s2, c);
+    }
+}
+// over a workgroup of T threads; buf has a place for every wavefront and is free again after the call's last barrier
+template <int T> __device__ __forceinline__ void block_join(MaxSum &a, float c, float2 *buf) {
+    wave_join(a, c);
+    if (T == kWave) return;
+    if ((threadIdx.x & (kWave - 1)) == 0) buf[threadIdx.x / kWave] = make_float2(a.m, a.s);
+    __syncthreads();
+    a = MaxSum();
+#pragma unroll
+    for (int w = 0; w < T / kWave; ++w) a.join(buf[w].x, buf[w].y, c);
+    __syncthreads();
+}
+template <int T, class F> __device__ __forceinline__ double block_reduce(double v, F f, double *buf) {
+    v = wave_reduce(v, f);
+    if (T == kWave) return v;
+    if ((threadIdx.x & (kWave - 1)) == 0) buf[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = buf[0];
+#pragma unroll
+    for (int w = 1; w < T / kWave; ++w) v = f(v, buf[w]);
+    __syncthreads();
+    return v;
+}
+struct Add { template <class X> __device__ X operator()(X a, X b) const { return a + b; } };
+struct Max { __device__ double operator()(double a, double b) const { return a != a || a > b ? a : b; } };   // a NaN on the left stays
+
+// ---- order ------------------------------------------------------------------------------------------------------
+// An unsigned number whose order is that of the float (-0 as 0).
+__device__ __forceinline__ uint32_t order_of(float z) {
+    const uint32_t u = __float_as_uint(z + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+    return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+// Larger value first, then lower column; 0 is less than every key of an element that can be kept.
+__device__ __forceinline__ uint64_t key_of(float z, uint32_t column) { return (uint64_t)order_of(z) << 32 | (uint32_t)~column; }
+__device__ __forceinline__ uint32_t column_of(uint64_t key) { return ~(uint32_t)key; }
+__device__ __forceinline__ float value_of_key(uint64_t key) { return value_of((uint32_t)(key >> 32)); }
+
+}  // namespace comet

@@ -1,0 +1,44 @@
+// Launchers of the operators on dense rows (rows_topk.hip, rows_distill.hip, rows_beam.hip).  Arguments are checked by the
+// entry points (rows_api.hip); every launcher only enqueues work on `st`.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+#include "../../include/comet.h"
+
+namespace comet {
+
+int64_t rows_topk_work(int type, int64_t N, int64_t V, int64_t K);
+hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, double scale, int64_t K, bool by_coordinate,
+                     int32_t *crd, float *vals, float *lse, void *work, hipStream_t st);
+// The K largest keys of every row, largest first (0 where there are fewer), and its log-sum-exp as a Log (16 bytes); `finished` as in comet_beam_select.
+hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, const uint8_t *finished, int32_t eos,
+                         uint64_t *keys, void *logs, hipStream_t st);
+
+struct DistillArgs {
+    const void *Z;
+    int type;
+    int64_t N, V, ldz;
+    const int32_t *pos;
+    int64_t K;
+    const int32_t *crd;
+    const float *tvals, *tlse;
+    double scale;
+    const float *weight;
+};
+int64_t distill_work(int type, int64_t N, int64_t V);
+hipError_t distill_forward(const DistillArgs &a, float *loss, double *stat, void *work, hipStream_t st);
+hipError_t distill_backward(const DistillArgs &a, const double *stat, const float *dloss, void *dZ, int64_t lddz, hipStream_t st);
+hipError_t distill_step(const DistillArgs &a, float *loss, void *dZ, int64_t lddz, void *work, hipStream_t st);
+
+int64_t beam_select_work(int type, int64_t B, int64_t W, int64_t V, int64_t n);
+hipError_t beam_select(const void *Z, int type, int64_t B, int64_t W, int64_t V, int64_t ldz, const float *score, const uint8_t *finished,
+                       int32_t eos, int64_t n, float *out_score, int32_t *out_parent, int32_t *out_token, void *work, hipStream_t st);
+
+struct StateLayout {
+    int64_t B, W, batch_stride, beam_stride, outer, outer_stride, inner;      // strides and inner in bytes
+};
+hipError_t beam_reorder(void *const *states, int64_t nstates, const StateLayout &l, const int32_t *parent, hipStream_t st);
+
+}  // namespace comet

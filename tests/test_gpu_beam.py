@@ -1,0 +1,274 @@
+"""Beam search's selection and the reordering of states."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import rows_reference as ref
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+INF = math.inf
+
+
+def _comet():
+    import paper_2102_05187_amd as comet
+    return comet
+
+
+def bound(V, s):
+    """Error of a score: the log-sum-exp's, and rounding to 32 bits."""
+    return ref.sum_error(V) + 2.0 ** -24 * abs(s) if math.isfinite(s) else 0.0
+
+
+def check_select(Z, score, n, finished=None, eos=0, stream=None):
+    comet = _comet()
+    B, W, V = Z.shape
+    best, parent, token = comet.comet_beam_select(Z, score, n, finished=finished, eos=eos, stream=stream)
+    torch.cuda.synchronize()
+    host, c = Z.double().cpu().numpy(), score.double().cpu().numpy()
+    for b in range(B):
+        done = None if finished is None else finished[b].cpu().numpy()
+        s, p, t, every = ref.select_batch(host[b], c[b], n, done, eos)
+        got = list(zip(best[b].tolist(), parent[b].tolist(), token[b].tolist()))
+        assert len(set((y, z) for _, y, z in got if y >= 0)) == sum(y >= 0 for _, y, _ in got)
+        for i, (x, y, z) in enumerate(got):
+            assert (x == s[i]) if not math.isfinite(s[i]) else abs(x - s[i]) <= bound(V, s[i]), (b, i, x, s[i])
+            # the same candidate wherever the scores around it are further apart than they may be off
+            near = [abs(s[i] - every[j]) for j in (i - 1, i + 1) if 0 <= j < len(every)] if i < len(every) else []
+            if not near or min(near) > 4 * ref.sum_error(V) or min(near) == 0:
+                assert (y, z) == (p[i], t[i]), (b, i, got[i], (s[i], p[i], t[i]))
+
+
+def logits(B, W, V, dtype, seed=0, spread=3.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn((B, W, V), generator=g) * spread).to(dtype).cuda(), (-torch.rand((B, W), generator=g) * 5).cuda()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,W,V,n", [(1, 1, 1, 1), (2, 1, 7, 3), (1, 3, 2, 6), (2, 3, 2, 9), (3, 4, 100, 8), (2, 5, 1001, 10), (1, 8, 5003, 16), (2, 2, 32003, 4),
+                                     (1, 16, 9001, 32), (1, 4, 131072, 8), (2, 3, 140001, 6), (1, 64, 301, 128), (1, 256, 33, 32), (1, 8, 2003, 1024)])
+def test_sizes(B, W, V, n, dtype):
+    check_select(*logits(B, W, V, dtype, seed=B + W + V + n), n)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_ended_beams_and_beams_not_in_use(dtype):
+    Z, c = logits(4, 4, 501, dtype, seed=1)
+    done = torch.zeros((4, 4), dtype=torch.bool, device="cuda")
+    done[0, 1] = done[1, 0] = done[1, 2] = True
+    done[2] = True                                            # all have ended
+    c[3, 1:] = -INF                                           # the first step: one beam
+    Z[0, 1] = math.nan                                        # an ended beam's row is not read
+    check_select(Z, c, 8, done, eos=500)
+    c[2, 3] = -INF                                            # ended and not in use
+    check_select(Z, c, 8, done, eos=0)
+    check_select(Z, torch.full_like(c, -INF), 5)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [40, 5003])
+def test_masked_tokens_and_fewer_candidates_than_wanted(V, dtype):
+    Z, c = logits(3, 3, V, dtype, seed=2)
+    Z[0, :, 2:] = -INF
+    Z[1, 0] = -INF
+    Z[1, 1] = torch.finfo(dtype).min
+    Z[1, 2, 1:] = torch.finfo(dtype).min
+    Z[2, 0, 7] = math.nan
+    Z[2, 1, 3] = INF
+    check_select(Z, c, 9)
+
+
+def test_equal_scores_go_to_the_lower_beam_then_token():
+    comet = _comet()
+    Z = torch.zeros((1, 3, 50), device="cuda")
+    Z[:, :, 10] = Z[:, :, 4] = Z[:, :, 30] = 2.0
+    c = torch.zeros((1, 3), device="cuda")
+    _, parent, token = comet.comet_beam_select(Z, c, 11)
+    assert parent.tolist() == [[0, 0, 0, 1, 1, 1, 2, 2, 2, 0, 0]]
+    assert token.tolist() == [[4, 10, 30] * 3 + [0, 1]]
+    Z, c = logits(1, 1, 3001, torch.bfloat16, seed=3)
+    Z = Z.expand(1, 4, 3001).contiguous()                     # the same row in each beam
+    check_select(Z, c.expand(1, 4).contiguous(), 12)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_strides(dtype):
+    Z, c = logits(3, 4, 1010, dtype, seed=4)
+    check_select(Z[:, :, 3:1004], c, 8)
+    check_select(Z[:1, 1:3], c[:1, 1:3].contiguous(), 4)
+
+
+def test_many_batches():
+    check_select(*logits(150, 3, 200, torch.bfloat16, seed=5), 6)
+
+
+def test_selection_on_another_stream_and_in_a_graph():
+    comet = _comet()
+    Z, c = logits(2, 4, 20011, torch.bfloat16, seed=6)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    check_select(Z, c, 8, stream=side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = comet.comet_beam_select(Z, c, 8)
+    for seed in range(4):
+        Z.copy_(logits(2, 4, 20011, torch.bfloat16, seed=30 + seed)[0])
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in out]
+        eager = comet.comet_beam_select(Z, c, 8)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, eager))
+
+
+def test_selection_refusals():
+    comet = _comet()
+    Z, c = logits(2, 3, 50, torch.float32)
+    done = torch.zeros((2, 3), dtype=torch.bool, device="cuda")
+    for bad, error in ((lambda: comet.comet_beam_select(Z, c, 0), comet.CometError), (lambda: comet.comet_beam_select(Z, c, 1025), comet.CometError),
+                       (lambda: comet.comet_beam_select(Z, c, 4, finished=done, eos=50), comet.CometError),
+                       (lambda: comet.comet_beam_select(Z, c, 4, finished=done, eos=-1), comet.CometError),
+                       (lambda: comet.comet_beam_select(Z[0], c, 4), ValueError), (lambda: comet.comet_beam_select(Z, c[:1], 4), ValueError),
+                       (lambda: comet.comet_beam_select(Z, c.double(), 4), TypeError), (lambda: comet.comet_beam_select(Z.double(), c, 4), TypeError),
+                       (lambda: comet.comet_beam_select(Z, c, 4, finished=done[:, :2]), ValueError),
+                       (lambda: comet.comet_beam_select(Z[:, :2], c[:, :2].contiguous(), 4), ValueError),
+                       (lambda: comet.comet_beam_select(Z.permute(0, 2, 1), c, 4), ValueError),
+                       (lambda: comet.comet_beam_select(torch.zeros((1, 16, 30), device="cuda"), torch.zeros((1, 16), device="cuda"), 600), comet.CometError)):
+        with pytest.raises(error):
+            bad()
+
+
+# ---- reordering ----------------------------------------------------------------------------------------------------
+def check_reorder(states, parent, stream=None):
+    comet = _comet()
+    B, W = parent.shape
+    at = parent.long()
+    at = torch.where((at < 0) | (at >= W), torch.arange(W, device="cuda"), at)
+    want = [x[torch.arange(B, device="cuda")[:, None], at].clone() for x in states]
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())
+    comet.comet_beam_reorder(states, parent, stream=stream)
+    torch.cuda.synchronize()
+    for x, y in zip(states, want):
+        assert torch.equal(x.contiguous().view(torch.uint8), y.contiguous().view(torch.uint8))
+
+
+def state(shape, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randint(-120, 120, shape, generator=g).to(dtype).cuda()
+
+
+def parents(B, W, seed):
+    return torch.from_numpy(np.random.RandomState(seed).randint(0, W, (B, W)).astype(np.int32)).cuda()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.int64, torch.float64])
+@pytest.mark.parametrize("B,W,rest", [(1, 1, (5,)), (1, 2, (1,)), (3, 4, (3, 5, 7)), (2, 5, (2, 33, 64)), (1, 8, (4, 100, 96)), (2, 16, (257,)), (1, 17, (3, 64)),
+                                      (1, 33, (70,)), (2, 64, (129,)), (1, 256, (40,)), (5, 3, ())])
+def test_reorder_sizes(B, W, rest, dtype):
+    check_reorder([state((B, W, *rest), dtype, i) for i in range(3)], parents(B, W, B + W))
+
+
+def test_reorder_kinds_of_parents():
+    W = 6
+    kinds = [list(range(W)), [0] * W, [5] * W, [1, 0, 2, 3, 4, 5], [1, 2, 3, 4, 5, 0], [5, 4, 3, 2, 1, 0], [-1] * W, [0, -1, W, 2 ** 31 - 1, -2 ** 31, 1]]
+    check_reorder([state((len(kinds), W, 3, 50, 16), torch.bfloat16, 1)], torch.tensor(kinds, dtype=torch.int32, device="cuda"))
+
+
+def test_reorder_parts_of_a_cache():
+    """Only the places in use move; the rest of the cache stays as it is."""
+    for dtype in (torch.bfloat16, torch.uint8):
+        whole = state((2, 4, 3, 100, 24), dtype, 2)
+        before = whole.clone()
+        check_reorder([whole[:, :, :, :37]], parents(2, 4, 3))
+        assert torch.equal(whole[:, :, :, 37:], before[:, :, :, 37:])
+        check_reorder([whole[:, :, :, 5:6]], parents(2, 4, 4))
+        check_reorder([whole[:, :, :, :, 1:4][:, :, 1]], parents(2, 4, 5))
+        check_reorder([whole[:, :, 1:3, :, :]], parents(2, 4, 6))
+
+
+def test_reorder_beams_behind_other_dimensions():
+    """Layouts whose beams or batches are not the slowest dimension."""
+    x = state((3, 5, 2, 40), torch.float32, 3)                # [tokens, W, B, dim]
+    check_reorder([x.permute(2, 1, 0, 3)], parents(2, 5, 1))
+    check_reorder([state((4, 2, 64), torch.bfloat16, 4).transpose(0, 1)], parents(2, 4, 2))
+
+
+def test_reorder_many_states_of_several_layouts():
+    states = [state((2, 3, 7 + i % 3), torch.bfloat16, i) for i in range(150)] + [state((2, 3), torch.int32, 9)]
+    check_reorder(states, parents(2, 3, 7))
+
+
+def test_reorder_many_batches():
+    check_reorder([state((70000, 2, 3), torch.int32, 8)], parents(70000, 2, 9))
+
+
+def test_reorder_beyond_four_gib():
+    x = torch.empty((1, 3, (1 << 31) + 64), dtype=torch.uint8, device="cuda")
+    for w in range(3):
+        x[0, w] = w + 1
+        x[0, w, -5:] = 50 + w
+    _comet().comet_beam_reorder([x], torch.tensor([[2, 0, 2]], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    for w, old in enumerate((2, 0, 2)):
+        assert bool((x[0, w, :-5] == old + 1).all()) and bool((x[0, w, -5:] == 50 + old).all())
+
+
+def test_reorder_on_another_stream_and_in_a_graph():
+    comet = _comet()
+    check_reorder([state((2, 4, 3, 501), torch.bfloat16, 9)], parents(2, 4, 8), stream=torch.cuda.Stream())
+    x, par = state((2, 4, 1003), torch.bfloat16, 10), parents(2, 4, 11)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        comet.comet_beam_reorder([x], par)
+    for seed in range(4):
+        x.copy_(state((2, 4, 1003), torch.bfloat16, 40 + seed))
+        par.copy_(parents(2, 4, 50 + seed))
+        want = x[torch.arange(2, device="cuda")[:, None], par.long()].clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(x, want)
+
+
+def test_reorder_refusals():
+    comet = _comet()
+    par = parents(2, 4, 0)
+    x = state((2, 4, 10), torch.float32, 0)
+    comet.comet_beam_reorder([], par)
+    comet.comet_beam_reorder([x[:, :, :0]], par)
+    for bad, error in ((lambda: comet.comet_beam_reorder([x.cpu()], par), TypeError), (lambda: comet.comet_beam_reorder([x], par.long()), TypeError),
+                       (lambda: comet.comet_beam_reorder([x[:1]], par), ValueError), (lambda: comet.comet_beam_reorder([x], par[0]), ValueError),
+                       (lambda: comet.comet_beam_reorder([x[:, :1].expand(2, 4, 10)], par), comet.CometError),
+                       (lambda: comet.comet_beam_reorder([state((2, 4, 3, 4, 6), torch.float32, 0)[:, :, :, :2, :3]], par), ValueError),
+                       (lambda: comet.comet_beam_reorder([torch.zeros((1, 257, 2), device="cuda")], torch.zeros((1, 257), dtype=torch.int32, device="cuda")), comet.CometError)):
+        with pytest.raises(error):
+            bad()
+
+
+def test_a_search_step_by_step():
+    """Selection, history and states together: every beam's state says which tokens it was made of."""
+    comet = _comet()
+    B, W, V, steps = 2, 3, 41, 6
+    g = torch.Generator().manual_seed(5)
+    table = (torch.randn((V, V), generator=g) * 2).cuda()
+    last = torch.zeros((B, W), dtype=torch.int64, device="cuda")
+    score = torch.full((B, W), -INF, device="cuda")
+    score[:, 0] = 0
+    history = torch.zeros((B, W, steps), dtype=torch.int32, device="cuda")
+    cache = torch.zeros((B, W, 2, steps, 4), dtype=torch.bfloat16, device="cuda")
+    for step in range(steps):
+        score, parent, token = comet.comet_beam_select(table[last], score, W)
+        comet.comet_beam_reorder([history, cache], parent)
+        history[:, :, step] = token
+        cache[:, :, :, step] = token[:, :, None, None].to(torch.bfloat16)
+        last = token.long()
+    assert torch.equal(cache[:, :, 1, :, 2].int(), history)
+    logp = torch.log_softmax(table.double(), 1)
+    for b in range(B):
+        for w in range(W):
+            s, at = 0.0, 0
+            for t in history[b, w].tolist():
+                s, at = s + float(logp[at, t]), t
+            assert abs(s - float(score[b, w])) < 1e-5 * steps
