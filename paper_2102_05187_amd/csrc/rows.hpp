@@ -19,6 +19,7 @@ template <int TYPE> struct Elem;
 template <> struct Elem<COMET_F32> {
     using T = uint32_t;
     static constexpr int kPer = 4;                          // elements of a 16-byte vector
+    static constexpr uint32_t kNone = 0xff800000u;          // 32 bits of -inf
     static __device__ __forceinline__ float one(uint32_t x) { return __uint_as_float(x); }
     static __device__ __forceinline__ void widen(const uint4 &v, float *f) {
         f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
@@ -31,6 +32,7 @@ template <> struct Elem<COMET_F32> {
 template <> struct Elem<COMET_BF16> {
     using T = uint16_t;
     static constexpr int kPer = 8;
+    static constexpr uint32_t kNone = 0xff80ff80u;
     static __device__ __forceinline__ float one(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
     static __device__ __forceinline__ void widen(const uint4 &v, float *f) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -55,6 +57,7 @@ template <> struct Elem<COMET_BF16> {
 template <> struct Elem<COMET_F16> {
     using T = uint16_t;
     static constexpr int kPer = 8;
+    static constexpr uint32_t kNone = 0xfc00fc00u;
     static __device__ __forceinline__ float one(uint16_t x) { return (float)__builtin_bit_cast(_Float16, x); }
     static __device__ __forceinline__ void widen(const uint4 &v, float *f) {
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -111,23 +114,46 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 struct MaxSum {
     float m = kNegInf, s = 0.f;
-    template <int N> __device__ __forceinline__ void take(const float *f, float c) {
-        float b = f[0];
-#pragma unroll
-        for (int k = 1; k < N; ++k) b = fmaxf(b, f[k]);
-        if (b > m) { s *= exp2_fast((m - b) * c); m = b; }
-        if (m > kNegInf) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) s += exp2_fast((f[k] - m) * c);
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) if (f[k] != f[k]) s = f[k];
-        }
-    }
     __device__ __forceinline__ void join(float m2, float s2, float c) {
         const float M = fmaxf(m, m2);
         s = s * (m == M ? 1.f : exp2_fast((m - M) * c)) + s2 * (m2 == M ? 1.f : exp2_fast((m2 - M) * c));
         m = M;
+    }
+};
+
+// The same while it is taken in, with one multiply-add and one exp2 an element: s holds exp2(c z - shift), where shift is c m rounded,
+// and what that rounding did to all terms alike is taken out at the end.  Where c m is 1e30 or more (rows masked by the
+// lowest value of a type) the difference comes first.
+struct Running {
+    float m = kNegInf, s = 0.f, shift = 0.f;
+    bool plain = false;
+    // N elements, b the largest
+    template <int N> __device__ __forceinline__ void take(const float *f, float b, float c) {
+        raise(b, c);
+        add<N>(f, c);
+    }
+    __device__ __forceinline__ void raise(float b, float c) {
+        if (b > m) {
+            const float sh = b * c;
+            const bool p = fabsf(sh) < 1e30f;
+            s *= p && plain ? exp2_fast(shift - sh) : exp2_fast((m - b) * c);
+            m = b, shift = sh, plain = p;
+        }
+    }
+    template <int N> __device__ __forceinline__ void add(const float *f, float c) {
+        if (plain) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) s += exp2_fast(__builtin_fmaf(f[k], c, -shift));
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) s += m > kNegInf ? exp2_fast((f[k] - m) * c) : f[k] != f[k] ? f[k] : 0.f;
+        }
+    }
+    __device__ __forceinline__ MaxSum sum(float c) const {
+        MaxSum r;
+        r.m = m;
+        r.s = plain ? s * exp2_fast(-__builtin_fmaf(m, c, -shift)) : s;
+        return r;
     }
 };
 
@@ -152,22 +178,33 @@ __device__ __forceinline__ double prob(double x, const Log &l) { return x == kNe
 __device__ __forceinline__ Log log_sum(const MaxSum &a, double scale) { return make_log((double)a.m * scale, (double)a.s); }
 
 // ---- reductions ---------------------------------------------------------------------------------------------
-template <class F> __device__ __forceinline__ float wave_reduce(float v, F f) {
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
-    return v;
+// Over a wavefront with data-parallel moves (lanes 1, 2, 4, 8 back in rows of 16, then row ends onto the rows behind them):
+// the last lane ends up with everything, in one fixed order.  A lane that a move does not reach sees `none`.
+template <int CTRL, int ROWS> __device__ __forceinline__ float dpp(float none, float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
 }
+template <class F> __device__ __forceinline__ float wave_reduce(float v, float none, F f) {
+    v = f(v, dpp<0x111, 0xf>(none, v));
+    v = f(v, dpp<0x112, 0xf>(none, v));
+    v = f(v, dpp<0x114, 0xf>(none, v));
+    v = f(v, dpp<0x118, 0xf>(none, v));
+    v = f(v, dpp<0x142, 0xa>(none, v));
+    v = f(v, dpp<0x143, 0xc>(none, v));
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+struct Add { template <class X> __device__ __forceinline__ X operator()(X a, X b) const { return a + b; } };
+struct Larger { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct Max { __device__ __forceinline__ double operator()(double a, double b) const { return a != a || a > b ? a : b; } };   // a NaN on the left stays
+
 template <class F> __device__ __forceinline__ double wave_reduce(double v, F f) {
 #pragma unroll
     for (int d = kWave / 2; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
     return v;
 }
 __device__ __forceinline__ void wave_join(MaxSum &a, float c) {
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d >>= 1) {
-        const float m2 = __shfl_xor(a.m, d), s2 = __shfl_xor(a.s, d);
-        a.join(m2, s2, c);
-    }
+    const float M = wave_reduce(a.m, kNegInf, Larger());
+    a.s = wave_reduce(a.m == M ? a.s : a.s * exp2_fast((a.m - M) * c), 0.f, Add());
+    a.m = M;
 }
 // over a workgroup of T threads; buf has a place for every wavefront and is free again after the call's last barrier
 template <int T> __device__ __forceinline__ void block_join(MaxSum &a, float c, float2 *buf) {
@@ -191,8 +228,6 @@ template <int T, class F> __device__ __forceinline__ double block_reduce(double 
     __syncthreads();
     return v;
 }
-struct Add { template <class X> __device__ X operator()(X a, X b) const { return a + b; } };
-struct Max { __device__ double operator()(double a, double b) const { return a != a || a > b ? a : b; } };   // a NaN on the left stays
 
 // ---- order ------------------------------------------------------------------------------------------------------
 // An unsigned number whose order is that of the float (-0 as 0).

@@ -8,6 +8,8 @@ namespace {
 constexpr int64_t kLim = int64_t(1) << 31;
 constexpr int64_t kRows = int64_t(1) << 23;      // a grid holds a workgroup or more for each row
 
+constexpr int64_t kTop = int64_t(1) << 30;       // V * K: the pieces of one row and their lists are joined by one workgroup
+
 int element_size(int type) { return type == COMET_F32 ? 4 : 2; }
 bool known(comet_type_t type) { return type == COMET_F32 || type == COMET_BF16 || type == COMET_F16; }
 bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -56,7 +58,7 @@ comet_status check_gradient(const comet::DistillArgs &a, const void *dZ, int64_t
 
 comet_status check_select(comet_type_t type, int64_t B, int64_t W, int64_t V, int64_t n) {
     if (!known(type) || B < 0 || W < 1 || V < 0 || n < 1) return COMET_ERR_INVALID_ARG;
-    if (B > kRows || W > COMET_MAX_BEAMS || n > COMET_MAX_TOP || W * n > 8192 || V >= (1 << 24) || B * W > kRows) return COMET_ERR_UNSUPPORTED;
+    if (B > kRows || W > COMET_MAX_BEAMS || n > COMET_MAX_TOP || W * n > 8192 || V >= (1 << 24) || V * n > kTop || B * W > kRows) return COMET_ERR_UNSUPPORTED;
     return COMET_OK;
 }
 
@@ -77,7 +79,7 @@ extern "C" {
 
 comet_status comet_rows_topk_work(comet_type_t type, int64_t N, int64_t V, int64_t K, int64_t *bytes) {
     if (!bytes || !known(type) || N < 0 || V < 0 || K < 1) return COMET_ERR_INVALID_ARG;
-    if (N > kRows || V >= kLim || K > COMET_MAX_TOP) return COMET_ERR_UNSUPPORTED;
+    if (N > kRows || V >= kLim || K > COMET_MAX_TOP || V * K > kTop) return COMET_ERR_UNSUPPORTED;
     *bytes = comet::rows_topk_work(type, N, V, K);
     return COMET_OK;
 }
@@ -87,7 +89,7 @@ comet_status comet_rows_topk(const void *Z, comet_type_t type, int64_t N, int64_
     comet_status s = check_rows(Z, type, N, V, ldz);
     if (s != COMET_OK) return s;
     if (!good_scale(scale) || K < 1 || (flags & ~COMET_BY_COORDINATE)) return COMET_ERR_INVALID_ARG;
-    if (K > COMET_MAX_TOP) return COMET_ERR_UNSUPPORTED;
+    if (K > COMET_MAX_TOP || V * K > kTop) return COMET_ERR_UNSUPPORTED;
     if (N == 0) return COMET_OK;
     if (!crd || !vals || !aligned(crd, 4) || !aligned(vals, 4) || !aligned(lse, 4)) return COMET_ERR_INVALID_ARG;
     s = check_work(work, work_bytes, comet::rows_topk_work(type, N, V, K));

@@ -69,13 +69,16 @@ __global__ void __launch_bounds__(kThreads) k_beam_reorder(StatePointers states,
 
 }  // namespace
 
-int64_t beam_select_work(int, int64_t B, int64_t W, int64_t, int64_t n) { return B * W * (n * (int64_t)sizeof(uint64_t) + (int64_t)sizeof(Log)); }
+int64_t beam_select_work(int type, int64_t B, int64_t W, int64_t V, int64_t n) {
+    return (B * W * (n * (int64_t)sizeof(uint64_t) + (int64_t)sizeof(Log)) + 15) / 16 * 16 + rows_top_keys_work(type, B * W, V, n);
+}
 
 hipError_t beam_select(const void *Z, int type, int64_t B, int64_t W, int64_t V, int64_t ldz, const float *score, const uint8_t *finished,
                        int32_t eos, int64_t n, float *out_score, int32_t *out_parent, int32_t *out_token, void *work, hipStream_t st) {
     Log *lse = (Log *)work;
     uint64_t *keys = (uint64_t *)(lse + B * W);
-    const hipError_t e = rows_top_keys(Z, type, B * W, V, ldz, n, finished, eos, keys, lse, st);
+    const hipError_t e = rows_top_keys(Z, type, B * W, V, ldz, n, finished, eos, keys, lse,
+                                     (char *)work + (B * W * (n * (int64_t)sizeof(uint64_t) + (int64_t)sizeof(Log)) + 15) / 16 * 16, st);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)B), dim3(kThreads), 0, st, keys, lse, score, (int)W, (int)n, out_score, out_parent, out_token);
     return hipGetLastError();

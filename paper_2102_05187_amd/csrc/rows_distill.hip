@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, flo
     if (w == 0) { if (threadIdx.x == 0) loss[r] = 0; return; }
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
     const Entries en(a, r);
-    MaxSum d;
+    Running run;
     const int64_t nv = row.nvec(), per = kSpan / E::kPer;
     for (int64_t v0 = 0; v0 < nv; v0 += per) {
         const int64_t base = row.first(v0);
@@ -141,9 +141,13 @@ __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, flo
 #pragma unroll
                 for (int k = 0; k < E::kPer; ++k) if (m >> k & 1) f[k] = kNegInf;
             }
-            d.take<E::kPer>(f, c2);
+            float b = f[0];
+#pragma unroll
+            for (int k = 1; k < E::kPer; ++k) b = fmaxf(b, f[k]);
+            run.take<E::kPer>(f, b, c2);
         }
     }
+    MaxSum d = run.sum(c2);
     block_join<kThreads>(d, c2, buf);
     Stat s;
     const double l = finish_row<TYPE, kThreads>(a, r, row, en, d, w, dbuf, &s);

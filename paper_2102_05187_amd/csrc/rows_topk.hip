@@ -1,110 +1,358 @@
-// The K largest elements of dense rows.
-#include "rows.hpp"
+// The K largest elements of dense rows, with the rows' log-sum-exp.
+//
+// A workgroup reads a piece of a row once (up to 256 KB; rows beyond that, and rows that are too few to fill the device, are cut into
+// several pieces whose results a second kernel joins) and keeps of every vector of 16 bytes its largest element in a register.
+// From these:
+//   1. a bound that K to 1.25 K of the threads' largest elements reach (bound()): of a row in no particular order about
+//      K (1 + K / 2T) elements reach it, of T threads; all others are out;
+//   2. the vectors whose largest element reaches it are read again, K or so of them, and their elements that do go into
+//      LDS as 64-bit keys (value, then lower column);
+//   3. the keys are put in order by counting.
+// Where more than 2048 reach the bound (equal elements, or the large ones next to each other in a few threads) the K-th largest key is
+// found exactly, by halving, with the vectors that matter read again each time.
 #include "rows_kernels.hpp"
+#include "rows_select.hpp"
 
 namespace comet {
 
 namespace {
 
-constexpr int kThreads = 256;
+struct TopArgs {
+    const void *Z;
+    int64_t V, ldz;
+    float c2;                             // scale log2(e)
+    double scale;
+    int K, splits;
+    bool by_coordinate;
+    int32_t *crd;                         // results, where a row is one piece and no keys are asked for
+    float *vals, *lse;
+    const uint8_t *finished;
+    int32_t eos;
+    uint64_t *keys;                       // [rows x splits x K], largest first, 0 where there are fewer
+    float2 *sums;                         // [rows x splits] running maximum and sum
+};
 
-// One workgroup a row.  The K-th largest key (value, then lower column; all different) is found bit by bit, the row being
-// counted once for each; then the keys from there on are collected and put in order by counting.
-template <int TYPE>
-__global__ void __launch_bounds__(kThreads) k_rows_topk(const void *Z, int64_t V, int64_t ldz, float c2, double scale, int K, bool by_coordinate,
-                                                        int32_t *__restrict__ crd, float *__restrict__ vals, float *__restrict__ lse,
-                                                        const uint8_t *__restrict__ finished, int32_t eos,
-                                                        uint64_t *__restrict__ out_keys, Log *__restrict__ logs) {
+struct TopShared {
+    uint64_t keys[kCandidates];
+    int ranks[kCandidates];
+    int tries[2 * kTries];
+    float2 buf[16];
+    float ends[16];
+    int found;
+};
+
+// The keys that were found become the row's result: places 0 .. K-1 of the row, by value or by coordinate.
+template <int T> __device__ __forceinline__ void write_row(TopShared &sh, int n, int K, bool by_coordinate, int32_t *crd, float *vals) {
+    const int kept = n < K ? n : K;
+    rank_keys<T>(sh.keys, n, sh.ranks);
+    if (by_coordinate) {
+        // the kept keys again, with the coordinate as the order: its complement is a key's low half
+        __shared__ uint64_t by_column[COMET_MAX_TOP];
+        for (int i = threadIdx.x; i < n; i += T)
+            if (sh.ranks[i] < K) by_column[sh.ranks[i]] = sh.keys[i] << 32 | sh.keys[i] >> 32;
+        __syncthreads();
+        rank_keys<T>(by_column, kept, sh.ranks);
+        for (int i = threadIdx.x; i < kept; i += T) {
+            const uint64_t key = by_column[i] << 32 | by_column[i] >> 32;
+            crd[sh.ranks[i]] = (int32_t)column_of(key);
+            vals[sh.ranks[i]] = value_of_key(key);
+        }
+    } else {
+        for (int i = threadIdx.x; i < n; i += T)
+            if (sh.ranks[i] < K) {
+                crd[sh.ranks[i]] = (int32_t)column_of(sh.keys[i]);
+                vals[sh.ranks[i]] = value_of_key(sh.keys[i]);
+            }
+    }
+    for (int i = kept + threadIdx.x; i < K; i += T) crd[i] = -1, vals[i] = kNegInf;
+}
+
+// A piece of a row: vectors [piece * T * NV, ..), vector j of thread t at j * T + t.
+template <int TYPE, int T, int NV>
+__global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     using E = Elem<TYPE>;
-    __shared__ float2 buf[kThreads / kWave];
-    __shared__ double dbuf[kThreads / kWave];
-    __shared__ uint64_t keys[COMET_MAX_TOP];
-    __shared__ int found;
-    const int64_t r = blockIdx.x;
-    if (out_keys && finished && finished[r]) {               // an ended beam: one candidate, whatever its row holds
-        for (int i = threadIdx.x; i < K; i += kThreads) out_keys[r * K + i] = i == 0 ? key_of(0.f, (uint32_t)eos) : 0;
-        if (threadIdx.x == 0) logs[r] = Log{0.0, 0.0};
+    constexpr int P = E::kPer, U = NV < 4 ? NV : 4;          // vectors that a thread has in flight
+    __shared__ TopShared sh;
+    const int64_t piece = blockIdx.x, r = piece / a.splits;
+    const int split = (int)(piece - r * a.splits), K = a.K;
+    if (a.keys && a.finished && a.finished[r]) {             // an ended beam: one candidate, whatever its row holds
+        for (int i = threadIdx.x; i < K; i += T) a.keys[piece * K + i] = i == 0 && split == 0 ? key_of(0.f, (uint32_t)a.eos) : 0;
+        if (threadIdx.x == 0) a.sums[piece] = make_float2(split == 0 ? 0.f : kNegInf, split == 0 ? 1.f : 0.f);
         return;
     }
-    const Row<TYPE> row(Z, r, ldz, V);
-    const int64_t nv = row.nvec();
-    MaxSum a;
-    double some = 0;                                         // elements that can be kept
-    for (int64_t i = threadIdx.x; i < nv; i += kThreads) {
-        float f[E::kPer];
-        row.load(i, f);
-        a.take<E::kPer>(f, c2);
+    const Row<TYPE> row(a.Z, r, a.ldz, a.V);
+    const int64_t v0 = (int64_t)split * T * NV, full = row.n / P;
+    const int own = (int)(full - v0 < T * NV ? full - v0 : T * NV);           // whole vectors of this piece
+    const bool ends_here = row.n % P != 0 && full >= v0 && full < v0 + T * NV;    // ... and the one that the row ends in: thread 0's
+    for (int i = threadIdx.x; i < 2 * kTries; i += T) sh.tries[i] = 0;
+    if (threadIdx.x == 0) sh.found = 0;
+    float top[NV], last = kNegInf;                           // `last`: of the row's last, shorter vector
+    Running run;
+    uint4 v[U];
+    auto fetch = [&](int j0) {
+        if ((j0 + U) * T <= own) {
 #pragma unroll
-        for (int k = 0; k < E::kPer; ++k) some += f[k] > kNegInf ? 1 : 0;
-    }
-    block_join<kThreads>(a, c2, buf);
-    some = block_reduce<kThreads>(some, Add(), dbuf);
-    if (lse && threadIdx.x == 0) lse[r] = a.m == -kNegInf ? a.m : (float)log_sum(a, scale).value();
-    if (out_keys && threadIdx.x == 0) logs[r] = log_sum(a, scale);
-    // the largest t with at least K keys >= t
-    uint64_t t = 0;
-    if (some > K)
-        for (int bit = 63; bit >= 0; --bit) {
-            const uint64_t mid = t | uint64_t(1) << bit;
-            double n = 0;
-            for (int64_t i = threadIdx.x; i < nv; i += kThreads) {
-                float f[E::kPer];
-                row.load(i, f);
+            for (int u = 0; u < U; ++u) v[u] = row.raw(v0 + (j0 + u) * T + threadIdx.x);
+        } else {
 #pragma unroll
-                for (int k = 0; k < E::kPer; ++k) n += f[k] > kNegInf && key_of(f[k], (uint32_t)(row.first(i) + k)) >= mid ? 1 : 0;
+            for (int u = 0; u < U; ++u) {
+                const int i = (j0 + u) * T + threadIdx.x;
+                v[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+                if (i < own) v[u] = row.raw(v0 + i);
             }
-            n = block_reduce<kThreads>(n, Add(), dbuf);
-            if (n >= K) t = mid;
-            if (n == K) break;
         }
-    if (threadIdx.x == 0) found = 0;
-    __syncthreads();
-    for (int64_t i = threadIdx.x; i < nv; i += kThreads) {
-        float f[E::kPer];
-        row.load(i, f);
+    };
+    fetch(0);
 #pragma unroll
-        for (int k = 0; k < E::kPer; ++k) {
-            const uint64_t key = key_of(f[k], (uint32_t)(row.first(i) + k));
-            if (f[k] > kNegInf && key >= t) keys[atomicAdd(&found, 1)] = key;
+    for (int j0 = 0; j0 < NV; j0 += U) {
+        uint4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = v[u];
+        if (j0 + U < NV) fetch(j0 + U);
+        float b = kNegInf;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[P];
+            E::widen(w[u], f);
+            float t = f[0];
+#pragma unroll
+            for (int k = 1; k < P; ++k) t = fmaxf(t, f[k]);
+            top[j0 + u] = t;
+            b = fmaxf(b, t);
+        }
+        run.raise(b, a.c2);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[P];
+            E::widen(w[u], f);
+            run.template add<P>(f, a.c2);
         }
     }
+    if (ends_here && threadIdx.x == 0) {
+        float f[P];
+        row.load(full, f);
+        last = f[0];
+#pragma unroll
+        for (int k = 1; k < P; ++k) last = fmaxf(last, f[k]);
+        run.template take<P>(f, last, a.c2);
+    }
+    const float m = run.m;
+    MaxSum sum = run.sum(a.c2);
+    const float least = wave_reduce(m > kNegInf ? m : -kNegInf, -kNegInf, [](float p, float q) { return fminf(p, q); });
+    if ((threadIdx.x & (kWave - 1)) == 0) sh.ends[threadIdx.x / kWave] = least;
+    block_join<T>(sum, a.c2, sh.buf);                        // also makes tries, found and ends visible
+    if (threadIdx.x == 0) {
+        if (a.sums) a.sums[piece] = make_float2(sum.m, sum.s);
+        else if (a.lse) a.lse[r] = sum.m == -kNegInf ? sum.m : (float)log_sum(sum, a.scale).value();
+    }
+    // 1: the bound.  `lowest`: nothing that can be kept is below it.
+    const uint32_t lowest = order_of(kNegInf) + 1, highest = sum.m > kNegInf ? order_of(sum.m) : lowest;
+    uint32_t L = lowest;
+    if (K <= T / 2) {
+        float lo = sh.ends[0];
+#pragma unroll
+        for (int w = 1; w < T / kWave; ++w) lo = fminf(lo, sh.ends[w]);
+        // the least of the largest elements; where fewer threads than K have one, everything is a candidate
+        const uint32_t mine = m > kNegInf ? order_of(m) : 0;
+        const uint32_t from = sum.m > kNegInf ? order_of(lo) : lowest;
+        if (block_count<T>(mine >= from, &sh.tries[kTries]) >= K) L = bound<T>(from, highest, K, [&](uint32_t t) { return mine >= t; }, sh.tries);
+    } else if (T * NV * P > kCandidates) {
+        L = bound<T>(lowest, highest, K, [&](uint32_t t) {
+            int n = last >= value_of(t) ? 1 : 0;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) n += top[j] >= value_of(t) ? 1 : 0;
+            return n;
+        }, sh.tries);
+    }
+    // 2: every element from a value (above -inf) on, with its column
+    auto each = [&](float from, auto use) {
+        if (!(m >= from)) return;
+        uint32_t which = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) which |= top[j] >= from ? 1u << j : 0u;
+        while (which) {
+            const int64_t i = v0 + (__builtin_ctz(which)) * T + threadIdx.x;
+            which &= which - 1;
+            float f[P];
+            E::widen(row.raw(i), f);
+#pragma unroll
+            for (int k = 0; k < P; ++k) if (f[k] >= from) use(key_of(f[k], (uint32_t)(i * P + k)));
+        }
+        if (last >= from)
+            for (int64_t c = full * P; c < row.n; ++c) if (E::one(row.p[c]) >= from) use(key_of(E::one(row.p[c]), (uint32_t)c));
+    };
+    each(value_of(L), [&](uint64_t key) {
+        const int at = atomicAdd(&sh.found, 1);
+        if (at < kCandidates) sh.keys[at] = key;
+    });
     __syncthreads();
-    const int n = found;
-    for (int i = threadIdx.x; i < K; i += kThreads) {
-        if (i >= n) {
-            if (out_keys) out_keys[r * K + i] = 0;
-            else crd[r * K + i] = -1, vals[r * K + i] = kNegInf;
-            continue;
+    int n = sh.found;
+    if (n > kCandidates) {
+        // the K-th largest key: all keys are different, so exactly K reach it
+        uint64_t lo = (uint64_t)L << 32, hi = (uint64_t)highest << 32 | 0xffffffffu;
+        for (int i = 0; lo < hi; ++i) {
+            __syncthreads();
+            if (threadIdx.x == 0) sh.tries[kTries + (i + 2) % kTries] = 0;
+            const uint64_t mid = lo + (hi - lo) / 2 + 1;
+            int c = 0;
+            each(value_of((uint32_t)(mid >> 32)), [&](uint64_t key) { c += key >= mid ? 1 : 0; });
+            const int reach = block_count<T>(c, &sh.tries[kTries + (i + 1) % kTries]);
+            if (reach >= K) lo = mid;
+            else hi = mid - 1;
+            if (reach == K) break;
         }
-        const uint64_t key = keys[i];
-        int at = 0;
-        for (int j = 0; j < n; ++j) at += by_coordinate ? column_of(keys[j]) < column_of(key) : keys[j] > key;
-        if (out_keys) { out_keys[r * K + at] = key; continue; }
-        crd[r * K + at] = (int32_t)column_of(key);
-        vals[r * K + at] = value_of_key(key);
+        __syncthreads();
+        if (threadIdx.x == 0) sh.found = 0;
+        __syncthreads();
+        each(value_of((uint32_t)(lo >> 32)), [&](uint64_t key) {
+            if (key < lo) return;
+            const int at = atomicAdd(&sh.found, 1);
+            if (at < kCandidates) sh.keys[at] = key;
+        });
+        __syncthreads();
+        n = sh.found < kCandidates ? sh.found : kCandidates;
     }
+    // 3
+    if (a.keys) {
+        rank_keys<T>(sh.keys, n, sh.ranks);
+        for (int i = threadIdx.x; i < n; i += T)
+            if (sh.ranks[i] < K) a.keys[piece * K + sh.ranks[i]] = sh.keys[i];
+        for (int i = n + threadIdx.x; i < K; i += T) a.keys[piece * K + i] = 0;
+    } else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
 }
+
+// Joins the pieces of a row: `splits` lists of K keys, at most kMerge in all, and as many sums.
+constexpr int kMergeThreads = 1024;
+constexpr int kMergePer = 16;
+constexpr int kMerge = kMergeThreads * kMergePer;
+
+__global__ void __launch_bounds__(kMergeThreads) k_topk_merge(TopArgs a, int64_t out_stride, uint64_t *__restrict__ out_keys, Log *__restrict__ logs) {
+    constexpr int T = kMergeThreads;
+    __shared__ TopShared sh;
+    const int64_t r = blockIdx.x;
+    const int K = a.K, total = a.splits * K;
+    const uint64_t *from = a.keys + r * total;
+    uint64_t key[kMergePer], mine = 0;
+#pragma unroll
+    for (int j = 0; j < kMergePer; ++j) {
+        const int i = j * T + threadIdx.x;
+        key[j] = i < total ? from[i] : 0;
+        mine = key[j] > mine ? key[j] : mine;
+    }
+    for (int i = threadIdx.x; i < 2 * kTries; i += T) sh.tries[i] = 0;
+    if (threadIdx.x == 0) sh.found = 0;
+    MaxSum sum;
+    for (int i = threadIdx.x; i < a.splits; i += T) {
+        const float2 p = a.sums[r * a.splits + i];
+        sum.join(p.x, p.y, a.c2);
+    }
+    block_join<T>(sum, a.c2, sh.buf);
+    if (threadIdx.x == 0) {
+        if (logs) logs[r] = log_sum(sum, a.scale);
+        else if (a.lse) a.lse[r] = sum.m == -kNegInf ? sum.m : (float)log_sum(sum, a.scale).value();
+    }
+    const uint32_t lowest = order_of(kNegInf) + 1, highest = sum.m > kNegInf ? order_of(sum.m) : lowest;
+    const uint32_t top = (uint32_t)(mine >> 32);
+    uint64_t lo = (uint64_t)bound<T>(lowest, highest, K, [&](uint32_t t) { return top >= t; }, sh.tries) << 32;
+    for (int pass = 0;; ++pass) {
+#pragma unroll
+        for (int j = 0; j < kMergePer; ++j)
+            if (key[j] && key[j] >= lo) {
+                const int at = atomicAdd(&sh.found, 1);
+                if (at < kCandidates) sh.keys[at] = key[j];
+            }
+        __syncthreads();
+        if (pass == 1 || sh.found <= kCandidates) break;
+        uint64_t hi = (uint64_t)highest << 32 | 0xffffffffu;
+        for (int i = 0; lo < hi; ++i) {
+            __syncthreads();
+            if (threadIdx.x == 0) sh.tries[kTries + (i + 1) % kTries] = 0;
+            const uint64_t mid = lo + (hi - lo) / 2 + 1;
+            int c = 0;
+#pragma unroll
+            for (int j = 0; j < kMergePer; ++j) c += key[j] >= mid ? 1 : 0;
+            const int reach = block_count<T>(c, &sh.tries[kTries + i % kTries]);
+            if (reach >= K) lo = mid;
+            else hi = mid - 1;
+            if (reach == K) break;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) sh.found = 0;
+        __syncthreads();
+    }
+    const int n = sh.found < kCandidates ? sh.found : kCandidates;
+    if (out_keys) {
+        rank_keys<T>(sh.keys, n, sh.ranks);
+        for (int i = threadIdx.x; i < n; i += T)
+            if (sh.ranks[i] < K) out_keys[r * out_stride + sh.ranks[i]] = sh.keys[i];
+        for (int i = n + threadIdx.x; i < K; i += T) out_keys[r * out_stride + i] = 0;
+    } else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
+}
+
+// How rows are cut: workgroups of `threads` with `vectors` vectors in each thread's registers, `splits` of them for a row.
+struct Cut { int threads, vectors, splits; };
+
+Cut cut_rows(int type, int64_t N, int64_t V, int64_t K) {
+    const int64_t per = type == COMET_F32 ? 4 : 8, nv = (V + per - 1) / per;
+    const int sizes[][2] = {{512, 32}, {256, 32}, {256, 16}, {256, 8}, {256, 4}, {256, 2}, {256, 1}};
+    Cut best{0, 0, 0};
+    for (const auto &s : sizes) {
+        const int64_t piece = (int64_t)s[0] * s[1], splits = nv > piece ? (nv + piece - 1) / piece : 1;
+        // a smaller piece: where it holds the row too, or where the rows' pieces are too few for the device so far
+        if (best.threads && splits > 1 && (N * best.splits >= 256 || splits * K > kMerge || piece * per < 4 * K)) break;
+        best = Cut{s[0], s[1], (int)splits};
+    }
+    return best;
+}
+
+template <int TYPE> hipError_t launch(const Cut &c, const TopArgs &a, int64_t N, hipStream_t st) {
+    const auto kernel = c.threads == 512 ? k_rows_topk<TYPE, 512, 32> : c.vectors == 32 ? k_rows_topk<TYPE, 256, 32>
+                      : c.vectors == 16 ? k_rows_topk<TYPE, 256, 16> : c.vectors == 8 ? k_rows_topk<TYPE, 256, 8>
+                      : c.vectors == 4 ? k_rows_topk<TYPE, 256, 4> : c.vectors == 2 ? k_rows_topk<TYPE, 256, 2> : k_rows_topk<TYPE, 256, 1>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(N * a.splits)), dim3(c.threads), 0, st, a);
+    return hipGetLastError();
+}
+hipError_t launch(int type, const Cut &c, const TopArgs &a, int64_t N, hipStream_t st) {
+    return type == COMET_F32 ? launch<COMET_F32>(c, a, N, st) : type == COMET_BF16 ? launch<COMET_BF16>(c, a, N, st) : launch<COMET_F16>(c, a, N, st);
+}
+
+int64_t round16(int64_t b) { return (b + 15) / 16 * 16; }
 
 }  // namespace
 
-int64_t rows_topk_work(int, int64_t, int64_t, int64_t) { return 0; }
-
-template <class... Args> static hipError_t launch(int type, int64_t N, hipStream_t st, Args... args) {
-    const auto kernel = type == COMET_F32 ? k_rows_topk<COMET_F32> : type == COMET_BF16 ? k_rows_topk<COMET_BF16> : k_rows_topk<COMET_F16>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)N), dim3(kThreads), 0, st, args...);
-    return hipGetLastError();
+int64_t rows_topk_work(int type, int64_t N, int64_t V, int64_t K) {
+    const Cut c = cut_rows(type, N, V, K);
+    return c.splits == 1 ? 0 : round16(N * c.splits * (int64_t)sizeof(float2)) + N * c.splits * K * (int64_t)sizeof(uint64_t);
 }
 
 hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, double scale, int64_t K, bool by_coordinate,
-                     int32_t *crd, float *vals, float *lse, void *, hipStream_t st) {
-    return launch(type, N, st, Z, V, ldz, (float)(scale * 1.4426950408889634), scale, (int)K, by_coordinate, crd, vals, lse,
-                  (const uint8_t *)nullptr, 0, (uint64_t *)nullptr, (Log *)nullptr);
+                     int32_t *crd, float *vals, float *lse, void *work, hipStream_t st) {
+    const Cut c = cut_rows(type, N, V, K);
+    TopArgs a{Z, V, ldz, (float)(scale * 1.4426950408889634), scale, (int)K, c.splits, by_coordinate, crd, vals, lse, nullptr, 0, nullptr, nullptr};
+    if (c.splits > 1) {
+        a.sums = (float2 *)work;
+        a.keys = (uint64_t *)((char *)work + round16(N * c.splits * (int64_t)sizeof(float2)));
+    }
+    const hipError_t e = launch(type, c, a, N, st);
+    if (e != hipSuccess || c.splits == 1) return e;
+    hipLaunchKernelGGL(k_topk_merge, dim3((unsigned)N), dim3(kMergeThreads), 0, st, a, (int64_t)0, (uint64_t *)nullptr, (Log *)nullptr);
+    return hipGetLastError();
+}
+
+int64_t rows_top_keys_work(int type, int64_t N, int64_t V, int64_t K) {
+    const Cut c = cut_rows(type, N, V, K);
+    return round16(N * c.splits * (int64_t)sizeof(float2)) + N * c.splits * K * (int64_t)sizeof(uint64_t);
 }
 
 hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, const uint8_t *finished, int32_t eos,
-                         uint64_t *keys, void *logs, hipStream_t st) {
-    return launch(type, N, st, Z, V, ldz, kLog2e, 1.0, (int)K, false, (int32_t *)nullptr, (float *)nullptr, (float *)nullptr, finished, eos,
-                  keys, (Log *)logs);
+                         uint64_t *keys, void *logs, void *work, hipStream_t st) {
+    const Cut c = cut_rows(type, N, V, K);
+    const TopArgs a{Z, V, ldz, kLog2e, 1.0, (int)K, c.splits, false, nullptr, nullptr, nullptr, finished, eos,
+                    (uint64_t *)((char *)work + round16(N * c.splits * (int64_t)sizeof(float2))), (float2 *)work};
+    const hipError_t e = launch(type, c, a, N, st);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_topk_merge, dim3((unsigned)N), dim3(kMergeThreads), 0, st, a, K, keys, (Log *)logs);
+    return hipGetLastError();
 }
 
 }  // namespace comet
