@@ -108,6 +108,14 @@ template <int TYPE> struct Row {
     }
 };
 
+// A copy of registers that the compiler knows nothing about: what is computed from it is computed anew, and not kept from the last
+// time.  Nothing is moved across, either: the floats of one vector are live at a time.
+__device__ __forceinline__ uint4 again(uint4 v) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w));
+    return v;
+}
+
 // ---- running maximum and sum ------------------------------------------------------------------------------
 // s = sum of exp2(c (z - m)) over what was taken in, m its largest element.  An element that is -inf adds nothing, a NaN makes s a NaN.
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -196,10 +204,19 @@ struct Add { template <class X> __device__ __forceinline__ X operator()(X a, X b
 struct Larger { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 struct Max { __device__ __forceinline__ double operator()(double a, double b) const { return a != a || a > b ? a : b; } };   // a NaN on the left stays
 
-template <class F> __device__ __forceinline__ double wave_reduce(double v, F f) {
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
-    return v;
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp(double none, double v) {
+    const int lo = __builtin_amdgcn_update_dpp(__double2loint(none), __double2loint(v), CTRL, ROWS, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(__double2hiint(none), __double2hiint(v), CTRL, ROWS, 0xf, false);
+    return __hiloint2double(hi, lo);
+}
+template <class F> __device__ __forceinline__ double wave_reduce(double v, double none, F f) {
+    v = f(v, dpp<0x111, 0xf>(none, v));
+    v = f(v, dpp<0x112, 0xf>(none, v));
+    v = f(v, dpp<0x114, 0xf>(none, v));
+    v = f(v, dpp<0x118, 0xf>(none, v));
+    v = f(v, dpp<0x142, 0xa>(none, v));
+    v = f(v, dpp<0x143, 0xc>(none, v));
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), 63), __builtin_amdgcn_readlane(__double2loint(v), 63));
 }
 __device__ __forceinline__ void wave_join(MaxSum &a, float c) {
     const float M = wave_reduce(a.m, kNegInf, Larger());
@@ -217,18 +234,6 @@ template <int T> __device__ __forceinline__ void block_join(MaxSum &a, float c, 
     for (int w = 0; w < T / kWave; ++w) a.join(buf[w].x, buf[w].y, c);
     __syncthreads();
 }
-template <int T, class F> __device__ __forceinline__ double block_reduce(double v, F f, double *buf) {
-    v = wave_reduce(v, f);
-    if (T == kWave) return v;
-    if ((threadIdx.x & (kWave - 1)) == 0) buf[threadIdx.x / kWave] = v;
-    __syncthreads();
-    v = buf[0];
-#pragma unroll
-    for (int w = 1; w < T / kWave; ++w) v = f(v, buf[w]);
-    __syncthreads();
-    return v;
-}
-
 // ---- order ------------------------------------------------------------------------------------------------------
 // An unsigned number whose order is that of the float (-0 as 0).
 __device__ __forceinline__ uint32_t order_of(float z) {
