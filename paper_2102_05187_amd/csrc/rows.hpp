@@ -15,6 +15,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWave = 64;
 
 // ---- element types ------------------------------------------------------------------------------------
+typedef float F2 __attribute__((ext_vector_type(2)));
+typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+typedef _Float16 H2 __attribute__((ext_vector_type(2)));
+
 template <int TYPE> struct Elem;
 template <> struct Elem<COMET_F32> {
     using T = uint32_t;
@@ -50,7 +54,10 @@ template <> struct Elem<COMET_BF16> {
     static __device__ __forceinline__ uint4 narrow(const float *f) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)bits(f[2 * i]) | (uint32_t)bits(f[2 * i + 1]) << 16;
+        for (int i = 0; i < 4; ++i) {
+            const F2 two = {f[2 * i], f[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, B2));
+        }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
@@ -71,7 +78,10 @@ template <> struct Elem<COMET_F16> {
     static __device__ __forceinline__ uint4 narrow(const float *f) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)bits(f[2 * i]) | (uint32_t)bits(f[2 * i + 1]) << 16;
+        for (int i = 0; i < 4; ++i) {
+            const F2 two = {f[2 * i], f[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(two, H2));
+        }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
@@ -130,37 +140,35 @@ struct MaxSum {
 };
 
 // The same while it is taken in, with one multiply-add and one exp2 an element: s holds exp2(c z - shift), where shift is c m rounded,
-// and what that rounding did to all terms alike is taken out at the end.  Where c m is 1e30 or more (rows masked by the
-// lowest value of a type) the difference comes first.
+// and what that rounding did to all terms alike is taken out at the end.  Where |c m| reaches kWild (rows masked by the lowest value of a
+// type throughout, or with +inf) this loses what is left: the sum of a row whose maximum is wild() is taken again by slow_sum.
+constexpr float kWild = 1e30f;
+__device__ __forceinline__ bool wild(float m, float c) { return m > kNegInf && !(fabsf(m * c) < kWild); }
+
 struct Running {
-    float m = kNegInf, s = 0.f, shift = 0.f;
-    bool plain = false;
+    float m = kNegInf, s = 0.f, shift = -kWild;
+    __device__ __forceinline__ void raise(float b, float c) {
+        if (b > m) {
+            const float sh = fminf(fmaxf(b * c, -kWild), kWild);
+            s *= exp2_fast(shift - sh);
+            m = b, shift = sh;
+        }
+    }
+    template <int N> __device__ __forceinline__ void add(const float *f, float c) {
+        float t[4] = {s, 0.f, 0.f, 0.f};                         // four sums: an addition need not wait for the one before
+#pragma unroll
+        for (int k = 0; k < N; ++k) t[k % 4] += exp2_fast(__builtin_fmaf(f[k], c, -shift));
+        s = (t[0] + t[1]) + (t[2] + t[3]);
+    }
     // N elements, b the largest
     template <int N> __device__ __forceinline__ void take(const float *f, float b, float c) {
         raise(b, c);
         add<N>(f, c);
     }
-    __device__ __forceinline__ void raise(float b, float c) {
-        if (b > m) {
-            const float sh = b * c;
-            const bool p = fabsf(sh) < 1e30f;
-            s *= p && plain ? exp2_fast(shift - sh) : exp2_fast((m - b) * c);
-            m = b, shift = sh, plain = p;
-        }
-    }
-    template <int N> __device__ __forceinline__ void add(const float *f, float c) {
-        if (plain) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) s += exp2_fast(__builtin_fmaf(f[k], c, -shift));
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) s += m > kNegInf ? exp2_fast((f[k] - m) * c) : f[k] != f[k] ? f[k] : 0.f;
-        }
-    }
     __device__ __forceinline__ MaxSum sum(float c) const {
         MaxSum r;
         r.m = m;
-        r.s = plain ? s * exp2_fast(-__builtin_fmaf(m, c, -shift)) : s;
+        r.s = fabsf(shift) < kWild ? s * exp2_fast(-__builtin_fmaf(m, c, -shift)) : s;
         return r;
     }
 };
@@ -234,6 +242,18 @@ template <int T> __device__ __forceinline__ void block_join(MaxSum &a, float c, 
     for (int w = 0; w < T / kWave; ++w) a.join(buf[w].x, buf[w].y, c);
     __syncthreads();
 }
+// The sum over columns [begin, end) of a row whose maximum there is m, against m itself: what Running loses where m is wild.  A column
+// that `skip` names is left out.  By a workgroup of T threads.
+template <int TYPE, int T, class SKIP>
+__device__ __forceinline__ float slow_sum(const Row<TYPE> &row, int64_t begin, int64_t end, float m, float c, float2 *buf, SKIP skip) {
+    MaxSum a;
+    a.m = m;
+    for (int64_t i = begin + threadIdx.x; i < end && i < row.n; i += T)
+        if (!skip(i)) a.s += exp2_fast((Elem<TYPE>::one(row.p[i]) - m) * c);
+    block_join<T>(a, c, buf);
+    return a.s;
+}
+
 // ---- order ------------------------------------------------------------------------------------------------------
 // An unsigned number whose order is that of the float (-0 as 0).
 __device__ __forceinline__ uint32_t order_of(float z) {

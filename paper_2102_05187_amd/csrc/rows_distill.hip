@@ -109,116 +109,155 @@ __device__ double finish(const Taught &t, MaxSum d, bool tail, double tlse, doub
 }
 
 // ---- marks --------------------------------------------------------------------------------------------------
-// A bit for each of `columns` places from `base` on, a multiple of 32; all threads call this, and a barrier has to follow.
-template <int T> __device__ __forceinline__ void clear_marks(uint32_t *marks, int columns) {
-    for (int i = threadIdx.x; i < (columns + 31) / 32; i += T) marks[i] = 0;
-    __syncthreads();
+// A piece of a row: `vectors` vectors from v0 on, vector j T + t of them thread t's j-th.  `own` of them are whole in the row; `ends` says that
+// the row ends inside of the vector behind those.
+template <int P> struct Piece {
+    int64_t v0, vectors;
+    int own;
+    bool ends;
+    __device__ __forceinline__ Piece(int64_t V, int64_t v0_, int64_t vectors_) : v0(v0_), vectors(vectors_) {
+        const int64_t full = V / P;
+        own = (int)(full - v0 < vectors ? full - v0 : vectors);                // below 1: none
+        ends = V % P != 0 && full >= v0 && full < v0 + vectors;
+    }
+    __device__ __forceinline__ int64_t base() const { return v0 * P; }
+    __device__ __forceinline__ int64_t columns() const { return vectors * P; }
+};
+
+// The places of the row's entries in a piece: a bit for each place (`bits`), and for each thread a word that names its vectors with such
+// places (WORD has a bit for each of them).  Both are LDS.
+template <int T, int P, class WORD> struct Marks {
+    uint32_t *bits;
+    WORD *words;
+    __device__ __forceinline__ void clear(const Piece<P> &p) const {
+        for (int i = threadIdx.x; i < (int)((p.columns() + 31) / 32); i += T) bits[i] = 0;
+        words[threadIdx.x] = 0;
+        __syncthreads();
+    }
+    __device__ __forceinline__ void set(const Piece<P> &p, const Entries &en) const {          // a barrier has to follow
+        int64_t c;
+        for (int64_t e = en.begin + threadIdx.x; e < en.end; e += T)
+            if (en.at(e, &c) && c >= p.base() && c < p.base() + p.columns()) {
+                const int at = (int)(c - p.base()), i = at / P;
+                atomicOr(&bits[at >> 5], 1u << (at & 31));
+                atomicOr(&words[i % T], (WORD)1 << (i / T));
+            }
+    }
+    __device__ __forceinline__ uint32_t of(int i) const {                                        // the marks of the piece's vector i
+        const int c = i * P;
+        return bits[c >> 5] >> (c & 31) & ((1u << P) - 1);
+    }
+    __device__ __forceinline__ bool at(int c) const { return bits[c >> 5] >> (c & 31) & 1; }
+};
+
+// The bit of the vector that the row ends in, for its thread.
+template <int T, int P, class WORD> __device__ __forceinline__ WORD last_vector(const Piece<P> &p) {
+    return p.ends && (int)threadIdx.x == p.own % T ? (WORD)1 << (p.own / T) : (WORD)0;
 }
-template <int T> __device__ __forceinline__ void set_marks(uint32_t *marks, const Entries &en, int64_t base, int columns) {
-    int64_t c;
-    for (int64_t e = en.begin + threadIdx.x; e < en.end; e += T)
-        if (en.at(e, &c) && c >= base && c < base + columns) atomicOr(&marks[(c - base) >> 5], 1u << ((c - base) & 31));
-}
-// The marks of vector i of the piece.
-template <int P> __device__ __forceinline__ uint32_t marks_at(const uint32_t *marks, int i) {
-    const int c = i * P;
-    return marks[c >> 5] >> (c & 31) & ((1u << P) - 1);
-}
-template <int P> __device__ __forceinline__ void leave_out(float *f, uint32_t mk) {
-    if (mk) {
+
+// Takes in the vectors that `word` names, without the marked places where there is a tail.
+template <int TYPE, int T, bool TAIL, class WORD>
+__device__ __forceinline__ void take_some(Running &run, const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, WORD word,
+                                          const Marks<T, Elem<TYPE>::kPer, WORD> &marks, float c2) {
+    constexpr int P = Elem<TYPE>::kPer;
+    while (word) {
+        const int i = (sizeof(WORD) == 8 ? __builtin_ctzll(word) : __builtin_ctz((uint32_t)word)) * T + threadIdx.x;
+        word &= word - 1;
+        float f[P], b = kNegInf;
+        row.load(p.v0 + i, f);
+        const uint32_t mk = TAIL ? marks.of(i) : 0;
 #pragma unroll
-        for (int k = 0; k < P; ++k) if (mk >> k & 1) f[k] = kNegInf;
+        for (int k = 0; k < P; ++k) {
+            if (TAIL && mk >> k & 1) f[k] = kNegInf;
+            b = fmaxf(b, f[k]);
+        }
+        run.template take<P>(f, b, c2);
     }
 }
 
 // ---- forward --------------------------------------------------------------------------------------------------
 constexpr int kThreads = 256;
-constexpr int kPiece = 16384;             // vectors of a piece at most: its marks take 16 KB
+constexpr int kPiece = 64 * kThreads;     // vectors of a piece at most: a bit for each of a thread's, and marks of 16 KB
 constexpr int kAhead = 4;                 // vectors that a thread has in flight
 
 struct Pieces {                           // how a row is cut: `count` pieces of `vectors` vectors
     int vectors, count;
 };
 
+// Reads a piece once: the running maximum and sum of its places, without the marked ones where there is a tail.  Vectors with marks, and the
+// one that the row ends in, are read again at the end, in part.  `mark` sets the marks, once the first loads are on their way.
+template <int TYPE, int T, bool TAIL, class WORD, class MARK>
+__device__ __forceinline__ MaxSum read_piece(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, const Marks<T, Elem<TYPE>::kPer, WORD> &marks,
+                                             float c2, float2 *buf, MARK mark) {
+    using E = Elem<TYPE>;
+    constexpr int P = E::kPer, U = kAhead;
+    uint4 v[U];
+    auto fetch = [&](int i0) {
+        if (i0 + U * T <= p.own) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = row.raw(p.v0 + i0 + u * T + threadIdx.x);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * T + threadIdx.x;
+                v[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+                if (i < p.own) v[u] = row.raw(p.v0 + i);
+            }
+        }
+    };
+    fetch(0);
+    mark();
+    WORD word = TAIL ? marks.words[threadIdx.x] : (WORD)0;
+    Running run;
+    for (int i0 = 0, j0 = 0; i0 < p.own; i0 += U * T, j0 += U) {
+        uint4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = v[u];
+        if (i0 + U * T < p.own) fetch(i0 + U * T);
+        if (TAIL && (word >> j0 & ((1 << U) - 1))) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) if (word >> (j0 + u) & 1) x[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+        }
+        float f[U * P], b = kNegInf;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            E::widen(x[u], f + u * P);
+#pragma unroll
+            for (int k = 0; k < P; ++k) b = fmaxf(b, f[u * P + k]);
+        }
+        run.template take<U * P>(f, b, c2);
+    }
+    take_some<TYPE, T, TAIL>(run, row, p, word | last_vector<T, P, WORD>(p), marks, c2);
+    MaxSum d = run.sum(c2);
+    block_join<T>(d, c2, buf);
+    if (wild(d.m, c2))
+        d.s = slow_sum<TYPE, T>(row, p.base(), p.base() + p.columns(), d.m, c2, buf, [&](int64_t c) { return TAIL && marks.at((int)(c - p.base())); });
+    return d;
+}
+
 template <int TYPE, bool TAIL>
 __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, float c2, Pieces cut, float *__restrict__ loss, Stat *__restrict__ stat,
                                                               float2 *__restrict__ partial) {
     using E = Elem<TYPE>;
-    constexpr int P = E::kPer, T = kThreads, U = kAhead;
+    constexpr int P = E::kPer, T = kThreads;
     __shared__ float2 buf[T / kWave];
-    extern __shared__ uint32_t marks[];
+    __shared__ uint64_t words[TAIL ? T : 1];
+    extern __shared__ uint32_t bits[];
     const int64_t r = blockIdx.x / (unsigned)cut.count;
-    const int piece = (int)(blockIdx.x - r * cut.count);
     const float w = a.weight ? a.weight[r] : 1.f;
     if (w == 0) {
         if (threadIdx.x == 0 && cut.count == 1) loss[r] = 0;
         return;
     }
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
-    const int64_t v0 = (int64_t)piece * cut.vectors, full = a.V / P;
-    const int own = (int)(full - v0 < cut.vectors ? full - v0 : cut.vectors);
-    const bool ends_here = a.V % P != 0 && full >= v0 && full < v0 + cut.vectors;
-    uint4 v[U];
-    auto fetch = [&](int i0) {
-        if (i0 + U * T <= own) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = row.raw(v0 + i0 + u * T + threadIdx.x);
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = i0 + u * T + threadIdx.x;
-                v[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
-                if (i < own) v[u] = row.raw(v0 + i);
-            }
-        }
-    };
-    fetch(0);
-    if (TAIL) {
-        const Entries en(a, r);
-        clear_marks<T>(marks, cut.vectors * P);
-        set_marks<T>(marks, en, v0 * P, cut.vectors * P);
+    const Piece<P> p(a.V, (blockIdx.x - r * cut.count) * cut.vectors, cut.vectors);
+    const Marks<T, P, uint64_t> marks{bits, words};
+    const MaxSum d = read_piece<TYPE, T, TAIL>(row, p, marks, c2, buf, [&] {
+        if (!TAIL) return;
+        marks.clear(p);
+        marks.set(p, Entries(a, r));
         __syncthreads();
-    }
-    Running run;
-    for (int i0 = 0; i0 < own; i0 += U * T) {
-        uint4 x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = v[u];
-        if (i0 + U * T < own) fetch(i0 + U * T);
-        float b = kNegInf;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[P];
-            E::widen(x[u], f);
-            if (TAIL) {
-                const int i = i0 + u * T + threadIdx.x;
-                const uint32_t mk = i < own ? marks_at<P>(marks, i) : 0;
-                if (mk) {                                        // rare: the places' bits become -inf
-                    leave_out<P>(f, mk);
-                    x[u] = E::narrow(f);
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < P; ++k) b = fmaxf(b, f[k]);
-        }
-        run.raise(b, c2);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[P];
-            E::widen(x[u], f);
-            run.template add<P>(f, c2);
-        }
-    }
-    if (ends_here && threadIdx.x == 0) {
-        float f[P], b = kNegInf;
-        row.load(full, f);
-        if (TAIL) leave_out<P>(f, marks_at<P>(marks, (int)(full - v0)));
-#pragma unroll
-        for (int k = 0; k < P; ++k) b = fmaxf(b, f[k]);
-        run.template take<P>(f, b, c2);
-    }
-    MaxSum d = run.sum(c2);
-    block_join<T>(d, c2, buf);
+    });
     if (cut.count > 1) {
         if (threadIdx.x == 0) partial[blockIdx.x] = make_float2(d.m, d.s);
     } else if (threadIdx.x < kWave) {
@@ -272,35 +311,57 @@ __device__ __forceinline__ void write_entries(const Row<TYPE> &row, const Entrie
         }
 }
 
-// The dense pass of the gradient: g = A exp2(c2 (z - m)).
+// The dense pass of the gradient: g = A exp2(c2 (z - m)), with one multiply-add, one exp2 and one product an element.
 struct Dense {
     float A, m, c2, shift;
-    bool plain;
-    __device__ __forceinline__ Dense(const Stat &s, double up, float c2_) : m((float)s.m), c2(c2_), shift(m * c2_), plain(fabsf(shift) < 1e30f) {
-        A = (float)(up * s.A);
-        if (plain) A *= exp2_fast(-__builtin_fmaf(m, c2, -shift));
+    __device__ __forceinline__ Dense(const Stat &s, double up, float c2_) : A((float)(up * s.A)), m((float)s.m), c2(c2_), shift(m * c2_) {
+        if (plain()) A *= exp2_fast(-__builtin_fmaf(m, c2, -shift));
     }
-    template <int N> __device__ __forceinline__ void of(const float *f, float *g) const {
-        if (plain) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) g[k] = A * exp2_fast(__builtin_fmaf(f[k], c2, -shift));
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k) g[k] = A * exp2_fast((f[k] - m) * c2);
-        }
-    }
+    __device__ __forceinline__ bool plain() const { return fabsf(shift) < kWild; }
+    __device__ __forceinline__ float of(float z) const { return A * exp2_fast(__builtin_fmaf(z, c2, -shift)); }        // where plain()
+    __device__ __forceinline__ float slow(float z) const { return A * exp2_fast(plain() ? __builtin_fmaf(z, c2, -shift) : (z - m) * c2); }
 };
 
-// Vector `first` .. of a row's gradient: as one where no place is marked.
-template <int TYPE> __device__ __forceinline__ void write_vector(typename Elem<TYPE>::T *out, const float *g, uint32_t mk) {
+// A vector of the gradient element by element: those that are in the row and not marked.
+template <int TYPE> __device__ __forceinline__ void write_some(const Row<TYPE> &row, int64_t i, const Dense &d, uint32_t mk, typename Elem<TYPE>::T *out) {
+    constexpr int P = Elem<TYPE>::kPer;
+    for (int k = 0; k < P; ++k) {
+        const int64_t c = i * P + k;
+        if (c < row.n && !(mk >> k & 1)) out[c] = Elem<TYPE>::bits(d.slow(Elem<TYPE>::one(row.p[c])));
+    }
+}
+
+// A piece of the gradient, whose logits v[] holds.  The few vectors with marked places, the one that the row ends in, and all where the row's
+// maximum is wild are read again and written one element after the other.
+template <int TYPE, int T, int NV>
+__device__ __forceinline__ void write_piece(const Row<TYPE> &row, const uint4 (&v)[NV], const Piece<Elem<TYPE>::kPer> &p, const Dense &d,
+                                            const Marks<T, Elem<TYPE>::kPer, uint32_t> &marks, typename Elem<TYPE>::T *out) {
     using E = Elem<TYPE>;
-    if (mk == 0) {
-        const uint4 n = E::narrow(g);
-        typename Row<TYPE>::V4 q = {n.x, n.y, n.z, n.w};
-        *(typename Row<TYPE>::V4 *)out = q;
-    } else {
+    constexpr int P = E::kPer;
+    static_assert(NV <= 32, "a bit for each");
+    const int n = p.own > (int)threadIdx.x ? (p.own - (int)threadIdx.x + T - 1) / T : 0;        // this thread's whole vectors
+    const uint32_t whole = n >= 32 ? ~0u : (1u << n) - 1;
+    uint32_t left = d.plain() ? marks.words[threadIdx.x] & whole : whole;
+    const uint32_t now = whole & ~left;
+    left |= last_vector<T, P, uint32_t>(p);
+    typename E::T *to = out + p.base() + threadIdx.x * P;
+    if (d.plain()) {
 #pragma unroll
-        for (int k = 0; k < E::kPer; ++k) if (!(mk >> k & 1)) out[k] = E::bits(g[k]);
+        for (int j = 0; j < NV; ++j)
+            if (now >> j & 1) {
+                float f[P];
+                E::widen(again(v[j]), f);
+#pragma unroll
+                for (int k = 0; k < P; ++k) f[k] = d.of(f[k]);
+                const uint4 q = E::narrow(f);
+                const typename Row<TYPE>::V4 q4 = {q.x, q.y, q.z, q.w};
+                __builtin_nontemporal_store(q4, (typename Row<TYPE>::V4 *)(to + j * T * P));
+            }
+    }
+    while (left) {
+        const int i = __builtin_ctz(left) * T + threadIdx.x;
+        left &= left - 1;
+        write_some(row, p.v0 + i, d, marks.of(i), out);
     }
 }
 
@@ -313,63 +374,54 @@ __device__ __forceinline__ void write_zeros(typename Elem<TYPE>::T *out, int64_t
     for (int64_t c = begin + whole + threadIdx.x; c < end; c += T) out[c] = 0;
 }
 
+// Loads a piece into registers.
+template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, uint4 (&v)[NV]) {
+    using E = Elem<TYPE>;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if ((j + 1) * T <= p.own) v[j] = row.raw(p.v0 + j * T + threadIdx.x);
+        else {
+            v[j] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+            if (j * T + (int)threadIdx.x < p.own) v[j] = row.raw(p.v0 + j * T + threadIdx.x);
+        }
+    }
+}
+
 // Vectors [piece * T * NV, ..) of a row, from its stat.
 template <int TYPE, int T, int NV>
 __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2, int count, const Stat *__restrict__ stat,
                                                         const float *__restrict__ dloss, void *dZ, int64_t lddz) {
     using E = Elem<TYPE>;
     constexpr int P = E::kPer;
-    __shared__ uint32_t marks[T * NV * P / 32];
+    __shared__ uint32_t bits[T * NV * P / 32], words[T];
     const int64_t r = blockIdx.x / (unsigned)count;
-    const int64_t v0 = (int64_t)(blockIdx.x - r * count) * T * NV, base = v0 * P;
+    const Piece<P> p(a.V, (blockIdx.x - r * count) * T * NV, T * NV);
     const float w = a.weight ? a.weight[r] : 1.f;
     typename E::T *out = (typename E::T *)dZ + r * lddz;
     if (w == 0) {
-        write_zeros<TYPE, T>(out, base, base + T * NV * P < a.V ? base + T * NV * P : a.V);
+        write_zeros<TYPE, T>(out, p.base(), p.base() + p.columns() < a.V ? p.base() + p.columns() : a.V);
         return;
     }
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
-    const int64_t full = a.V / P;
-    const int own = (int)(full - v0 < T * NV ? full - v0 : T * NV);
+    const Marks<T, P, uint32_t> marks{bits, words};
     uint4 v[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int i = j * T + threadIdx.x;
-        v[j] = make_uint4(0, 0, 0, 0);
-        if (i < own) v[j] = row.raw(v0 + i);
-    }
+    hold<TYPE, T>(row, p, v);
     const Entries en(a, r);
-    clear_marks<T>(marks, T * NV * P);
-    set_marks<T>(marks, en, base, T * NV * P);
+    marks.clear(p);
+    marks.set(p, en);
     const Stat s = stat[r];
     const double up = (double)w * a.scale * (dloss ? (double)dloss[r] : 1.0);
-    write_entries<TYPE, T>(row, en, s, up, base, T * NV * P, out);
+    write_entries<TYPE, T>(row, en, s, up, p.base(), p.columns(), out);
     __syncthreads();
-    const Dense d(s, up, c2);
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int i = j * T + threadIdx.x;
-        if (i >= own) continue;
-        float f[P], g[P];
-        E::widen(v[j], f);
-        d.of<P>(f, g);
-        write_vector<TYPE>(out + (v0 + i) * P, g, marks_at<P>(marks, i));
-    }
-    if (a.V % P != 0 && full >= v0 && full < v0 + T * NV && threadIdx.x == 0) {
-        float f[P], g[P];
-        row.load(full, f);
-        d.of<P>(f, g);
-        const uint32_t mk = marks_at<P>(marks, (int)(full - v0));
-        for (int k = 0; k < P; ++k) if (full * P + k < a.V && !(mk >> k & 1)) out[full * P + k] = E::bits(g[k]);
-    }
+    write_piece<TYPE, T>(row, v, p, Dense(s, up, c2), marks, out);
 }
 
 // Loss and gradient of a row that a workgroup holds in registers: Z is read once.
 template <int TYPE, int T, int NV, bool TAIL>
 __global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_step(DistillArgs a, float c2, float *__restrict__ loss, void *dZ, int64_t lddz) {
     using E = Elem<TYPE>;
-    constexpr int P = E::kPer;
-    __shared__ uint32_t marks[T * NV * P / 32];
+    constexpr int P = E::kPer, U = NV < 4 ? NV : 4;
+    __shared__ uint32_t bits[T * NV * P / 32], words[T];
     __shared__ float2 buf[T / kWave];
     __shared__ Taught taught;
     const int64_t r = blockIdx.x;
@@ -381,86 +433,44 @@ __global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_
         return;
     }
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
-    const int full = (int)(a.V / P);
-    const bool ends = a.V % P != 0;
+    const Piece<P> p(a.V, 0, T * NV);
+    const Marks<T, P, uint32_t> marks{bits, words};
     uint4 v[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int i = j * T + threadIdx.x;
-        v[j] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
-        if (i < full) v[j] = row.raw(i);
-    }
+    hold<TYPE, T>(row, p, v);
     const Entries en(a, r);
-    clear_marks<T>(marks, T * NV * P);
-    set_marks<T>(marks, en, 0, T * NV * P);
+    marks.clear(p);
+    marks.set(p, en);
     if (threadIdx.x >= T - kWave) {                              // one wavefront, while the row is on its way
         const Taught t = teach(row, en);
         if (threadIdx.x == T - 1) taught = t;
     }
     __syncthreads();
     Running run;
-    constexpr int U = NV < 4 ? NV : 4;
+    const uint32_t word = TAIL ? words[threadIdx.x] : 0;
 #pragma unroll
     for (int j0 = 0; j0 < NV; j0 += U) {
-        float b = kNegInf;
+        float f[U * P], b = kNegInf;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float f[P];
-            E::widen(again(v[j0 + u]), f);
-            if (TAIL) {
-                const uint32_t mk = marks_at<P>(marks, (j0 + u) * T + threadIdx.x);
-                if (mk) {
-                    leave_out<P>(f, mk);
-                    v[j0 + u] = E::narrow(f);
-                }
-            }
+            if (TAIL && (word >> (j0 + u) & 1)) v[j0 + u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+            E::widen(v[j0 + u], f + u * P);
 #pragma unroll
-            for (int k = 0; k < P; ++k) b = fmaxf(b, f[k]);
+            for (int k = 0; k < P; ++k) b = fmaxf(b, f[u * P + k]);
         }
-        run.raise(b, c2);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[P];
-            E::widen(again(v[j0 + u]), f);
-            run.template add<P>(f, c2);
-        }
+        run.template take<U * P>(f, b, c2);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    float last[P];                                               // the vector that the row ends in: thread 0's
-    uint32_t last_marks = 0;
-    if (ends && threadIdx.x == 0) {
-        float f[P], b = kNegInf;
-        row.load(full, f);
-        last_marks = marks_at<P>(marks, full);
-#pragma unroll
-        for (int k = 0; k < P; ++k) last[k] = f[k];
-        if (TAIL) leave_out<P>(f, last_marks);
-#pragma unroll
-        for (int k = 0; k < P; ++k) b = fmaxf(b, f[k]);
-        run.template take<P>(f, b, c2);
-    }
+    take_some<TYPE, T, TAIL>(run, row, p, word | last_vector<T, P, uint32_t>(p), marks, c2);
     MaxSum d = run.sum(c2);
     block_join<T>(d, c2, buf);
+    if (wild(d.m, c2)) d.s = slow_sum<TYPE, T>(row, 0, a.V, d.m, c2, buf, [&](int64_t c) { return TAIL && marks.at((int)c); });
     const Taught t = taught;
     Stat s;
     const double l = finish(t, d, TAIL, TAIL ? a.tlse[r] : 0.0, a.scale, w, &s);
     if (threadIdx.x == 0) loss[r] = (float)l;
     const double up = (double)w * a.scale;
     write_entries<TYPE, T>(row, en, s, up, 0, a.V, out);
-    const Dense g(s, up, c2);
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int i = j * T + threadIdx.x;
-        if (i >= full) continue;
-        float f[P], o[P];
-        E::widen(again(v[j]), f);
-        g.of<P>(f, o);
-        write_vector<TYPE>(out + (int64_t)i * P, o, marks_at<P>(marks, i));
-    }
-    if (ends && threadIdx.x == 0) {
-        float o[P];
-        g.of<P>(last, o);
-        for (int k = 0; k < P; ++k) if ((int64_t)full * P + k < a.V && !(last_marks >> k & 1)) out[(int64_t)full * P + k] = E::bits(o[k]);
-    }
+    write_piece<TYPE, T>(row, v, p, Dense(s, up, c2), marks, out);
 }
 
 int64_t vectors_of(int type, int64_t V) {

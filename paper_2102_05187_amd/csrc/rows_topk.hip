@@ -109,24 +109,17 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = v[u];
         if (j0 + U < NV) fetch(j0 + U);
-        float b = kNegInf;
+        float f[U * P], b = kNegInf;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            float f[P];
-            E::widen(w[u], f);
-            float t = f[0];
+            E::widen(w[u], f + u * P);
+            float t = f[u * P];
 #pragma unroll
-            for (int k = 1; k < P; ++k) t = fmaxf(t, f[k]);
+            for (int k = 1; k < P; ++k) t = fmaxf(t, f[u * P + k]);
             top[j0 + u] = t;
             b = fmaxf(b, t);
         }
-        run.raise(b, a.c2);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float f[P];
-            E::widen(w[u], f);
-            run.template add<P>(f, a.c2);
-        }
+        run.template take<U * P>(f, b, a.c2);
     }
     if (ends_here && threadIdx.x == 0) {
         float f[P];
@@ -141,6 +134,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     const float least = wave_reduce(m > kNegInf ? m : -kNegInf, -kNegInf, [](float p, float q) { return fminf(p, q); });
     if ((threadIdx.x & (kWave - 1)) == 0) sh.ends[threadIdx.x / kWave] = least;
     block_join<T>(sum, a.c2, sh.buf);                        // also makes tries, found and ends visible
+    if (wild(sum.m, a.c2)) sum.s = slow_sum<TYPE, T>(row, v0 * P, (v0 + T * NV) * P, sum.m, a.c2, sh.buf, [](int64_t) { return false; });
     if (threadIdx.x == 0) {
         if (a.sums) a.sums[piece] = make_float2(sum.m, sum.s);
         else if (a.lse) a.lse[r] = sum.m == -kNegInf ? sum.m : (float)log_sum(sum, a.scale).value();
