@@ -190,6 +190,12 @@ __device__ __forceinline__ Log make_log(double big, double sum) {
 // x - l and exp(x - l); what is -inf stays so, and has the probability 0
 __device__ __forceinline__ double minus(double x, const Log &l) { return x == kNegInfD ? x : (x - l.big) - l.rest; }
 __device__ __forceinline__ double prob(double x, const Log &l) { return x == kNegInfD ? 0.0 : exp((x - l.big) - l.rest); }
+// ln of a 32-bit sum, to about 2^-24 whatever its size: the exponent is taken off first.  0 gives -inf, a NaN itself.
+__device__ __forceinline__ double log_of(float s) {
+    const int e = s >= 0x1p-126f && s < __builtin_huge_valf() ? (int)(__float_as_uint(s) >> 23) - 127 : 0;
+    const float m = __builtin_ldexpf(s, -e);                                   // 1 <= m < 2
+    return ((double)e + (double)__builtin_amdgcn_logf(m)) * 0.6931471805599453;
+}
 // log sum exp(scale z) from the running maximum and sum.  With +inf among the z the differences are NaN, and so is the result.
 __device__ __forceinline__ Log log_sum(const MaxSum &a, double scale) { return make_log((double)a.m * scale, (double)a.s); }
 

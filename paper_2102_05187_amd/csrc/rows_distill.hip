@@ -42,68 +42,88 @@ template <int TYPE> __device__ __forceinline__ double student(const Row<TYPE> &r
     return (double)Elem<TYPE>::one(row.p[c]) * scale;
 }
 
-// What the entries alone give, with ta and xa the largest of the a and of the x:
-//   S = sum exp(a - ta),  D = sum exp(a - ta) ((a - ta) - (x - xa)),  X = sum exp(x - xa)
-struct Taught { double ta, xa, S, D, X; };
+// What the entries alone give.  With ta and xa the largest of the a and of the x,
+//   S = sum exp(a - ta),  D = sum exp(a - ta) ((a - ta) - (x - xa)),  X = sum exp(x - xa),
+// norm the teacher's normaliser (ta + ln S, or tlse) and f = exp(ta - norm):
+struct Taught {
+    Log norm;
+    double xa, X;
+    double mass, rest;                    // f S, and what is missing to 1 where there is a tail
+    double part;                          // the loss but for mass (lse - xa) - rest outside
+};
 
-// By one wavefront.
-template <int TYPE> __device__ Taught teach(const Row<TYPE> &row, const Entries &en) {
+// By one wavefront; the same in all its lanes.  A lane keeps its first entry.
+template <int TYPE> __device__ Taught teach(const Row<TYPE> &row, const Entries &en, bool tail, double tlse) {
     const int lane = threadIdx.x & (kWave - 1);
-    Taught t{kNegInfD, kNegInfD, 0, 0, 0};
+    const int64_t e0 = en.begin + lane;
     int64_t c;
-    for (int64_t e = en.begin + lane; e < en.end; e += kWave)
+    double a0 = kNegInfD, x0 = kNegInfD, ta, xa, S = 0, D = 0, X = 0;
+    const bool own = e0 < en.end && en.at(e0, &c);
+    if (own) a0 = en.a(e0), x0 = student(row, c, en.scale);
+    ta = a0, xa = x0;
+    for (int64_t e = e0 + kWave; e < en.end; e += kWave)
         if (en.at(e, &c)) {
-            t.ta = Max()(t.ta, en.a(e));
-            t.xa = Max()(t.xa, student(row, c, en.scale));
+            ta = Max()(ta, en.a(e));
+            xa = Max()(xa, student(row, c, en.scale));
         }
-    t.ta = wave_reduce(t.ta, kNegInfD, Max());
-    t.xa = wave_reduce(t.xa, kNegInfD, Max());
-    for (int64_t e = en.begin + lane; e < en.end; e += kWave)
-        if (en.at(e, &c)) {
-            const double a = en.a(e), x = student(row, c, en.scale);
-            const double p = a == kNegInfD ? 0.0 : exp(a - t.ta);
-            t.S += p;
-            if (p != 0) t.D += p * ((a - t.ta) - (x == kNegInfD ? x : x - t.xa));
-            t.X += x == kNegInfD ? 0.0 : exp(x - t.xa);
-        }
-    t.S = wave_reduce(t.S, 0.0, Add());
-    t.D = wave_reduce(t.D, 0.0, Add());
-    t.X = wave_reduce(t.X, 0.0, Add());
+    ta = wave_reduce(ta, kNegInfD, Max());
+    xa = wave_reduce(xa, kNegInfD, Max());
+    const auto take = [&](double a, double x) {
+        const double p = a == kNegInfD ? 0.0 : exp(a - ta);
+        S += p;
+        if (p != 0) D += p * ((a - ta) - (x == kNegInfD ? x : x - xa));
+        X += x == kNegInfD ? 0.0 : exp(x - xa);
+    };
+    if (own) take(a0, x0);
+    for (int64_t e = e0 + kWave; e < en.end; e += kWave)
+        if (en.at(e, &c)) take(en.a(e), student(row, c, en.scale));
+    S = wave_reduce(S, 0.0, Add());
+    D = wave_reduce(D, 0.0, Add());
+    X = wave_reduce(X, 0.0, Add());
+    Taught t;
+    const bool some = ta != kNegInfD;                            // an entry has a probability
+    t.xa = xa, t.X = X;
+    t.norm = tail ? Log{tlse, 0.0} : make_log(ta, S);
+    const double f = !some ? 0.0 : tail ? exp(ta - tlse) : 1.0 / S;
+    t.mass = tail ? f * S : some ? 1.0 : 0.0;
+    if (t.norm.big != t.norm.big || S != S) t.mass = t.norm.big + S;            // NaN among the entries
+    t.rest = tail ? 1.0 - t.mass : 0.0;
+    if (t.rest < kNoTailBelow) t.rest = 0.0;
+    t.part = 0;
+    if (some) t.part = f * D + t.mass * ((ta - t.norm.big) - t.norm.rest);
+    if (t.rest != 0) t.part += t.rest * log(t.rest);
     return t;
 }
 
 // Loss of a row (times its weight) and what its gradient needs, from the entries' sums and the dense pass's.
-__device__ double finish(const Taught &t, MaxSum d, bool tail, double tlse, double scale, double w, Stat *out) {
-    const Log dense = log_sum(d, scale);
-    const bool some = t.ta != kNegInfD;                          // an entry has a probability
-    Log norm = make_log(t.ta, t.S), lse = dense;
-    double mass = some ? 1.0 : 0.0, share = mass;                // share: the factor of exp(a - ta)
-    if (tail) {
-        norm = Log{tlse, 0.0};
-        share = some ? exp(t.ta - tlse) : 0.0;
-        mass = tlse != tlse ? tlse : share * t.S;
-        if (t.xa != kNegInfD) {
-            const double m = dense.none() || t.xa != t.xa || t.xa > dense.big ? t.xa : dense.big;
-            lse = make_log(m, t.X * exp(t.xa - m) + (dense.none() ? 0.0 : exp((dense.big - m) + dense.rest)));
-        }
-    } else if (some) share = 1.0 / t.S;
-    double loss = 0;
-    if (some) loss = share * t.D + mass * ((t.ta - norm.big) - norm.rest + (t.xa == kNegInfD ? 0.0 : (lse.big - t.xa) + lse.rest));
-    const double outside = dense.none() ? kNegInfD : (dense.big - lse.big) + (dense.rest - lse.rest);      // log of the dense pass's share
-    double rest = 0;
-    if (tail) {
-        rest = 1.0 - mass;
-        if (rest < kNoTailBelow) rest = 0;
-        if (rest != 0) loss += rest * (log(rest) - outside);
+__device__ __forceinline__ double finish(const Taught &t, MaxSum d, bool tail, double scale, double w, Stat *out) {
+    const double P = t.mass + t.rest, big = (double)d.m * scale;
+    const bool none = d.m == kNegInf;                            // nothing is left for the dense pass
+    Log lse;
+    double tot = d.s, outside = 1;                               // sum of exp(x - lse.big), and of it the factor of the dense pass's sum
+    lse.big = none ? kNegInfD : big;
+    lse.rest = none ? 0.0 : log_of(d.s);
+    double share = none ? kNegInfD : 0.0;                        // log of the dense pass's share
+    if (tail && t.xa != kNegInfD) {
+        const bool dense_first = !none && !(t.xa > big);
+        const float other = none || t.xa != t.xa ? 0.f : exp2_fast((float)((dense_first ? t.xa - big : big - t.xa) * 1.4426950408889634));
+        const double log_s = lse.rest;
+        lse.big = dense_first ? big : t.xa;
+        outside = dense_first ? 1.0 : (double)other;
+        tot = t.X * (dense_first ? (double)other : 1.0) + outside * (none ? 0.0 : (double)d.s);
+        lse.rest = log_of((float)tot);
+        if (!none) share = (big - lse.big) + (log_s - lse.rest);
     }
-    const double P = mass + rest;
+    if (d.s != d.s) lse.big = d.s;
+    double loss = t.part;
+    if (t.mass != 0 && t.xa != kNegInfD) loss += t.mass * ((lse.big - t.xa) + lse.rest);
+    if (t.rest != 0) loss -= t.rest * share;
     out->P = P;
-    out->norm = norm;
+    out->norm = t.norm;
     out->lse = lse;
-    out->m = d.m == kNegInf ? 0.0 : (double)d.m;
-    if (d.m == kNegInf) out->A = d.s != d.s ? (double)d.s : 0.0;   // nothing is left for the dense pass, or it is NaN
-    else out->A = ((tail ? P * exp(outside) : P) - rest) / (double)d.s;
-    const double bad = (lse.big + P) + t.S;                        // NaN and +inf in the row or its entries
+    out->m = none ? 0.0 : (double)d.m;
+    out->A = none ? 0.0 : tail ? P * outside / tot - t.rest / (double)d.s : P / (double)d.s;
+    const double bad = lse.big + P;                              // NaN and +inf in the row or its entries
     if (bad != bad) loss = out->A = bad;
     return w * loss;
 }
@@ -261,9 +281,9 @@ __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, flo
     if (cut.count > 1) {
         if (threadIdx.x == 0) partial[blockIdx.x] = make_float2(d.m, d.s);
     } else if (threadIdx.x < kWave) {
-        const Taught t = teach(row, Entries(a, r));
+        const Taught t = teach(row, Entries(a, r), TAIL, TAIL ? a.tlse[r] : 0.0);
         Stat s;
-        const double l = finish(t, d, TAIL, TAIL ? a.tlse[r] : 0.0, a.scale, w, &s);
+        const double l = finish(t, d, TAIL, a.scale, w, &s);
         if (threadIdx.x == 0) { loss[r] = (float)l; stat[r] = s; }
     }
 }
@@ -286,10 +306,10 @@ __global__ void __launch_bounds__(kThreads) k_distill_finish(DistillArgs a, floa
         d.join(p.x, p.y, c2);
     }
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
-    const Taught t = teach(row, Entries(a, r));
+    const Taught t = teach(row, Entries(a, r), a.tlse != nullptr, a.tlse ? a.tlse[r] : 0.0);
     wave_join(d, c2);
     Stat s;
-    const double l = finish(t, d, a.tlse != nullptr, a.tlse ? a.tlse[r] : 0.0, a.scale, w, &s);
+    const double l = finish(t, d, a.tlse != nullptr, a.scale, w, &s);
     if (lane == 0) { loss[r] = (float)l; stat[r] = s; }
 }
 
@@ -322,13 +342,14 @@ struct Dense {
     __device__ __forceinline__ float slow(float z) const { return A * exp2_fast(plain() ? __builtin_fmaf(z, c2, -shift) : (z - m) * c2); }
 };
 
-// A vector of the gradient element by element: those that are in the row and not marked.
+// Vector i of the gradient element by element: those that are in the row and not marked.
 template <int TYPE> __device__ __forceinline__ void write_some(const Row<TYPE> &row, int64_t i, const Dense &d, uint32_t mk, typename Elem<TYPE>::T *out) {
     constexpr int P = Elem<TYPE>::kPer;
-    for (int k = 0; k < P; ++k) {
-        const int64_t c = i * P + k;
-        if (c < row.n && !(mk >> k & 1)) out[c] = Elem<TYPE>::bits(d.slow(Elem<TYPE>::one(row.p[c])));
-    }
+    float f[P];
+    row.load(i, f);
+#pragma unroll
+    for (int k = 0; k < P; ++k)
+        if (i * P + k < row.n && !(mk >> k & 1)) out[i * P + k] = Elem<TYPE>::bits(d.slow(f[k]));
 }
 
 // A piece of the gradient, whose logits v[] holds.  The few vectors with marked places, the one that the row ends in, and all where the row's
@@ -441,7 +462,7 @@ __global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_
     marks.clear(p);
     marks.set(p, en);
     if (threadIdx.x >= T - kWave) {                              // one wavefront, while the row is on its way
-        const Taught t = teach(row, en);
+        const Taught t = teach(row, en, TAIL, TAIL ? a.tlse[r] : 0.0);
         if (threadIdx.x == T - 1) taught = t;
     }
     __syncthreads();
@@ -466,7 +487,7 @@ __global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_
     if (wild(d.m, c2)) d.s = slow_sum<TYPE, T>(row, 0, a.V, d.m, c2, buf, [&](int64_t c) { return TAIL && marks.at((int)c); });
     const Taught t = taught;
     Stat s;
-    const double l = finish(t, d, TAIL, TAIL ? a.tlse[r] : 0.0, a.scale, w, &s);
+    const double l = finish(t, d, TAIL, a.scale, w, &s);
     if (threadIdx.x == 0) loss[r] = (float)l;
     const double up = (double)w * a.scale;
     write_entries<TYPE, T>(row, en, s, up, 0, a.V, out);
