@@ -1,6 +1,6 @@
 // Beam search: selection over beams and vocabulary, and the reordering of the beams' states.
-#include "rows.hpp"
 #include "rows_kernels.hpp"
+#include "rows_select.hpp"
 
 namespace comet {
 
@@ -8,36 +8,123 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// One workgroup a batch: the n best of the W lists of n keys (each in order), by counting.
-__global__ void __launch_bounds__(kThreads) k_beam_merge(const uint64_t *__restrict__ keys, const Log *__restrict__ logs,
-                                                         const float *__restrict__ score, int W, int n, float *__restrict__ out_score,
-                                                         int32_t *__restrict__ out_parent, int32_t *__restrict__ out_token) {
+// A candidate as a number of 128 bits whose order is that of the candidates: the score; then the lower beam, the larger logit, the lower
+// token.
+__device__ __forceinline__ uint64_t order64(double s) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
+    return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double score_of(uint64_t o) { return __builtin_bit_cast(double, o >> 63 ? o & ~(1ull << 63) : ~o); }
+__device__ __forceinline__ uint64_t rest_of(uint64_t key, int beam) {
+    return (uint64_t)(~beam & 0xff) << 56 | key >> 32 << 24 | ((uint32_t)key & 0xffffff);
+}
+// The score in 32 bits, above -inf.
+__device__ __forceinline__ float rough(uint64_t o) { return fmaxf((float)score_of(o), -3.402823466e38f); }
+
+struct BeamArgs {
+    const uint64_t *keys;                 // [B x W x lists x n], each list in order, 0 where there are fewer
+    const float2 *sums;                   // [B x W x lists]
+    const float *score;
+    int W, lists, n;
+    float *out_score;
+    int32_t *out_parent, *out_token;
+};
+
+// One workgroup a batch: the n best of all its lists' keys, T * PER at most, which the threads hold as scores.
+template <int T, int PER>
+__global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
     __shared__ double big[COMET_MAX_BEAMS], off[COMET_MAX_BEAMS];       // a candidate's score is (z - big) + off
+    __shared__ uint64_t high[kCandidates], low[kCandidates];
+    __shared__ int ranks[2 * kWave], tries[2 * kTries], found;
+    __shared__ float ends[2][T / kWave];
     const int64_t b = blockIdx.x;
-    for (int w = threadIdx.x; w < W; w += kThreads) {
-        big[w] = logs[b * W + w].big;
-        off[w] = (double)score[b * W + w] - logs[b * W + w].rest;
+    const int n = a.n, total = a.W * a.lists * n, per_beam = a.lists * n;
+    const uint64_t *keys = a.keys + b * total;
+    uint64_t key[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int i = j * T + threadIdx.x;
+        key[j] = i < total ? keys[i] : 0;
     }
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        out_score[b * n + i] = kNegInf;
-        out_parent[b * n + i] = -1;
-        out_token[b * n + i] = -1;
-    }
-    __syncthreads();
-    const uint64_t *k = keys + b * W * n;
-    const int total = W * n;
-    for (int i = threadIdx.x; i < total; i += kThreads) {
-        const double s = ((double)value_of_key(k[i]) - big[i / n]) + off[i / n];
-        if (k[i] == 0 || !(s > kNegInfD)) continue;
-        int at = 0;
-        for (int j = 0; j < total && at < n; ++j) {
-            const double t = ((double)value_of_key(k[j]) - big[j / n]) + off[j / n];
-            at += k[j] != 0 && (t > s || (t == s && j < i));
+    for (int w = threadIdx.x; w < a.W; w += T) {
+        MaxSum sum;
+#pragma unroll 4
+        for (int l = 0; l < a.lists; ++l) {
+            const float2 p = a.sums[(b * a.W + w) * a.lists + l];
+            sum.join(p.x, p.y, kLog2e);
         }
-        if (at >= n) continue;
-        out_score[b * n + at] = (float)s;
-        out_parent[b * n + at] = i / n;
-        out_token[b * n + at] = (int32_t)column_of(k[i]);
+        const Log log = log_sum(sum, 1.0);
+        big[w] = log.big;
+        off[w] = (double)a.score[b * a.W + w] - log.rest;
+    }
+    for (int i = threadIdx.x; i < 2 * kTries; i += T) tries[i] = 0;
+    if (threadIdx.x == 0) found = 0;
+    __syncthreads();
+    uint64_t s[PER], most = 0;                                           // orders of the scores, 0: no candidate
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int w = (j * T + (int)threadIdx.x) / per_beam;
+        const double x = key[j] ? ((double)value_of_key(key[j]) - big[w]) + off[w] : kNegInfD;
+        s[j] = x > kNegInfD ? order64(x) : 0;
+        most = s[j] > most ? s[j] : most;
+    }
+    const float mine = most ? rough(most) : kNegInf;
+    const float least = wave_reduce(most ? mine : -kNegInf, -kNegInf, [](float p, float q) { return fminf(p, q); });
+    const float largest = wave_reduce(mine, kNegInf, Larger());
+    if ((threadIdx.x & (kWave - 1)) == 0) ends[0][threadIdx.x / kWave] = least, ends[1][threadIdx.x / kWave] = largest;
+    __syncthreads();
+    float from = ends[0][0], to = ends[1][0];
+#pragma unroll
+    for (int w = 1; w < T / kWave; ++w) from = fminf(from, ends[0][w]), to = fmaxf(to, ends[1][w]);
+    float bar = kNegInf;                                                 // scores below it are out
+    if (to > kNegInf && block_count<T>(most != 0, &tries[kTries]) >= n) {
+        const uint32_t o = most ? order_of(mine) : 0;
+        bar = value_of(bound<T>(order_of(from), order_of(to), n, [&](uint32_t t) { return o >= t; }, tries));
+    }
+    uint64_t bar64 = 0, bar_rest = 0;                                    // ... and those below this one, once it is known
+    for (int pass = 0;; ++pass) {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const uint64_t rest = rest_of(key[j], (j * T + (int)threadIdx.x) / per_beam);
+            if (s[j] && rough(s[j]) >= bar && (s[j] > bar64 || (s[j] == bar64 && rest >= bar_rest))) {
+                const int at = atomicAdd(&found, 1);
+                if (at < kCandidates) high[at] = s[j], low[at] = rest;
+            }
+        }
+        __syncthreads();
+        if (pass == 1 || found <= kCandidates) break;
+        // many equal ones: the n-th largest score exactly, and of the candidates that have it as many as are missing
+        if (threadIdx.x == 0) tries[kTries] = 0;
+        __syncthreads();
+        bar64 = kth<T>(1, order64(1.7976931348623157e308), n, [&](uint64_t t) {
+            int c = 0;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) c += s[j] >= t ? 1 : 0;
+            return c;
+        }, tries + kTries);
+        int above = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) above += s[j] > bar64 ? 1 : 0;
+        above = block_count<T>(above, &tries[kTries]);
+        __syncthreads();
+        if (threadIdx.x == 0) tries[kTries] = 0;
+        __syncthreads();
+        bar_rest = kth<T>(0, ~0ull, n - above, [&](uint64_t t) {
+            int c = 0;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) c += s[j] == bar64 && rest_of(key[j], (j * T + (int)threadIdx.x) / per_beam) >= t ? 1 : 0;
+            return c;
+        }, tries + kTries);
+        if (threadIdx.x == 0) found = 0;
+        __syncthreads();
+    }
+    const int some = found < kCandidates ? found : kCandidates;
+    sort_items<T>(WideKeys{high, low}, some, ranks);
+    for (int i = threadIdx.x; i < n; i += T) {
+        const bool there = i < some;
+        a.out_score[b * n + i] = there ? (float)score_of(high[i]) : kNegInf;
+        a.out_parent[b * n + i] = there ? (int32_t)(~(low[i] >> 56) & 0xff) : -1;
+        a.out_token[b * n + i] = there ? (int32_t)(~(uint32_t)low[i] & 0xffffff) : -1;
     }
 }
 
@@ -69,18 +156,19 @@ __global__ void __launch_bounds__(kThreads) k_beam_reorder(StatePointers states,
 
 }  // namespace
 
-int64_t beam_select_work(int type, int64_t B, int64_t W, int64_t V, int64_t n) {
-    return (B * W * (n * (int64_t)sizeof(uint64_t) + (int64_t)sizeof(Log)) + 15) / 16 * 16 + rows_top_keys_work(type, B * W, V, n);
-}
+int64_t beam_select_work(int type, int64_t B, int64_t W, int64_t V, int64_t n) { return rows_top_lists(type, B * W, V, n, W).bytes; }
 
 hipError_t beam_select(const void *Z, int type, int64_t B, int64_t W, int64_t V, int64_t ldz, const float *score, const uint8_t *finished,
                        int32_t eos, int64_t n, float *out_score, int32_t *out_parent, int32_t *out_token, void *work, hipStream_t st) {
-    Log *lse = (Log *)work;
-    uint64_t *keys = (uint64_t *)(lse + B * W);
-    const hipError_t e = rows_top_keys(Z, type, B * W, V, ldz, n, finished, eos, keys, lse,
-                                     (char *)work + (B * W * (n * (int64_t)sizeof(uint64_t) + (int64_t)sizeof(Log)) + 15) / 16 * 16, st);
+    const TopLists l = rows_top_lists(type, B * W, V, n, W);
+    const hipError_t e = rows_top_keys(Z, type, B * W, V, ldz, n, l, finished, eos, work, st);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_beam_merge, dim3((unsigned)B), dim3(kThreads), 0, st, keys, lse, score, (int)W, (int)n, out_score, out_parent, out_token);
+    const char *lists = (const char *)work + l.at;
+    const BeamArgs a{(const uint64_t *)(lists + l.sums), (const float2 *)lists, score, (int)W, (int)l.lists, (int)n, out_score, out_parent, out_token};
+    const int64_t total = W * l.lists * n;
+    if (total <= 1024) hipLaunchKernelGGL((k_beam_join<256, 4>), dim3((unsigned)B), dim3(256), 0, st, a);
+    else if (total <= 4096) hipLaunchKernelGGL((k_beam_join<512, 8>), dim3((unsigned)B), dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((k_beam_join<1024, 16>), dim3((unsigned)B), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 

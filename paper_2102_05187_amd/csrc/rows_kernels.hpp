@@ -12,10 +12,13 @@ namespace comet {
 int64_t rows_topk_work(int type, int64_t N, int64_t V, int64_t K);
 hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, double scale, int64_t K, bool by_coordinate,
                      int32_t *crd, float *vals, float *lse, void *work, hipStream_t st);
-// The K largest keys of every row, largest first (0 where there are fewer), and its log-sum-exp as a Log (16 bytes); `finished` as in comet_beam_select.
-int64_t rows_top_keys_work(int type, int64_t N, int64_t V, int64_t K);
-hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, const uint8_t *finished, int32_t eos,
-                         uint64_t *keys, void *logs, void *work, hipStream_t st);
+// The K largest keys of every row as `lists` lists of K each (largest first, 0 where there are fewer), with as many running maxima and sums (float2):
+// the sums begin at byte `at` of the work space, the keys `sums` bytes behind them; it takes `bytes`.  A workgroup can join `together` rows'
+// lists afterwards: a row's lists are made one where those would be more than 16384 keys.  `finished` as in comet_beam_select.
+struct TopLists { int64_t lists, at = 0, sums, bytes; bool joined; };
+TopLists rows_top_lists(int type, int64_t N, int64_t V, int64_t K, int64_t together);
+hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, const TopLists &l, const uint8_t *finished, int32_t eos,
+                         void *work, hipStream_t st);
 
 struct DistillArgs {
     const void *Z;

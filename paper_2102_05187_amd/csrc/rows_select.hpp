@@ -48,32 +48,80 @@ template <int T, class COUNT> __device__ __forceinline__ uint32_t bound(uint32_t
     return lo;
 }
 
-// The rank of every key among n in LDS (all different), each counted by one or several threads; ranks[] is LDS too.
-template <int T> __device__ __forceinline__ void rank_keys(const uint64_t *keys, int n, int *ranks) {
-    const int wide = n > 0 ? (n + kWave - 1) & ~(kWave - 1) : kWave;          // threads of one part
-    const int parts = wide >= T ? 1 : T / wide;
-    for (int i = threadIdx.x; i < n; i += T) ranks[i] = 0;
-    __syncthreads();
-    if (parts == 1) {
-        for (int i = threadIdx.x; i < n; i += T) {
-            const uint64_t key = keys[i];
-            int at = 0;
-#pragma unroll 8
-            for (int j = 0; j < n; ++j) at += keys[j] > key;
-            ranks[i] = at;
-        }
-    } else {
+// Things that sort_items() puts in order: plain keys, largest first ...
+struct Keys {
+    using Item = uint64_t;
+    uint64_t *keys;
+    __device__ __forceinline__ Item get(int i) const { return keys[i]; }
+    __device__ __forceinline__ void put(int i, Item v) const { keys[i] = v; }
+    static __device__ __forceinline__ bool before(Item a, Item b) { return a > b; }
+    static __device__ __forceinline__ Item none() { return 0; }
+};
+// ... and keys of 128 bits.
+struct WideKey { uint64_t high, low; };
+struct WideKeys {
+    using Item = WideKey;
+    uint64_t *high, *low;
+    __device__ __forceinline__ Item get(int i) const { return Item{high[i], low[i]}; }
+    __device__ __forceinline__ void put(int i, Item v) const { high[i] = v.high, low[i] = v.low; }
+    static __device__ __forceinline__ bool before(Item a, Item b) { return a.high > b.high || (a.high == b.high && a.low > b.low); }
+    static __device__ __forceinline__ Item none() { return Item{0, 0}; }
+};
+
+// Puts n different items in LDS in order; places up to the next power of two (256 at least where n > 128) are used too.  Few
+// are moved to their rank, counted by several threads each; more go through a bitonic network, whose steps over distances of up to 64
+// stay inside of a wavefront's 128 items and need no barrier.  `ranks`: 128 places.
+template <int T, class S> __device__ __forceinline__ void sort_items(const S &s, int n, int *ranks) {
+    static_assert(T >= 2 * kWave, "ranks are counted by two wavefronts or more");
+    if (n <= 2 * kWave) {
+        const int wide = n <= kWave ? kWave : 2 * kWave, parts = T / wide;     // threads of one part
         const int part = threadIdx.x / wide, i = threadIdx.x - part * wide, per = (n + parts - 1) / parts;
         const int j0 = part * per, j1 = j0 + per < n ? j0 + per : n;
-        if (part < parts && i < n) {
-            const uint64_t key = keys[i];
+        if (threadIdx.x < 2 * kWave) ranks[threadIdx.x] = 0;
+        const typename S::Item mine = i < n ? s.get(i) : S::none();
+        __syncthreads();
+        if (i < n) {
             int at = 0;
-#pragma unroll 8
-            for (int j = j0; j < j1; ++j) at += keys[j] > key;
+#pragma unroll 4
+            for (int j = j0; j < j1; ++j) at += S::before(s.get(j), mine) ? 1 : 0;
             if (at) atomicAdd(&ranks[i], at);
         }
+        __syncthreads();
+        if (part == 0 && i < n) s.put(ranks[i], mine);
+        __syncthreads();
+        return;
+    }
+    int N = 4 * kWave;
+    while (N < n) N *= 2;
+    for (int i = n + threadIdx.x; i < N; i += T) s.put(i, S::none());
+    __syncthreads();
+    for (int k = 2; k <= N; k *= 2)
+        for (int j = k / 2; j > 0; j /= 2) {
+            for (int t = threadIdx.x; t < N / 2; t += T) {
+                const int i = 2 * t - (t & (j - 1)), o = i + j;                // t's pair, j apart
+                const typename S::Item a = s.get(i), b = s.get(o);
+                if (S::before(b, a) == ((i & k) == 0)) { s.put(i, b); s.put(o, a); }
+            }
+            if (j > kWave || (j == 1 && k >= 2 * kWave)) __syncthreads();
+            else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+}
+
+// The K-th largest of different numbers of 64 bits between lo and hi, of which K at least are `lo` or more: COUNT(t) says how many of a thread's
+// are t or more.  `tries` has kTries places that hold 0, and is left so.
+template <int T, class COUNT> __device__ __forceinline__ uint64_t kth(uint64_t lo, uint64_t hi, int K, COUNT count, int *tries) {
+    for (int i = 0; lo < hi; ++i) {
+        const uint64_t mid = lo + (hi - lo) / 2 + 1;
+        const int reach = block_count<T>(count(mid), &tries[i % kTries]);
+        if (threadIdx.x == 0) tries[(i + kTries - 1) % kTries] = 0;            // the one before, which all have read
+        if (reach >= K) lo = mid;
+        else hi = mid - 1;
+        if (reach == K) break;
     }
     __syncthreads();
+    for (int i = threadIdx.x; i < kTries; i += T) tries[i] = 0;
+    __syncthreads();
+    return lo;
 }
 
 }  // namespace comet

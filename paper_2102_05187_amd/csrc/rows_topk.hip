@@ -34,37 +34,29 @@ struct TopArgs {
 
 struct TopShared {
     uint64_t keys[kCandidates];
-    int ranks[kCandidates];
+    int ranks[2 * kWave];
     int tries[2 * kTries];
     float2 buf[16];
     float ends[16];
     int found;
 };
 
-// The keys that were found become the row's result: places 0 .. K-1 of the row, by value or by coordinate.
+// The n keys that were found become the row's result: places 0 .. K-1 of the row, by value or by coordinate.
 template <int T> __device__ __forceinline__ void write_row(TopShared &sh, int n, int K, bool by_coordinate, int32_t *crd, float *vals) {
+    const Keys keys{sh.keys};
     const int kept = n < K ? n : K;
-    rank_keys<T>(sh.keys, n, sh.ranks);
+    sort_items<T>(keys, n, sh.ranks);
     if (by_coordinate) {
         // the kept keys again, with the coordinate as the order: its complement is a key's low half
-        __shared__ uint64_t by_column[COMET_MAX_TOP];
-        for (int i = threadIdx.x; i < n; i += T)
-            if (sh.ranks[i] < K) by_column[sh.ranks[i]] = sh.keys[i] << 32 | sh.keys[i] >> 32;
+        for (int i = threadIdx.x; i < kept; i += T) sh.keys[i] = sh.keys[i] << 32 | sh.keys[i] >> 32;
         __syncthreads();
-        rank_keys<T>(by_column, kept, sh.ranks);
-        for (int i = threadIdx.x; i < kept; i += T) {
-            const uint64_t key = by_column[i] << 32 | by_column[i] >> 32;
-            crd[sh.ranks[i]] = (int32_t)column_of(key);
-            vals[sh.ranks[i]] = value_of_key(key);
-        }
-    } else {
-        for (int i = threadIdx.x; i < n; i += T)
-            if (sh.ranks[i] < K) {
-                crd[sh.ranks[i]] = (int32_t)column_of(sh.keys[i]);
-                vals[sh.ranks[i]] = value_of_key(sh.keys[i]);
-            }
+        sort_items<T>(keys, kept, sh.ranks);
     }
-    for (int i = kept + threadIdx.x; i < K; i += T) crd[i] = -1, vals[i] = kNegInf;
+    for (int i = threadIdx.x; i < K; i += T) {
+        const uint64_t key = by_coordinate ? sh.keys[i] << 32 | sh.keys[i] >> 32 : sh.keys[i];
+        crd[i] = i < kept ? (int32_t)column_of(key) : -1;
+        vals[i] = i < kept ? value_of_key(key) : kNegInf;
+    }
 }
 
 // A piece of a row: vectors [piece * T * NV, ..), vector j of thread t at j * T + t.
@@ -182,20 +174,13 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     __syncthreads();
     int n = sh.found;
     if (n > kCandidates) {
-        // the K-th largest key: all keys are different, so exactly K reach it
-        uint64_t lo = (uint64_t)L << 32, hi = (uint64_t)highest << 32 | 0xffffffffu;
-        for (int i = 0; lo < hi; ++i) {
-            __syncthreads();
-            if (threadIdx.x == 0) sh.tries[kTries + (i + 2) % kTries] = 0;
-            const uint64_t mid = lo + (hi - lo) / 2 + 1;
-            int c = 0;
-            each(value_of((uint32_t)(mid >> 32)), [&](uint64_t key) { c += key >= mid ? 1 : 0; });
-            const int reach = block_count<T>(c, &sh.tries[kTries + (i + 1) % kTries]);
-            if (reach >= K) lo = mid;
-            else hi = mid - 1;
-            if (reach == K) break;
-        }
+        if (threadIdx.x == 0) sh.tries[kTries] = 0;
         __syncthreads();
+        const uint64_t lo = kth<T>((uint64_t)L << 32, (uint64_t)highest << 32 | 0xffffffffu, K, [&](uint64_t t) {
+            int c = 0;
+            each(value_of((uint32_t)(t >> 32)), [&](uint64_t key) { c += key >= t ? 1 : 0; });
+            return c;
+        }, sh.tries + kTries);
         if (threadIdx.x == 0) sh.found = 0;
         __syncthreads();
         each(value_of((uint32_t)(lo >> 32)), [&](uint64_t key) {
@@ -208,79 +193,82 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     }
     // 3
     if (a.keys) {
-        rank_keys<T>(sh.keys, n, sh.ranks);
-        for (int i = threadIdx.x; i < n; i += T)
-            if (sh.ranks[i] < K) a.keys[piece * K + sh.ranks[i]] = sh.keys[i];
-        for (int i = n + threadIdx.x; i < K; i += T) a.keys[piece * K + i] = 0;
+        sort_items<T>(Keys{sh.keys}, n, sh.ranks);
+        for (int i = threadIdx.x; i < K; i += T) a.keys[piece * K + i] = i < n ? sh.keys[i] : 0;
     } else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
 }
 
-// Joins the pieces of a row: `splits` lists of K keys, at most kMerge in all, and as many sums.
-constexpr int kMergeThreads = 1024;
-constexpr int kMergePer = 16;
-constexpr int kMerge = kMergeThreads * kMergePer;
+// Joins the pieces of a row: `splits` lists of K keys, at most T * PER in all, and as many sums.
+constexpr int kMerge = 16384;
 
-__global__ void __launch_bounds__(kMergeThreads) k_topk_merge(TopArgs a, int64_t out_stride, uint64_t *__restrict__ out_keys, Log *__restrict__ logs) {
-    constexpr int T = kMergeThreads;
+template <int T, int PER>
+__global__ void __launch_bounds__(T) k_topk_merge(TopArgs a, uint64_t *__restrict__ out_keys, float2 *__restrict__ out_sums) {
     __shared__ TopShared sh;
     const int64_t r = blockIdx.x;
     const int K = a.K, total = a.splits * K;
     const uint64_t *from = a.keys + r * total;
-    uint64_t key[kMergePer], mine = 0;
+    uint64_t key[PER], most = 0;
 #pragma unroll
-    for (int j = 0; j < kMergePer; ++j) {
+    for (int j = 0; j < PER; ++j) {
         const int i = j * T + threadIdx.x;
         key[j] = i < total ? from[i] : 0;
-        mine = key[j] > mine ? key[j] : mine;
+        most = key[j] > most ? key[j] : most;
     }
-    for (int i = threadIdx.x; i < 2 * kTries; i += T) sh.tries[i] = 0;
-    if (threadIdx.x == 0) sh.found = 0;
     MaxSum sum;
     for (int i = threadIdx.x; i < a.splits; i += T) {
         const float2 p = a.sums[r * a.splits + i];
         sum.join(p.x, p.y, a.c2);
     }
+    for (int i = threadIdx.x; i < 2 * kTries; i += T) sh.tries[i] = 0;
+    if (threadIdx.x == 0) sh.found = 0;
+    const float least = wave_reduce(most ? value_of_key(most) : -kNegInf, -kNegInf, [](float p, float q) { return fminf(p, q); });
+    if ((threadIdx.x & (kWave - 1)) == 0) sh.ends[threadIdx.x / kWave] = least;
     block_join<T>(sum, a.c2, sh.buf);
     if (threadIdx.x == 0) {
-        if (logs) logs[r] = log_sum(sum, a.scale);
+        if (out_sums) out_sums[r] = make_float2(sum.m, sum.s);
         else if (a.lse) a.lse[r] = sum.m == -kNegInf ? sum.m : (float)log_sum(sum, a.scale).value();
     }
+    float low = sh.ends[0];
+#pragma unroll
+    for (int w = 1; w < T / kWave; ++w) low = fminf(low, sh.ends[w]);
     const uint32_t lowest = order_of(kNegInf) + 1, highest = sum.m > kNegInf ? order_of(sum.m) : lowest;
-    const uint32_t top = (uint32_t)(mine >> 32);
-    uint64_t lo = (uint64_t)bound<T>(lowest, highest, K, [&](uint32_t t) { return top >= t; }, sh.tries) << 32;
+    const uint32_t start = sum.m > kNegInf ? order_of(low) : lowest, mine = (uint32_t)(most >> 32);
+    // threads that have a key: fewer than K, and all keys are candidates
+    uint64_t lo = (uint64_t)lowest << 32;
+    if (block_count<T>(mine >= start, &sh.tries[kTries]) >= K)
+        lo = (uint64_t)bound<T>(start, highest, K, [&](uint32_t t) { return mine >= t; }, sh.tries) << 32;
     for (int pass = 0;; ++pass) {
 #pragma unroll
-        for (int j = 0; j < kMergePer; ++j)
+        for (int j = 0; j < PER; ++j)
             if (key[j] && key[j] >= lo) {
                 const int at = atomicAdd(&sh.found, 1);
                 if (at < kCandidates) sh.keys[at] = key[j];
             }
         __syncthreads();
         if (pass == 1 || sh.found <= kCandidates) break;
-        uint64_t hi = (uint64_t)highest << 32 | 0xffffffffu;
-        for (int i = 0; lo < hi; ++i) {
-            __syncthreads();
-            if (threadIdx.x == 0) sh.tries[kTries + (i + 1) % kTries] = 0;
-            const uint64_t mid = lo + (hi - lo) / 2 + 1;
+        if (threadIdx.x == 0) sh.tries[kTries] = 0;
+        __syncthreads();
+        lo = kth<T>(lo, (uint64_t)highest << 32 | 0xffffffffu, K, [&](uint64_t t) {
             int c = 0;
 #pragma unroll
-            for (int j = 0; j < kMergePer; ++j) c += key[j] >= mid ? 1 : 0;
-            const int reach = block_count<T>(c, &sh.tries[kTries + i % kTries]);
-            if (reach >= K) lo = mid;
-            else hi = mid - 1;
-            if (reach == K) break;
-        }
-        __syncthreads();
+            for (int j = 0; j < PER; ++j) c += key[j] >= t ? 1 : 0;
+            return c;
+        }, sh.tries + kTries);
         if (threadIdx.x == 0) sh.found = 0;
         __syncthreads();
     }
     const int n = sh.found < kCandidates ? sh.found : kCandidates;
     if (out_keys) {
-        rank_keys<T>(sh.keys, n, sh.ranks);
-        for (int i = threadIdx.x; i < n; i += T)
-            if (sh.ranks[i] < K) out_keys[r * out_stride + sh.ranks[i]] = sh.keys[i];
-        for (int i = n + threadIdx.x; i < K; i += T) out_keys[r * out_stride + i] = 0;
+        sort_items<T>(Keys{sh.keys}, n, sh.ranks);
+        for (int i = threadIdx.x; i < K; i += T) out_keys[r * K + i] = i < n ? sh.keys[i] : 0;
     } else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
+}
+
+hipError_t merge(const TopArgs &a, int64_t N, uint64_t *out_keys, float2 *out_sums, hipStream_t st) {
+    const int total = a.splits * a.K;
+    if (total <= 2048) hipLaunchKernelGGL((k_topk_merge<256, 8>), dim3((unsigned)N), dim3(256), 0, st, a, out_keys, out_sums);
+    else hipLaunchKernelGGL((k_topk_merge<1024, 16>), dim3((unsigned)N), dim3(1024), 0, st, a, out_keys, out_sums);
+    return hipGetLastError();
 }
 
 // How rows are cut: workgroups of `threads` with `vectors` vectors in each thread's registers, `splits` of them for a row.
@@ -329,24 +317,34 @@ hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz,
     }
     const hipError_t e = launch(type, c, a, N, st);
     if (e != hipSuccess || c.splits == 1) return e;
-    hipLaunchKernelGGL(k_topk_merge, dim3((unsigned)N), dim3(kMergeThreads), 0, st, a, (int64_t)0, (uint64_t *)nullptr, (Log *)nullptr);
-    return hipGetLastError();
+    return merge(a, N, nullptr, nullptr, st);
 }
 
-int64_t rows_top_keys_work(int type, int64_t N, int64_t V, int64_t K) {
-    const Cut c = cut_rows(type, N, V, K);
-    return round16(N * c.splits * (int64_t)sizeof(float2)) + N * c.splits * K * (int64_t)sizeof(uint64_t);
+TopLists rows_top_lists(int type, int64_t N, int64_t V, int64_t K, int64_t together) {
+    TopLists l;
+    l.lists = cut_rows(type, N, V, K).splits;
+    l.joined = l.lists > 1 && together * l.lists * K > kMerge;
+    const int64_t pieces = N * l.lists;
+    l.sums = round16(pieces * (int64_t)sizeof(float2));
+    l.bytes = l.sums + pieces * K * (int64_t)sizeof(uint64_t);
+    if (l.joined) {
+        l.at = round16(l.bytes);
+        l.lists = 1;
+        l.sums = round16(N * (int64_t)sizeof(float2));
+        l.bytes = l.at + l.sums + N * K * (int64_t)sizeof(uint64_t);
+    }
+    return l;
 }
 
-hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, const uint8_t *finished, int32_t eos,
-                         uint64_t *keys, void *logs, void *work, hipStream_t st) {
+hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, const TopLists &l, const uint8_t *finished, int32_t eos,
+                         void *work, hipStream_t st) {
     const Cut c = cut_rows(type, N, V, K);
     const TopArgs a{Z, V, ldz, kLog2e, 1.0, (int)K, c.splits, false, nullptr, nullptr, nullptr, finished, eos,
                     (uint64_t *)((char *)work + round16(N * c.splits * (int64_t)sizeof(float2))), (float2 *)work};
     const hipError_t e = launch(type, c, a, N, st);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(k_topk_merge, dim3((unsigned)N), dim3(kMergeThreads), 0, st, a, K, keys, (Log *)logs);
-    return hipGetLastError();
+    if (e != hipSuccess || !l.joined) return e;
+    char *to = (char *)work + l.at;
+    return merge(a, N, (uint64_t *)(to + l.sums), (float2 *)to, st);
 }
 
 }  // namespace comet

@@ -94,6 +94,18 @@ def test_equal_scores_go_to_the_lower_beam_then_token():
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_thousands_of_equal_scores(dtype):
+    """More candidates with the last selected score than a workgroup keeps: the lower beams and tokens win."""
+    Z = torch.zeros((2, 64, 300), dtype=dtype, device="cuda")
+    c = torch.zeros((2, 64), device="cuda")
+    Z[1, :, 100:] = 1.0
+    Z[1, 40, 7] = 2.0
+    c[1, 3] = -0.5
+    check_select(Z, c, 128)
+    check_select(torch.zeros((1, 16, 70001), dtype=dtype, device="cuda"), torch.zeros((1, 16), device="cuda"), 500)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_strides(dtype):
     Z, c = logits(3, 4, 1010, dtype, seed=4)
     check_select(Z[:, :, 3:1004], c, 8)
