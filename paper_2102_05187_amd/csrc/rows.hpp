@@ -216,6 +216,7 @@ template <class F> __device__ __forceinline__ float wave_reduce(float v, float n
 }
 struct Add { template <class X> __device__ __forceinline__ X operator()(X a, X b) const { return a + b; } };
 struct Larger { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
+struct Smaller { __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); } };
 struct Max { __device__ __forceinline__ double operator()(double a, double b) const { return a != a || a > b ? a : b; } };   // a NaN on the left stays
 
 template <int CTRL, int ROWS> __device__ __forceinline__ double dpp(double none, double v) {

@@ -10,16 +10,11 @@ constexpr int kThreads = 256;
 
 // A candidate as a number of 128 bits whose order is that of the candidates: the score; then the lower beam, the larger logit, the lower
 // token.
-__device__ __forceinline__ uint64_t order64(double s) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);
-    return u >> 63 ? ~u : u | 1ull << 63;
-}
-__device__ __forceinline__ double score_of(uint64_t o) { return __builtin_bit_cast(double, o >> 63 ? o & ~(1ull << 63) : ~o); }
 __device__ __forceinline__ uint64_t rest_of(uint64_t key, int beam) {
     return (uint64_t)(~beam & 0xff) << 56 | key >> 32 << 24 | ((uint32_t)key & 0xffffff);
 }
 // The score in 32 bits, above -inf.
-__device__ __forceinline__ float rough(uint64_t o) { return fmaxf((float)score_of(o), -3.402823466e38f); }
+__device__ __forceinline__ float rough(uint64_t o) { return finite((float)score_of(o)); }
 
 struct BeamArgs {
     const uint64_t *keys;                 // [B x W x lists x n], each list in order, 0 where there are fewer
@@ -35,7 +30,8 @@ template <int T, int PER>
 __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
     __shared__ double big[COMET_MAX_BEAMS], off[COMET_MAX_BEAMS];       // a candidate's score is (z - big) + off
     __shared__ uint64_t high[kCandidates], low[kCandidates];
-    __shared__ int ranks[2 * kWave], tries[2 * kTries], found;
+    __shared__ SortSpace sort;
+    __shared__ int tries[2 * kTries], found;
     __shared__ float ends[2][T / kWave];
     const int64_t b = blockIdx.x;
     const int n = a.n, total = a.W * a.lists * n, per_beam = a.lists * n;
@@ -68,9 +64,9 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
         s[j] = x > kNegInfD ? order64(x) : 0;
         most = s[j] > most ? s[j] : most;
     }
-    const float mine = most ? rough(most) : kNegInf;
-    const float least = wave_reduce(most ? mine : -kNegInf, -kNegInf, [](float p, float q) { return fminf(p, q); });
-    const float largest = wave_reduce(mine, kNegInf, Larger());
+    const float best = most ? rough(most) : kNegInf;
+    const float least = wave_reduce(most ? best : -kNegInf, -kNegInf, Smaller());
+    const float largest = wave_reduce(best, kNegInf, Larger());
     if ((threadIdx.x & (kWave - 1)) == 0) ends[0][threadIdx.x / kWave] = least, ends[1][threadIdx.x / kWave] = largest;
     __syncthreads();
     float from = ends[0][0], to = ends[1][0];
@@ -78,17 +74,24 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
     for (int w = 1; w < T / kWave; ++w) from = fminf(from, ends[0][w]), to = fmaxf(to, ends[1][w]);
     float bar = kNegInf;                                                 // scores below it are out
     if (to > kNegInf && block_count<T>(most != 0, &tries[kTries]) >= n) {
-        const uint32_t o = most ? order_of(mine) : 0;
+        const uint32_t o = most ? order_of(best) : 0;
         bar = value_of(bound<T>(order_of(from), order_of(to), n, [&](uint32_t t) { return o >= t; }, tries));
     }
     uint64_t bar64 = 0, bar_rest = 0;                                    // ... and those below this one, once it is known
     for (int pass = 0;; ++pass) {
+        const auto chosen = [&](int j, uint64_t rest) {
+            return s[j] && rough(s[j]) >= bar && (s[j] > bar64 || (s[j] == bar64 && rest >= bar_rest));
+        };
+        int mine = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) mine += chosen(j, rest_of(key[j], (j * T + (int)threadIdx.x) / per_beam)) ? 1 : 0;
+        int at = append(mine, &found);
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const uint64_t rest = rest_of(key[j], (j * T + (int)threadIdx.x) / per_beam);
-            if (s[j] && rough(s[j]) >= bar && (s[j] > bar64 || (s[j] == bar64 && rest >= bar_rest))) {
-                const int at = atomicAdd(&found, 1);
+            if (chosen(j, rest)) {
                 if (at < kCandidates) high[at] = s[j], low[at] = rest;
+                ++at;
             }
         }
         __syncthreads();
@@ -119,7 +122,7 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
         __syncthreads();
     }
     const int some = found < kCandidates ? found : kCandidates;
-    sort_items<T>(WideKeys{high, low}, some, ranks);
+    sort_items<T>(WideKeys{high, low}, some, sort);
     for (int i = threadIdx.x; i < n; i += T) {
         const bool there = i < some;
         a.out_score[b * n + i] = there ? (float)score_of(high[i]) : kNegInf;
@@ -161,7 +164,7 @@ int64_t beam_select_work(int type, int64_t B, int64_t W, int64_t V, int64_t n) {
 hipError_t beam_select(const void *Z, int type, int64_t B, int64_t W, int64_t V, int64_t ldz, const float *score, const uint8_t *finished,
                        int32_t eos, int64_t n, float *out_score, int32_t *out_parent, int32_t *out_token, void *work, hipStream_t st) {
     const TopLists l = rows_top_lists(type, B * W, V, n, W);
-    const hipError_t e = rows_top_keys(Z, type, B * W, V, ldz, n, l, finished, eos, work, st);
+    const hipError_t e = rows_top_keys(Z, type, B * W, V, ldz, n, W, l, finished, eos, work, st);
     if (e != hipSuccess) return e;
     const char *lists = (const char *)work + l.at;
     const BeamArgs a{(const uint64_t *)(lists + l.sums), (const float2 *)lists, score, (int)W, (int)l.lists, (int)n, out_score, out_parent, out_token};

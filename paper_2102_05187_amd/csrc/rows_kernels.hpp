@@ -17,7 +17,7 @@ hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz,
 // lists afterwards: a row's lists are made one where those would be more than 16384 keys.  `finished` as in comet_beam_select.
 struct TopLists { int64_t lists, at = 0, sums, bytes; bool joined; };
 TopLists rows_top_lists(int type, int64_t N, int64_t V, int64_t K, int64_t together);
-hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, const TopLists &l, const uint8_t *finished, int32_t eos,
+hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, int64_t together, const TopLists &l, const uint8_t *finished, int32_t eos,
                          void *work, hipStream_t st);
 
 struct DistillArgs {

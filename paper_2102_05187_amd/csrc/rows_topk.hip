@@ -34,23 +34,23 @@ struct TopArgs {
 
 struct TopShared {
     uint64_t keys[kCandidates];
-    int ranks[2 * kWave];
+    SortSpace sort;
     int tries[2 * kTries];
     float2 buf[16];
     float ends[16];
-    int found;
+    int found, listed;
 };
 
 // The n keys that were found become the row's result: places 0 .. K-1 of the row, by value or by coordinate.
 template <int T> __device__ __forceinline__ void write_row(TopShared &sh, int n, int K, bool by_coordinate, int32_t *crd, float *vals) {
     const Keys keys{sh.keys};
     const int kept = n < K ? n : K;
-    sort_items<T>(keys, n, sh.ranks);
+    sort_items<T>(keys, n, sh.sort);
     if (by_coordinate) {
         // the kept keys again, with the coordinate as the order: its complement is a key's low half
         for (int i = threadIdx.x; i < kept; i += T) sh.keys[i] = sh.keys[i] << 32 | sh.keys[i] >> 32;
         __syncthreads();
-        sort_items<T>(keys, kept, sh.ranks);
+        sort_items<T>(NumberKeys{sh.keys}, kept, sh.sort);
     }
     for (int i = threadIdx.x; i < K; i += T) {
         const uint64_t key = by_coordinate ? sh.keys[i] << 32 | sh.keys[i] >> 32 : sh.keys[i];
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     const int own = (int)(full - v0 < T * NV ? full - v0 : T * NV);           // whole vectors of this piece
     const bool ends_here = row.n % P != 0 && full >= v0 && full < v0 + T * NV;    // ... and the one that the row ends in: thread 0's
     for (int i = threadIdx.x; i < 2 * kTries; i += T) sh.tries[i] = 0;
-    if (threadIdx.x == 0) sh.found = 0;
+    if (threadIdx.x == 0) sh.found = 0, sh.listed = 0;
     float top[NV], last = kNegInf;                           // `last`: of the row's last, shorter vector
     Running run;
     uint4 v[U];
@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     }
     const float m = run.m;
     MaxSum sum = run.sum(a.c2);
-    const float least = wave_reduce(m > kNegInf ? m : -kNegInf, -kNegInf, [](float p, float q) { return fminf(p, q); });
+    const float least = wave_reduce(m > kNegInf ? m : -kNegInf, -kNegInf, Smaller());
     if ((threadIdx.x & (kWave - 1)) == 0) sh.ends[threadIdx.x / kWave] = least;
     block_join<T>(sum, a.c2, sh.buf);                        // also makes tries, found and ends visible
     if (wild(sum.m, a.c2)) sum.s = slow_sum<TYPE, T>(row, v0 * P, (v0 + T * NV) * P, sum.m, a.c2, sh.buf, [](int64_t) { return false; });
@@ -150,50 +150,122 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
             return n;
         }, sh.tries);
     }
-    // 2: every element from a value (above -inf) on, with its column
+    // 2: every vector with an element from a value (above -inf) on; whole wavefronts, the next vector on its way while one is looked at
     auto each = [&](float from, auto use) {
-        if (!(m >= from)) return;
         uint32_t which = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) which |= top[j] >= from ? 1u << j : 0u;
-        while (which) {
-            const int64_t i = v0 + (__builtin_ctz(which)) * T + threadIdx.x;
-            which &= which - 1;
+        bool end = last >= from;
+        const auto next = [&](int64_t &i, uint4 &x) {
+            i = -1;
+            x = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+            if (which) {
+                i = v0 + __builtin_ctz(which) * T + threadIdx.x;
+                which &= which - 1;
+                x = row.raw(i);
+            } else if (end) {
+                i = full;
+                end = false;
+                float f[P];
+                row.load(full, f);
+                x = E::narrow(f);
+            }
+        };
+        int64_t i, i2;
+        uint4 x, x2;
+        next(i, x);
+        while (__ballot(i >= 0)) {
+            next(i2, x2);
             float f[P];
-            E::widen(row.raw(i), f);
-#pragma unroll
-            for (int k = 0; k < P; ++k) if (f[k] >= from) use(key_of(f[k], (uint32_t)(i * P + k)));
+            E::widen(x, f);
+            use(f, (uint32_t)(i * P));
+            i = i2, x = x2;
         }
-        if (last >= from)
-            for (int64_t c = full * P; c < row.n; ++c) if (E::one(row.p[c]) >= from) use(key_of(E::one(row.p[c]), (uint32_t)c));
     };
-    each(value_of(L), [&](uint64_t key) {
-        const int at = atomicAdd(&sh.found, 1);
-        if (at < kCandidates) sh.keys[at] = key;
-    });
-    __syncthreads();
+    // The elements of a vector from a value and a key on go into LDS.
+    const auto keep = [&](const float *f, uint32_t column, float from, uint64_t least) {
+        int mine = 0;
+#pragma unroll
+        for (int k = 0; k < P; ++k) mine += f[k] >= from && key_of(f[k], column + k) >= least ? 1 : 0;
+        int at = append(mine, &sh.found);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const uint64_t key = key_of(f[k], column + k);
+            if (f[k] >= from && key >= least) {
+                if (at < kCandidates) sh.keys[at] = key;
+                ++at;
+            }
+        }
+    };
+    // The vectors that matter are listed first and then shared out: a thread may hold several of them, and most hold none.
+    const float from = value_of(L);
+    {
+        uint16_t *list = sh.sort.next;
+        uint32_t which = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) which |= top[j] >= from ? 1u << j : 0u;
+        int at = append(__popc(which), &sh.listed);
+        for (; which; which &= which - 1, ++at)
+            if (at < kCandidates) list[at] = (uint16_t)(__builtin_ctz(which) * T + threadIdx.x);
+        __syncthreads();
+        const int listed = sh.listed;
+        if (listed <= kCandidates) {
+            constexpr int A = 2;                             // vectors on their way
+            for (int i0 = 0; i0 < listed; i0 += A * T) {
+                uint4 x[A];
+                uint32_t column[A];
+#pragma unroll
+                for (int q = 0; q < A; ++q) {
+                    const int i = i0 + q * T + threadIdx.x;
+                    x[q] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
+                    column[q] = 0;
+                    if (i < listed) {
+                        column[q] = (uint32_t)((v0 + list[i]) * P);
+                        x[q] = row.raw(v0 + list[i]);
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < A; ++q) {
+                    if (i0 + q * T >= listed) break;
+                    float f[P];
+                    E::widen(x[q], f);
+                    keep(f, column[q], from, 0);
+                }
+            }
+            if (ends_here && threadIdx.x < kWave) {
+                float f[P];
+                row.load(full, f);
+#pragma unroll
+                for (int k = 0; k < P; ++k) f[k] = threadIdx.x == 0 ? f[k] : kNegInf;
+                keep(f, (uint32_t)(full * P), from, 0);
+            }
+        } else if (threadIdx.x == 0) sh.found = kCandidates + 1;
+        __syncthreads();
+    }
     int n = sh.found;
     if (n > kCandidates) {
+        // the K-th largest key: all keys are different, so exactly K reach it
         if (threadIdx.x == 0) sh.tries[kTries] = 0;
         __syncthreads();
         const uint64_t lo = kth<T>((uint64_t)L << 32, (uint64_t)highest << 32 | 0xffffffffu, K, [&](uint64_t t) {
+            const float from = value_of((uint32_t)(t >> 32));
             int c = 0;
-            each(value_of((uint32_t)(t >> 32)), [&](uint64_t key) { c += key >= t ? 1 : 0; });
+            each(from, [&](const float *f, uint32_t column) {
+#pragma unroll
+                for (int k = 0; k < P; ++k) c += f[k] >= from && key_of(f[k], column + k) >= t ? 1 : 0;
+            });
             return c;
         }, sh.tries + kTries);
         if (threadIdx.x == 0) sh.found = 0;
         __syncthreads();
-        each(value_of((uint32_t)(lo >> 32)), [&](uint64_t key) {
-            if (key < lo) return;
-            const int at = atomicAdd(&sh.found, 1);
-            if (at < kCandidates) sh.keys[at] = key;
-        });
+        const float least = value_of((uint32_t)(lo >> 32));
+        each(least, [&](const float *f, uint32_t column) { keep(f, column, least, lo); });
         __syncthreads();
         n = sh.found < kCandidates ? sh.found : kCandidates;
     }
     // 3
     if (a.keys) {
-        sort_items<T>(Keys{sh.keys}, n, sh.ranks);
+        sort_items<T>(Keys{sh.keys}, n, sh.sort);
         for (int i = threadIdx.x; i < K; i += T) a.keys[piece * K + i] = i < n ? sh.keys[i] : 0;
     } else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
 }
@@ -221,7 +293,7 @@ __global__ void __launch_bounds__(T) k_topk_merge(TopArgs a, uint64_t *__restric
     }
     for (int i = threadIdx.x; i < 2 * kTries; i += T) sh.tries[i] = 0;
     if (threadIdx.x == 0) sh.found = 0;
-    const float least = wave_reduce(most ? value_of_key(most) : -kNegInf, -kNegInf, [](float p, float q) { return fminf(p, q); });
+    const float least = wave_reduce(most ? value_of_key(most) : -kNegInf, -kNegInf, Smaller());
     if ((threadIdx.x & (kWave - 1)) == 0) sh.ends[threadIdx.x / kWave] = least;
     block_join<T>(sum, a.c2, sh.buf);
     if (threadIdx.x == 0) {
@@ -238,11 +310,15 @@ __global__ void __launch_bounds__(T) k_topk_merge(TopArgs a, uint64_t *__restric
     if (block_count<T>(mine >= start, &sh.tries[kTries]) >= K)
         lo = (uint64_t)bound<T>(start, highest, K, [&](uint32_t t) { return mine >= t; }, sh.tries) << 32;
     for (int pass = 0;; ++pass) {
+        int chosen = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) chosen += key[j] && key[j] >= lo ? 1 : 0;
+        int at = append(chosen, &sh.found);
 #pragma unroll
         for (int j = 0; j < PER; ++j)
             if (key[j] && key[j] >= lo) {
-                const int at = atomicAdd(&sh.found, 1);
                 if (at < kCandidates) sh.keys[at] = key[j];
+                ++at;
             }
         __syncthreads();
         if (pass == 1 || sh.found <= kCandidates) break;
@@ -259,7 +335,7 @@ __global__ void __launch_bounds__(T) k_topk_merge(TopArgs a, uint64_t *__restric
     }
     const int n = sh.found < kCandidates ? sh.found : kCandidates;
     if (out_keys) {
-        sort_items<T>(Keys{sh.keys}, n, sh.ranks);
+        sort_items<T>(Keys{sh.keys}, n, sh.sort);
         for (int i = threadIdx.x; i < K; i += T) out_keys[r * K + i] = i < n ? sh.keys[i] : 0;
     } else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
 }
@@ -274,14 +350,27 @@ hipError_t merge(const TopArgs &a, int64_t N, uint64_t *out_keys, float2 *out_su
 // How rows are cut: workgroups of `threads` with `vectors` vectors in each thread's registers, `splits` of them for a row.
 struct Cut { int threads, vectors, splits; };
 
-Cut cut_rows(int type, int64_t N, int64_t V, int64_t K) {
+// The smallest piece that holds a row whole; one workgroup takes a row of 16384 vectors in 13 us alone (131072 elements of 16 bits), and a second
+// launch that joins pieces costs 4 to 5 more than pieces save: 16 such rows take 15 us whole and 17 to 25 cut, one row of 32000
+// 32-bit elements 9 whole and 13 or more cut.
+Cut cut_rows(int type, int64_t V) {
     const int64_t per = type == COMET_F32 ? 4 : 8, nv = (V + per - 1) / per;
-    const int sizes[][2] = {{512, 32}, {256, 32}, {256, 16}, {256, 8}, {256, 4}, {256, 2}, {256, 1}};
-    Cut best{0, 0, 0};
+    const int sizes[][2] = {{256, 1}, {256, 2}, {256, 4}, {256, 8}, {256, 16}, {256, 32}, {512, 32}};
+    for (const auto &s : sizes)
+        if (nv <= s[0] * s[1]) return Cut{s[0], s[1], 1};
+    return Cut{512, 32, (int)((nv + 512 * 32 - 1) / (512 * 32))};
+}
+
+// Where a row's pieces are joined with those of other rows anyway, a cut costs nothing: pieces get smaller until 512 of them are there, or
+// `together` rows' lists are more than the 1024 keys that are joined fastest.
+Cut cut_lists(int type, int64_t N, int64_t V, int64_t K, int64_t together) {
+    const int64_t per = type == COMET_F32 ? 4 : 8, nv = (V + per - 1) / per;
+    Cut best = cut_rows(type, V);
+    const int sizes[][2] = {{256, 32}, {256, 16}, {256, 8}, {256, 4}, {256, 2}, {256, 1}};
     for (const auto &s : sizes) {
-        const int64_t piece = (int64_t)s[0] * s[1], splits = nv > piece ? (nv + piece - 1) / piece : 1;
-        // a smaller piece: where it holds the row too, or where the rows' pieces are too few for the device so far
-        if (best.threads && splits > 1 && (N * best.splits >= 256 || splits * K > kMerge || piece * per < 4 * K)) break;
+        const int64_t piece = (int64_t)s[0] * s[1], splits = (nv + piece - 1) / piece;
+        if (piece >= (int64_t)best.threads * best.vectors) continue;
+        if (N * best.splits >= 512 || together * splits * K > 1024) break;
         best = Cut{s[0], s[1], (int)splits};
     }
     return best;
@@ -303,13 +392,13 @@ int64_t round16(int64_t b) { return (b + 15) / 16 * 16; }
 }  // namespace
 
 int64_t rows_topk_work(int type, int64_t N, int64_t V, int64_t K) {
-    const Cut c = cut_rows(type, N, V, K);
+    const Cut c = cut_rows(type, V);
     return c.splits == 1 ? 0 : round16(N * c.splits * (int64_t)sizeof(float2)) + N * c.splits * K * (int64_t)sizeof(uint64_t);
 }
 
 hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, double scale, int64_t K, bool by_coordinate,
                      int32_t *crd, float *vals, float *lse, void *work, hipStream_t st) {
-    const Cut c = cut_rows(type, N, V, K);
+    const Cut c = cut_rows(type, V);
     TopArgs a{Z, V, ldz, (float)(scale * 1.4426950408889634), scale, (int)K, c.splits, by_coordinate, crd, vals, lse, nullptr, 0, nullptr, nullptr};
     if (c.splits > 1) {
         a.sums = (float2 *)work;
@@ -322,7 +411,7 @@ hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz,
 
 TopLists rows_top_lists(int type, int64_t N, int64_t V, int64_t K, int64_t together) {
     TopLists l;
-    l.lists = cut_rows(type, N, V, K).splits;
+    l.lists = cut_lists(type, N, V, K, together).splits;
     l.joined = l.lists > 1 && together * l.lists * K > kMerge;
     const int64_t pieces = N * l.lists;
     l.sums = round16(pieces * (int64_t)sizeof(float2));
@@ -336,9 +425,9 @@ TopLists rows_top_lists(int type, int64_t N, int64_t V, int64_t K, int64_t toget
     return l;
 }
 
-hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, const TopLists &l, const uint8_t *finished, int32_t eos,
+hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, int64_t together, const TopLists &l, const uint8_t *finished, int32_t eos,
                          void *work, hipStream_t st) {
-    const Cut c = cut_rows(type, N, V, K);
+    const Cut c = cut_lists(type, N, V, K, together);
     const TopArgs a{Z, V, ldz, kLog2e, 1.0, (int)K, c.splits, false, nullptr, nullptr, nullptr, finished, eos,
                     (uint64_t *)((char *)work + round16(N * c.splits * (int64_t)sizeof(float2))), (float2 *)work};
     const hipError_t e = launch(type, c, a, N, st);
