@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
     __shared__ double big[COMET_MAX_BEAMS], off[COMET_MAX_BEAMS];       // a candidate's score is (z - big) + off
     __shared__ uint64_t high[kCandidates], low[kCandidates];
     __shared__ SortSpace sort;
-    __shared__ int tries[2 * kTries], found;
+    __shared__ int tries[kTries], found;
     __shared__ float ends[2][T / kWave];
     const int64_t b = blockIdx.x;
     const int n = a.n, total = a.W * a.lists * n, per_beam = a.lists * n;
@@ -49,11 +49,11 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
             const float2 p = a.sums[(b * a.W + w) * a.lists + l];
             sum.join(p.x, p.y, kLog2e);
         }
-        const Log log = log_sum(sum, 1.0);
-        big[w] = log.big;
-        off[w] = (double)a.score[b * a.W + w] - log.rest;
+        big[w] = sum.s != sum.s ? (double)sum.s : (double)sum.m;
+        off[w] = (double)a.score[b * a.W + w] - log_of(sum.s);
     }
-    for (int i = threadIdx.x; i < 2 * kTries; i += T) tries[i] = 0;
+    for (int i = threadIdx.x; i < kBins; i += T) sort.count[i] = 0;
+    if (threadIdx.x < kTries) tries[threadIdx.x] = 0;
     if (threadIdx.x == 0) found = 0;
     __syncthreads();
     uint64_t s[PER], most = 0;                                           // orders of the scores, 0: no candidate
@@ -73,10 +73,7 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
 #pragma unroll
     for (int w = 1; w < T / kWave; ++w) from = fminf(from, ends[0][w]), to = fmaxf(to, ends[1][w]);
     float bar = kNegInf;                                                 // scores below it are out
-    if (to > kNegInf && block_count<T>(most != 0, &tries[kTries]) >= n) {
-        const uint32_t o = most ? order_of(best) : 0;
-        bar = value_of(bound<T>(order_of(from), order_of(to), n, [&](uint32_t t) { return o >= t; }, tries));
-    }
+    if (to > kNegInf) bar = bound<T>(from, to, n, [&](auto f) { if (most) f(best); }, sort.count);
     uint64_t bar64 = 0, bar_rest = 0;                                    // ... and those below this one, once it is known
     for (int pass = 0;; ++pass) {
         const auto chosen = [&](int j, uint64_t rest) {
@@ -97,37 +94,39 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
         __syncthreads();
         if (pass == 1 || found <= kCandidates) break;
         // many equal ones: the n-th largest score exactly, and of the candidates that have it as many as are missing
-        if (threadIdx.x == 0) tries[kTries] = 0;
-        __syncthreads();
         bar64 = kth<T>(1, order64(1.7976931348623157e308), n, [&](uint64_t t) {
             int c = 0;
 #pragma unroll
             for (int j = 0; j < PER; ++j) c += s[j] >= t ? 1 : 0;
             return c;
-        }, tries + kTries);
+        }, tries);
         int above = 0;
 #pragma unroll
         for (int j = 0; j < PER; ++j) above += s[j] > bar64 ? 1 : 0;
-        above = block_count<T>(above, &tries[kTries]);
+        above = block_count<T>(above, &tries[0]);
         __syncthreads();
-        if (threadIdx.x == 0) tries[kTries] = 0;
+        if (threadIdx.x == 0) tries[0] = 0;
         __syncthreads();
         bar_rest = kth<T>(0, ~0ull, n - above, [&](uint64_t t) {
             int c = 0;
 #pragma unroll
             for (int j = 0; j < PER; ++j) c += s[j] == bar64 && rest_of(key[j], (j * T + (int)threadIdx.x) / per_beam) >= t ? 1 : 0;
             return c;
-        }, tries + kTries);
+        }, tries);
         if (threadIdx.x == 0) found = 0;
         __syncthreads();
     }
     const int some = found < kCandidates ? found : kCandidates;
-    sort_items<T>(WideKeys{high, low}, some, sort);
-    for (int i = threadIdx.x; i < n; i += T) {
-        const bool there = i < some;
-        a.out_score[b * n + i] = there ? (float)score_of(high[i]) : kNegInf;
-        a.out_parent[b * n + i] = there ? (int32_t)(~(low[i] >> 56) & 0xff) : -1;
-        a.out_token[b * n + i] = there ? (int32_t)(~(uint32_t)low[i] & 0xffffff) : -1;
+    sort_items<T>(WideKeys{high, low}, some, sort, [&](int rank, const WideKey &c) {
+        if (rank >= n) return;
+        a.out_score[b * n + rank] = (float)score_of(c.high);
+        a.out_parent[b * n + rank] = (int32_t)(~(c.low >> 56) & 0xff);
+        a.out_token[b * n + rank] = (int32_t)(~(uint32_t)c.low & 0xffffff);
+    });
+    for (int i = some + threadIdx.x; i < n; i += T) {
+        a.out_score[b * n + i] = kNegInf;
+        a.out_parent[b * n + i] = -1;
+        a.out_token[b * n + i] = -1;
     }
 }
 

@@ -5,9 +5,9 @@
 // From these:
 //   1. a bound that K to 1.25 K of the threads' largest elements reach (bound()): of a row in no particular order about
 //      K (1 + K / 2T) elements reach it, of T threads; all others are out;
-//   2. the vectors whose largest element reaches it are read again, K or so of them, and their elements that do go into
-//      LDS as 64-bit keys (value, then lower column);
-//   3. the keys are put in order by counting.
+//   2. the vectors whose largest element reaches it are listed and read again, K or so of them, and their elements that do go
+//      into LDS as 64-bit keys (value, then lower column);
+//   3. the keys are put in order (sort_items()).
 // Where more than 2048 reach the bound (equal elements, or the large ones next to each other in a few threads) the K-th largest key is
 // found exactly, by halving, with the vectors that matter read again each time.
 #include "rows_kernels.hpp"
@@ -35,7 +35,7 @@ struct TopArgs {
 struct TopShared {
     uint64_t keys[kCandidates];
     SortSpace sort;
-    int tries[2 * kTries];
+    int tries[kTries];
     float2 buf[16];
     float ends[16];
     int found, listed;
@@ -43,20 +43,35 @@ struct TopShared {
 
 // The n keys that were found become the row's result: places 0 .. K-1 of the row, by value or by coordinate.
 template <int T> __device__ __forceinline__ void write_row(TopShared &sh, int n, int K, bool by_coordinate, int32_t *crd, float *vals) {
-    const Keys keys{sh.keys};
     const int kept = n < K ? n : K;
-    sort_items<T>(keys, n, sh.sort);
     if (by_coordinate) {
         // the kept keys again, with the coordinate as the order: its complement is a key's low half
-        for (int i = threadIdx.x; i < kept; i += T) sh.keys[i] = sh.keys[i] << 32 | sh.keys[i] >> 32;
+        if (n > K || K > kWave) {
+            sort_items<T>(Keys{sh.keys}, n, sh.sort, [&](int rank, uint64_t key) { if (rank < K) sh.keys[rank] = key << 32 | key >> 32; });
+        } else if (threadIdx.x < kWave && (int)threadIdx.x < n) sh.keys[threadIdx.x] = sh.keys[threadIdx.x] << 32 | sh.keys[threadIdx.x] >> 32;
         __syncthreads();
-        sort_items<T>(NumberKeys{sh.keys}, kept, sh.sort);
+        sort_items<T>(NumberKeys{sh.keys}, kept, sh.sort, [&](int rank, uint64_t key) {
+            crd[rank] = (int32_t)column_of(key >> 32);
+            vals[rank] = value_of((uint32_t)key);
+        });
+    } else {
+        sort_items<T>(Keys{sh.keys}, n, sh.sort, [&](int rank, uint64_t key) {
+            if (rank >= K) return;
+            crd[rank] = (int32_t)column_of(key);
+            vals[rank] = value_of_key(key);
+        });
     }
-    for (int i = threadIdx.x; i < K; i += T) {
-        const uint64_t key = by_coordinate ? sh.keys[i] << 32 | sh.keys[i] >> 32 : sh.keys[i];
-        crd[i] = i < kept ? (int32_t)column_of(key) : -1;
-        vals[i] = i < kept ? value_of_key(key) : kNegInf;
-    }
+    for (int i = kept + threadIdx.x; i < K; i += T) crd[i] = -1, vals[i] = kNegInf;
+}
+// ... or a list of K keys, 0 at its end where there are fewer.
+template <int T> __device__ __forceinline__ void write_keys(TopShared &sh, int n, int K, uint64_t *keys) {
+    sort_items<T>(Keys{sh.keys}, n, sh.sort, [&](int rank, uint64_t key) { if (rank < K) keys[rank] = key; });
+    for (int i = n + threadIdx.x; i < K; i += T) keys[i] = 0;
+}
+// A row's log-sum-exp.
+__device__ __forceinline__ float lse_of(const MaxSum &a, double scale) {
+    if (a.m == -kNegInf || (a.m == kNegInf && a.s == a.s)) return a.m;
+    return (float)((double)a.m * scale + log_of(a.s));
 }
 
 // A piece of a row: vectors [piece * T * NV, ..), vector j of thread t at j * T + t.
@@ -76,7 +91,8 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     const int64_t v0 = (int64_t)split * T * NV, full = row.n / P;
     const int own = (int)(full - v0 < T * NV ? full - v0 : T * NV);           // whole vectors of this piece
     const bool ends_here = row.n % P != 0 && full >= v0 && full < v0 + T * NV;    // ... and the one that the row ends in: thread 0's
-    for (int i = threadIdx.x; i < 2 * kTries; i += T) sh.tries[i] = 0;
+    for (int i = threadIdx.x; i < kBins; i += T) sh.sort.count[i] = 0;
+    if (threadIdx.x < kTries) sh.tries[threadIdx.x] = 0;
     if (threadIdx.x == 0) sh.found = 0, sh.listed = 0;
     float top[NV], last = kNegInf;                           // `last`: of the row's last, shorter vector
     Running run;
@@ -123,33 +139,36 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     }
     const float m = run.m;
     MaxSum sum = run.sum(a.c2);
-    const float least = wave_reduce(m > kNegInf ? m : -kNegInf, -kNegInf, Smaller());
+    // 1: the bound, from the threads' largest elements, or those of eighths of their vectors where K is more than half of the threads
+    constexpr int G = NV < 8 ? NV : 8;
+    const bool few = K <= T / 2;
+    const auto numbers = [&](auto f) {
+        if (few) f(m);
+        else {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                float t = top[g];
+#pragma unroll
+                for (int j = g + G; j < NV; j += G) t = fmaxf(t, top[j]);
+                f(t);
+            }
+            f(last);
+        }
+    };
+    float least = -kNegInf;
+    numbers([&](float x) { least = fminf(least, x > kNegInf ? x : -kNegInf); });
+    least = wave_reduce(least, -kNegInf, Smaller());
     if ((threadIdx.x & (kWave - 1)) == 0) sh.ends[threadIdx.x / kWave] = least;
-    block_join<T>(sum, a.c2, sh.buf);                        // also makes tries, found and ends visible
+    block_join<T>(sum, a.c2, sh.buf);                        // also makes bins, tries, found and ends visible
     if (wild(sum.m, a.c2)) sum.s = slow_sum<TYPE, T>(row, v0 * P, (v0 + T * NV) * P, sum.m, a.c2, sh.buf, [](int64_t) { return false; });
     if (threadIdx.x == 0) {
         if (a.sums) a.sums[piece] = make_float2(sum.m, sum.s);
-        else if (a.lse) a.lse[r] = sum.m == -kNegInf ? sum.m : (float)log_sum(sum, a.scale).value();
+        else if (a.lse) a.lse[r] = lse_of(sum, a.scale);
     }
-    // 1: the bound.  `lowest`: nothing that can be kept is below it.
-    const uint32_t lowest = order_of(kNegInf) + 1, highest = sum.m > kNegInf ? order_of(sum.m) : lowest;
-    uint32_t L = lowest;
-    if (K <= T / 2) {
-        float lo = sh.ends[0];
 #pragma unroll
-        for (int w = 1; w < T / kWave; ++w) lo = fminf(lo, sh.ends[w]);
-        // the least of the largest elements; where fewer threads than K have one, everything is a candidate
-        const uint32_t mine = m > kNegInf ? order_of(m) : 0;
-        const uint32_t from = sum.m > kNegInf ? order_of(lo) : lowest;
-        if (block_count<T>(mine >= from, &sh.tries[kTries]) >= K) L = bound<T>(from, highest, K, [&](uint32_t t) { return mine >= t; }, sh.tries);
-    } else if (T * NV * P > kCandidates) {
-        L = bound<T>(lowest, highest, K, [&](uint32_t t) {
-            int n = last >= value_of(t) ? 1 : 0;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) n += top[j] >= value_of(t) ? 1 : 0;
-            return n;
-        }, sh.tries);
-    }
+    for (int w = 0; w < T / kWave; ++w) least = fminf(least, sh.ends[w]);
+    float from = -3.402823466e38f;                           // nothing that can be kept is below it
+    if (sum.m > kNegInf && (few || T * NV * P > kCandidates)) from = bound<T>(least, sum.m, K, [&](auto f) { numbers([&](float x) { if (x > kNegInf) f(x); }); }, sh.sort.count);
     // 2: every vector with an element from a value (above -inf) on; whole wavefronts, the next vector on its way while one is looked at
     auto each = [&](float from, auto use) {
         uint32_t which = 0;
@@ -198,7 +217,6 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
         }
     };
     // The vectors that matter are listed first and then shared out: a thread may hold several of them, and most hold none.
-    const float from = value_of(L);
     {
         uint16_t *list = sh.sort.next;
         uint32_t which = 0;
@@ -245,9 +263,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     int n = sh.found;
     if (n > kCandidates) {
         // the K-th largest key: all keys are different, so exactly K reach it
-        if (threadIdx.x == 0) sh.tries[kTries] = 0;
-        __syncthreads();
-        const uint64_t lo = kth<T>((uint64_t)L << 32, (uint64_t)highest << 32 | 0xffffffffu, K, [&](uint64_t t) {
+        const uint64_t lo = kth<T>((uint64_t)order_of(from) << 32, (uint64_t)order_of(sum.m) << 32 | 0xffffffffu, K, [&](uint64_t t) {
             const float from = value_of((uint32_t)(t >> 32));
             int c = 0;
             each(from, [&](const float *f, uint32_t column) {
@@ -255,7 +271,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
                 for (int k = 0; k < P; ++k) c += f[k] >= from && key_of(f[k], column + k) >= t ? 1 : 0;
             });
             return c;
-        }, sh.tries + kTries);
+        }, sh.tries);
         if (threadIdx.x == 0) sh.found = 0;
         __syncthreads();
         const float least = value_of((uint32_t)(lo >> 32));
@@ -264,10 +280,8 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
         n = sh.found < kCandidates ? sh.found : kCandidates;
     }
     // 3
-    if (a.keys) {
-        sort_items<T>(Keys{sh.keys}, n, sh.sort);
-        for (int i = threadIdx.x; i < K; i += T) a.keys[piece * K + i] = i < n ? sh.keys[i] : 0;
-    } else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
+    if (a.keys) write_keys<T>(sh, n, K, a.keys + piece * K);
+    else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
 }
 
 // Joins the pieces of a row: `splits` lists of K keys, at most T * PER in all, and as many sums.
@@ -291,24 +305,22 @@ __global__ void __launch_bounds__(T) k_topk_merge(TopArgs a, uint64_t *__restric
         const float2 p = a.sums[r * a.splits + i];
         sum.join(p.x, p.y, a.c2);
     }
-    for (int i = threadIdx.x; i < 2 * kTries; i += T) sh.tries[i] = 0;
+    for (int i = threadIdx.x; i < kBins; i += T) sh.sort.count[i] = 0;
+    if (threadIdx.x < kTries) sh.tries[threadIdx.x] = 0;
     if (threadIdx.x == 0) sh.found = 0;
-    const float least = wave_reduce(most ? value_of_key(most) : -kNegInf, -kNegInf, Smaller());
+    const float top = most ? value_of_key(most) : kNegInf;
+    float least = wave_reduce(most ? top : -kNegInf, -kNegInf, Smaller());
     if ((threadIdx.x & (kWave - 1)) == 0) sh.ends[threadIdx.x / kWave] = least;
     block_join<T>(sum, a.c2, sh.buf);
     if (threadIdx.x == 0) {
         if (out_sums) out_sums[r] = make_float2(sum.m, sum.s);
-        else if (a.lse) a.lse[r] = sum.m == -kNegInf ? sum.m : (float)log_sum(sum, a.scale).value();
+        else if (a.lse) a.lse[r] = lse_of(sum, a.scale);
     }
-    float low = sh.ends[0];
 #pragma unroll
-    for (int w = 1; w < T / kWave; ++w) low = fminf(low, sh.ends[w]);
-    const uint32_t lowest = order_of(kNegInf) + 1, highest = sum.m > kNegInf ? order_of(sum.m) : lowest;
-    const uint32_t start = sum.m > kNegInf ? order_of(low) : lowest, mine = (uint32_t)(most >> 32);
-    // threads that have a key: fewer than K, and all keys are candidates
-    uint64_t lo = (uint64_t)lowest << 32;
-    if (block_count<T>(mine >= start, &sh.tries[kTries]) >= K)
-        lo = (uint64_t)bound<T>(start, highest, K, [&](uint32_t t) { return mine >= t; }, sh.tries) << 32;
+    for (int w = 0; w < T / kWave; ++w) least = fminf(least, sh.ends[w]);
+    float bar = -3.402823466e38f;
+    if (sum.m > kNegInf) bar = bound<T>(least, sum.m, K, [&](auto f) { if (most) f(top); }, sh.sort.count);
+    uint64_t lo = (uint64_t)order_of(bar) << 32;
     for (int pass = 0;; ++pass) {
         int chosen = 0;
 #pragma unroll
@@ -322,22 +334,18 @@ __global__ void __launch_bounds__(T) k_topk_merge(TopArgs a, uint64_t *__restric
             }
         __syncthreads();
         if (pass == 1 || sh.found <= kCandidates) break;
-        if (threadIdx.x == 0) sh.tries[kTries] = 0;
-        __syncthreads();
-        lo = kth<T>(lo, (uint64_t)highest << 32 | 0xffffffffu, K, [&](uint64_t t) {
+        lo = kth<T>(lo, (uint64_t)order_of(sum.m) << 32 | 0xffffffffu, K, [&](uint64_t t) {
             int c = 0;
 #pragma unroll
             for (int j = 0; j < PER; ++j) c += key[j] >= t ? 1 : 0;
             return c;
-        }, sh.tries + kTries);
+        }, sh.tries);
         if (threadIdx.x == 0) sh.found = 0;
         __syncthreads();
     }
     const int n = sh.found < kCandidates ? sh.found : kCandidates;
-    if (out_keys) {
-        sort_items<T>(Keys{sh.keys}, n, sh.sort);
-        for (int i = threadIdx.x; i < K; i += T) out_keys[r * K + i] = i < n ? sh.keys[i] : 0;
-    } else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
+    if (out_keys) write_keys<T>(sh, n, K, out_keys + r * K);
+    else write_row<T>(sh, n, K, a.by_coordinate, a.crd + r * K, a.vals + r * K);
 }
 
 hipError_t merge(const TopArgs &a, int64_t N, uint64_t *out_keys, float2 *out_sums, hipStream_t st) {
