@@ -134,21 +134,21 @@ struct WideKeys {
 
 constexpr int kCrowd = 64;                // more than these in one bin: the bins are of no use
 struct SortSpace {
-    int count[kBins];
-    int head[kBins];
-    uint16_t next[kCandidates];
+    int count[kBins];                     // items of a bin, then the items in the bins above it
+    int size[kBins];
+    uint16_t order[kCandidates];          // items bin by bin
     float ends[3][16];
     int crowd;
 };
 
 // Calls emit(rank, item) once for each of n different items in LDS (n <= kCandidates; places up to the next power of two are used too), when
-// all have been read.  Up to 64 are compared with each other by one wavefront.  More are put into 512 bins by their rough value, and
-// compared with the others of their bin; of the largest of many numbers the number falls off exponentially with the value, so the
+// all have been read.  Up to 16 are compared with each other by one wavefront, up to 128 by several threads for each.  More are put
+// into 512 bins by their rough value, and compared with the others of their bin; of the largest of many numbers the number falls off exponentially with the value, so the
 // bins are even in 1 - exp(-(value - least) / mean).  Where the values crowd in a bin (equal ones, outliers), a bitonic network sorts them.
 template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items(const S &s, int n, SortSpace &sp, EMIT emit) {
     constexpr int E = kCandidates / T;                                         // items of a thread
     using Item = typename S::Item;
-    if (n <= kWave) {
+    if (n <= 16) {
         if (threadIdx.x < kWave) {
             const bool there = (int)threadIdx.x < n;
             Item mine{};
@@ -159,7 +159,25 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
         }
         return;
     }
-    for (int i = threadIdx.x; i < kBins; i += T) sp.count[i] = 0, sp.head[i] = -1;
+    if (n <= 2 * kWave) {
+        const int wide = n <= kWave ? kWave : 2 * kWave, parts = T / wide;     // threads of one part
+        const int part = threadIdx.x / wide, i = threadIdx.x - part * wide, per = (n + parts - 1) / parts;
+        const int j0 = part * per, j1 = j0 + per < n ? j0 + per : n;
+        if (threadIdx.x < 2 * kWave) sp.count[threadIdx.x] = 0;
+        Item mine{};
+        if (i < n) mine = s.get(i);
+        __syncthreads();
+        if (i < n) {
+            int at = 0;
+#pragma unroll 4
+            for (int j = j0; j < j1; ++j) at += S::before(s.get(j), mine) ? 1 : 0;
+            if (at) atomicAdd(&sp.count[i], at);
+        }
+        __syncthreads();
+        if (part == 0 && i < n) emit(sp.count[i], mine);
+        return;
+    }
+    for (int i = threadIdx.x; i < kBins; i += T) sp.count[i] = 0;
     if (threadIdx.x == 0) sp.crowd = 0;
     Item mine[E];
     float least = -kNegInf, most = kNegInf, sum = 0.f;
@@ -184,7 +202,7 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
     for (int w = 0; w < T / kWave; ++w) least = fminf(least, sp.ends[0][w]), most = fmaxf(most, sp.ends[1][w]), sum += sp.ends[2][w];
     const float mean = sum * ((float)kCandidates / (float)n) - least;
     const float per = S::kEven ? (float)(kBins - 1) / fmaxf(most - least, 1e-30f) : -kLog2e / fmaxf(mean, 1e-30f);
-    int bin[E];
+    int bin[E], slot[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int i = e * T + threadIdx.x;
@@ -192,8 +210,7 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
         const float x = (S::rough(mine[e]) - least) * per;
         const float b = S::kEven ? x : (float)kBins * (1.f - exp2_fast(x));
         bin[e] = b < (float)(kBins - 1) ? (int)b : kBins - 1;                  // NaN: the last one
-        atomicAdd(&sp.count[bin[e]], 1);
-        sp.next[i] = (uint16_t)atomicExch(&sp.head[bin[e]], i);                // 65535: none
+        slot[e] = atomicAdd(&sp.count[bin[e]], 1);
     }
     __syncthreads();
     if (threadIdx.x < kWave) {                                                 // count[b]: items in the bins above b
@@ -211,7 +228,7 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
         before += __builtin_amdgcn_update_dpp(0, before, 0x143, 0xc, 0xf, false);
         before -= mine_sum;
 #pragma unroll
-        for (int k = 0; k < B; ++k) sp.count[last - k] = before, before += c[k];
+        for (int k = 0; k < B; ++k) sp.count[last - k] = before, sp.size[last - k] = c[k], before += c[k];
         if (crowd) sp.crowd = 1;
     }
     __syncthreads();
@@ -236,9 +253,18 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
+            const int i = e * T + threadIdx.x;
+            if (i >= n) continue;
+            sp.order[sp.count[bin[e]] + slot[e]] = (uint16_t)i;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
             if (e * T + (int)threadIdx.x >= n) continue;
-            int at = sp.count[bin[e]];
-            for (int m = sp.head[bin[e]]; m != 65535; m = sp.next[m]) at += S::before(s.get(m), mine[e]) ? 1 : 0;
+            const int first = sp.count[bin[e]], end = first + sp.size[bin[e]];
+            int at = first;
+#pragma unroll 4
+            for (int p = first; p < end; ++p) at += S::before(s.get(sp.order[p]), mine[e]) ? 1 : 0;
             bin[e] = at;
         }
     }

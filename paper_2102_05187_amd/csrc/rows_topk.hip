@@ -201,24 +201,40 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
             i = i2, x = x2;
         }
     };
-    // The elements of a vector from a value and a key on go into LDS.
-    const auto keep = [&](const float *f, uint32_t column, float from, uint64_t least) {
+    // The elements of a vector that WANTED names go into LDS.
+    const auto keep = [&](const float *f, uint32_t column, auto wanted) {
         int mine = 0;
 #pragma unroll
-        for (int k = 0; k < P; ++k) mine += f[k] >= from && key_of(f[k], column + k) >= least ? 1 : 0;
+        for (int k = 0; k < P; ++k) mine += wanted(f[k], column + k) ? 1 : 0;
+        if (!__ballot(mine != 0)) return;
         int at = append(mine, &sh.found);
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const uint64_t key = key_of(f[k], column + k);
-            if (f[k] >= from && key >= least) {
-                if (at < kCandidates) sh.keys[at] = key;
+        for (int k = 0; k < P; ++k)
+            if (wanted(f[k], column + k)) {
+                if (at < kCandidates) sh.keys[at] = key_of(f[k], column + k);
                 ++at;
             }
-        }
     };
-    // The vectors that matter are listed first and then shared out: a thread may hold several of them, and most hold none.
-    {
-        uint16_t *list = sh.sort.next;
+    const auto reaches = [&](float x, uint32_t) { return x >= from; };
+    // The vectors that matter are listed first and then shared out: a thread may hold several of them, and most hold none.  Of a small
+    // piece all are still in registers.
+    if constexpr (NV <= U) {
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            float f[P];
+            E::widen(v[u], f);
+            keep(f, (uint32_t)((v0 + u * T + threadIdx.x) * P), reaches);
+        }
+        if (ends_here && threadIdx.x < kWave) {
+            float f[P];
+            row.load(full, f);
+#pragma unroll
+            for (int k = 0; k < P; ++k) f[k] = threadIdx.x == 0 ? f[k] : kNegInf;
+            keep(f, (uint32_t)(full * P), reaches);
+        }
+        __syncthreads();
+    } else {
+        uint16_t *list = sh.sort.order;
         uint32_t which = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) which |= top[j] >= from ? 1u << j : 0u;
@@ -247,7 +263,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
                     if (i0 + q * T >= listed) break;
                     float f[P];
                     E::widen(x[q], f);
-                    keep(f, column[q], from, 0);
+                    keep(f, column[q], reaches);
                 }
             }
             if (ends_here && threadIdx.x < kWave) {
@@ -255,7 +271,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
                 row.load(full, f);
 #pragma unroll
                 for (int k = 0; k < P; ++k) f[k] = threadIdx.x == 0 ? f[k] : kNegInf;
-                keep(f, (uint32_t)(full * P), from, 0);
+                keep(f, (uint32_t)(full * P), reaches);
             }
         } else if (threadIdx.x == 0) sh.found = kCandidates + 1;
         __syncthreads();
@@ -275,7 +291,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
         if (threadIdx.x == 0) sh.found = 0;
         __syncthreads();
         const float least = value_of((uint32_t)(lo >> 32));
-        each(least, [&](const float *f, uint32_t column) { keep(f, column, least, lo); });
+        each(least, [&](const float *f, uint32_t column) { keep(f, column, [&](float x, uint32_t c) { return x >= least && key_of(x, c) >= lo; }); });
         __syncthreads();
         n = sh.found < kCandidates ? sh.found : kCandidates;
     }
