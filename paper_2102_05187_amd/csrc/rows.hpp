@@ -90,6 +90,10 @@ template <> struct Elem<COMET_F16> {
 // Vector i holds the elements i * kPer .. of the row wherever the row starts, so that what is computed from a row does not
 // depend on its address.  The device loads and stores 16 bytes at any address: at multiples of 4 as fast as at multiples of
 // 16 (6.6 TB/s over rows of 256 KB), at odd multiples of 2 a fifth slower (5.2 TB/s).
+// Rows of 256 MB and more in all do not stay in the last cache (of that size), and are read past it: top 64 of 2048 x 131072 of 16 bits 100 us
+// through it, 95 past it.  Smaller ones are often there already, or are read again by the gradient: 5 to 11 us of 40 longer past it.
+inline bool read_once(int type, int64_t N, int64_t V) { return N * V * (type == COMET_F32 ? 4 : 2) >= (int64_t(256) << 20); }
+
 typedef uint32_t V4At4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t V4At2 __attribute__((ext_vector_type(4), aligned(2)));
 template <int ALIGN> struct Wide { using type = V4At4; };
@@ -107,6 +111,12 @@ template <int TYPE> struct Row {
     __device__ __forceinline__ bool whole(int64_t i) const { return first(i) + E::kPer <= n; }
     __device__ __forceinline__ uint4 raw(int64_t i) const {
         const V4 v = *(const V4 *)(p + first(i));
+        return make_uint4(v.x, v.y, v.z, v.w);
+    }
+    // the same, past the caches where `once`
+    __device__ __forceinline__ uint4 stream(int64_t i, bool once) const {
+        const V4 *at = (const V4 *)(p + first(i));
+        const V4 v = once ? __builtin_nontemporal_load(at) : *at;
         return make_uint4(v.x, v.y, v.z, v.w);
     }
     // elements of vector i as floats, -inf behind the row's end

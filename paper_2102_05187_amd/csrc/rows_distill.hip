@@ -208,20 +208,20 @@ struct Pieces {                           // how a row is cut: `count` pieces of
 // one that the row ends in, are read again at the end, in part.  `mark` sets the marks, once the first loads are on their way.
 template <int TYPE, int T, bool TAIL, class WORD, class MARK>
 __device__ __forceinline__ MaxSum read_piece(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, const Marks<T, Elem<TYPE>::kPer, WORD> &marks,
-                                             float c2, float2 *buf, MARK mark) {
+                                             float c2, bool once, float2 *buf, MARK mark) {
     using E = Elem<TYPE>;
     constexpr int P = E::kPer, U = kAhead;
     uint4 v[U];
     auto fetch = [&](int i0) {
         if (i0 + U * T <= p.own) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = row.raw(p.v0 + i0 + u * T + threadIdx.x);
+            for (int u = 0; u < U; ++u) v[u] = row.stream(p.v0 + i0 + u * T + threadIdx.x, once);
         } else {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * T + threadIdx.x;
                 v[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
-                if (i < p.own) v[u] = row.raw(p.v0 + i);
+                if (i < p.own) v[u] = row.stream(p.v0 + i, once);
             }
         }
     };
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, flo
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
     const Piece<P> p(a.V, (blockIdx.x - r * cut.count) * cut.vectors, cut.vectors);
     const Marks<T, P, uint64_t> marks{bits, words};
-    const MaxSum d = read_piece<TYPE, T, TAIL>(row, p, marks, c2, buf, [&] {
+    const MaxSum d = read_piece<TYPE, T, TAIL>(row, p, marks, c2, a.once, buf, [&] {
         if (!TAIL) return;
         marks.clear(p);
         marks.set(p, Entries(a, r));
@@ -396,14 +396,14 @@ __device__ __forceinline__ void write_zeros(typename Elem<TYPE>::T *out, int64_t
 }
 
 // Loads a piece into registers.
-template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, uint4 (&v)[NV]) {
+template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, bool once, uint4 (&v)[NV]) {
     using E = Elem<TYPE>;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        if ((j + 1) * T <= p.own) v[j] = row.raw(p.v0 + j * T + threadIdx.x);
+        if ((j + 1) * T <= p.own) v[j] = row.stream(p.v0 + j * T + threadIdx.x, once);
         else {
             v[j] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
-            if (j * T + (int)threadIdx.x < p.own) v[j] = row.raw(p.v0 + j * T + threadIdx.x);
+            if (j * T + (int)threadIdx.x < p.own) v[j] = row.stream(p.v0 + j * T + threadIdx.x, once);
         }
     }
 }
@@ -426,7 +426,7 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
     const Marks<T, P, uint32_t> marks{bits, words};
     uint4 v[NV];
-    hold<TYPE, T>(row, p, v);
+    hold<TYPE, T>(row, p, a.once, v);
     const Entries en(a, r);
     marks.clear(p);
     marks.set(p, en);
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_
     const Piece<P> p(a.V, 0, T * NV);
     const Marks<T, P, uint32_t> marks{bits, words};
     uint4 v[NV];
-    hold<TYPE, T>(row, p, v);
+    hold<TYPE, T>(row, p, a.once, v);
     const Entries en(a, r);
     marks.clear(p);
     marks.set(p, en);
@@ -525,9 +525,9 @@ template <int TYPE> hipError_t forward(const DistillArgs &a, float c2, const Pie
 
 template <int TYPE> hipError_t backward(const DistillArgs &a, float c2, const Stat *stat, const float *dloss, void *dZ, int64_t lddz, hipStream_t st) {
     const int64_t nv = vectors_of(TYPE, a.V);
-    const bool big = a.N * ((nv + 2047) / 2048) >= 512;
-    const int64_t piece = big ? 2048 : 512, count = (nv + piece - 1) / piece;
-    const auto kernel = big ? k_distill_backward<TYPE, 256, 8> : k_distill_backward<TYPE, 256, 2>;
+    const bool big = a.N * ((nv + 1023) / 1024) >= 512;
+    const int64_t piece = big ? 1024 : 512, count = (nv + piece - 1) / piece;
+    const auto kernel = big ? k_distill_backward<TYPE, 256, 4> : k_distill_backward<TYPE, 256, 2>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.N * count)), dim3(256), 0, st, a, c2, (int)count, stat, dloss, dZ, lddz);
     return hipGetLastError();
 }
@@ -554,7 +554,9 @@ int64_t distill_work(int type, int64_t N, int64_t V) {
     return round16(N * (int64_t)sizeof(Stat)) + partial_bytes(cut_forward(type, N, V), N);
 }
 
-hipError_t distill_forward(const DistillArgs &a, float *loss, double *stat, void *work, hipStream_t st) {
+hipError_t distill_forward(const DistillArgs &given, float *loss, double *stat, void *work, hipStream_t st) {
+    DistillArgs a = given;
+    a.once = read_once(a.type, a.N, a.V);
     const float c2 = log2_scale(a);
     const Pieces c = cut_forward(a.type, a.N, a.V);
     float2 *partial = (float2 *)((char *)work + round16(a.N * (int64_t)sizeof(Stat)));
@@ -563,14 +565,18 @@ hipError_t distill_forward(const DistillArgs &a, float *loss, double *stat, void
                                 : forward<COMET_F16>(a, c2, c, loss, (Stat *)stat, partial, st);
 }
 
-hipError_t distill_backward(const DistillArgs &a, const double *stat, const float *dloss, void *dZ, int64_t lddz, hipStream_t st) {
+hipError_t distill_backward(const DistillArgs &given, const double *stat, const float *dloss, void *dZ, int64_t lddz, hipStream_t st) {
+    DistillArgs a = given;
+    a.once = read_once(a.type, a.N, a.V);
     const float c2 = log2_scale(a);
     return a.type == COMET_F32 ? backward<COMET_F32>(a, c2, (const Stat *)stat, dloss, dZ, lddz, st)
          : a.type == COMET_BF16 ? backward<COMET_BF16>(a, c2, (const Stat *)stat, dloss, dZ, lddz, st)
                                 : backward<COMET_F16>(a, c2, (const Stat *)stat, dloss, dZ, lddz, st);
 }
 
-hipError_t distill_step(const DistillArgs &a, float *loss, void *dZ, int64_t lddz, void *work, hipStream_t st) {
+hipError_t distill_step(const DistillArgs &given, float *loss, void *dZ, int64_t lddz, void *work, hipStream_t st) {
+    DistillArgs a = given;
+    a.once = read_once(a.type, a.N, a.V);
     const int64_t nv = vectors_of(a.type, a.V);
     if (nv <= 512 * 32 && (a.N >= 64 || nv <= 2048)) {
         const float c2 = log2_scale(a);

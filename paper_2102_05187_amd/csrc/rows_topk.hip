@@ -23,7 +23,7 @@ struct TopArgs {
     float c2;                             // scale log2(e)
     double scale;
     int K, splits;
-    bool by_coordinate;
+    bool by_coordinate, once;
     int32_t *crd;                         // results, where a row is one piece and no keys are asked for
     float *vals, *lse;
     const uint8_t *finished;
@@ -100,13 +100,13 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     auto fetch = [&](int j0) {
         if ((j0 + U) * T <= own) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = row.raw(v0 + (j0 + u) * T + threadIdx.x);
+            for (int u = 0; u < U; ++u) v[u] = row.stream(v0 + (j0 + u) * T + threadIdx.x, a.once);
         } else {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = (j0 + u) * T + threadIdx.x;
                 v[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
-                if (i < own) v[u] = row.raw(v0 + i);
+                if (i < own) v[u] = row.stream(v0 + i, a.once);
             }
         }
     };
@@ -423,7 +423,7 @@ int64_t rows_topk_work(int type, int64_t N, int64_t V, int64_t K) {
 hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, double scale, int64_t K, bool by_coordinate,
                      int32_t *crd, float *vals, float *lse, void *work, hipStream_t st) {
     const Cut c = cut_rows(type, V);
-    TopArgs a{Z, V, ldz, (float)(scale * 1.4426950408889634), scale, (int)K, c.splits, by_coordinate, crd, vals, lse, nullptr, 0, nullptr, nullptr};
+    TopArgs a{Z, V, ldz, (float)(scale * 1.4426950408889634), scale, (int)K, c.splits, by_coordinate, read_once(type, N, V), crd, vals, lse, nullptr, 0, nullptr, nullptr};
     if (c.splits > 1) {
         a.sums = (float2 *)work;
         a.keys = (uint64_t *)((char *)work + round16(N * c.splits * (int64_t)sizeof(float2)));
@@ -452,7 +452,7 @@ TopLists rows_top_lists(int type, int64_t N, int64_t V, int64_t K, int64_t toget
 hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, int64_t together, const TopLists &l, const uint8_t *finished, int32_t eos,
                          void *work, hipStream_t st) {
     const Cut c = cut_lists(type, N, V, K, together);
-    const TopArgs a{Z, V, ldz, kLog2e, 1.0, (int)K, c.splits, false, nullptr, nullptr, nullptr, finished, eos,
+    const TopArgs a{Z, V, ldz, kLog2e, 1.0, (int)K, c.splits, false, read_once(type, N, V), nullptr, nullptr, nullptr, finished, eos,
                     (uint64_t *)((char *)work + round16(N * c.splits * (int64_t)sizeof(float2))), (float2 *)work};
     const hipError_t e = launch(type, c, a, N, st);
     if (e != hipSuccess || !l.joined) return e;
