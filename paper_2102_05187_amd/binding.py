@@ -9,6 +9,7 @@ the import of this module's functions fails with an error that says how to build
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -503,6 +504,13 @@ def _new(t: Optional[torch.Tensor], dtype, shape, what: str, device, stream) -> 
     return t
 
 
+@functools.lru_cache(maxsize=1024)
+def _work_bytes(call: str, *sizes) -> int:
+    need = ctypes.c_int64(0)
+    _check(getattr(_lib(), call + "_work")(*sizes, ctypes.byref(need)), call)
+    return need.value
+
+
 def _work(need: int, device, stream):
     """(tensor, pointer) of scratch for one call: its memory goes back to torch's allocator, which keeps it for the stream."""
     if need == 0:
@@ -516,14 +524,13 @@ def comet_rows_topk(Z: torch.Tensor, K: int, scale: float = 1.0, by_coordinate: 
     """(crd, vals, lse): the K largest elements of every row of Z and log sum exp(scale * row)."""
     ptr, kind, N, V, ld = _rows(Z)
     K, dev = int(K), Z.device
-    need = ctypes.c_int64(0)
-    _check(_lib().comet_rows_topk_work(kind, N, V, K, ctypes.byref(need)), "comet_rows_topk")
+    need = _work_bytes("comet_rows_topk", kind, N, V, K)
     crd = _new(crd, torch.int32, (N, K), "crd", dev, stream)
     vals = _new(vals, torch.float32, (N, K), "vals", dev, stream)
     lse = _new(lse, torch.float32, (N,), "lse", dev, stream)
-    work, wptr = _work(need.value, dev, stream)
+    work, wptr = _work(need, dev, stream)
     _check(_lib().comet_rows_topk(ptr, kind, N, V, ld, float(scale), K, COMET_BY_COORDINATE if by_coordinate else 0, crd.data_ptr(),
-                                  vals.data_ptr(), lse.data_ptr(), wptr, need.value, _stream(stream)), "comet_rows_topk")
+                                  vals.data_ptr(), lse.data_ptr(), wptr, need, _stream(stream)), "comet_rows_topk")
     return crd, vals, lse
 
 
@@ -552,12 +559,11 @@ def comet_distill_forward(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tenso
                           loss: Optional[torch.Tensor] = None, stat: Optional[torch.Tensor] = None, stream=None):
     """(loss, stat): the loss of every row, and what comet_distill_backward needs of it."""
     N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
-    need = ctypes.c_int64(0)
-    _check(_lib().comet_distill_work(kind, N, V, ctypes.byref(need)), "comet_distill_forward")
+    need = _work_bytes("comet_distill", kind, N, V)
     loss = _new(loss, torch.float32, (N,), "loss", dev, stream)
     stat = _new(stat, torch.float64, (N, COMET_DISTILL_STAT), "stat", dev, stream)
-    work, wptr = _work(need.value, dev, stream)
-    _check(_lib().comet_distill_forward(*args, loss.data_ptr(), stat.data_ptr(), wptr, need.value, _stream(stream)), "comet_distill_forward")
+    work, wptr = _work(need, dev, stream)
+    _check(_lib().comet_distill_forward(*args, loss.data_ptr(), stat.data_ptr(), wptr, need, _stream(stream)), "comet_distill_forward")
     return loss, stat
 
 
@@ -587,12 +593,11 @@ def comet_distill_step(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tensor, 
                        loss: Optional[torch.Tensor] = None, dZ: Optional[torch.Tensor] = None, stream=None):
     """(loss, dZ): both at once, for a training step that knows its rows' weights; dZ may be Z itself."""
     N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
-    need = ctypes.c_int64(0)
-    _check(_lib().comet_distill_work(kind, N, V, ctypes.byref(need)), "comet_distill_step")
+    need = _work_bytes("comet_distill", kind, N, V)
     loss = _new(loss, torch.float32, (N,), "loss", dev, stream)
     dZ, out, ldo = _gradient(Z, dZ, stream)
-    work, wptr = _work(need.value, dev, stream)
-    _check(_lib().comet_distill_step(*args, loss.data_ptr(), out, ldo, wptr, need.value, _stream(stream)), "comet_distill_step")
+    work, wptr = _work(need, dev, stream)
+    _check(_lib().comet_distill_step(*args, loss.data_ptr(), out, ldo, wptr, need, _stream(stream)), "comet_distill_step")
     return loss, dZ
 
 
@@ -610,31 +615,29 @@ def comet_beam_select(Z: torch.Tensor, score: torch.Tensor, n: int, finished: Op
         if isinstance(finished, torch.Tensor) and finished.dtype == torch.bool:
             finished = finished.view(torch.uint8)
         _given(finished, torch.uint8, (B, W), "finished", dev)
-    need = ctypes.c_int64(0)
-    _check(_lib().comet_beam_select_work(kind, B, W, V, n, ctypes.byref(need)), "comet_beam_select")
+    need = _work_bytes("comet_beam_select", kind, B, W, V, n)
     best = _new(None, torch.float32, (B, n), "score", dev, stream)
     parent = _new(None, torch.int32, (B, n), "parent", dev, stream)
     token = _new(None, torch.int32, (B, n), "token", dev, stream)
-    work, wptr = _work(need.value, dev, stream)
+    work, wptr = _work(need, dev, stream)
     _check(_lib().comet_beam_select(ptr, kind, B, W, V, ld, score.data_ptr(), _ptr(finished), int(eos), n, best.data_ptr(), parent.data_ptr(),
-                                    token.data_ptr(), wptr, need.value, _stream(stream)), "comet_beam_select")
+                                    token.data_ptr(), wptr, need, _stream(stream)), "comet_beam_select")
     return best, parent, token
 
 
-def _pieces(t: torch.Tensor):
-    """(outer, outer_stride, inner) in bytes of what a beam holds: the dimensions behind the first two as equal pieces."""
-    size, dims = t.element_size(), [(n, s) for n, s in zip(t.shape[2:], t.stride()[2:]) if n != 1]
+@functools.lru_cache(maxsize=256)
+def _pieces(shape, strides, size):
+    """The layout of [B, W, ...] states in bytes: strides of batch and beam, and what a beam holds as equal pieces (number, distance, length)."""
+    dims = [(n, s) for n, s in zip(shape[2:], strides[2:]) if n != 1]
     inner = 1
     while dims and dims[-1][1] == inner:
         inner *= dims.pop()[0]
-    if not dims:
-        return 1, 0, inner * size
-    outer, stride = dims.pop()
+    outer, stride = dims.pop() if dims else (1, 0)
     while dims and dims[-1][1] == outer * stride:
         outer *= dims.pop()[0]
     if dims:
         raise ValueError("a state's beam must be pieces of one length at one distance")
-    return outer, stride * size, inner * size
+    return strides[0] * size, strides[1] * size, outer, stride * size, inner * size
 
 
 def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, stream=None) -> None:
@@ -647,17 +650,14 @@ def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, str
     for t in states:
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise TypeError("states must be torch tensors in device memory")
-        if t.dim() < 2 or t.shape[0] != B or t.shape[1] != W:
-            raise ValueError("a state must have shape [%d, %d, ...], got %s" % (B, W, tuple(t.shape)))
-        if t.device != parent.device:
+        groups.setdefault((t.shape, t.stride(), t.dtype, t.device), []).append(t.data_ptr())
+    for (shape, strides, dtype, device), ptrs in groups.items():
+        if len(shape) < 2 or shape[0] != B or shape[1] != W:
+            raise ValueError("a state must have shape [%d, %d, ...], got %s" % (B, W, tuple(shape)))
+        if device != parent.device:
             raise ValueError("states must be on %s" % parent.device)
-        groups.setdefault((t.dtype, t.shape, t.stride()), []).append(t)
-    for group in groups.values():
-        t = group[0]
-        if t.numel() == 0:
-            continue
-        size = t.element_size()
-        outer, outer_stride, inner = _pieces(t)
-        ptrs = (ctypes.c_void_p * len(group))(*[x.data_ptr() for x in group])
-        _check(_lib().comet_beam_reorder(ptrs, len(group), B, W, t.stride(0) * size, t.stride(1) * size, outer, outer_stride, inner,
-                                         parent.data_ptr(), _stream(stream)), "comet_beam_reorder")
+    lib, st = _lib(), _stream(stream)
+    for (shape, strides, dtype, device), ptrs in groups.items():
+        if 0 not in shape:
+            layout = _pieces(shape, strides, dtype.itemsize)
+            _check(lib.comet_beam_reorder((ctypes.c_void_p * len(ptrs))(*ptrs), len(ptrs), B, W, *layout, parent.data_ptr(), st), "comet_beam_reorder")

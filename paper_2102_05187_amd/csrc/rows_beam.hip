@@ -6,8 +6,6 @@ namespace comet {
 
 namespace {
 
-constexpr int kThreads = 256;
-
 // A candidate as a number of 128 bits whose order is that of the candidates: the score; then the lower beam, the larger logit, the lower
 // token.
 __device__ __forceinline__ uint64_t rest_of(uint64_t key, int beam) {
@@ -133,9 +131,20 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
 constexpr int kStates = 64;               // state arrays of one launch
 struct StatePointers { char *p[kStates]; };
 
-// A thread moves the same unit of all beams of a batch: all are read into LDS before the first is written.
+template <class U> __device__ __forceinline__ void put_once(char *to, const U &u) { *(U *)to = u; }
+template <> __device__ __forceinline__ void put_once<uint4>(char *to, const uint4 &u) {
+    typedef uint32_t v4 __attribute__((ext_vector_type(4)));
+    const v4 v = {u.x, u.y, u.z, u.w};
+    __builtin_nontemporal_store(v, (v4 *)to);
+}
+
+// A thread moves the same unit of all beams of a batch: all are read into LDS before the first is written.  Bound by memory; what it has in
+// flight is set by LDS, and less of it is better than more: beams lie at large powers of two from each other, and the more of their
+// rows are open at once the worse.  8 batches of 8 beams, 5 of them moved, 4.7 GB read and written: 128 threads (16 KB) with stores past the
+// caches 803 us, 256 threads 820, 512 threads 854, stores through the caches 823, units in registers at full occupancy 921.
+constexpr int kMoveThreads = 128;
 template <class U>
-__global__ void __launch_bounds__(kThreads) k_beam_reorder(StatePointers states, StateLayout l, const int32_t *__restrict__ parent) {
+__global__ void __launch_bounds__(kMoveThreads) k_beam_reorder(StatePointers states, StateLayout l, const int32_t *__restrict__ parent) {
     extern __shared__ __align__(16) char raw[];
     U *tile = (U *)raw + threadIdx.x;
     const int W = (int)l.W, T = blockDim.x;
@@ -143,7 +152,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_reorder(StatePointers states,
     char *base = states.p[blockIdx.z] + b * l.batch_stride;
     const int32_t *par = parent + b * W;
     for (int64_t u = (int64_t)blockIdx.x * T + threadIdx.x; u < all; u += (int64_t)gridDim.x * T) {
-        const int64_t o = u / units;
+        const int64_t o = l.outer == 1 ? 0 : u / units;
         char *at = base + o * l.outer_stride + (u - o * units) * (int64_t)sizeof(U);
         for (int w = 0; w < W; ++w) {
             const int p = par[w];
@@ -151,7 +160,7 @@ __global__ void __launch_bounds__(kThreads) k_beam_reorder(StatePointers states,
         }
         for (int w = 0; w < W; ++w) {
             const int p = par[w];
-            if (p >= 0 && p < W && p != w) *(U *)(at + w * l.beam_stride) = tile[w * T];
+            if (p >= 0 && p < W && p != w) put_once<U>(at + w * l.beam_stride, tile[w * T]);
         }
     }
 }
@@ -185,8 +194,7 @@ hipError_t beam_reorder(void *const *states, int64_t nstates, const StateLayout 
     while (kWave * unit * l.W > 65536) unit /= 2;            // one wavefront's tile fits into LDS: 4 bytes at 256 beams
     const auto kernel = unit == 16 ? k_beam_reorder<uint4> : unit == 8 ? k_beam_reorder<uint2> : unit == 4 ? k_beam_reorder<uint32_t>
                       : unit == 2 ? k_beam_reorder<uint16_t> : k_beam_reorder<uint8_t>;
-    int threads = kThreads;
-    while (threads > kWave && threads * unit * l.W > 65536) threads /= 2;
+    const int threads = kMoveThreads * unit * l.W > 65536 ? kWave : kMoveThreads;
     const int64_t lds = (int64_t)threads * unit * l.W;
     const int64_t units = l.inner / unit * l.outer;
     int64_t gx = (units + threads - 1) / threads;

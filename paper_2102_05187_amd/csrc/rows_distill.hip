@@ -550,16 +550,21 @@ float log2_scale(const DistillArgs &a) { return (float)(a.scale * 1.442695040888
 
 }  // namespace
 
-int64_t distill_work(int type, int64_t N, int64_t V) {
-    return round16(N * (int64_t)sizeof(Stat)) + partial_bytes(cut_forward(type, N, V), N);
+// Whether a step holds its rows in registers; else it is the two calls, with the stat between them.
+static bool held(int type, int64_t N, int64_t V) {
+    const int64_t nv = vectors_of(type, V);
+    return nv <= 512 * 32 && (N >= 64 || nv <= 2048);
 }
+static int64_t stat_bytes(int type, int64_t N, int64_t V) { return held(type, N, V) ? 0 : round16(N * (int64_t)sizeof(Stat)); }
+
+int64_t distill_work(int type, int64_t N, int64_t V) { return stat_bytes(type, N, V) + partial_bytes(cut_forward(type, N, V), N); }
 
 hipError_t distill_forward(const DistillArgs &given, float *loss, double *stat, void *work, hipStream_t st) {
     DistillArgs a = given;
     a.once = read_once(a.type, a.N, a.V);
     const float c2 = log2_scale(a);
     const Pieces c = cut_forward(a.type, a.N, a.V);
-    float2 *partial = (float2 *)((char *)work + round16(a.N * (int64_t)sizeof(Stat)));
+    float2 *partial = (float2 *)((char *)work + stat_bytes(a.type, a.N, a.V));
     return a.type == COMET_F32 ? forward<COMET_F32>(a, c2, c, loss, (Stat *)stat, partial, st)
          : a.type == COMET_BF16 ? forward<COMET_BF16>(a, c2, c, loss, (Stat *)stat, partial, st)
                                 : forward<COMET_F16>(a, c2, c, loss, (Stat *)stat, partial, st);
@@ -577,8 +582,7 @@ hipError_t distill_backward(const DistillArgs &given, const double *stat, const 
 hipError_t distill_step(const DistillArgs &given, float *loss, void *dZ, int64_t lddz, void *work, hipStream_t st) {
     DistillArgs a = given;
     a.once = read_once(a.type, a.N, a.V);
-    const int64_t nv = vectors_of(a.type, a.V);
-    if (nv <= 512 * 32 && (a.N >= 64 || nv <= 2048)) {
+    if (held(a.type, a.N, a.V)) {
         const float c2 = log2_scale(a);
         return a.type == COMET_F32 ? step<COMET_F32>(a, c2, loss, dZ, lddz, st)
              : a.type == COMET_BF16 ? step<COMET_BF16>(a, c2, loss, dZ, lddz, st) : step<COMET_F16>(a, c2, loss, dZ, lddz, st);

@@ -58,8 +58,9 @@ def test_distill(lib, which):
         cases += [(dict(dZ=None), INVALID), (dict(ldd=99), SHAPE), (dict(dZ=ctypes.c_void_p(4097)), INVALID), (dict(dZ=P, ldd=120), INVALID)]
     if which == "step":
         need = ctypes.c_int64(-1)
-        assert lib.comet_distill_work(1, 4, 100, ctypes.byref(need)) == OK and need.value > 0
-        cases += [(dict(work=None), INVALID), (dict(size=need.value - 1), INVALID), (dict(work=ctypes.c_void_p(4104)), INVALID)]
+        long = dict(V=1 << 20, ld=1 << 20, ldd=1 << 20)          # rows that no workgroup holds
+        assert lib.comet_distill_work(1, 4, 1 << 20, ctypes.byref(need)) == OK and need.value > 0
+        cases += [(dict(long, work=None), INVALID), (dict(long, size=need.value - 1), INVALID), (dict(long, work=ctypes.c_void_p(4104)), INVALID)]
     for kw, status in cases:
         assert distill(lib, which, **kw) == status, kw
 
