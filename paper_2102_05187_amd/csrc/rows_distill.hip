@@ -154,9 +154,10 @@ template <int T, int P, class WORD> struct Marks {
         words[threadIdx.x] = 0;
         __syncthreads();
     }
-    __device__ __forceinline__ void set(const Piece<P> &p, const Entries &en) const {          // a barrier has to follow
+    // By `threads` threads, of which this is `thread`; a barrier has to follow.
+    __device__ __forceinline__ void set(const Piece<P> &p, const Entries &en, int thread = threadIdx.x, int threads = T) const {
         int64_t c;
-        for (int64_t e = en.begin + threadIdx.x; e < en.end; e += T)
+        for (int64_t e = en.begin + thread; e < en.end; e += threads)
             if (en.at(e, &c) && c >= p.base() && c < p.base() + p.columns()) {
                 const int at = (int)(c - p.base()), i = at / P;
                 atomicOr(&bits[at >> 5], 1u << (at & 31));
@@ -456,15 +457,21 @@ __global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
     const Piece<P> p(a.V, 0, T * NV);
     const Marks<T, P, uint32_t> marks{bits, words};
-    uint4 v[NV];
-    hold<TYPE, T>(row, p, a.once, v);
     const Entries en(a, r);
+    uint4 v[NV];
+    // A wavefront's loads come back in their order.  Of a long row the last wavefront goes through the entries before it asks for its part, while
+    // the others' parts keep the memory busy (4096 x 131072 of 16 bits: 450 us after it, SHORTER before it); of a short one all parts first.
+    constexpr bool kLong = NV >= 16;
+    const bool teacher = threadIdx.x >= T - kWave;
+    if (!kLong) hold<TYPE, T>(row, p, a.once, v);
     marks.clear(p);
-    marks.set(p, en);
-    if (threadIdx.x >= T - kWave) {                              // one wavefront, while the row is on its way
+    if (teacher) {
+        if (kLong) marks.set(p, en, threadIdx.x - (T - kWave), kWave);
+        else marks.set(p, en);
         const Taught t = teach(row, en, TAIL, TAIL ? a.tlse[r] : 0.0);
         if (threadIdx.x == T - 1) taught = t;
-    }
+    } else if (!kLong) marks.set(p, en);
+    if (kLong) hold<TYPE, T>(row, p, a.once, v);
     __syncthreads();
     Running run;
     const uint32_t word = TAIL ? words[threadIdx.x] : 0;
