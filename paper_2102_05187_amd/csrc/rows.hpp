@@ -14,6 +14,14 @@ constexpr double kNegInfD = -__builtin_huge_val();
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWave = 64;
 
+// A barrier for what the threads tell each other through LDS.  __syncthreads() also waits for every load and store to memory that the thread
+// has under way; here a row's loads go on across barriers, and nothing passes from thread to thread through memory.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // ---- element types ------------------------------------------------------------------------------------
 typedef float F2 __attribute__((ext_vector_type(2)));
 typedef __bf16 B2 __attribute__((ext_vector_type(2)));
@@ -253,11 +261,11 @@ template <int T> __device__ __forceinline__ void block_join(MaxSum &a, float c, 
     wave_join(a, c);
     if (T == kWave) return;
     if ((threadIdx.x & (kWave - 1)) == 0) buf[threadIdx.x / kWave] = make_float2(a.m, a.s);
-    __syncthreads();
+    lds_barrier();
     a = MaxSum();
 #pragma unroll
     for (int w = 0; w < T / kWave; ++w) a.join(buf[w].x, buf[w].y, c);
-    __syncthreads();
+    lds_barrier();
 }
 // The sum over columns [begin, end) of a row whose maximum there is m, against m itself: what Running loses where m is wild.  A column
 // that `skip` names is left out.  By a workgroup of T threads.

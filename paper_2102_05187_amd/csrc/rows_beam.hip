@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
     for (int i = threadIdx.x; i < kBins; i += T) sort.count[i] = 0;
     if (threadIdx.x < kTries) tries[threadIdx.x] = 0;
     if (threadIdx.x == 0) found = 0;
-    __syncthreads();
+    lds_barrier();
     uint64_t s[PER], most = 0;                                           // orders of the scores, 0: no candidate
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
     const float least = wave_reduce(most ? best : -kNegInf, -kNegInf, Smaller());
     const float largest = wave_reduce(best, kNegInf, Larger());
     if ((threadIdx.x & (kWave - 1)) == 0) ends[0][threadIdx.x / kWave] = least, ends[1][threadIdx.x / kWave] = largest;
-    __syncthreads();
+    lds_barrier();
     float from = ends[0][0], to = ends[1][0];
 #pragma unroll
     for (int w = 1; w < T / kWave; ++w) from = fminf(from, ends[0][w]), to = fmaxf(to, ends[1][w]);
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
                 ++at;
             }
         }
-        __syncthreads();
+        lds_barrier();
         if (pass == 1 || found <= kCandidates) break;
         // many equal ones: the n-th largest score exactly, and of the candidates that have it as many as are missing
         bar64 = kth<T>(1, order64(1.7976931348623157e308), n, [&](uint64_t t) {
@@ -102,9 +102,9 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
 #pragma unroll
         for (int j = 0; j < PER; ++j) above += s[j] > bar64 ? 1 : 0;
         above = block_count<T>(above, &tries[0]);
-        __syncthreads();
+        lds_barrier();
         if (threadIdx.x == 0) tries[0] = 0;
-        __syncthreads();
+        lds_barrier();
         bar_rest = kth<T>(0, ~0ull, n - above, [&](uint64_t t) {
             int c = 0;
 #pragma unroll
@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
             return c;
         }, tries);
         if (threadIdx.x == 0) found = 0;
-        __syncthreads();
+        lds_barrier();
     }
     const int some = found < kCandidates ? found : kCandidates;
     sort_items<T>(WideKeys{high, low}, some, sort, [&](int rank, const WideKey &c) {

@@ -14,13 +14,13 @@ template <int T> __device__ __forceinline__ int block_count(int n, int *slot) {
         const int sum = (int)wave_reduce((float)n, 0.f, Add());               // whole numbers far below 2^24
         if ((threadIdx.x & (kWave - 1)) == 0) atomicAdd(slot, sum);
     }
-    __syncthreads();
+    lds_barrier();
     return *slot;
 }
 template <int T> __device__ __forceinline__ int block_count(bool yes, int *slot) {
     const uint64_t b = __ballot(yes);
     if (b && (threadIdx.x & (kWave - 1)) == 0) atomicAdd(slot, (int)__popcll(b));
-    __syncthreads();
+    lds_barrier();
     return *slot;
 }
 
@@ -43,9 +43,9 @@ template <int T, class EACH> __device__ __forceinline__ float bound(float lo, fl
         const float per = (float)B / (hi - lo);
         const int shift = to - from < (uint32_t)B ? 0 : 24 - __builtin_clz(to - from);
         if (round > 0) {
-            __syncthreads();                                                   // the other half has been read
+            lds_barrier();                                                   // the other half has been read
             for (int i = threadIdx.x; i < B; i += T) bin[i] = 0;
-            __syncthreads();
+            lds_barrier();
         }
         each([&](float x) {
             if (!(x >= lo)) return;
@@ -54,7 +54,7 @@ template <int T, class EACH> __device__ __forceinline__ float bound(float lo, fl
             const int i = by_value ? (at < (float)(B - 1) ? (int)at : B - 1) : (step < (uint32_t)B ? (int)step : B - 1);
             atomicAdd(&bin[i], 1);
         });
-        __syncthreads();
+        lds_barrier();
         // every wavefront by itself, the highest bins first
         const int4 c = ((const int4 *)bin)[kWave - 1 - lane];
         const int sum = c.x + c.y + c.z + c.w;
@@ -166,14 +166,14 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
         if (threadIdx.x < 2 * kWave) sp.count[threadIdx.x] = 0;
         Item mine{};
         if (i < n) mine = s.get(i);
-        __syncthreads();
+        lds_barrier();
         if (i < n) {
             int at = 0;
 #pragma unroll 4
             for (int j = j0; j < j1; ++j) at += S::before(s.get(j), mine) ? 1 : 0;
             if (at) atomicAdd(&sp.count[i], at);
         }
-        __syncthreads();
+        lds_barrier();
         if (part == 0 && i < n) emit(sp.count[i], mine);
         return;
     }
@@ -196,7 +196,7 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
         const int w = threadIdx.x / kWave;
         sp.ends[0][w] = least, sp.ends[1][w] = most, sp.ends[2][w] = sum;
     }
-    __syncthreads();
+    lds_barrier();
     sum = 0.f;
 #pragma unroll
     for (int w = 0; w < T / kWave; ++w) least = fminf(least, sp.ends[0][w]), most = fmaxf(most, sp.ends[1][w]), sum += sp.ends[2][w];
@@ -212,7 +212,7 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
         bin[e] = b < (float)(kBins - 1) ? (int)b : kBins - 1;                  // NaN: the last one
         slot[e] = atomicAdd(&sp.count[bin[e]], 1);
     }
-    __syncthreads();
+    lds_barrier();
     if (threadIdx.x < kWave) {                                                 // count[b]: items in the bins above b
         constexpr int B = kBins / kWave;
         const int last = kBins - 1 - (int)threadIdx.x * B;
@@ -231,12 +231,12 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
         for (int k = 0; k < B; ++k) sp.count[last - k] = before, sp.size[last - k] = c[k], before += c[k];
         if (crowd) sp.crowd = 1;
     }
-    __syncthreads();
+    lds_barrier();
     if (sp.crowd) {
         int N = 4 * kWave;
         while (N < n) N *= 2;
         for (int i = n + threadIdx.x; i < N; i += T) s.put(i, S::none());
-        __syncthreads();
+        lds_barrier();
         // steps over distances of up to 64 stay inside of a wavefront's 128 items and need no barrier
         for (int k = 2; k <= N; k *= 2)
             for (int j = k / 2; j > 0; j /= 2) {
@@ -245,7 +245,7 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
                     const Item a = s.get(i), b = s.get(o);
                     if (S::before(b, a) == ((i & k) == 0)) { s.put(i, b); s.put(o, a); }
                 }
-                if (j > kWave || (j == 1 && k >= 2 * kWave)) __syncthreads();
+                if (j > kWave || (j == 1 && k >= 2 * kWave)) lds_barrier();
                 else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
 #pragma unroll
@@ -257,7 +257,7 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
             if (i >= n) continue;
             sp.order[sp.count[bin[e]] + slot[e]] = (uint16_t)i;
         }
-        __syncthreads();
+        lds_barrier();
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             if (e * T + (int)threadIdx.x >= n) continue;
@@ -268,7 +268,7 @@ template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items
             bin[e] = at;
         }
     }
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (e * T + (int)threadIdx.x < n) emit(bin[e], mine[e]);
@@ -299,9 +299,9 @@ template <int T, class COUNT> __device__ __forceinline__ uint64_t kth(uint64_t l
         else hi = mid - 1;
         if (reach == K) break;
     }
-    __syncthreads();
+    lds_barrier();
     for (int i = threadIdx.x; i < kTries; i += T) tries[i] = 0;
-    __syncthreads();
+    lds_barrier();
     return lo;
 }
 

@@ -49,7 +49,7 @@ template <int T> __device__ __forceinline__ void write_row(TopShared &sh, int n,
         if (n > K || K > kWave) {
             sort_items<T>(Keys{sh.keys}, n, sh.sort, [&](int rank, uint64_t key) { if (rank < K) sh.keys[rank] = key << 32 | key >> 32; });
         } else if (threadIdx.x < kWave && (int)threadIdx.x < n) sh.keys[threadIdx.x] = sh.keys[threadIdx.x] << 32 | sh.keys[threadIdx.x] >> 32;
-        __syncthreads();
+        lds_barrier();
         sort_items<T>(NumberKeys{sh.keys}, kept, sh.sort, [&](int rank, uint64_t key) {
             crd[rank] = (int32_t)column_of(key >> 32);
             vals[rank] = value_of((uint32_t)key);
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
             for (int k = 0; k < P; ++k) f[k] = threadIdx.x == 0 ? f[k] : kNegInf;
             keep(f, (uint32_t)(full * P), reaches);
         }
-        __syncthreads();
+        lds_barrier();
     } else {
         uint16_t *list = sh.sort.order;
         uint32_t which = 0;
@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
         int at = append(__popc(which), &sh.listed);
         for (; which; which &= which - 1, ++at)
             if (at < kCandidates) list[at] = (uint16_t)(__builtin_ctz(which) * T + threadIdx.x);
-        __syncthreads();
+        lds_barrier();
         const int listed = sh.listed;
         if (listed <= kCandidates) {
             constexpr int A = 2;                             // vectors on their way
@@ -274,7 +274,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
                 keep(f, (uint32_t)(full * P), reaches);
             }
         } else if (threadIdx.x == 0) sh.found = kCandidates + 1;
-        __syncthreads();
+        lds_barrier();
     }
     int n = sh.found;
     if (n > kCandidates) {
@@ -289,10 +289,10 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
             return c;
         }, sh.tries);
         if (threadIdx.x == 0) sh.found = 0;
-        __syncthreads();
+        lds_barrier();
         const float least = value_of((uint32_t)(lo >> 32));
         each(least, [&](const float *f, uint32_t column) { keep(f, column, [&](float x, uint32_t c) { return x >= least && key_of(x, c) >= lo; }); });
-        __syncthreads();
+        lds_barrier();
         n = sh.found < kCandidates ? sh.found : kCandidates;
     }
     // 3
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(T) k_topk_merge(TopArgs a, uint64_t *__restric
                 if (at < kCandidates) sh.keys[at] = key[j];
                 ++at;
             }
-        __syncthreads();
+        lds_barrier();
         if (pass == 1 || sh.found <= kCandidates) break;
         lo = kth<T>(lo, (uint64_t)order_of(sum.m) << 32 | 0xffffffffu, K, [&](uint64_t t) {
             int c = 0;
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(T) k_topk_merge(TopArgs a, uint64_t *__restric
             return c;
         }, sh.tries);
         if (threadIdx.x == 0) sh.found = 0;
-        __syncthreads();
+        lds_barrier();
     }
     const int n = sh.found < kCandidates ? sh.found : kCandidates;
     if (out_keys) write_keys<T>(sh, n, K, out_keys + r * K);
