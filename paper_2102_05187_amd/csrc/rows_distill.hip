@@ -11,8 +11,6 @@
 //
 // The entries' places are marked in LDS, a bit each.  The dense pass of the gradient leaves marked places alone, and the entries'
 // gradients are written on their own: no order between the two is needed, also where dZ is Z.
-#include <atomic>
-
 #include "rows.hpp"
 #include "rows_kernels.hpp"
 
@@ -355,45 +353,37 @@ template <int TYPE> __device__ __forceinline__ void write_some(const Row<TYPE> &
         if (i * P + k < row.n && !(mk >> k & 1)) out[i * P + k] = Elem<TYPE>::bits(d.slow(f[k]));
 }
 
-// Of a thread's vectors in a piece of the gradient: those that it writes whole (`now`), after having written the others one element after the
-// other: the few with marked places, the one that the row ends in, and all where the row's maximum is wild.  These are read again.
-template <int TYPE, int T>
-__device__ __forceinline__ uint32_t write_odd(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, const Dense &d,
-                                              const Marks<T, Elem<TYPE>::kPer, uint32_t> &marks, typename Elem<TYPE>::T *out) {
+// A piece of the gradient, whose logits v[] holds.  The few vectors with marked places, the one that the row ends in, and all where the row's
+// maximum is wild are read again and written one element after the other.
+template <int TYPE, int T, int NV>
+__device__ __forceinline__ void write_piece(const Row<TYPE> &row, const uint4 (&v)[NV], const Piece<Elem<TYPE>::kPer> &p, const Dense &d,
+                                            const Marks<T, Elem<TYPE>::kPer, uint32_t> &marks, typename Elem<TYPE>::T *out) {
+    using E = Elem<TYPE>;
+    constexpr int P = E::kPer;
+    static_assert(NV <= 32, "a bit for each");
     const int n = p.own > (int)threadIdx.x ? (p.own - (int)threadIdx.x + T - 1) / T : 0;        // this thread's whole vectors
     const uint32_t whole = n >= 32 ? ~0u : (1u << n) - 1;
     uint32_t left = d.plain() ? marks.words[threadIdx.x] & whole : whole;
     const uint32_t now = whole & ~left;
-    left |= last_vector<T, Elem<TYPE>::kPer, uint32_t>(p);
+    left |= last_vector<T, P, uint32_t>(p);
+    if (d.plain()) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (now >> j & 1) {
+                float f[P];
+                E::widen(again(v[j]), f);
+#pragma unroll
+                for (int k = 0; k < P; ++k) f[k] = d.of(f[k]);
+                const uint4 q = E::narrow(f);
+                const typename Row<TYPE>::V4 q4 = {q.x, q.y, q.z, q.w};
+                __builtin_nontemporal_store(q4, (typename Row<TYPE>::V4 *)(out + p.base() + j * T * P) + threadIdx.x);
+            }
+    }
     while (left) {
         const int i = __builtin_ctz(left) * T + threadIdx.x;
         left &= left - 1;
         write_some(row, p.v0 + i, d, marks.of(i), out);
     }
-    return now;
-}
-// A vector of the gradient.
-template <int TYPE> __device__ __forceinline__ void write_vector(typename Elem<TYPE>::T *to, const uint4 &v, const Dense &d) {   // `to` the same for all threads
-    using E = Elem<TYPE>;
-    float f[E::kPer];
-    E::widen(again(v), f);
-#pragma unroll
-    for (int k = 0; k < E::kPer; ++k) f[k] = d.of(f[k]);
-    const uint4 q = E::narrow(f);
-    const typename Row<TYPE>::V4 q4 = {q.x, q.y, q.z, q.w};
-    __builtin_nontemporal_store(q4, (typename Row<TYPE>::V4 *)to + threadIdx.x);
-}
-// A piece of the gradient, whose logits v[] holds.
-template <int TYPE, int T, int NV>
-__device__ __forceinline__ void write_piece(const Row<TYPE> &row, const uint4 (&v)[NV], const Piece<Elem<TYPE>::kPer> &p, const Dense &d,
-                                            const Marks<T, Elem<TYPE>::kPer, uint32_t> &marks, typename Elem<TYPE>::T *out) {
-    constexpr int P = Elem<TYPE>::kPer;
-    static_assert(NV <= 32, "a bit for each");
-    const uint32_t now = write_odd<TYPE, T>(row, p, d, marks, out);
-    typename Elem<TYPE>::T *to = out + p.base();
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (now >> j & 1) write_vector<TYPE>(to + j * T * P, v[j], d);
 }
 
 template <int TYPE, int T>
@@ -405,19 +395,17 @@ __device__ __forceinline__ void write_zeros(typename Elem<TYPE>::T *out, int64_t
     for (int64_t c = begin + whole + threadIdx.x; c < end; c += T) out[c] = 0;
 }
 
-// A thread's j-th vector of a piece; nothing where the row has ended.
-template <int TYPE, int T> __device__ __forceinline__ uint4 fetch(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, int j, bool once) {
+// Loads a piece into registers; nothing where the row has ended.
+template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, bool once, uint4 (&v)[NV]) {
     using E = Elem<TYPE>;
     using V4 = typename Row<TYPE>::V4;
-    const V4 *at = (const V4 *)(row.p + (p.v0 + j * T) * E::kPer);             // one address for all threads
-    V4 v = {E::kNone, E::kNone, E::kNone, E::kNone};
-    if ((j + 1) * T <= p.own || j * T + (int)threadIdx.x < p.own) v = once ? __builtin_nontemporal_load(at + threadIdx.x) : at[threadIdx.x];
-    return make_uint4(v.x, v.y, v.z, v.w);
-}
-// Loads a piece into registers.
-template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, bool once, uint4 (&v)[NV]) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = fetch<TYPE, T>(row, p, j, once);
+    for (int j = 0; j < NV; ++j) {
+        const V4 *at = (const V4 *)(row.p + (p.v0 + j * T) * E::kPer);         // one address for all threads
+        V4 x = {E::kNone, E::kNone, E::kNone, E::kNone};
+        if ((j + 1) * T <= p.own || j * T + (int)threadIdx.x < p.own) x = once ? __builtin_nontemporal_load(at + threadIdx.x) : at[threadIdx.x];
+        v[j] = make_uint4(x.x, x.y, x.z, x.w);
+    }
 }
 
 // Vectors [piece * T * NV, ..) of a row, from its stat.
@@ -449,14 +437,43 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
     write_piece<TYPE, T>(row, v, p, Dense(s, up, c2), marks, out);
 }
 
-// The running maximum and sum of a row that is held, joined over the workgroup.  Where there is a tail, vectors with marked places become -inf in v.
+// Loss and gradient of a row that a workgroup holds in registers: Z is read once.
 template <int TYPE, int T, int NV, bool TAIL>
-__device__ __forceinline__ MaxSum sum_held(const Row<TYPE> &row, uint4 (&v)[NV], const Piece<Elem<TYPE>::kPer> &p,
-                                           const Marks<T, Elem<TYPE>::kPer, uint32_t> &marks, float c2, float2 *buf) {
+__global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_step(DistillArgs a, float c2, float *__restrict__ loss, void *dZ, int64_t lddz) {
     using E = Elem<TYPE>;
     constexpr int P = E::kPer, U = NV < 4 ? NV : 4;
+    __shared__ uint32_t bits[T * NV * P / 32], words[T];
+    __shared__ float2 buf[T / kWave];
+    __shared__ Taught taught;
+    const int64_t r = blockIdx.x;
+    const float w = a.weight ? a.weight[r] : 1.f;
+    typename E::T *out = (typename E::T *)dZ + r * lddz;
+    if (w == 0) {
+        write_zeros<TYPE, T>(out, 0, a.V);
+        if (threadIdx.x == 0) loss[r] = 0;
+        return;
+    }
+    const Row<TYPE> row(a.Z, r, a.ldz, a.V);
+    const Piece<P> p(a.V, 0, T * NV);
+    const Marks<T, P, uint32_t> marks{bits, words};
+    const Entries en(a, r);
+    uint4 v[NV];
+    // A wavefront's loads come back in their order.  Of a long row the last wavefront goes through the entries before it asks for its part, while
+    // the others' parts keep the memory busy (4096 x 131072 of 16 bits: 450 us after it, SHORTER before it); of a short one all parts first.
+    constexpr bool kLong = NV >= 16;
+    const bool teacher = threadIdx.x >= T - kWave;
+    if (!kLong) hold<TYPE, T>(row, p, a.once, v);
+    marks.clear(p);
+    if (teacher) {
+        if (kLong) marks.set(p, en, threadIdx.x - (T - kWave), kWave);
+        else marks.set(p, en);
+        const Taught t = teach(row, en, TAIL, TAIL ? a.tlse[r] : 0.0);
+        if (threadIdx.x == T - 1) taught = t;
+    } else if (!kLong) marks.set(p, en);
+    if (kLong) hold<TYPE, T>(row, p, a.once, v);
+    lds_barrier();
     Running run;
-    const uint32_t word = TAIL ? marks.words[threadIdx.x] : 0;
+    const uint32_t word = TAIL ? words[threadIdx.x] : 0;
 #pragma unroll
     for (int j0 = 0; j0 < NV; j0 += U) {
         float f[U * P], b = kNegInf;
@@ -473,135 +490,14 @@ __device__ __forceinline__ MaxSum sum_held(const Row<TYPE> &row, uint4 (&v)[NV],
     take_some<TYPE, T, TAIL>(run, row, p, word | last_vector<T, P, uint32_t>(p), marks, c2);
     MaxSum d = run.sum(c2);
     block_join<T>(d, c2, buf);
-    if (wild(d.m, c2)) d.s = slow_sum<TYPE, T>(row, 0, row.n, d.m, c2, buf, [&](int64_t c) { return TAIL && marks.at((int)c); });
-    return d;
-}
-
-// Loss and gradient of a short row, which a workgroup holds in registers: Z is read once.
-template <int TYPE, int T, int NV, bool TAIL>
-__global__ void __launch_bounds__(T, 4) k_distill_step(DistillArgs a, float c2, float *__restrict__ loss, void *dZ, int64_t lddz) {
-    using E = Elem<TYPE>;
-    constexpr int P = E::kPer;
-    __shared__ uint32_t bits[T * NV * P / 32], words[T];
-    __shared__ float2 buf[T / kWave];
-    __shared__ Taught taught;
-    const int64_t r = blockIdx.x;
-    const float w = a.weight ? a.weight[r] : 1.f;
-    typename E::T *out = (typename E::T *)dZ + r * lddz;
-    if (w == 0) {
-        write_zeros<TYPE, T>(out, 0, a.V);
-        if (threadIdx.x == 0) loss[r] = 0;
-        return;
-    }
-    const Row<TYPE> row(a.Z, r, a.ldz, a.V);
-    const Piece<P> p(a.V, 0, T * NV);
-    const Marks<T, P, uint32_t> marks{bits, words};
-    uint4 v[NV];
-    hold<TYPE, T>(row, p, a.once, v);
-    const Entries en(a, r);
-    marks.clear(p);
-    marks.set(p, en);
-    if (threadIdx.x >= T - kWave) {                              // one wavefront, while the row is on its way
-        const Taught t = teach(row, en, TAIL, TAIL ? a.tlse[r] : 0.0);
-        if (threadIdx.x == T - 1) taught = t;
-    }
-    lds_barrier();
-    const MaxSum d = sum_held<TYPE, T, NV, TAIL>(row, v, p, marks, c2, buf);
+    if (wild(d.m, c2)) d.s = slow_sum<TYPE, T>(row, 0, a.V, d.m, c2, buf, [&](int64_t c) { return TAIL && marks.at((int)c); });
+    const Taught t = taught;
     Stat s;
-    const double l = finish(taught, d, TAIL, a.scale, w, &s);
+    const double l = finish(t, d, TAIL, a.scale, w, &s);
     if (threadIdx.x == 0) loss[r] = (float)l;
     const double up = (double)w * a.scale;
     write_entries<TYPE, T>(row, en, s, up, 0, a.V, out);
     write_piece<TYPE, T>(row, v, p, Dense(s, up, c2), marks, out);
-}
-
-// The rows with a weight in front, the others behind, both in order: head[0] of the former.  By one workgroup.
-__global__ void __launch_bounds__(1024) k_list_rows(const float *__restrict__ weight, int N, int32_t *__restrict__ head, int32_t *__restrict__ rows) {
-    __shared__ int counts[16];
-    int before = 0;                                              // rows with a weight so far
-    for (int r0 = 0; r0 < N; r0 += 1024) {
-        const int r = r0 + (int)threadIdx.x;
-        const bool live = r < N && weight[r] != 0;
-        const uint64_t b = __ballot(live);
-        lds_barrier();
-        if ((threadIdx.x & (kWave - 1)) == 0) counts[threadIdx.x / kWave] = (int)__popcll(b);
-        lds_barrier();
-        int mine = before + (int)__popcll(b & ((1ull << (threadIdx.x & (kWave - 1))) - 1)), all = 0;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) {
-            if (w < (int)threadIdx.x / kWave) mine += counts[w];
-            all += counts[w];
-        }
-        if (r < N) rows[live ? mine : N - 1 - (r - mine)] = r;
-        before += all;
-    }
-    if (threadIdx.x == 0) head[0] = before;
-}
-
-// The same for long rows: a workgroup goes from row to row, and each vector's registers take up the next row's as soon as its gradient is
-// written.  So the memory is read while gradients are computed, also where one row takes all of a compute unit's registers.  A wavefront's
-// loads come back in their order: the last one goes through the next row's entries before it asks for its part of that row.
-template <int TYPE, int T, int NV, bool TAIL>
-__global__ void __launch_bounds__(T, NV == 32 ? 2 : 3) k_distill_rows(DistillArgs a, float c2, const int32_t *__restrict__ head, const int32_t *__restrict__ rows,
-                                                                      float *__restrict__ loss, void *dZ, int64_t lddz) {
-    using E = Elem<TYPE>;
-    constexpr int P = E::kPer;
-    __shared__ uint32_t bits[2][T * NV * P / 32], words[2][T];
-    __shared__ float2 buf[T / kWave];
-    __shared__ Taught taught[2];
-    const int N = (int)a.N, live = head ? head[0] : N;
-    const bool teacher = threadIdx.x >= T - kWave;
-    const Piece<P> p(a.V, 0, T * NV);
-    const auto learn = [&](int64_t r, int set) {                 // by the last wavefront
-        const Marks<T, P, uint32_t> marks{bits[set], words[set]};
-        const Entries en(a, r);
-        marks.set(p, en, threadIdx.x - (T - kWave), kWave);
-        const Taught t = teach(Row<TYPE>(a.Z, r, a.ldz, a.V), en, TAIL, TAIL ? a.tlse[r] : 0.0);
-        if (threadIdx.x == T - 1) taught[set] = t;
-    };
-    int set = 0;
-    int64_t r = 0;
-    uint4 v[NV];
-    if ((int)blockIdx.x < live) {
-        r = head ? rows[blockIdx.x] : (int)blockIdx.x;
-        Marks<T, P, uint32_t>{bits[0], words[0]}.clear(p);
-        if (teacher) learn(r, 0);
-        hold<TYPE, T>(Row<TYPE>(a.Z, r, a.ldz, a.V), p, a.once, v);
-    }
-    for (int i = blockIdx.x; i < live; i += gridDim.x) {
-        lds_barrier();                                         // this row's marks are there, and nobody needs the other ones any more
-        const Marks<T, P, uint32_t> marks{bits[set], words[set]};
-        for (int k = threadIdx.x; k < T * NV * P / 32; k += T) bits[set ^ 1][k] = 0;
-        words[set ^ 1][threadIdx.x] = 0;
-        const Row<TYPE> row(a.Z, r, a.ldz, a.V);
-        const float w = a.weight ? a.weight[r] : 1.f;
-        const MaxSum d = sum_held<TYPE, T, NV, TAIL>(row, v, p, marks, c2, buf);
-        Stat s;
-        const double l = finish(taught[set], d, TAIL, a.scale, w, &s);
-        if (threadIdx.x == 0) loss[r] = (float)l;
-        const double up = (double)w * a.scale;
-        typename E::T *out = (typename E::T *)dZ + r * lddz;
-        write_entries<TYPE, T>(row, Entries(a, r), s, up, 0, a.V, out);
-        const Dense g(s, up, c2);
-        const uint32_t now = write_odd<TYPE, T>(row, p, g, marks, out);
-        const bool more = i + (int)gridDim.x < live;
-        if (more) {
-            r = head ? rows[i + gridDim.x] : i + (int)gridDim.x;
-            if (teacher) learn(r, set ^ 1);
-        }
-        const Row<TYPE> next(a.Z, r, a.ldz, a.V);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (now >> j & 1) write_vector<TYPE>(out + j * T * P, v[j], g);
-            if (more) v[j] = fetch<TYPE, T>(next, p, j, a.once);
-        }
-        set ^= 1;
-    }
-    for (int i = blockIdx.x; i < N - live; i += gridDim.x) {     // the rows of weight 0
-        const int64_t z = rows[N - 1 - i];
-        write_zeros<TYPE, T>((typename E::T *)dZ + z * lddz, 0, a.V);
-        if (threadIdx.x == 0) loss[z] = 0;
-    }
 }
 
 int64_t vectors_of(int type, int64_t V) {
@@ -647,39 +543,13 @@ template <int TYPE, int T, int NV> hipError_t launch_step(const DistillArgs &a, 
     hipLaunchKernelGGL(kernel, dim3((unsigned)a.N), dim3(T), 0, st, a, c2, loss, dZ, lddz);
     return hipGetLastError();
 }
-
-int compute_units() {
-    static std::atomic<int> known[64];
-    int device = 0, n = 0;
-    if (hipGetDevice(&device) != hipSuccess) return 256;
-    std::atomic<int> *at = device >= 0 && device < 64 ? &known[device] : nullptr;
-    if (at && (n = at->load()) > 0) return n;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || n < 1) return 256;
-    if (at) at->store(n);
-    return n;
-}
-
-// list: N + 4 numbers of scratch
-template <int TYPE, int T, int NV> hipError_t launch_rows(const DistillArgs &a, float c2, float *loss, void *dZ, int64_t lddz, int32_t *list, hipStream_t st) {
-    const int32_t *head = nullptr;
-    if (a.weight) {
-        head = list;
-        hipLaunchKernelGGL(k_list_rows, dim3(1), dim3(1024), 0, st, a.weight, (int)a.N, list, list + 4);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    const int64_t most = (int64_t)compute_units() * (NV == 16 ? 3 : T == 256 ? 2 : 1);           // what the registers hold at a time
-    const auto kernel = a.tlse ? k_distill_rows<TYPE, T, NV, true> : k_distill_rows<TYPE, T, NV, false>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.N < most ? a.N : most)), dim3(T), 0, st, a, c2, head, list + 4, loss, dZ, lddz);
-    return hipGetLastError();
-}
-template <int TYPE> hipError_t step(const DistillArgs &a, float c2, float *loss, void *dZ, int64_t lddz, int32_t *list, hipStream_t st) {
+template <int TYPE> hipError_t step(const DistillArgs &a, float c2, float *loss, void *dZ, int64_t lddz, hipStream_t st) {
     const int64_t nv = vectors_of(TYPE, a.V);
     if (nv <= 256 * 4) return launch_step<TYPE, 256, 4>(a, c2, loss, dZ, lddz, st);
     if (nv <= 256 * 8) return launch_step<TYPE, 256, 8>(a, c2, loss, dZ, lddz, st);
-    if (nv <= 256 * 16) return launch_rows<TYPE, 256, 16>(a, c2, loss, dZ, lddz, list, st);
-    if (nv <= 256 * 32) return launch_rows<TYPE, 256, 32>(a, c2, loss, dZ, lddz, list, st);
-    return launch_rows<TYPE, 512, 32>(a, c2, loss, dZ, lddz, list, st);
+    if (nv <= 256 * 16) return launch_step<TYPE, 256, 16>(a, c2, loss, dZ, lddz, st);
+    if (nv <= 256 * 32) return launch_step<TYPE, 256, 32>(a, c2, loss, dZ, lddz, st);
+    return launch_step<TYPE, 512, 32>(a, c2, loss, dZ, lddz, st);
 }
 
 float log2_scale(const DistillArgs &a) { return (float)(a.scale * 1.4426950408889634); }
@@ -691,19 +561,16 @@ static bool held(int type, int64_t N, int64_t V) {
     const int64_t nv = vectors_of(type, V);
     return nv <= 512 * 32 && (N >= 64 || nv <= 2048);
 }
-// The stat of a step that is two calls, or the list of rows of one that goes from row to row.
-static int64_t step_bytes(int type, int64_t N, int64_t V) {
-    return !held(type, N, V) ? round16(N * (int64_t)sizeof(Stat)) : vectors_of(type, V) > 256 * 8 ? round16((N + 4) * (int64_t)sizeof(int32_t)) : 0;
-}
+static int64_t stat_bytes(int type, int64_t N, int64_t V) { return held(type, N, V) ? 0 : round16(N * (int64_t)sizeof(Stat)); }
 
-int64_t distill_work(int type, int64_t N, int64_t V) { return step_bytes(type, N, V) + partial_bytes(cut_forward(type, N, V), N); }
+int64_t distill_work(int type, int64_t N, int64_t V) { return stat_bytes(type, N, V) + partial_bytes(cut_forward(type, N, V), N); }
 
 hipError_t distill_forward(const DistillArgs &given, float *loss, double *stat, void *work, hipStream_t st) {
     DistillArgs a = given;
     a.once = read_once(a.type, a.N, a.V);
     const float c2 = log2_scale(a);
     const Pieces c = cut_forward(a.type, a.N, a.V);
-    float2 *partial = (float2 *)((char *)work + step_bytes(a.type, a.N, a.V));
+    float2 *partial = (float2 *)((char *)work + stat_bytes(a.type, a.N, a.V));
     return a.type == COMET_F32 ? forward<COMET_F32>(a, c2, c, loss, (Stat *)stat, partial, st)
          : a.type == COMET_BF16 ? forward<COMET_BF16>(a, c2, c, loss, (Stat *)stat, partial, st)
                                 : forward<COMET_F16>(a, c2, c, loss, (Stat *)stat, partial, st);
@@ -723,8 +590,8 @@ hipError_t distill_step(const DistillArgs &given, float *loss, void *dZ, int64_t
     a.once = read_once(a.type, a.N, a.V);
     if (held(a.type, a.N, a.V)) {
         const float c2 = log2_scale(a);
-        return a.type == COMET_F32 ? step<COMET_F32>(a, c2, loss, dZ, lddz, (int32_t *)work, st)
-             : a.type == COMET_BF16 ? step<COMET_BF16>(a, c2, loss, dZ, lddz, (int32_t *)work, st) : step<COMET_F16>(a, c2, loss, dZ, lddz, (int32_t *)work, st);
+        return a.type == COMET_F32 ? step<COMET_F32>(a, c2, loss, dZ, lddz, st)
+             : a.type == COMET_BF16 ? step<COMET_BF16>(a, c2, loss, dZ, lddz, st) : step<COMET_F16>(a, c2, loss, dZ, lddz, st);
     }
     const hipError_t e = distill_forward(a, loss, (double *)work, work, st);
     return e != hipSuccess || a.V == 0 ? e : distill_backward(a, (const double *)work, nullptr, dZ, lddz, st);
