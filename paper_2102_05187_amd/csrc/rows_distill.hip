@@ -263,6 +263,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, flo
     constexpr int P = E::kPer, T = kThreads;
     __shared__ float2 buf[T / kWave];
     __shared__ uint64_t words[TAIL ? T : 1];
+    __shared__ Taught taught;
     extern __shared__ uint32_t bits[];
     const int64_t r = blockIdx.x / (unsigned)cut.count;
     const float w = a.weight ? a.weight[r] : 1.f;
@@ -273,19 +274,29 @@ __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, flo
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
     const Piece<P> p(a.V, (blockIdx.x - r * cut.count) * cut.vectors, cut.vectors);
     const Marks<T, P, uint64_t> marks{bits, words};
+    // The last wavefront goes through the entries of a long row before it reads its part of it, while the others' parts keep the memory busy; of
+    // a short one, when the row has been read (4096 rows of 8000 elements of 16 bits: 28 us so, 32 the other way; 2048 of 50021: 51 and 49).
+    const bool teacher = cut.count == 1 && threadIdx.x >= T - kWave, early = p.own > 16 * T;
+    const auto learn = [&] {
+        const Taught t = teach(row, Entries(a, r), TAIL, TAIL ? a.tlse[r] : 0.0);
+        if (threadIdx.x == T - 1) taught = t;
+    };
     const MaxSum d = read_piece<TYPE, T, TAIL>(row, p, marks, c2, a.once, buf, [&] {
-        if (!TAIL) return;
-        marks.clear(p);
-        marks.set(p, Entries(a, r));
-        lds_barrier();
+        if (TAIL) {
+            marks.clear(p);
+            marks.set(p, Entries(a, r));
+            lds_barrier();
+        }
+        if (teacher && early) learn();
     });
     if (cut.count > 1) {
         if (threadIdx.x == 0) partial[blockIdx.x] = make_float2(d.m, d.s);
-    } else if (threadIdx.x < kWave) {
-        const Taught t = teach(row, Entries(a, r), TAIL, TAIL ? a.tlse[r] : 0.0);
+    } else if (teacher) {
+        if (!early) learn();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         Stat s;
-        const double l = finish(t, d, TAIL, a.scale, w, &s);
-        if (threadIdx.x == 0) { loss[r] = (float)l; stat[r] = s; }
+        const double l = finish(taught, d, TAIL, a.scale, w, &s);
+        if (threadIdx.x == T - 1) { loss[r] = (float)l; stat[r] = s; }
     }
 }
 
@@ -505,11 +516,13 @@ int64_t vectors_of(int type, int64_t V) {
     return (V + per - 1) / per;
 }
 
-// Pieces of the forward pass: as few as a row needs, more where the rows are too few for the device.
+// Pieces of the forward pass: as few as a row needs, more where long rows are too few for the device: a second launch joins them, and
+// costs more than a row of 8192 vectors takes one workgroup.
 Pieces cut_forward(int type, int64_t N, int64_t V) {
     const int64_t nv = vectors_of(type, V);
     int64_t vectors = kPiece;
-    while (vectors > 512 && N * ((nv + vectors - 1) / vectors) < 256) vectors /= 2;
+    if (nv > 8192)
+        while (vectors > 512 && N * ((nv + vectors - 1) / vectors) < 256) vectors /= 2;
     const int64_t count = nv > 0 ? (nv + vectors - 1) / vectors : 1;
     return Pieces{(int)(count == 1 ? (nv + 31) / 32 * 32 : vectors), (int)count};
 }
@@ -559,7 +572,7 @@ float log2_scale(const DistillArgs &a) { return (float)(a.scale * 1.442695040888
 // Whether a step holds its rows in registers; else it is the two calls, with the stat between them.
 static bool held(int type, int64_t N, int64_t V) {
     const int64_t nv = vectors_of(type, V);
-    return nv <= 512 * 32 && (N >= 64 || nv <= 2048);
+    return nv <= 512 * 32 && (N >= 64 || nv <= 8192);
 }
 static int64_t stat_bytes(int type, int64_t N, int64_t V) { return held(type, N, V) ? 0 : round16(N * (int64_t)sizeof(Stat)); }
 
