@@ -52,7 +52,7 @@ comet_status check_gradient(const comet::DistillArgs &a, const void *dZ, int64_t
     if (lddz < a.V) return COMET_ERR_SHAPE;
     if (lddz > (int64_t(1) << 40)) return COMET_ERR_UNSUPPORTED;
     if (a.N > 0 && a.V > 0 && !dZ) return COMET_ERR_INVALID_ARG;
-    if (!aligned(dZ, element_size(a.type)) || (dZ == a.Z && lddz != a.ldz)) return COMET_ERR_INVALID_ARG;
+    if (!aligned(dZ, element_size(a.type)) || (dZ && dZ == a.Z && lddz != a.ldz)) return COMET_ERR_INVALID_ARG;
     return COMET_OK;
 }
 
