@@ -323,7 +323,7 @@ typedef enum { COMET_F32 = 0, COMET_BF16 = 1, COMET_F16 = 2 } comet_type_t;
  *              (a masked place) or NaN is no entry; where a row has fewer than K, the places at its end hold -1 and -inf.
  *   lse        device, [N], may be NULL: log sum_j exp(scale z_rj) over the whole row; -inf for a row without an element
  *              over -inf, +inf with a +inf in it, NaN with a NaN.
- *   K          1 <= K <= COMET_MAX_TOP, V * K <= 2^30. */
+ *   K          1 <= K <= COMET_MAX_TOP, V * K <= 2^29. */
 #define COMET_BY_COORDINATE 1u
 #define COMET_MAX_TOP 1024
 comet_status comet_rows_topk_work(comet_type_t type, int64_t N, int64_t V, int64_t K, int64_t *bytes /* host */);
@@ -374,7 +374,7 @@ comet_status comet_distill_step(const void *Z, comet_type_t type, int64_t N, int
  *   out_score, out_parent, out_token   device, [B x n]: score, beam and token of each selected candidate.
  *              A candidate whose score is -inf or NaN is none (masked tokens, beams that are not in use); where a batch has fewer than
  *              n, the places at its end hold -inf, -1 and -1.
- *   1 <= W <= COMET_MAX_BEAMS, 1 <= n <= COMET_MAX_TOP, W * n <= 8192, V < 2^24, V * n <= 2^30. */
+ *   1 <= W <= COMET_MAX_BEAMS, 1 <= n <= COMET_MAX_TOP, W * n <= 8192, V < 2^24, V * n <= 2^29. */
 #define COMET_MAX_BEAMS 256
 comet_status comet_beam_select_work(comet_type_t type, int64_t B, int64_t W, int64_t V, int64_t n, int64_t *bytes /* host */);
 comet_status comet_beam_select(const void *Z, comet_type_t type, int64_t B, int64_t W, int64_t V, int64_t ldz, const float *score,

@@ -112,6 +112,11 @@ def test_strides(dtype):
     check_select(Z[:1, 1:3], c[:1, 1:3].contiguous(), 4)
 
 
+def test_long_rows_and_many_lists():
+    check_select(*logits(1, 3, 1000003, torch.bfloat16, seed=7), 100)
+    check_select(*logits(1, 16, 300007, torch.float32, seed=8), 500)
+
+
 def test_many_batches():
     check_select(*logits(150, 3, 200, torch.bfloat16, seed=5), 6)
 

@@ -111,6 +111,13 @@ def test_sizes(N, V, K, tail, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("N,V", [(2, 1024), (2, 4097), (2, 8193), (2, 16384), (2, 16391), (70, 16400), (3, 32768), (3, 65536), (2, 65543), (66, 65537), (2, 131079),
+                                 (3, 300007)])
+def test_around_the_sizes_of_pieces(N, V, dtype):
+    Problem(N, V, 9, dtype, seed=V, tail=True, weighted=N > 60).check()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("tail", [False, True])
 def test_ragged_rows(tail, dtype):
     Problem(12, 3001, 40, dtype, seed=1, tail=tail, ragged=True).check()

@@ -54,6 +54,18 @@ def test_sizes(N, V, K, by_coordinate, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1024, 1025, 2048, 2056, 8191, 16384, 16385, 32768, 32769, 65536, 65537, 131073, 262145])
+def test_around_the_sizes_of_pieces(V, dtype):
+    check(matrix(2, V, dtype, seed=V), 17)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_rows(dtype):
+    check(matrix(2, 524288, dtype, seed=1), 1024, by_coordinate=True)
+    check(matrix(1, 3000001, dtype, seed=2), 100)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_more_kept_than_there_are(dtype):
     check(matrix(3, 5, dtype), 9)
     check(matrix(3, 5, dtype), 9, by_coordinate=True)
@@ -190,6 +202,7 @@ def test_refusals():
     Z = matrix(4, 100, torch.float32)
     for bad, error in ((lambda: comet.comet_rows_topk(Z, 0), comet.CometError), (lambda: comet.comet_rows_topk(Z, 1025), comet.CometError),
                        (lambda: comet.comet_rows_topk(Z, 3, scale=0.0), comet.CometError),
+                       (lambda: comet.comet_rows_topk(torch.empty((1, 1 << 20), device="cuda"), 513), comet.CometError),
                        (lambda: comet.comet_rows_topk(Z, 3, scale=math.nan), comet.CometError),
                        (lambda: comet.comet_rows_topk(Z.double(), 3), TypeError), (lambda: comet.comet_rows_topk(Z.cpu(), 3), TypeError),
                        (lambda: comet.comet_rows_topk(Z.t(), 3), ValueError), (lambda: comet.comet_rows_topk(Z[0], 3), ValueError),
