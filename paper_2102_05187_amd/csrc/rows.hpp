@@ -98,6 +98,9 @@ template <> struct Elem<COMET_F16> {
 // Vector i holds the elements i * kPer .. of the row wherever the row starts, so that what is computed from a row does not
 // depend on its address.  The device loads and stores 16 bytes at any address: at multiples of 4 as fast as at multiples of
 // 16 (6.6 TB/s over rows of 256 KB), at odd multiples of 2 a fifth slower (5.2 TB/s).
+// A row of 16-bit elements at such an odd multiple (`odd`: every other row where the rows' distance is odd) is therefore read from one
+// element before it on, which is the row before's, and every vector gets its last element from the vector behind it: the next lane's, or,
+// for the wavefront's last lane, from edges(), one load for all of a thread's vectors.  Row 0 has none before it, and is read as it lies.
 // Rows of 256 MB and more in all do not stay in the last cache (of that size), and are read past it: top 64 of 2048 x 131072 of 16 bits 100 us
 // through it, 95 past it.  Smaller ones are often there already, or are read again by the gradient: 5 to 11 us of 40 longer past it.
 inline bool read_once(int type, int64_t N, int64_t V) { return N * V * (type == COMET_F32 ? 4 : 2) >= (int64_t(256) << 20); }
@@ -107,25 +110,50 @@ typedef uint32_t V4At2 __attribute__((ext_vector_type(4), aligned(2)));
 template <int ALIGN> struct Wide { using type = V4At4; };
 template <> struct Wide<2> { using type = V4At2; };
 
+constexpr int64_t kOddFrom = 16384;
+
 template <int TYPE> struct Row {
     using E = Elem<TYPE>;
     using T = typename E::T;
     using V4 = typename Wide<sizeof(T)>::type;
     const T *p;              // the row's first element
     int64_t n;               // its length
-    __device__ __forceinline__ Row(const void *base, int64_t row, int64_t ld, int64_t len) : p((const T *)base + row * ld), n(len) {}
-    __device__ __forceinline__ int64_t nvec() const { return (n + E::kPer - 1) / E::kPer; }
+    bool odd;
+    __device__ __forceinline__ Row(const void *base, int64_t row, int64_t ld, int64_t len)
+        : p((const T *)base + row * ld), n(len), odd(sizeof(T) == 2 && row > 0 && len >= kOddFrom && ((uintptr_t)p & 2)) {}
     __device__ __forceinline__ int64_t first(int64_t i) const { return i * E::kPer; }           // column of the vector's first element
     __device__ __forceinline__ bool whole(int64_t i) const { return first(i) + E::kPer <= n; }
     __device__ __forceinline__ uint4 raw(int64_t i) const {
         const V4 v = *(const V4 *)(p + first(i));
         return make_uint4(v.x, v.y, v.z, v.w);
     }
-    // the same, past the caches where `once`
+    // 16 bytes from vector i's first element on, or from the one before it of an odd row; past the caches where `once`
     __device__ __forceinline__ uint4 stream(int64_t i, bool once) const {
-        const V4 *at = (const V4 *)(p + first(i));
+        const V4 *at = (const V4 *)(p + first(i) - (odd ? 1 : 0));
         const V4 v = once ? __builtin_nontemporal_load(at) : *at;
         return make_uint4(v.x, v.y, v.z, v.w);
+    }
+    // What settle() needs of a piece of `own` whole vectors from v0 on: lane j's `each` is the last element of the wavefront's 64 vectors j THREADS + t,
+    // `last` that of the piece's last vector.
+    struct Edges { uint32_t each, last; };
+    template <int THREADS> __device__ __forceinline__ Edges edges(int64_t v0, int own) const {
+        Edges e{0, 0};
+        if constexpr (sizeof(T) == 2) {
+            if (odd && own > 0) {
+                const int i = (int)(threadIdx.x & (kWave - 1)) * THREADS + (int)(threadIdx.x | (kWave - 1));
+                if (i < own) e.each = p[first(v0 + i) + E::kPer - 1];
+                e.last = p[first(v0 + own) - 1];
+            }
+        }
+        return e;
+    }
+    // Of an odd row, the piece's vector i = j THREADS + t from what stream() gave the wavefront; nothing where it is not of the `own`.  By whole wavefronts.
+    __device__ __forceinline__ uint4 settle(uint4 v, const Edges &e, int j, int i, int own) const {
+        uint32_t next = __builtin_amdgcn_update_dpp(__builtin_amdgcn_readlane(e.each, j), v.x, 0x130, 0xf, 0xf, false);      // the next lane's
+        next = i == own - 1 ? e.last : next;
+        const uint4 r = make_uint4(__builtin_amdgcn_alignbit(v.y, v.x, 16), __builtin_amdgcn_alignbit(v.z, v.y, 16),
+                                   __builtin_amdgcn_alignbit(v.w, v.z, 16), __builtin_amdgcn_alignbit(next, v.w, 16));
+        return i < own ? r : make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
     }
     // elements of vector i as floats, -inf behind the row's end
     __device__ __forceinline__ void load(int64_t i, float *f) const {
@@ -195,7 +223,6 @@ struct Running {
 // the second part would be lost in one number.
 struct Log {
     double big, rest;
-    __device__ __forceinline__ double value() const { return big + rest; }
     __device__ __forceinline__ bool none() const { return big == kNegInfD; }                      // of nothing
 };
 __device__ __forceinline__ Log make_log(double big, double sum) {
@@ -205,17 +232,12 @@ __device__ __forceinline__ Log make_log(double big, double sum) {
     if (sum != sum) l.big = sum;
     return l;
 }
-// x - l and exp(x - l); what is -inf stays so, and has the probability 0
-__device__ __forceinline__ double minus(double x, const Log &l) { return x == kNegInfD ? x : (x - l.big) - l.rest; }
-__device__ __forceinline__ double prob(double x, const Log &l) { return x == kNegInfD ? 0.0 : exp((x - l.big) - l.rest); }
 // ln of a 32-bit sum, to about 2^-24 whatever its size: the exponent is taken off first.  0 gives -inf, a NaN itself.
 __device__ __forceinline__ double log_of(float s) {
     const int e = s >= 0x1p-126f && s < __builtin_huge_valf() ? (int)(__float_as_uint(s) >> 23) - 127 : 0;
     const float m = __builtin_ldexpf(s, -e);                                   // 1 <= m < 2
     return ((double)e + (double)__builtin_amdgcn_logf(m)) * 0.6931471805599453;
 }
-// log sum exp(scale z) from the running maximum and sum.  With +inf among the z the differences are NaN, and so is the result.
-__device__ __forceinline__ Log log_sum(const MaxSum &a, double scale) { return make_log((double)a.m * scale, (double)a.s); }
 
 // ---- reductions ---------------------------------------------------------------------------------------------
 // Over a wavefront with data-parallel moves (lanes 1, 2, 4, 8 back in rows of 16, then row ends onto the rows behind them):

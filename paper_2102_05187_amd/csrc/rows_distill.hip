@@ -226,6 +226,7 @@ __device__ __forceinline__ MaxSum read_piece(const Row<TYPE> &row, const Piece<E
             }
         }
     };
+    const auto edge = row.template edges<T>(p.v0, p.own);
     fetch(0);
     mark();
     WORD word = TAIL ? marks.words[threadIdx.x] : (WORD)0;
@@ -235,6 +236,10 @@ __device__ __forceinline__ MaxSum read_piece(const Row<TYPE> &row, const Piece<E
 #pragma unroll
         for (int u = 0; u < U; ++u) x[u] = v[u];
         if (i0 + U * T < p.own) fetch(i0 + U * T);
+        if (row.odd) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = row.settle(x[u], edge, j0 + u, i0 + u * T + threadIdx.x, p.own);
+        }
         if (TAIL && (word >> j0 & ((1 << U) - 1))) {
 #pragma unroll
             for (int u = 0; u < U; ++u) if (word >> (j0 + u) & 1) x[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
@@ -450,7 +455,7 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
 
 // Loss and gradient of a row that a workgroup holds in registers: Z is read once.
 template <int TYPE, int T, int NV, bool TAIL>
-__global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_step(DistillArgs a, float c2, float *__restrict__ loss, void *dZ, int64_t lddz) {
+__global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_step(DistillArgs a, float c2, float *__restrict__ loss, void *dZ, int64_t lddz) {
     using E = Elem<TYPE>;
     constexpr int P = E::kPer, U = NV < 4 ? NV : 4;
     __shared__ uint32_t bits[T * NV * P / 32], words[T];
@@ -487,6 +492,7 @@ __global__ void __launch_bounds__(T, NV == 32 ? 2 : NV == 16 ? 3 : 4) k_distill_
     const uint32_t word = TAIL ? words[threadIdx.x] : 0;
 #pragma unroll
     for (int j0 = 0; j0 < NV; j0 += U) {
+        if (j0 * T >= p.own) continue;                           // the row has ended
         float f[U * P], b = kNegInf;
 #pragma unroll
         for (int u = 0; u < U; ++u) {

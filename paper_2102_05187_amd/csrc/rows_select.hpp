@@ -17,12 +17,6 @@ template <int T> __device__ __forceinline__ int block_count(int n, int *slot) {
     lds_barrier();
     return *slot;
 }
-template <int T> __device__ __forceinline__ int block_count(bool yes, int *slot) {
-    const uint64_t b = __ballot(yes);
-    if (b && (threadIdx.x & (kWave - 1)) == 0) atomicAdd(slot, (int)__popcll(b));
-    lds_barrier();
-    return *slot;
-}
 
 constexpr int kBins = 512;
 

@@ -110,13 +110,27 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
             }
         }
     };
+    const auto edge = row.template edges<T>(v0, own);
     fetch(0);
 #pragma unroll
     for (int j0 = 0; j0 < NV; j0 += U) {
+        if (j0 * T >= own) {                                 // the row has ended
+#pragma unroll
+            for (int u = 0; u < U; ++u) top[j0 + u] = kNegInf;
+            continue;
+        }
         uint4 w[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = v[u];
-        if (j0 + U < NV) fetch(j0 + U);
+        if (j0 + U < NV && (j0 + U) * T < own) fetch(j0 + U);
+        if (row.odd) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[u] = row.settle(w[u], edge, j0 + u, (j0 + u) * T + threadIdx.x, own);
+        }
+        if constexpr (NV <= U) {                             // kept for later
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = w[u];
+        }
         float f[U * P], b = kNegInf;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
