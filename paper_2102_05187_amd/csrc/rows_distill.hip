@@ -176,13 +176,20 @@ template <int T, int P, class WORD> __device__ __forceinline__ WORD last_vector(
     return p.ends && (int)threadIdx.x == p.own % T ? (WORD)1 << (p.own / T) : (WORD)0;
 }
 
+// The words of a piece of NV vectors a thread.
+template <int NV> struct WordOf { using type = uint32_t; };
+template <> struct WordOf<40> { using type = uint64_t; };
+
+__device__ __forceinline__ int lowest(uint32_t w) { return __builtin_ctz(w); }
+__device__ __forceinline__ int lowest(uint64_t w) { return __builtin_ctzll(w); }
+
 // Takes in the vectors that `word` names, without the marked places where there is a tail.
 template <int TYPE, int T, bool TAIL, class WORD>
 __device__ __forceinline__ void take_some(Running &run, const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, WORD word,
                                           const Marks<T, Elem<TYPE>::kPer, WORD> &marks, float c2) {
     constexpr int P = Elem<TYPE>::kPer;
     while (word) {
-        const int i = (sizeof(WORD) == 8 ? __builtin_ctzll(word) : __builtin_ctz((uint32_t)word)) * T + threadIdx.x;
+        const int i = lowest(word) * T + threadIdx.x;
         word &= word - 1;
         float f[P], b = kNegInf;
         row.load(p.v0 + i, f);
@@ -371,17 +378,17 @@ template <int TYPE> __device__ __forceinline__ void write_some(const Row<TYPE> &
 
 // A piece of the gradient, whose logits v[] holds.  The few vectors with marked places, the one that the row ends in, and all where the row's
 // maximum is wild are read again and written one element after the other.
-template <int TYPE, int T, int NV>
+template <int TYPE, int T, int NV, class WORD>
 __device__ __forceinline__ void write_piece(const Row<TYPE> &row, const uint4 (&v)[NV], const Piece<Elem<TYPE>::kPer> &p, const Dense &d,
-                                            const Marks<T, Elem<TYPE>::kPer, uint32_t> &marks, typename Elem<TYPE>::T *out) {
+                                            const Marks<T, Elem<TYPE>::kPer, WORD> &marks, typename Elem<TYPE>::T *out) {
     using E = Elem<TYPE>;
     constexpr int P = E::kPer;
-    static_assert(NV <= 32, "a bit for each");
+    static_assert(NV <= 8 * sizeof(WORD), "a bit for each");
     const int n = p.own > (int)threadIdx.x ? (p.own - (int)threadIdx.x + T - 1) / T : 0;        // this thread's whole vectors
-    const uint32_t whole = n >= 32 ? ~0u : (1u << n) - 1;
-    uint32_t left = d.plain() ? marks.words[threadIdx.x] & whole : whole;
-    const uint32_t now = whole & ~left;
-    left |= last_vector<T, P, uint32_t>(p);
+    const WORD whole = n >= 8 * (int)sizeof(WORD) ? ~(WORD)0 : ((WORD)1 << n) - 1;
+    WORD left = d.plain() ? marks.words[threadIdx.x] & whole : whole;
+    const WORD now = whole & ~left;
+    left |= last_vector<T, P, WORD>(p);
     if (d.plain()) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -396,7 +403,7 @@ __device__ __forceinline__ void write_piece(const Row<TYPE> &row, const uint4 (&
             }
     }
     while (left) {
-        const int i = __builtin_ctz(left) * T + threadIdx.x;
+        const int i = lowest(left) * T + threadIdx.x;
         left &= left - 1;
         write_some(row, p.v0 + i, d, marks.of(i), out);
     }
@@ -417,7 +424,7 @@ template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Ro
     using V4 = typename Row<TYPE>::V4;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const V4 *at = (const V4 *)(row.p + (p.v0 + j * T) * E::kPer);         // one address for all threads
+        const V4 *at = (const V4 *)(row.p + (p.v0 + j * T) * E::kPer - (row.odd ? 1 : 0));         // one address for all threads
         V4 x = {E::kNone, E::kNone, E::kNone, E::kNone};
         if ((j + 1) * T <= p.own || j * T + (int)threadIdx.x < p.own) x = once ? __builtin_nontemporal_load(at + threadIdx.x) : at[threadIdx.x];
         v[j] = make_uint4(x.x, x.y, x.z, x.w);
@@ -442,6 +449,7 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
     const Marks<T, P, uint32_t> marks{bits, words};
     uint4 v[NV];
+    const auto edge = row.template edges<T>(p.v0, p.own);
     hold<TYPE, T>(row, p, a.once, v);
     const Entries en(a, r);
     marks.clear(p);
@@ -450,6 +458,10 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
     const double up = (double)w * a.scale * (dloss ? (double)dloss[r] : 1.0);
     write_entries<TYPE, T>(row, en, s, up, p.base(), p.columns(), out);
     lds_barrier();
+    if (row.odd) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) v[j] = row.settle(v[j], edge, j, j * T + threadIdx.x, p.own);
+    }
     write_piece<TYPE, T>(row, v, p, Dense(s, up, c2), marks, out);
 }
 
@@ -458,7 +470,9 @@ template <int TYPE, int T, int NV, bool TAIL>
 __global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_step(DistillArgs a, float c2, float *__restrict__ loss, void *dZ, int64_t lddz) {
     using E = Elem<TYPE>;
     constexpr int P = E::kPer, U = NV < 4 ? NV : 4;
-    __shared__ uint32_t bits[T * NV * P / 32], words[T];
+    using WORD = typename WordOf<NV>::type;
+    __shared__ uint32_t bits[T * NV * P / 32];
+    __shared__ WORD words[T];
     __shared__ float2 buf[T / kWave];
     __shared__ Taught taught;
     const int64_t r = blockIdx.x;
@@ -471,7 +485,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_
     }
     const Row<TYPE> row(a.Z, r, a.ldz, a.V);
     const Piece<P> p(a.V, 0, T * NV);
-    const Marks<T, P, uint32_t> marks{bits, words};
+    const Marks<T, P, WORD> marks{bits, words};
     const Entries en(a, r);
     uint4 v[NV];
     // A wavefront's loads come back in their order.  Of a long row the last wavefront goes through the entries before it asks for its part, while
@@ -486,13 +500,18 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_
         const Taught t = teach(row, en, TAIL, TAIL ? a.tlse[r] : 0.0);
         if (threadIdx.x == T - 1) taught = t;
     } else if (!kLong) marks.set(p, en);
+    const auto edge = row.template edges<T>(0, p.own);
     if (kLong) hold<TYPE, T>(row, p, a.once, v);
     lds_barrier();
     Running run;
-    const uint32_t word = TAIL ? words[threadIdx.x] : 0;
+    const WORD word = TAIL ? words[threadIdx.x] : 0;
 #pragma unroll
     for (int j0 = 0; j0 < NV; j0 += U) {
         if (j0 * T >= p.own) continue;                           // the row has ended
+        if (row.odd) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[j0 + u] = row.settle(v[j0 + u], edge, j0 + u, (j0 + u) * T + threadIdx.x, p.own);
+        }
         float f[U * P], b = kNegInf;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -504,7 +523,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_
         run.template take<U * P>(f, b, c2);
         __builtin_amdgcn_sched_barrier(0);
     }
-    take_some<TYPE, T, TAIL>(run, row, p, word | last_vector<T, P, uint32_t>(p), marks, c2);
+    take_some<TYPE, T, TAIL>(run, row, p, word | last_vector<T, P, WORD>(p), marks, c2);
     MaxSum d = run.sum(c2);
     block_join<T>(d, c2, buf);
     if (wild(d.m, c2)) d.s = slow_sum<TYPE, T>(row, 0, a.V, d.m, c2, buf, [&](int64_t c) { return TAIL && marks.at((int)c); });
@@ -530,7 +549,7 @@ Pieces cut_forward(int type, int64_t N, int64_t V) {
     if (nv > 8192)
         while (vectors > 512 && N * ((nv + vectors - 1) / vectors) < 256) vectors /= 2;
     const int64_t count = nv > 0 ? (nv + vectors - 1) / vectors : 1;
-    return Pieces{(int)(count == 1 ? (nv + 31) / 32 * 32 : vectors), (int)count};
+    return Pieces{(int)(((nv + count - 1) / count + 31) / 32 * 32), (int)count};           // of one length
 }
 
 int64_t round16(int64_t b) { return (b + 15) / 16 * 16; }
@@ -568,17 +587,20 @@ template <int TYPE> hipError_t step(const DistillArgs &a, float c2, float *loss,
     if (nv <= 256 * 8) return launch_step<TYPE, 256, 8>(a, c2, loss, dZ, lddz, st);
     if (nv <= 256 * 16) return launch_step<TYPE, 256, 16>(a, c2, loss, dZ, lddz, st);
     if (nv <= 256 * 32) return launch_step<TYPE, 256, 32>(a, c2, loss, dZ, lddz, st);
-    return launch_step<TYPE, 512, 32>(a, c2, loss, dZ, lddz, st);
+    if (nv <= 512 * 32) return launch_step<TYPE, 512, 32>(a, c2, loss, dZ, lddz, st);
+    return launch_step<TYPE, 512, 40>(a, c2, loss, dZ, lddz, st);
 }
 
 float log2_scale(const DistillArgs &a) { return (float)(a.scale * 1.4426950408889634); }
 
 }  // namespace
 
-// Whether a step holds its rows in registers; else it is the two calls, with the stat between them.
+// Whether a step holds its rows in registers; else it is the two calls, with the stat between them.  A row of more than 8192 vectors takes a
+// compute unit to itself, so that it is not read while the one before it is computed on: 4096 rows of 66000 elements of 16 bits 321 us, the two
+// calls 298; of 81920 334 and 347, of 131072 462 and 545.
 static bool held(int type, int64_t N, int64_t V) {
     const int64_t nv = vectors_of(type, V);
-    return nv <= 512 * 32 && (N >= 64 || nv <= 8192);
+    return nv <= 256 * 32 || (N >= 64 && nv > 10240 && nv <= 512 * 40);
 }
 static int64_t stat_bytes(int type, int64_t N, int64_t V) { return held(type, N, V) ? 0 : round16(N * (int64_t)sizeof(Stat)); }
 

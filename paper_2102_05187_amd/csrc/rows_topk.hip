@@ -396,7 +396,10 @@ Cut cut_rows(int type, int64_t V) {
     const int sizes[][2] = {{256, 1}, {256, 2}, {256, 4}, {256, 8}, {256, 16}, {256, 32}, {512, 32}};
     for (const auto &s : sizes)
         if (nv <= s[0] * s[1]) return Cut{s[0], s[1], 1};
-    return Cut{512, 32, (int)((nv + 512 * 32 - 1) / (512 * 32))};
+    // Of the two largest pieces the smaller where fewer of its places stay empty (4096 x 131074 of 16 bits: 214 us in 3 pieces, 294 in 2).  Of
+    // many pieces the larger: their number times K, 1024 at most, has to stay below kMerge.
+    const int64_t large = (nv + 16383) / 16384, small = (nv + 8191) / 8192;
+    return small < 2 * large && small <= 16 ? Cut{256, 32, (int)small} : Cut{512, 32, (int)large};
 }
 
 // Where a row's pieces are joined with those of other rows anyway, a cut costs nothing: pieces get smaller until 512 of them are there, or
