@@ -98,9 +98,13 @@ template <> struct Elem<COMET_F16> {
 // Vector i holds the elements i * kPer .. of the row wherever the row starts, so that what is computed from a row does not
 // depend on its address.  The device loads and stores 16 bytes at any address: at multiples of 4 as fast as at multiples of
 // 16 (6.6 TB/s over rows of 256 KB), at odd multiples of 2 a fifth slower (5.2 TB/s).
-// A row of 16-bit elements at such an odd multiple (`odd`: every other row where the rows' distance is odd) is therefore read from one
-// element before it on, which is the row before's, and every vector gets its last element from the vector behind it: the next lane's, or,
-// for the wavefront's last lane, from edges(), one load for all of a thread's vectors.  Row 0 has none before it, and is read as it lies.
+// A row of 16-bit elements at such an odd multiple (`odd`: every other row where the rows' distance is odd) can therefore be read from one
+// element before it on, which is the row before's; every vector gets its last element from the vector behind it: the next lane's, or,
+// for the wavefront's last lane, from edges(), one load for all of a thread's vectors.  Row 0 has none before it, and is read as it lies.  So
+// are rows that are short or few, which memory does not bound: top 64 of 4096 x 131071 of 16 bits 213 us shifted, 251 as they lie, of
+// 4096 x 24001 53 and 60, top 500 of 300 x 60013 25.8 and 23.6; forward of 8192 x 8003 58 and 54;
+// gradient of 1000 x 32003 32 and 35.
+inline bool read_shifted(int type, int64_t N, int64_t V) { return type != COMET_F32 && V >= 16384 && N * V * 2 >= (int64_t(48) << 20); }
 // Rows of 256 MB and more in all do not stay in the last cache (of that size), and are read past it: top 64 of 2048 x 131072 of 16 bits 100 us
 // through it, 95 past it.  Smaller ones are often there already, or are read again by the gradient: 5 to 11 us of 40 longer past it.
 inline bool read_once(int type, int64_t N, int64_t V) { return N * V * (type == COMET_F32 ? 4 : 2) >= (int64_t(256) << 20); }
@@ -110,8 +114,6 @@ typedef uint32_t V4At2 __attribute__((ext_vector_type(4), aligned(2)));
 template <int ALIGN> struct Wide { using type = V4At4; };
 template <> struct Wide<2> { using type = V4At2; };
 
-constexpr int64_t kOddFrom = 16384;
-
 template <int TYPE> struct Row {
     using E = Elem<TYPE>;
     using T = typename E::T;
@@ -119,8 +121,8 @@ template <int TYPE> struct Row {
     const T *p;              // the row's first element
     int64_t n;               // its length
     bool odd;
-    __device__ __forceinline__ Row(const void *base, int64_t row, int64_t ld, int64_t len)
-        : p((const T *)base + row * ld), n(len), odd(sizeof(T) == 2 && row > 0 && len >= kOddFrom && ((uintptr_t)p & 2)) {}
+    __device__ __forceinline__ Row(const void *base, int64_t row, int64_t ld, int64_t len, bool shift = false)
+        : p((const T *)base + row * ld), n(len), odd(sizeof(T) == 2 && shift && row > 0 && ((uintptr_t)p & 2)) {}
     __device__ __forceinline__ int64_t first(int64_t i) const { return i * E::kPer; }           // column of the vector's first element
     __device__ __forceinline__ bool whole(int64_t i) const { return first(i) + E::kPer <= n; }
     __device__ __forceinline__ uint4 raw(int64_t i) const {

@@ -268,6 +268,9 @@ __device__ __forceinline__ MaxSum read_piece(const Row<TYPE> &row, const Piece<E
     return d;
 }
 
+// One workgroup a row or a piece of one, four vectors a thread under way while four are taken in.  Bound by memory where rows are long and many
+// (4096 x 131072 of 16 bits in 195 us: 5.5 TB/s) and by the exponentials and their additions where they are shorter: 2048 x 50021 of 16 bits
+// 46 us in the kernel, 29 for its bytes alone at 7.1 TB/s.
 template <int TYPE, bool TAIL>
 __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, float c2, Pieces cut, float *__restrict__ loss, Stat *__restrict__ stat,
                                                               float2 *__restrict__ partial) {
@@ -283,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, flo
         if (threadIdx.x == 0 && cut.count == 1) loss[r] = 0;
         return;
     }
-    const Row<TYPE> row(a.Z, r, a.ldz, a.V);
+    const Row<TYPE> row(a.Z, r, a.ldz, a.V, a.shift);
     const Piece<P> p(a.V, (blockIdx.x - r * cut.count) * cut.vectors, cut.vectors);
     const Marks<T, P, uint64_t> marks{bits, words};
     // The last wavefront goes through the entries of a long row before it reads its part of it, while the others' parts keep the memory busy; of
@@ -431,7 +434,10 @@ template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Ro
     }
 }
 
-// Vectors [piece * T * NV, ..) of a row, from its stat.
+// Vectors [piece * T * NV, ..) of a row, from its stat.  Bound by memory, half of it stores, which go past the caches: nobody in the call reads
+// them again.  4096 x 131072 of 16 bits, 2.1 GB read and written, 350 us (6.1 TB/s); pieces of 1024 vectors, and of 512 where those would be
+// fewer than two workgroups a compute unit.  Rows of odd 16-bit elements are stored as they lie: shifted to whole words like their loads, with
+// single elements at the ends of wavefronts, 2048 x 50021 took 82 us and not 79.
 template <int TYPE, int T, int NV>
 __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2, int count, const Stat *__restrict__ stat,
                                                         const float *__restrict__ dloss, void *dZ, int64_t lddz) {
@@ -446,7 +452,7 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
         write_zeros<TYPE, T>(out, p.base(), p.base() + p.columns() < a.V ? p.base() + p.columns() : a.V);
         return;
     }
-    const Row<TYPE> row(a.Z, r, a.ldz, a.V);
+    const Row<TYPE> row(a.Z, r, a.ldz, a.V, a.shift);
     const Marks<T, P, uint32_t> marks{bits, words};
     uint4 v[NV];
     const auto edge = row.template edges<T>(p.v0, p.own);
@@ -465,7 +471,12 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
     write_piece<TYPE, T>(row, v, p, Dense(s, up, c2), marks, out);
 }
 
-// Loss and gradient of a row that a workgroup holds in registers: Z is read once.
+// Loss and gradient of a row that a workgroup holds in registers: Z is read once and dZ written once, where the two calls read Z twice.  Bound
+// by memory, and for rows of more than 8192 vectors by there being one workgroup a compute unit: 64 KB to 320 KB of its 512 KB of registers
+// are the row, so that one row's loads, sums and stores follow each other.  4096 x 131072 of 16 bits with a quarter of its rows ignored, 1.88 GB, 420 us
+// (4.5 TB/s; a copy of that size by the same kind of loop 6.2); of 24001 107 us (3.7 TB/s).  Going from row to row in one workgroup, the next row's loads
+// before the stores of the last, was no faster (425).  Three wavefronts a SIMD with a few registers spilled are better than two without (2048 x
+// 50016: 100 us and 117).
 template <int TYPE, int T, int NV, bool TAIL>
 __global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_step(DistillArgs a, float c2, float *__restrict__ loss, void *dZ, int64_t lddz) {
     using E = Elem<TYPE>;
@@ -483,13 +494,13 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_
         if (threadIdx.x == 0) loss[r] = 0;
         return;
     }
-    const Row<TYPE> row(a.Z, r, a.ldz, a.V);
+    const Row<TYPE> row(a.Z, r, a.ldz, a.V, a.shift);
     const Piece<P> p(a.V, 0, T * NV);
     const Marks<T, P, WORD> marks{bits, words};
     const Entries en(a, r);
     uint4 v[NV];
     // A wavefront's loads come back in their order.  Of a long row the last wavefront goes through the entries before it asks for its part, while
-    // the others' parts keep the memory busy (4096 x 131072 of 16 bits: 450 us after it, SHORTER before it); of a short one all parts first.
+    // the others' parts keep the memory busy (4096 x 131072 of 16 bits: 450 us after it, 412 before it); of a short one all parts first.
     constexpr bool kLong = NV >= 16;
     const bool teacher = threadIdx.x >= T - kWave;
     if (!kLong) hold<TYPE, T>(row, p, a.once, v);
@@ -608,7 +619,7 @@ int64_t distill_work(int type, int64_t N, int64_t V) { return stat_bytes(type, N
 
 hipError_t distill_forward(const DistillArgs &given, float *loss, double *stat, void *work, hipStream_t st) {
     DistillArgs a = given;
-    a.once = read_once(a.type, a.N, a.V);
+    a.once = read_once(a.type, a.N, a.V), a.shift = read_shifted(a.type, a.N, a.V);
     const float c2 = log2_scale(a);
     const Pieces c = cut_forward(a.type, a.N, a.V);
     float2 *partial = (float2 *)((char *)work + stat_bytes(a.type, a.N, a.V));
@@ -619,7 +630,7 @@ hipError_t distill_forward(const DistillArgs &given, float *loss, double *stat, 
 
 hipError_t distill_backward(const DistillArgs &given, const double *stat, const float *dloss, void *dZ, int64_t lddz, hipStream_t st) {
     DistillArgs a = given;
-    a.once = read_once(a.type, a.N, a.V);
+    a.once = read_once(a.type, a.N, a.V), a.shift = read_shifted(a.type, a.N, a.V);
     const float c2 = log2_scale(a);
     return a.type == COMET_F32 ? backward<COMET_F32>(a, c2, (const Stat *)stat, dloss, dZ, lddz, st)
          : a.type == COMET_BF16 ? backward<COMET_BF16>(a, c2, (const Stat *)stat, dloss, dZ, lddz, st)
@@ -628,7 +639,7 @@ hipError_t distill_backward(const DistillArgs &given, const double *stat, const 
 
 hipError_t distill_step(const DistillArgs &given, float *loss, void *dZ, int64_t lddz, void *work, hipStream_t st) {
     DistillArgs a = given;
-    a.once = read_once(a.type, a.N, a.V);
+    a.once = read_once(a.type, a.N, a.V), a.shift = read_shifted(a.type, a.N, a.V);
     if (held(a.type, a.N, a.V)) {
         const float c2 = log2_scale(a);
         return a.type == COMET_F32 ? step<COMET_F32>(a, c2, loss, dZ, lddz, st)

@@ -1,13 +1,17 @@
 // The K largest elements of dense rows, with the rows' log-sum-exp.
 //
-// A workgroup reads a piece of a row once (up to 256 KB; rows beyond that, and rows that are too few to fill the device, are cut into
-// several pieces whose results a second kernel joins) and keeps of every vector of 16 bytes its largest element in a register.
+// A workgroup reads a piece of a row once (up to 256 KB; rows beyond that, and those of beams that are too few to fill the device, are cut
+// into several pieces whose results a second kernel joins) and keeps of every vector of 16 bytes its largest element in a register.
 // From these:
 //   1. a bound that K to 1.25 K of the threads' largest elements reach (bound()): of a row in no particular order about
 //      K (1 + K / 2T) elements reach it, of T threads; all others are out;
 //   2. the vectors whose largest element reaches it are listed and read again, K or so of them, and their elements that do go
 //      into LDS as 64-bit keys (value, then lower column);
 //   3. the keys are put in order (sort_items()).
+// Bound by memory where rows are long and many: top 64 of 2048 x 131072 of 16 bits in 101 us, 5.3 TB/s (a plain read of
+// that size 7.1).  A single row is bound by the latency of
+// these steps: 8 us of 32000 32-bit elements, 13 of 131072 of 16 bits.  Shapes of more threads with fewer vectors each were slower throughout
+// (1024 threads: 146 us, and 13 for 11.5 with 4 rows).
 // Where more than 2048 reach the bound (equal elements, or the large ones next to each other in a few threads) the K-th largest key is
 // found exactly, by halving, with the vectors that matter read again each time.
 #include "rows_kernels.hpp"
@@ -23,7 +27,7 @@ struct TopArgs {
     float c2;                             // scale log2(e)
     double scale;
     int K, splits;
-    bool by_coordinate, once;
+    bool by_coordinate, once, shift;      // once, shift: how rows are read
     int32_t *crd;                         // results, where a row is one piece and no keys are asked for
     float *vals, *lse;
     const uint8_t *finished;
@@ -87,7 +91,7 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
         if (threadIdx.x == 0) a.sums[piece] = make_float2(split == 0 ? 0.f : kNegInf, split == 0 ? 1.f : 0.f);
         return;
     }
-    const Row<TYPE> row(a.Z, r, a.ldz, a.V);
+    const Row<TYPE> row(a.Z, r, a.ldz, a.V, a.shift);
     const int64_t v0 = (int64_t)split * T * NV, full = row.n / P;
     const int own = (int)(full - v0 < T * NV ? full - v0 : T * NV);           // whole vectors of this piece
     const bool ends_here = row.n % P != 0 && full >= v0 && full < v0 + T * NV;    // ... and the one that the row ends in: thread 0's
@@ -440,7 +444,7 @@ int64_t rows_topk_work(int type, int64_t N, int64_t V, int64_t K) {
 hipError_t rows_topk(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, double scale, int64_t K, bool by_coordinate,
                      int32_t *crd, float *vals, float *lse, void *work, hipStream_t st) {
     const Cut c = cut_rows(type, V);
-    TopArgs a{Z, V, ldz, (float)(scale * 1.4426950408889634), scale, (int)K, c.splits, by_coordinate, read_once(type, N, V), crd, vals, lse, nullptr, 0, nullptr, nullptr};
+    TopArgs a{Z, V, ldz, (float)(scale * 1.4426950408889634), scale, (int)K, c.splits, by_coordinate, read_once(type, N, V), read_shifted(type, N, V), crd, vals, lse, nullptr, 0, nullptr, nullptr};
     if (c.splits > 1) {
         a.sums = (float2 *)work;
         a.keys = (uint64_t *)((char *)work + round16(N * c.splits * (int64_t)sizeof(float2)));
@@ -469,7 +473,7 @@ TopLists rows_top_lists(int type, int64_t N, int64_t V, int64_t K, int64_t toget
 hipError_t rows_top_keys(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t K, int64_t together, const TopLists &l, const uint8_t *finished, int32_t eos,
                          void *work, hipStream_t st) {
     const Cut c = cut_lists(type, N, V, K, together);
-    const TopArgs a{Z, V, ldz, kLog2e, 1.0, (int)K, c.splits, false, read_once(type, N, V), nullptr, nullptr, nullptr, finished, eos,
+    const TopArgs a{Z, V, ldz, kLog2e, 1.0, (int)K, c.splits, false, read_once(type, N, V), read_shifted(type, N, V), nullptr, nullptr, nullptr, finished, eos,
                     (uint64_t *)((char *)work + round16(N * c.splits * (int64_t)sizeof(float2))), (float2 *)work};
     const hipError_t e = launch(type, c, a, N, st);
     if (e != hipSuccess || !l.joined) return e;
