@@ -8,7 +8,7 @@ namespace {
 constexpr int64_t kLim = int64_t(1) << 31;
 constexpr int64_t kRows = int64_t(1) << 23;      // a grid holds a workgroup or more for each row
 
-constexpr int64_t kTop = int64_t(1) << 29;       // V * K: one workgroup joins the lists of a row's pieces, 2^29 / 65536 + 1024 keys at most
+constexpr int64_t kTop = int64_t(1) << 29;       // V * K: one workgroup joins the lists of a row's pieces, 2^29 / 65536 + 1024 keys at most, or 16 * 1024
 
 int element_size(int type) { return type == COMET_F32 ? 4 : 2; }
 bool known(comet_type_t type) { return type == COMET_F32 || type == COMET_BF16 || type == COMET_F16; }
