@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
 }
 
 // Loss and gradient of a row that a workgroup holds in registers: Z is read once and dZ written once, where the two calls read Z twice.  Bound
-// by memory, and for rows of more than 8192 vectors by there being one workgroup a compute unit: 64 KB to 320 KB of its 512 KB of registers
+// by memory, and for rows of more than 8192 vectors by there being one workgroup a compute unit: 160 KB to 320 KB of its 512 KB of registers
 // are the row, so that one row's loads, sums and stores follow each other.  4096 x 131072 of 16 bits with a quarter of its rows ignored, 1.88 GB, 420 us
 // (4.5 TB/s; a copy of that size by the same kind of loop 6.2); of 24001 107 us (3.7 TB/s).  Going from row to row in one workgroup, the next row's loads
 // before the stores of the last, was no faster (425).  Three wavefronts a SIMD with a few registers spilled are better than two without (2048 x
@@ -608,7 +608,7 @@ float log2_scale(const DistillArgs &a) { return (float)(a.scale * 1.442695040888
 
 // Whether a step holds its rows in registers; else it is the two calls, with the stat between them.  A row of more than 8192 vectors takes a
 // compute unit to itself, so that it is not read while the one before it is computed on: 4096 rows of 66000 elements of 16 bits 321 us, the two
-// calls 298; of 81920 334 and 347, of 131072 462 and 545.
+// calls 298; of 81920 334 and 347, of 131072 462 and 545, of 151936 554 and 644.
 static bool held(int type, int64_t N, int64_t V) {
     const int64_t nv = vectors_of(type, V);
     return nv <= 256 * 32 || (N >= 64 && nv > 10240 && nv <= 512 * 40);
