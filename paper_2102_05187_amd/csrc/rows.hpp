@@ -188,9 +188,11 @@ struct MaxSum {
 };
 
 // The same while it is taken in, with one multiply-add and one exp2 an element: s holds exp2(c z - shift), where shift is c m rounded,
-// and what that rounding did to all terms alike is taken out at the end.  Where |c m| reaches kWild (rows masked by the lowest value of a
-// type throughout, or with +inf) this loses what is left: the sum of a row whose maximum is wild() is taken again by slow_sum.
-constexpr float kWild = 1e30f;
+// and what that rounding did to all terms alike is taken out at the end.  It is half a unit of c m at most: 64 below 2^31, and a sum of 2^31
+// terms of 2^64 is still a number.  From there on (masks of -2e9 and beyond, the lowest value of a type among them, +inf) shift stays at the limit:
+// a thread whose places are all far below it has a sum of 0, as they have in a row with an ordinary maximum; the sum of a row, or a
+// piece of one, whose maximum is itself wild() is taken again by slow_sum.
+constexpr float kWild = 0x1p31f;
 __device__ __forceinline__ bool wild(float m, float c) { return m > kNegInf && !(fabsf(m * c) < kWild); }
 
 struct Running {
@@ -216,7 +218,8 @@ struct Running {
     __device__ __forceinline__ MaxSum sum(float c) const {
         MaxSum r;
         r.m = m;
-        r.s = fabsf(shift) < kWild ? s * exp2_fast(-__builtin_fmaf(m, c, -shift)) : s;
+        const float e = -__builtin_fmaf(m, c, -shift);            // what makes s relative to m: up to any size where shift is at its lower limit
+        r.s = s * (e < 100.f ? exp2_fast(e) : 0.f);
         return r;
     }
 };
@@ -291,7 +294,7 @@ template <int T> __device__ __forceinline__ void block_join(MaxSum &a, float c, 
     for (int w = 0; w < T / kWave; ++w) a.join(buf[w].x, buf[w].y, c);
     lds_barrier();
 }
-// The sum over columns [begin, end) of a row whose maximum there is m, against m itself: what Running loses where m is wild.  A column
+// The sum over columns [begin, end) of a row whose maximum there is m, against m itself: what Running does not have where m is wild.  A column
 // that `skip` names is left out.  By a workgroup of T threads.
 template <int TYPE, int T, class SKIP>
 __device__ __forceinline__ float slow_sum(const Row<TYPE> &row, int64_t begin, int64_t end, float m, float c, float2 *buf, SKIP skip) {

@@ -358,13 +358,16 @@ __device__ __forceinline__ void write_entries(const Row<TYPE> &row, const Entrie
         }
 }
 
-// The dense pass of the gradient: g = A exp2(c2 (z - m)), with one multiply-add, one exp2 and one product an element.
+// The dense pass of the gradient: g = A exp2(c2 (z - m)), with one multiply-add, one exp2 and one product an element.  What rounding c2 m does
+// to the exponentials is put into A: a factor of 2^16 at most below kFlat, which leaves every A a number that has one to round to.  Rows beyond
+// it (masked throughout by -4e8 or less) are computed from z - m, element by element.
+constexpr float kFlat = 0x1p29f;
 struct Dense {
     float A, m, c2, shift;
     __device__ __forceinline__ Dense(const Stat &s, double up, float c2_) : A((float)(up * s.A)), m((float)s.m), c2(c2_), shift(m * c2_) {
         if (plain()) A *= exp2_fast(-__builtin_fmaf(m, c2, -shift));
     }
-    __device__ __forceinline__ bool plain() const { return fabsf(shift) < kWild; }
+    __device__ __forceinline__ bool plain() const { return fabsf(shift) < kFlat; }
     __device__ __forceinline__ float of(float z) const { return A * exp2_fast(__builtin_fmaf(z, c2, -shift)); }        // where plain()
     __device__ __forceinline__ float slow(float z) const { return A * exp2_fast(plain() ? __builtin_fmaf(z, c2, -shift) : (z - m) * c2); }
 };
@@ -379,8 +382,8 @@ template <int TYPE> __device__ __forceinline__ void write_some(const Row<TYPE> &
         if (i * P + k < row.n && !(mk >> k & 1)) out[i * P + k] = Elem<TYPE>::bits(d.slow(f[k]));
 }
 
-// A piece of the gradient, whose logits v[] holds.  The few vectors with marked places, the one that the row ends in, and all where the row's
-// maximum is wild are read again and written one element after the other.
+// A piece of the gradient, whose logits v[] holds.  The few vectors with marked places, the one that the row ends in, and all of a row that is
+// not plain() are read again and written one element after the other.
 template <int TYPE, int T, int NV, class WORD>
 __device__ __forceinline__ void write_piece(const Row<TYPE> &row, const uint4 (&v)[NV], const Piece<Elem<TYPE>::kPer> &p, const Dense &d,
                                             const Marks<T, Elem<TYPE>::kPer, WORD> &marks, typename Elem<TYPE>::T *out) {
