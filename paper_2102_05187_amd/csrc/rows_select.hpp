@@ -21,17 +21,17 @@ template <int T> __device__ __forceinline__ int block_count(int n, int *slot) {
 constexpr int kBins = 512;
 
 // A value that at least K of the held numbers reach and not many more: those between `lo` and `hi` (the largest) are counted in 256 bins, by
-// value first, then, while more than 1.25 K + 4 reach the bin that the K-th largest is in, by their order inside of that bin (each time a
-// 256th of the range, so that outliers do no harm).  EACH(f) calls f with every number of the thread; those below lo are not counted.  Elements below
-// the value that comes back cannot be among the K largest of the workgroup's where each number is one of them.  Where fewer
-// than K numbers are counted it is the lowest there is.  The same for all threads.  `bins`: kBins places of LDS that hold 0 and have been
-// since a barrier.
+// value first, where the bins' width and its inverse are ordinary numbers, then, while more than 1.25 K + 4 reach the bin that the K-th largest
+// is in, by their order inside of that bin (each time a 256th of the range, so that outliers do no harm).  EACH(f) calls f with every number of
+// the thread; those below lo are not counted.  Elements below the value that comes back cannot be among the K largest of the workgroup's where
+// each number is one of them.  Where fewer than K numbers are counted it is the lowest there is.  The same for all threads.  `bins`: kBins
+// places of LDS that hold 0 and have been since a barrier.
 template <int T, class EACH> __device__ __forceinline__ float bound(float lo, float hi, int K, EACH each, int *bins) {
     constexpr int B = kBins / 2;
     const int lane = threadIdx.x & (kWave - 1), most = K + K / 4 + 4;
     const float everything = -3.402823466e38f;
     uint32_t from = order_of(lo), to = order_of(hi);
-    bool by_value = hi - lo < __builtin_huge_valf();
+    bool by_value = hi - lo > 1e-30f && hi - lo < __builtin_huge_valf();
     for (int round = 0; round < 6; ++round) {
         int *bin = bins + (round & 1) * B;
         const float per = (float)B / (hi - lo);
