@@ -495,13 +495,22 @@ def _given(t: Optional[torch.Tensor], dtype, shape, what: str, device) -> Option
     return t
 
 
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """Memory for a call on `stream`, from that stream's pool: what the current stream's pool has free may still be in use by work that
+    the current stream has before it."""
+    if stream is None:
+        return torch.empty(*shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(*shape, dtype=dtype, device=device)
+
+
 def _new(t: Optional[torch.Tensor], dtype, shape, what: str, device, stream) -> torch.Tensor:
-    """A result: the caller's tensor, or a new one, which other streams than the current one are told about."""
+    """A result: the caller's tensor, or a new one, which the current stream is expected to go on with."""
     if t is not None:
         return _given(t, dtype, shape, what, device)
-    t = torch.empty(*shape, dtype=dtype, device=device)
+    t = _empty(shape, dtype, device, stream)
     if stream is not None:
-        t.record_stream(stream)
+        t.record_stream(torch.cuda.current_stream(device))
     return t
 
 
@@ -513,10 +522,10 @@ def _work_bytes(call: str, *sizes) -> int:
 
 
 def _work(need: int, device, stream):
-    """(tensor, pointer) of scratch for one call: its memory goes back to torch's allocator, which keeps it for the stream."""
+    """(tensor, pointer) of scratch for one call: its memory goes back to the pool of the stream that the call runs on."""
     if need == 0:
         return None, None
-    t = _new(None, torch.uint8, (need,), "work", device, stream)
+    t = _empty((need,), torch.uint8, device, stream)
     return t, t.data_ptr()
 
 
