@@ -529,6 +529,19 @@ def _work(need: int, device, stream):
     return t, t.data_ptr()
 
 
+def _call(name: str, device, stream, *args) -> None:
+    """One of the calls on dense rows, on its operands' device, with the stream (that device's current one: None) as the last argument."""
+    if stream is not None and stream.device != device:
+        raise ValueError("stream must be one of %s, where the operands are" % device)
+    call = getattr(_lib(), name)
+    if _raw_device is not None and _raw_device() == device.index:
+        status = call(*args, _stream(stream))
+    else:
+        with torch.cuda.device(device):
+            status = call(*args, _stream(stream))
+    _check(status, name)
+
+
 def comet_rows_topk(Z: torch.Tensor, K: int, scale: float = 1.0, by_coordinate: bool = False, crd: Optional[torch.Tensor] = None,
                     vals: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None):
     """(crd, vals, lse): the K largest elements of every row of Z and log sum exp(scale * row)."""
@@ -539,8 +552,8 @@ def comet_rows_topk(Z: torch.Tensor, K: int, scale: float = 1.0, by_coordinate: 
     vals = _new(vals, torch.float32, (N, K), "vals", dev, stream)
     lse = _new(lse, torch.float32, (N,), "lse", dev, stream)
     work, wptr = _work(need, dev, stream)
-    _check(_lib().comet_rows_topk(ptr, kind, N, V, ld, float(scale), K, COMET_BY_COORDINATE if by_coordinate else 0, crd.data_ptr(),
-                                  vals.data_ptr(), lse.data_ptr(), wptr, need, _stream(stream)), "comet_rows_topk")
+    _call("comet_rows_topk", dev, stream, ptr, kind, N, V, ld, float(scale), K, COMET_BY_COORDINATE if by_coordinate else 0, crd.data_ptr(),
+          vals.data_ptr(), lse.data_ptr(), wptr, need)
     return crd, vals, lse
 
 
@@ -575,7 +588,7 @@ def comet_distill_forward(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tenso
     loss = _new(loss, torch.float32, (N,), "loss", dev, stream)
     stat = _new(stat, torch.float64, (N, COMET_DISTILL_STAT), "stat", dev, stream)
     work, wptr = _work(need, dev, stream)
-    _check(_lib().comet_distill_forward(*args, loss.data_ptr(), stat.data_ptr(), wptr, need, _stream(stream)), "comet_distill_forward")
+    _call("comet_distill_forward", dev, stream, *args, loss.data_ptr(), stat.data_ptr(), wptr, need)
     return loss, stat
 
 
@@ -597,7 +610,7 @@ def comet_distill_backward(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tens
     _given(stat, torch.float64, (N, COMET_DISTILL_STAT), "stat", dev)
     _given(dloss, torch.float32, (N,), "dloss", dev)
     dZ, out, ldo = _gradient(Z, dZ, stream)
-    _check(_lib().comet_distill_backward(*args, _ptr(stat), _ptr(dloss), out, ldo, _stream(stream)), "comet_distill_backward")
+    _call("comet_distill_backward", dev, stream, *args, _ptr(stat), _ptr(dloss), out, ldo)
     return dZ
 
 
@@ -610,7 +623,7 @@ def comet_distill_step(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tensor, 
     loss = _new(loss, torch.float32, (N,), "loss", dev, stream)
     dZ, out, ldo = _gradient(Z, dZ, stream)
     work, wptr = _work(need, dev, stream)
-    _check(_lib().comet_distill_step(*args, loss.data_ptr(), out, ldo, wptr, need, _stream(stream)), "comet_distill_step")
+    _call("comet_distill_step", dev, stream, *args, loss.data_ptr(), out, ldo, wptr, need)
     return loss, dZ
 
 
@@ -633,8 +646,8 @@ def comet_beam_select(Z: torch.Tensor, score: torch.Tensor, n: int, finished: Op
     parent = _new(None, torch.int32, (B, n), "parent", dev, stream)
     token = _new(None, torch.int32, (B, n), "token", dev, stream)
     work, wptr = _work(need, dev, stream)
-    _check(_lib().comet_beam_select(ptr, kind, B, W, V, ld, score.data_ptr(), _ptr(finished), int(eos), n, best.data_ptr(), parent.data_ptr(),
-                                    token.data_ptr(), wptr, need, _stream(stream)), "comet_beam_select")
+    _call("comet_beam_select", dev, stream, ptr, kind, B, W, V, ld, score.data_ptr(), _ptr(finished), int(eos), n, best.data_ptr(), parent.data_ptr(),
+          token.data_ptr(), wptr, need)
     return best, parent, token
 
 
@@ -669,8 +682,7 @@ def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, str
             raise ValueError("a state must have shape [%d, %d, ...], got %s" % (B, W, tuple(shape)))
         if device != parent.device:
             raise ValueError("states must be on %s" % parent.device)
-    lib, st = _lib(), _stream(stream)
     for (shape, strides, dtype, device), ptrs in groups.items():
         if 0 not in shape:
             layout = _pieces(shape, strides, dtype.itemsize)
-            _check(lib.comet_beam_reorder((ctypes.c_void_p * len(ptrs))(*ptrs), len(ptrs), B, W, *layout, parent.data_ptr(), st), "comet_beam_reorder")
+            _call("comet_beam_reorder", parent.device, stream, (ctypes.c_void_p * len(ptrs))(*ptrs), len(ptrs), B, W, *layout, parent.data_ptr())
