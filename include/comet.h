@@ -351,7 +351,7 @@ comet_status comet_rows_topk(const void *Z, comet_type_t type, int64_t N, int64_
  * comet_distill_step is the forward and the backward call (dloss all 1) in one, without a stat.
  * Where the row's distribution is empty: no entry with a probability and no rest gives loss 0 and gradient 0.  A place of Z that
  * is -inf has q = 0; where the teacher gives it mass the loss is +inf, and the gradient still finite (q - p).  NaN and +inf
- * in a row of Z, a row's tvals, tlse or weight make that row's loss and gradient NaN, and no other row's. */
+ * in a row of Z, a row's tvals, tlse or weight (-inf too in the weight) make that row's loss and gradient NaN, and no other row's. */
 #define COMET_DISTILL_STAT 7
 comet_status comet_distill_work(comet_type_t type, int64_t N, int64_t V, int64_t *bytes /* host */);
 comet_status comet_distill_forward(const void *Z, comet_type_t type, int64_t N, int64_t V, int64_t ldz, const int32_t *pos, int64_t K,

@@ -125,6 +125,7 @@ __device__ __forceinline__ double finish(const Taught &t, MaxSum d, bool tail, d
     out->A = none ? 0.0 : tail ? P * outside / tot - t.rest / (double)d.s : P / (double)d.s;
     const double bad = lse.big + P;                              // NaN and +inf in the row or its entries
     if (bad != bad) loss = out->A = bad;
+    if (t.norm.big == -kNegInfD || w - w != 0) loss = out->A = __builtin_nan("");        // ... in tlse or the weight
     return w * loss;
 }
 
