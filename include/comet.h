@@ -322,7 +322,7 @@ typedef enum { COMET_F32 = 0, COMET_BF16 = 1, COMET_F16 = 2 } comet_type_t;
  *              their coordinates, so that crd and vals with pos = {0, K, 2K, ..} are a [D,CU] matrix.  An element that is -inf
  *              (a masked place) or NaN is no entry; where a row has fewer than K, the places at its end hold -1 and -inf.
  *   lse        device, [N], may be NULL: log sum_j exp(scale z_rj) over the whole row; -inf for a row without an element
- *              over -inf, +inf with a +inf in it, NaN with a NaN.
+ *              over -inf, NaN with a NaN, else +inf with a +inf in it.
  *   K          1 <= K <= COMET_MAX_TOP, V * K <= 2^29. */
 #define COMET_BY_COORDINATE 1u
 #define COMET_MAX_TOP 1024

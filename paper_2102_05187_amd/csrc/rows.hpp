@@ -295,13 +295,16 @@ template <int T> __device__ __forceinline__ void block_join(MaxSum &a, float c, 
     lds_barrier();
 }
 // The sum over columns [begin, end) of a row whose maximum there is m, against m itself: what Running does not have where m is wild.  A column
-// that `skip` names is left out.  By a workgroup of T threads.
+// that `skip` names is left out.  Where m is +inf it is the number of its places, or a NaN.  By a workgroup of T threads.
 template <int TYPE, int T, class SKIP>
 __device__ __forceinline__ float slow_sum(const Row<TYPE> &row, int64_t begin, int64_t end, float m, float c, float2 *buf, SKIP skip) {
     MaxSum a;
     a.m = m;
     for (int64_t i = begin + threadIdx.x; i < end && i < row.n; i += T)
-        if (!skip(i)) a.s += exp2_fast((Elem<TYPE>::one(row.p[i]) - m) * c);
+        if (!skip(i)) {
+            const float z = Elem<TYPE>::one(row.p[i]);
+            a.s += z == m ? 1.f : exp2_fast((z - m) * c);
+        }
     block_join<T>(a, c, buf);
     return a.s;
 }

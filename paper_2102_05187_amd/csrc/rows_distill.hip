@@ -114,7 +114,7 @@ __device__ __forceinline__ double finish(const Taught &t, MaxSum d, bool tail, d
         lse.rest = log_of((float)tot);
         if (!none) share = (big - lse.big) + (log_s - lse.rest);
     }
-    if (d.s != d.s) lse.big = d.s;
+    if (d.s != d.s || d.m == -kNegInf) lse.big = __builtin_nan("");
     double loss = t.part;
     if (t.mass != 0 && t.xa != kNegInfD) loss += t.mass * ((lse.big - t.xa) + lse.rest);
     if (t.rest != 0) loss -= t.rest * share;

@@ -74,7 +74,7 @@ template <int T> __device__ __forceinline__ void write_keys(TopShared &sh, int n
 }
 // A row's log-sum-exp.
 __device__ __forceinline__ float lse_of(const MaxSum &a, double scale) {
-    if (a.m == -kNegInf || (a.m == kNegInf && a.s == a.s)) return a.m;
+    if (fabsf(a.m) == -kNegInf && a.s == a.s) return a.m;
     return (float)((double)a.m * scale + log_of(a.s));
 }
 
