@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
         lds_barrier();
         if (pass == 1 || found <= kCandidates) break;
         // many equal ones: the n-th largest score exactly, and of the candidates that have it as many as are missing
-        bar64 = kth<T>(1, order64(1.7976931348623157e308), n, [&](uint64_t t) {
+        bar64 = kth<T>(1, order64(-kNegInfD), n, [&](uint64_t t) {
             int c = 0;
 #pragma unroll
             for (int j = 0; j < PER; ++j) c += s[j] >= t ? 1 : 0;
