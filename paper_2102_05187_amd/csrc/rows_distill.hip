@@ -582,13 +582,32 @@ template <int TYPE> hipError_t forward(const DistillArgs &a, float c2, const Pie
     return hipGetLastError();
 }
 
+// The call's rows from r0 on, n of them.
+template <int TYPE> DistillArgs rows_from(const DistillArgs &a, int64_t r0, int64_t n) {
+    DistillArgs b = a;
+    b.Z = (const typename Elem<TYPE>::T *)a.Z + r0 * a.ldz;
+    b.N = n;
+    if (a.pos) b.pos += r0;
+    else b.crd += r0 * a.K, b.tvals += r0 * a.K;
+    if (a.tlse) b.tlse += r0;
+    if (a.weight) b.weight += r0;
+    return b;
+}
+
 template <int TYPE> hipError_t backward(const DistillArgs &a, float c2, const Stat *stat, const float *dloss, void *dZ, int64_t lddz, hipStream_t st) {
     const int64_t nv = vectors_of(TYPE, a.V);
     const bool big = a.N * ((nv + 1023) / 1024) >= 512;
     const int64_t piece = big ? 1024 : 512, count = (nv + piece - 1) / piece;
     const auto kernel = big ? k_distill_backward<TYPE, 256, 4> : k_distill_backward<TYPE, 256, 2>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.N * count)), dim3(256), 0, st, a, c2, (int)count, stat, dloss, dZ, lddz);
-    return hipGetLastError();
+    const int64_t most = ((int64_t(1) << 24) - 1) / count;       // a launch has fewer than 2^32 threads
+    for (int64_t r0 = 0; r0 < a.N; r0 += most) {
+        const int64_t n = a.N - r0 < most ? a.N - r0 : most;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(n * count)), dim3(256), 0, st, rows_from<TYPE>(a, r0, n), c2, (int)count, stat + r0,
+                           dloss ? dloss + r0 : nullptr, (typename Elem<TYPE>::T *)dZ + r0 * lddz, lddz);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <int TYPE, int T, int NV> hipError_t launch_step(const DistillArgs &a, float c2, float *loss, void *dZ, int64_t lddz, hipStream_t st) {
