@@ -542,18 +542,27 @@ def _call(name: str, device, stream, *args) -> None:
     _check(status, name)
 
 
+def _written(*results: Optional[torch.Tensor]) -> None:
+    """The caller's tensors that a call has overwritten: automatic differentiation refuses to use what it kept of them."""
+    given = [t for t in results if t is not None]
+    if given:
+        torch.autograd.graph.increment_version(given)
+
+
 def comet_rows_topk(Z: torch.Tensor, K: int, scale: float = 1.0, by_coordinate: bool = False, crd: Optional[torch.Tensor] = None,
                     vals: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None):
     """(crd, vals, lse): the K largest elements of every row of Z and log sum exp(scale * row)."""
     ptr, kind, N, V, ld = _rows(Z)
     K, dev = int(K), Z.device
     need = _work_bytes("comet_rows_topk", kind, N, V, K)
+    given = crd, vals, lse
     crd = _new(crd, torch.int32, (N, K), "crd", dev, stream)
     vals = _new(vals, torch.float32, (N, K), "vals", dev, stream)
     lse = _new(lse, torch.float32, (N,), "lse", dev, stream)
     work, wptr = _work(need, dev, stream)
     _call("comet_rows_topk", dev, stream, ptr, kind, N, V, ld, float(scale), K, COMET_BY_COORDINATE if by_coordinate else 0, crd.data_ptr(),
           vals.data_ptr(), lse.data_ptr(), wptr, need)
+    _written(*given)
     return crd, vals, lse
 
 
@@ -585,10 +594,12 @@ def comet_distill_forward(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tenso
     """(loss, stat): the loss of every row, and what comet_distill_backward needs of it."""
     N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
     need = _work_bytes("comet_distill", kind, N, V)
+    given = loss, stat
     loss = _new(loss, torch.float32, (N,), "loss", dev, stream)
     stat = _new(stat, torch.float64, (N, COMET_DISTILL_STAT), "stat", dev, stream)
     work, wptr = _work(need, dev, stream)
     _call("comet_distill_forward", dev, stream, *args, loss.data_ptr(), stat.data_ptr(), wptr, need)
+    _written(*given)
     return loss, stat
 
 
@@ -609,8 +620,10 @@ def comet_distill_backward(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tens
     N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
     _given(stat, torch.float64, (N, COMET_DISTILL_STAT), "stat", dev)
     _given(dloss, torch.float32, (N,), "dloss", dev)
+    given = dZ
     dZ, out, ldo = _gradient(Z, dZ, stream)
     _call("comet_distill_backward", dev, stream, *args, _ptr(stat), _ptr(dloss), out, ldo)
+    _written(given)
     return dZ
 
 
@@ -620,10 +633,12 @@ def comet_distill_step(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tensor, 
     """(loss, dZ): both at once, for a training step that knows its rows' weights; dZ may be Z itself."""
     N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
     need = _work_bytes("comet_distill", kind, N, V)
+    given = loss, dZ
     loss = _new(loss, torch.float32, (N,), "loss", dev, stream)
     dZ, out, ldo = _gradient(Z, dZ, stream)
     work, wptr = _work(need, dev, stream)
     _call("comet_distill_step", dev, stream, *args, loss.data_ptr(), out, ldo, wptr, need)
+    _written(*given)
     return loss, dZ
 
 
@@ -672,7 +687,7 @@ def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, str
         raise ValueError("parent must have two dimensions")
     B, W = parent.shape
     _dev(parent, torch.int32, "parent")
-    groups = {}
+    states, groups = list(states), {}
     for t in states:
         if not isinstance(t, torch.Tensor) or not t.is_cuda:
             raise TypeError("states must be torch tensors in device memory")
@@ -682,6 +697,7 @@ def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, str
             raise ValueError("a state must have shape [%d, %d, ...], got %s" % (B, W, tuple(shape)))
         if device != parent.device:
             raise ValueError("states must be on %s" % parent.device)
+    _written(*states)
     for (shape, strides, dtype, device), ptrs in groups.items():
         if 0 not in shape:
             layout = _pieces(shape, strides, dtype.itemsize)
