@@ -668,8 +668,9 @@ def comet_beam_select(Z: torch.Tensor, score: torch.Tensor, n: int, finished: Op
 
 @functools.lru_cache(maxsize=256)
 def _pieces(shape, strides, size):
-    """The layout of [B, W, ...] states in bytes: strides of batch and beam, and what a beam holds as equal pieces (number, distance, length)."""
-    dims = [(n, s) for n, s in zip(shape[2:], strides[2:]) if n != 1]
+    """The layout of [B, W, ...] states in bytes: strides of batch and beam, and what a beam holds as equal pieces (number, distance, length).
+    A beam's dimensions are taken in the order of their memory: all of them move alike."""
+    dims = sorted(((n, s) for n, s in zip(shape[2:], strides[2:]) if n != 1), key=lambda d: -d[1])
     inner = 1
     while dims and dims[-1][1] == inner:
         inner *= dims.pop()[0]
