@@ -698,8 +698,7 @@ def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, str
             raise ValueError("a state must have shape [%d, %d, ...], got %s" % (B, W, tuple(shape)))
         if device != parent.device:
             raise ValueError("states must be on %s" % parent.device)
+    layouts = [(_pieces(shape, strides, dtype.itemsize), ptrs) for (shape, strides, dtype, device), ptrs in groups.items() if 0 not in shape]
     _written(*states)
-    for (shape, strides, dtype, device), ptrs in groups.items():
-        if 0 not in shape:
-            layout = _pieces(shape, strides, dtype.itemsize)
-            _call("comet_beam_reorder", parent.device, stream, (ctypes.c_void_p * len(ptrs))(*ptrs), len(ptrs), B, W, *layout, parent.data_ptr())
+    for layout, ptrs in layouts:
+        _call("comet_beam_reorder", parent.device, stream, (ctypes.c_void_p * len(ptrs))(*ptrs), len(ptrs), B, W, *layout, parent.data_ptr())

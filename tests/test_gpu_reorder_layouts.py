@@ -25,3 +25,13 @@ def test_refusals():
         comet.comet_beam_reorder([x[:, :, :, :2, :3].transpose(2, 3)], par)
     with pytest.raises((ValueError, comet.CometError)):
         comet.comet_beam_reorder([x[:, :, :1].expand(2, 4, 3, 4, 6)], par)
+
+
+def test_a_refused_layout_moves_none_of_the_others():
+    import paper_2102_05187_amd as comet
+    x = state((2, 4, 30), torch.float32, 1)
+    before = x.clone()
+    with pytest.raises(ValueError):
+        comet.comet_beam_reorder([x, state((2, 4, 3, 4, 6), torch.float32, 0)[:, :, :, :2, :3]], parents(2, 4, 6))
+    torch.cuda.synchronize()
+    assert torch.equal(x, before)
