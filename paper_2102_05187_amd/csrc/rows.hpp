@@ -105,8 +105,10 @@ template <> struct Elem<COMET_F16> {
 // 4096 x 24001 53 and 60, top 500 of 300 x 60013 25.8 and 23.6; forward of 8192 x 8003 58 and 54;
 // gradient of 1000 x 32003 32 and 35.
 inline bool read_shifted(int type, int64_t N, int64_t V) { return type != COMET_F32 && V >= 16384 && N * V * 2 >= (int64_t(48) << 20); }
-// Rows of 256 MB and more in all do not stay in the last cache (of that size), and are read past it: top 64 of 2048 x 131072 of 16 bits 100 us
-// through it, 95 past it.  Smaller ones are often there already, or are read again by the gradient: 5 to 11 us of 40 longer past it.
+// Rows of 256 MB and more in all do not stay in the last cache (of that size).  Where nothing is written that is of their size they are read past
+// it: top 64 of 2048 x 131072 of 16 bits 101 us through it, 95.6 past it, of 8192 x 32000 107 and 104, forward 102 and 91, 102 and 97.  Smaller ones
+// are often there already: forward of 256 x 131072 17 us through it, 21 past it.  The gradient gains nothing that way (4096 x 131072 349 us and 345, 16384 x
+// 32000 374 and 378, the step with a quarter of its rows ignored 424 and 431).
 inline bool read_once(int type, int64_t N, int64_t V) { return N * V * (type == COMET_F32 ? 4 : 2) >= (int64_t(256) << 20); }
 
 typedef uint32_t V4At4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -129,10 +131,17 @@ template <int TYPE> struct Row {
         const V4 v = *(const V4 *)(p + first(i));
         return make_uint4(v.x, v.y, v.z, v.w);
     }
-    // 16 bytes from vector i's first element on, or from the one before it of an odd row; past the caches where `once`
-    __device__ __forceinline__ uint4 stream(int64_t i, bool once) const {
+    // A load that goes past the caches.  Of two branches with a plain load and this one the compiler would make one, with the plain load: it is
+    // kept from seeing that the addresses are the same.
+    static __device__ __forceinline__ V4 load_once(const V4 *at) {
+        auto *g = (const __attribute__((address_space(1))) V4 *)at;
+        asm("" : "+v"(g));
+        return __builtin_nontemporal_load(g);
+    }
+    // 16 bytes from vector i's first element on, or from the one before it of an odd row
+    template <bool ONCE> __device__ __forceinline__ uint4 stream(int64_t i) const {
         const V4 *at = (const V4 *)(p + first(i) - (odd ? 1 : 0));
-        const V4 v = once ? __builtin_nontemporal_load(at) : *at;
+        const V4 v = ONCE ? load_once(at) : *at;
         return make_uint4(v.x, v.y, v.z, v.w);
     }
     // What settle() needs of a piece of `own` whole vectors from v0 on: lane j's `each` is the last element of the wavefront's 64 vectors j THREADS + t,

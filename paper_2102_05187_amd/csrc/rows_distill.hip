@@ -222,15 +222,18 @@ __device__ __forceinline__ MaxSum read_piece(const Row<TYPE> &row, const Piece<E
     constexpr int P = E::kPer, U = kAhead;
     uint4 v[U];
     auto fetch = [&](int i0) {
-        if (i0 + U * T <= p.own) {
+        if (i0 + U * T <= p.own && once) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = row.stream(p.v0 + i0 + u * T + threadIdx.x, once);
+            for (int u = 0; u < U; ++u) v[u] = row.template stream<true>(p.v0 + i0 + u * T + threadIdx.x);
+        } else if (i0 + U * T <= p.own) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = row.template stream<false>(p.v0 + i0 + u * T + threadIdx.x);
         } else {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = i0 + u * T + threadIdx.x;
                 v[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
-                if (i < p.own) v[u] = row.stream(p.v0 + i, once);
+                if (i < p.own) v[u] = row.template stream<false>(p.v0 + i);
             }
         }
     };
@@ -440,14 +443,14 @@ __device__ __forceinline__ void write_zeros(typename Elem<TYPE>::T *out, int64_t
 }
 
 // Loads a piece into registers; nothing where the row has ended.
-template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, bool once, uint4 (&v)[NV]) {
+template <int TYPE, int T, int NV> __device__ __forceinline__ void hold(const Row<TYPE> &row, const Piece<Elem<TYPE>::kPer> &p, uint4 (&v)[NV]) {
     using E = Elem<TYPE>;
     using V4 = typename Row<TYPE>::V4;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const V4 *at = (const V4 *)(row.p + (p.v0 + j * T) * E::kPer - (row.odd ? 1 : 0));         // one address for all threads
         V4 x = {E::kNone, E::kNone, E::kNone, E::kNone};
-        if ((j + 1) * T <= p.own || j * T + (int)threadIdx.x < p.own) x = once ? __builtin_nontemporal_load(at + threadIdx.x) : at[threadIdx.x];
+        if ((j + 1) * T <= p.own || j * T + (int)threadIdx.x < p.own) x = at[threadIdx.x];
         v[j] = make_uint4(x.x, x.y, x.z, x.w);
     }
 }
@@ -474,7 +477,7 @@ __global__ void __launch_bounds__(T) k_distill_backward(DistillArgs a, float c2,
     const Marks<T, P, uint32_t> marks{bits, words};
     uint4 v[NV];
     const auto edge = row.template edges<T>(p.v0, p.own);
-    hold<TYPE, T>(row, p, a.once, v);
+    hold<TYPE, T>(row, p, v);
     const Entries en(a, r);
     marks.clear(p);
     marks.set(p, en);
@@ -521,7 +524,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_
     // the others' parts keep the memory busy (4096 x 131072 of 16 bits: 450 us after it, 412 before it); of a short one all parts first.
     constexpr bool kLong = NV >= 16;
     const bool teacher = threadIdx.x >= T - kWave;
-    if (!kLong) hold<TYPE, T>(row, p, a.once, v);
+    if (!kLong) hold<TYPE, T>(row, p, v);
     marks.clear(p);
     if (teacher) {
         if (kLong) marks.set(p, en, threadIdx.x - (T - kWave), kWave);
@@ -530,7 +533,7 @@ __global__ void __launch_bounds__(T, T == 512 ? 2 : NV >= 16 ? 3 : 4) k_distill_
         if (threadIdx.x == T - 1) taught = t;
     } else if (!kLong) marks.set(p, en);
     const auto edge = row.template edges<T>(0, p.own);
-    if (kLong) hold<TYPE, T>(row, p, a.once, v);
+    if (kLong) hold<TYPE, T>(row, p, v);
     lds_barrier();
     Running run;
     const WORD word = TAIL ? words[threadIdx.x] : 0;
@@ -667,7 +670,7 @@ hipError_t distill_forward(const DistillArgs &given, float *loss, double *stat, 
 
 hipError_t distill_backward(const DistillArgs &given, const double *stat, const float *dloss, void *dZ, int64_t lddz, hipStream_t st) {
     DistillArgs a = given;
-    a.once = read_once(a.type, a.N, a.V), a.shift = read_shifted(a.type, a.N, a.V);
+    a.shift = read_shifted(a.type, a.N, a.V);
     const float c2 = log2_scale(a);
     return a.type == COMET_F32 ? backward<COMET_F32>(a, c2, (const Stat *)stat, dloss, dZ, lddz, st)
          : a.type == COMET_BF16 ? backward<COMET_BF16>(a, c2, (const Stat *)stat, dloss, dZ, lddz, st)
@@ -676,7 +679,7 @@ hipError_t distill_backward(const DistillArgs &given, const double *stat, const 
 
 hipError_t distill_step(const DistillArgs &given, float *loss, void *dZ, int64_t lddz, void *work, hipStream_t st) {
     DistillArgs a = given;
-    a.once = read_once(a.type, a.N, a.V), a.shift = read_shifted(a.type, a.N, a.V);
+    a.shift = read_shifted(a.type, a.N, a.V);
     if (held(a.type, a.N, a.V)) {
         const float c2 = log2_scale(a);
         return a.type == COMET_F32 ? step<COMET_F32>(a, c2, loss, dZ, lddz, st)

@@ -30,7 +30,7 @@ struct DistillArgs {
     const float *tvals, *tlse;
     double scale;
     const float *weight;
-    bool once = false, shift = false;     // how rows are read: set by the launchers
+    bool once = false, shift = false;     // how rows are read: set by the launchers (once: the forward pass alone)
 };
 int64_t distill_work(int type, int64_t N, int64_t V);
 hipError_t distill_forward(const DistillArgs &a, float *loss, double *stat, void *work, hipStream_t st);

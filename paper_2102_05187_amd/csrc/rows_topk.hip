@@ -102,15 +102,18 @@ __global__ void __launch_bounds__(T, 4) k_rows_topk(TopArgs a) {
     Running run;
     uint4 v[U];
     auto fetch = [&](int j0) {
-        if ((j0 + U) * T <= own) {
+        if ((j0 + U) * T <= own && a.once) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = row.stream(v0 + (j0 + u) * T + threadIdx.x, a.once);
+            for (int u = 0; u < U; ++u) v[u] = row.template stream<true>(v0 + (j0 + u) * T + threadIdx.x);
+        } else if ((j0 + U) * T <= own) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = row.template stream<false>(v0 + (j0 + u) * T + threadIdx.x);
         } else {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = (j0 + u) * T + threadIdx.x;
                 v[u] = make_uint4(E::kNone, E::kNone, E::kNone, E::kNone);
-                if (i < own) v[u] = row.stream(v0 + i, a.once);
+                if (i < own) v[u] = row.template stream<false>(v0 + i);
             }
         }
     };
