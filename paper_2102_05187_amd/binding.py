@@ -585,7 +585,7 @@ def _teacher(Z, crd, tvals, pos, tlse, scale, weight):
 def comet_distill_forward(Z: torch.Tensor, crd: torch.Tensor, tvals: torch.Tensor, pos: Optional[torch.Tensor] = None,
                           tlse: Optional[torch.Tensor] = None, scale: float = 1.0, weight: Optional[torch.Tensor] = None,
                           loss: Optional[torch.Tensor] = None, stat: Optional[torch.Tensor] = None, stream=None):
-    """(loss, stat): the loss of every row, and what comet_distill_backward needs of it."""
+    """(loss, stat): the loss of every row, and what comet_distill_backward needs of it.  Neither is part of an autograd graph."""
     N, V, kind, dev, args = _teacher(Z, crd, tvals, pos, tlse, scale, weight)
     need = _work_bytes("comet_distill", kind, N, V)
     loss = _new(loss, torch.float32, (N,), "loss", dev, stream)

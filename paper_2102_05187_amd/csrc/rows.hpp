@@ -101,9 +101,10 @@ template <> struct Elem<COMET_F16> {
 // A row of 16-bit elements at such an odd multiple (`odd`: every other row where the rows' distance is odd) can therefore be read from one
 // element before it on, which is the row before's; every vector gets its last element from the vector behind it: the next lane's, or,
 // for the wavefront's last lane, from edges(), one load for all of a thread's vectors.  Row 0 has none before it, and is read as it lies.  So
-// are rows that are short or few, which memory does not bound: top 64 of 4096 x 131071 of 16 bits 213 us shifted, 251 as they lie, of
-// 4096 x 24001 53 and 60, top 500 of 300 x 60013 25.8 and 23.6; forward of 8192 x 8003 58 and 54;
-// gradient of 1000 x 32003 32 and 35.
+// are short rows (forward of 8192 x 8003 58 us shifted, 54 as they lie).  Long ones gain where they come from memory and lose where the last
+// cache has them, at any size: top 64 of 1677 x 60013 55 us shifted and 57 as they lie from memory, 48 and 44 from the cache, forward of
+// 559 x 60013 23 and 24, 21 and 20, gradient of 512 x 131071 53 and 58, 44 and 45.  From 256 MB on (3494 x 60013: 95 and 108, 89 and 94, 157 and 176) they
+// come from memory, below 48 MB mostly from the cache, and in between it is as often one as the other.
 inline bool read_shifted(int type, int64_t N, int64_t V) { return type != COMET_F32 && V >= 16384 && N * V * 2 >= (int64_t(48) << 20); }
 // Rows of 256 MB and more in all do not stay in the last cache (of that size).  Where nothing is written that is of their size they are read past
 // it: top 64 of 2048 x 131072 of 16 bits 101 us through it, 95.6 past it, of 8192 x 32000 107 and 104, forward 102 and 91, 102 and 97.  Smaller ones
@@ -198,7 +199,7 @@ struct MaxSum {
 
 // The same while it is taken in, with one multiply-add and one exp2 an element: s holds exp2(c z - shift), where shift is c m rounded,
 // and what that rounding did to all terms alike is taken out at the end.  It is half a unit of c m at most: 64 below 2^31, and a sum of 2^31
-// terms of 2^64 is still a number.  From there on (masks of -2e9 and beyond, the lowest value of a type among them, +inf) shift stays at the limit:
+// terms of 2^64 is still a number.  From there on (at scale 1 masks of -1.5e9 and below, the lowest value of a type among them, +inf) shift stays at the limit:
 // a thread whose places are all far below it has a sum of 0, as they have in a row with an ordinary maximum; the sum of a row, or a
 // piece of one, whose maximum is itself wild() is taken again by slow_sum.
 constexpr float kWild = 0x1p31f;

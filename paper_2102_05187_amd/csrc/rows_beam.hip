@@ -25,7 +25,7 @@ struct BeamArgs {
 
 // One workgroup a batch: the n best of all its lists' keys, T * PER at most, which the threads hold as scores.  Bound by the latency of its steps, one
 // after the other (two reads, log-sum-exps, bound, list, order): 5 us for up to 1024 keys, whatever their number and that of the batches, of the 16
-// that the call takes; the kernel before it takes 5 to 11, the host the rest.
+// that the call takes; the kernel before it takes 5 to 12, the host the rest.
 template <int T, int PER>
 __global__ void __launch_bounds__(T) k_beam_join(BeamArgs a) {
     __shared__ double big[COMET_MAX_BEAMS], off[COMET_MAX_BEAMS];       // a candidate's score is (z - big) + off

@@ -273,8 +273,8 @@ __device__ __forceinline__ MaxSum read_piece(const Row<TYPE> &row, const Piece<E
 }
 
 // One workgroup a row or a piece of one, four vectors a thread under way while four are taken in.  Bound by memory where rows are long and many
-// (4096 x 131072 of 16 bits in 195 us: 5.5 TB/s) and by the exponentials and their additions where they are shorter: 2048 x 50021 of 16 bits
-// 46 us in the kernel, 29 for its bytes alone at 7.1 TB/s.
+// (4096 x 131072 of 16 bits in 173 us: 6.2 TB/s) and by the exponentials and their additions where they are shorter: 2048 x 50021 of 16 bits
+// 48 us in the kernel, 29 for its bytes alone at 7.1 TB/s.
 template <int TYPE, bool TAIL>
 __global__ void __launch_bounds__(kThreads) k_distill_forward(DistillArgs a, float c2, Pieces cut, float *__restrict__ loss, Stat *__restrict__ stat,
                                                               float2 *__restrict__ partial) {

@@ -138,7 +138,9 @@ struct SortSpace {
 // Calls emit(rank, item) once for each of n different items in LDS (n <= kCandidates; places up to the next power of two are used too), when
 // all have been read.  Up to 16 are compared with each other by one wavefront, up to 128 by several threads for each.  More are put
 // into 512 bins by their rough value, and compared with the others of their bin; of the largest of many numbers the number falls off exponentially with the value, so the
-// bins are even in 1 - exp(-(value - least) / mean).  Where the values crowd in a bin (equal ones, outliers), a bitonic network sorts them.
+// bins are even in 1 - exp(-(value - least) / mean).  That this never puts a larger value below a smaller one rests on the device's exp2 never
+// being larger for a smaller argument: it is not, for any two neighbouring 32-bit arguments up to 0.  Where the values crowd in a bin (equal
+// ones, outliers), a bitonic network sorts them.
 template <int T, class S, class EMIT> __device__ __forceinline__ void sort_items(const S &s, int n, SortSpace &sp, EMIT emit) {
     constexpr int E = kCandidates / T;                                         // items of a thread
     using Item = typename S::Item;

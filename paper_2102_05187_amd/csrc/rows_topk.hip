@@ -8,12 +8,15 @@
 //   2. the vectors whose largest element reaches it are listed and read again, K or so of them, and their elements that do go
 //      into LDS as 64-bit keys (value, then lower column);
 //   3. the keys are put in order (sort_items()).
-// Bound by memory where rows are long and many: top 64 of 2048 x 131072 of 16 bits in 101 us, 5.3 TB/s (a plain read of
-// that size 7.1).  A single row is bound by the latency of
-// these steps: 8 us of 32000 32-bit elements, 13 of 131072 of 16 bits.  Shapes of more threads with fewer vectors each were slower throughout
-// (1024 threads: 146 us, and 13 for 11.5 with 4 rows).
+// Bound by memory where rows are long and many: top 64 of 2048 x 131072 of 16 bits in 95.6 us, 5.6 TB/s (a plain read of
+// that size 7.1).  Few rows are bound by the latency of these steps: 8 us of one row of 32000 32-bit elements, 13 of 131072 of 16 bits.  Of a
+// workgroup's time over a row of 60013 of 16 bits with K = 500, reading and summing take 37 %, the bound 10 %, the list 5 %, reading its 600 vectors
+// again 23 %, the order 25 %; of 32000 of 32 bits with K = 50 58, 15, 7, 8 and 12 %.  Shapes of more threads with fewer vectors each were
+// slower throughout (1024 threads: 146 us, and 13 for 11.5 with 4 rows).
 // Where more than 2048 reach the bound (equal elements, or the large ones next to each other in a few threads) the K-th largest key is
-// found exactly, by halving, with the vectors that matter read again each time.
+// found exactly, by halving, with the vectors that matter read again each time.  That is slow: rows of equal elements take 2.8 ms for 0.1 at 2048 x
+// 131072 with K = 64, 0.34 ms for 0.01 at 1 x 32000; and so do rows with fewer than K allowed elements above a finite mask (2.7 and 0.28 ms), which
+// a mask of -inf does not (0.097 and 0.01).
 #include "rows_kernels.hpp"
 #include "rows_select.hpp"
 
