@@ -114,7 +114,7 @@ __device__ __forceinline__ double finish(const Taught &t, MaxSum d, bool tail, d
         lse.rest = log_of((float)tot);
         if (!none) share = (big - lse.big) + (log_s - lse.rest);
     }
-    if (d.s != d.s || d.m == -kNegInf) lse.big = __builtin_nan("");
+    if (d.s != d.s) lse.big = d.s;
     double loss = t.part;
     if (t.mass != 0 && t.xa != kNegInfD) loss += t.mass * ((lse.big - t.xa) + lse.rest);
     if (t.rest != 0) loss -= t.rest * share;
@@ -123,9 +123,8 @@ __device__ __forceinline__ double finish(const Taught &t, MaxSum d, bool tail, d
     out->lse = lse;
     out->m = none ? 0.0 : (double)d.m;
     out->A = none ? 0.0 : tail ? P * outside / tot - t.rest / (double)d.s : P / (double)d.s;
-    const double bad = lse.big + P;                              // NaN and +inf in the row or its entries
-    if (bad != bad) loss = out->A = bad;
-    if (t.norm.big == -kNegInfD || w - w != 0) loss = out->A = __builtin_nan("");        // ... in tlse or the weight
+    // NaN and +inf in the row, its entries, tlse or the weight
+    if (lse.big + P != lse.big + P || lse.big == -kNegInfD || t.norm.big == -kNegInfD || w - w != 0) loss = out->A = __builtin_nan("");
     return w * loss;
 }
 

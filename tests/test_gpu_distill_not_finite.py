@@ -52,3 +52,20 @@ def test_weight(V, tail, dtype):
     p.weight[5], p.weight[6], p.weight[7] = INF, math.nan, -INF
     p.args()
     check(p, (5, 6, 7))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("value", [INF, math.nan])
+@pytest.mark.parametrize("V", [9, 3001, 40009, 140001])
+def test_a_logit_at_an_entry(V, value, tail, dtype):
+    """... whatever the other places are."""
+    p = Problem(8, V, 6, dtype, seed=V + 2, tail=tail, weighted=False)
+    Z = torch.tensor(p.host)
+    Z[4:7] = -INF                                                # nothing is left but that
+    Z[5, torch.tensor(p.rows[5][0])] = 1.0                       # ... and the entries
+    Z[6] = torch.finfo(dtype).min
+    for r in range(4, 8):
+        Z[r, int(p.rows[r][0][2])] = value
+    p.set(Z.to(dtype))
+    check(p, (4, 5, 6, 7))
