@@ -391,6 +391,105 @@ comet_status comet_beam_select(const void *Z, comet_type_t type, int64_t B, int6
 comet_status comet_beam_reorder(void *const *states, int64_t nstates, int64_t B, int64_t W, int64_t batch_stride, int64_t beam_stride,
                                 int64_t outer, int64_t outer_stride, int64_t inner, const int32_t *parent, void *stream);
 
+/* ---- a cache in blocks -----------------------------------------------------------------------------------------------
+ * What a model keeps of the tokens it has read: keys and values, in blocks of `block` places that lie anywhere in one memory.  Requests
+ * b = 0 .. B-1 have length[b] tokens each, and row b of the table [B x M] (rows at b * ldt, ldt >= M) names the block
+ * that holds the places j * block .. j * block + block - 1 in its element j.  The tokens of one step are packed: request b has the
+ * rows pos[b] .. pos[b+1]-1 (pos: device, [B + 1], from 0 upwards), the newest ones that it has, so that row pos[b] + i is its token at
+ * place length[b] - (pos[b+1] - pos[b]) + i.  Rows from pos[B] on belong to no request: results for them are left as they were. */
+#define COMET_MAX_BLOCK 1024
+typedef struct comet_cache {
+    void *keys, *values;               /* device, element (p, i, h, d) at p * stride[0] + i * stride[1] + h * stride[2] + d */
+    void *mean;                        /* device, or NULL where a call does not need it: the mean key of every block, (p, h, d) */
+    comet_type_t type;                 /* of all three */
+    int64_t blocks, block, heads, size;            /* p < blocks <= 2^31 - 1, i < block, h < heads, d < size */
+    int64_t key_stride[3], value_stride[3];        /* in elements */
+    int64_t mean_stride[2];                        /* of p and h */
+} comet_cache;
+/* A block has a multiple of 16 places, COMET_MAX_BLOCK at most; size is a multiple of 8, 256 at most; pointers and strides are
+ * multiples of 16 bytes (COMET_ERR_UNSUPPORTED or COMET_ERR_INVALID_ARG where they are not), strides at most 2^40. */
+
+/* Tables and slots for the next tokens, from the lengths, on the device: nothing of it has to be known on the host.
+ *   add        device, [B]: tokens that each request wants to add (below 0: none).
+ *   ended      device, [B] bytes, or NULL: a request with a byte that is not 0 has ended; its blocks become spare, its length and its held
+ *              blocks 0, and what it adds is of a new request in its place.
+ *   length     device, [B]: tokens of each request so far; what is added is counted in.
+ *   held       device, [B]: blocks that each request has: the first held[b] of its row of the table.
+ *   table      device, [B x M]: new blocks are written behind those held.
+ *   spare, count   device, [S] and [1]: spare[0 .. count) are the blocks that no request has.  Blocks of ended requests are put
+ *              behind them (in the order of requests and places), then new blocks are taken from the end.
+ *   pos, slot, place   device, [B + 1], [N], [N]: the packed tokens: token i of request b goes to slot[pos[b] + i] =
+ *              (block) * block + (place in it), its place in the request is place[pos[b] + i].  Behind pos[B] both are -1.
+ * A request gets all that it asks for or nothing (pos[b+1] == pos[b]).  It gets it where it fits into its row of the table and, of the fitting
+ * requests from the first up to it, the tokens are N at most and, unless it needs no new block, the new blocks are
+ * spare.  A request keeps the blocks that it holds when its length is set back.
+ * Values of held, length and count that cannot be (more blocks than M or S, more tokens than the blocks hold) are taken as the nearest that can.
+ *   block <= COMET_MAX_BLOCK, B <= 2^20, B * M < 2^40, M * block < 2^31, S < 2^31, N < 2^31. */
+comet_status comet_cache_map_work(int64_t B, int64_t M, int64_t N, int64_t *bytes /* host */);
+comet_status comet_cache_map(int64_t B, int64_t M, int64_t block, const int32_t *add, const uint8_t *ended, int32_t *length, int32_t *held,
+                             int32_t *table, int64_t ldt, int32_t *spare, int64_t S, int32_t *count, int64_t N, int32_t *pos, int64_t *slot,
+                             int32_t *place, void *work, int64_t work_bytes, void *stream);
+
+/* New keys and values into their slots.  Row i of k and v (element (i, h, d) at i * stride[0] + h * stride[1] + d, of the cache's type)
+ * goes to slot[i]; a slot outside of [0, blocks * block) is left out.  Where a block's last place is written its mean (if
+ * the cache has one) becomes the mean of the keys of all its places, added in 32 bits and rounded once: of those that this call
+ * writes in the rows right before with the slots right before, and of what the cache holds for the places before them.
+ * No two rows may have the same slot.   N < 2^31. */
+comet_status comet_cache_write(const comet_cache *cache, int64_t N, const void *k, const int64_t k_stride[2], const void *v,
+                               const int64_t v_stride[2], const int64_t *slot, void *stream);
+
+/* Which blocks a query is to read.  q has Q = G * heads heads (element (n, x, d) at n * stride[0] + x * stride[1] + d, of
+ * the cache's type), G of them, h * G .. h * G + G - 1, with the cache's head h.  A token at place p sees the blocks 0 .. p / block.  For every
+ * token and h, K of them are chosen, or all where there are no more: the first `first`, the last `last` (its own block is
+ * the very last), and of the others those with the largest score
+ *     s_j = sum over the G heads and d of q[n, x, d] * mean[table[b, j], h, d],
+ * of equal ones the lower j; NaN comes last.  Scores are computed and compared in 64 bits: the choice is that of the exact numbers.
+ *   sel        device, [N x heads x K]: the chosen j, ascending, and -1 behind them.
+ *   first >= 0, last >= 1, first + last <= K <= COMET_MAX_CHOSEN, M <= COMET_MAX_CANDIDATES.
+ * A block whose number in the table is outside of [0, blocks) has the score NaN. */
+#define COMET_MAX_CHOSEN 1024
+#define COMET_MAX_CANDIDATES 16384
+comet_status comet_block_select_work(const comet_cache *cache, int64_t N, int64_t Q, int64_t B, int64_t M, int64_t K, int64_t *bytes /* host */);
+comet_status comet_block_select(const comet_cache *cache, int64_t N, int64_t Q, const void *q, const int64_t q_stride[2], int64_t B,
+                                const int32_t *pos, const int32_t *length, const int32_t *table, int64_t M, int64_t ldt, int64_t K,
+                                int64_t first, int64_t last, int32_t *sel, void *work, int64_t work_bytes, void *stream);
+
+/* Attention over the chosen blocks: out[n, x] = sum of w_i value_i, w = softmax of scale * (q[n, x] . key_i), over the places i <= p of the
+ * blocks that sel names for token n and the head's h.  sel is a set: the order does not matter, and a block that is named twice counts once;
+ * a number outside of [0, M), a block behind the token's own and one whose number in the table is outside of [0, blocks) are none.
+ *   out        device, [N x Q x size] without gaps, of the cache's type, 16-byte aligned.
+ *   lse        device, [N x Q], or NULL: ln sum exp(scale * (q . key)).
+ * A token that has no place to read gets out 0 and lse -inf.  What a token does not read does not reach it, NaN included.
+ *   M <= COMET_MAX_TABLE. */
+#define COMET_MAX_TABLE 262144
+comet_status comet_block_attend_work(const comet_cache *cache, int64_t N, int64_t Q, int64_t B, int64_t M, int64_t K, int64_t *bytes /* host */);
+comet_status comet_block_attend(const comet_cache *cache, int64_t N, int64_t Q, const void *q, const int64_t q_stride[2], int64_t B,
+                                const int32_t *pos, const int32_t *length, const int32_t *table, int64_t M, int64_t ldt, const int32_t *sel,
+                                int64_t K, double scale, void *out, float *lse, void *work, int64_t work_bytes, void *stream);
+
+/* Drafted tokens are taken as far as they pass for the target's.  The rows of request b (pos as above) are the target's logits behind its
+ * tokens: the first of the request's tokens is known, the others are drafted, and row r, unless it is the request's last, judges
+ * d = token[r+1].  With p = softmax(scale z_r) and q the distribution that d was drawn from, d is taken where u_r q_d < p_d.  At the
+ * first that is not, the next token is drawn from what is left of p, max(p - q, 0); where all are taken, from p of the
+ * last row: the first j whose running sum of these weights is larger than v_b times their sum.  So the tokens are distributed as p.
+ *   draft      device, rows of type draft_type and length V at r * ldd: q = softmax(scale draft_r).  Or NULL, and then
+ *   crd, vals  device, [N x K] coordinates (distinct in a row) and logits: q = softmax(scale vals) over a row's entries, 0 elsewhere; an
+ *              entry whose coordinate is outside of [0, V) is none.  With K = 0: q is 1 at d (the draft was no draw).
+ *   token      device, [N]: the packed tokens that the target has read.  A drafted token outside of [0, V) is not taken.
+ *   u, v       device, [N] and [B]: random numbers, uniform in [0, 1).
+ *   scale      1 / temperature; scales: device, [B], or NULL: one for each request in scale's place.  +inf: p is 1 at the largest logit (the
+ *              lowest token of equal ones), and a drafted token whose logit equals the largest is taken, whatever u and q.
+ *   accepted, next   device, [B]: how many drafted tokens are taken, and the token that follows them.  A request without rows has 0 and -1.
+ *   length     device, [B], or NULL: the tokens that are not taken are taken off.
+ * A row without probabilities (only -inf, a NaN or +inf in it, or a scale that is none) takes no drafted token, and where a token is to be drawn from
+ * it, that is -1.  A row of the draft without probabilities has q = 0.  Where nothing is left of p, p itself is drawn from.
+ * Probabilities and sums are computed in 64 bits.   K <= COMET_MAX_TOP, N <= 2^23, V < 2^31. */
+comet_status comet_draft_verify_work(comet_type_t type, int64_t N, int64_t V, int64_t B, int64_t K, int with_draft, int64_t *bytes /* host */);
+comet_status comet_draft_verify(const void *Z, comet_type_t type, int64_t N, int64_t V, int64_t ldz, int64_t B, const int32_t *pos,
+                                const int32_t *token, const float *u, const float *v, const void *draft, comet_type_t draft_type, int64_t ldd,
+                                const int32_t *crd, const float *vals, int64_t K, double scale, const float *scales, int32_t *accepted,
+                                int32_t *next, int32_t *length, void *work, int64_t work_bytes, void *stream);
+
 /* Calibration of the device's memory system, for the benchmark (no tensor involved): the two access
  * patterns the operations are made of, timed by the caller.
  *   comet_calibrate_read    streams n doubles (n >= 2, data 16-byte aligned) once through the device.

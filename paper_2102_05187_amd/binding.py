@@ -25,6 +25,7 @@ COMET_MAX_ORDER = 4
 COMET_F32, COMET_BF16, COMET_F16 = 0, 1, 2
 COMET_BY_COORDINATE = 1
 COMET_MAX_TOP, COMET_MAX_BEAMS, COMET_DISTILL_STAT = 1024, 256, 7
+COMET_MAX_BLOCK, COMET_MAX_CHOSEN, COMET_MAX_CANDIDATES, COMET_MAX_TABLE = 1024, 1024, 16384, 262144
 
 _STATUS_NAMES = {0: "COMET_OK", 1: "COMET_ERR_INVALID_ARG", 2: "COMET_ERR_BAD_FORMAT", 3: "COMET_ERR_SHAPE",
                  4: "COMET_ERR_UNSUPPORTED", 5: "COMET_ERR_ALLOC", 6: "COMET_ERR_DEVICE"}
@@ -34,7 +35,9 @@ EXPORTS = ["comet_tensor_create", "comet_tensor_destroy", "comet_tensor_info", "
            "comet_tensor_reorder", "comet_tensor_convert", "comet_tensor_reserve", "comet_spmv_static",
            "comet_calibrate_read", "comet_calibrate_gather", "comet_spmv_axpby", "comet_spmm_axpby",
            "comet_mttkrp_axpby", "comet_rows_topk_work", "comet_rows_topk", "comet_distill_work", "comet_distill_forward",
-           "comet_distill_backward", "comet_distill_step", "comet_beam_select_work", "comet_beam_select", "comet_beam_reorder"]
+           "comet_distill_backward", "comet_distill_step", "comet_beam_select_work", "comet_beam_select", "comet_beam_reorder",
+           "comet_cache_map_work", "comet_cache_map", "comet_cache_write", "comet_block_select_work", "comet_block_select", "comet_block_attend_work",
+           "comet_block_attend", "comet_draft_verify_work", "comet_draft_verify"]
 
 
 class CometError(RuntimeError):
@@ -58,6 +61,20 @@ class _Info(ctypes.Structure):
                 ("heavy_rows", ctypes.c_int64),
                 ("heavy_nnz", ctypes.c_int64),
                 ("heavy_stream_bytes", ctypes.c_int64)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("keys", ctypes.c_void_p),
+                ("values", ctypes.c_void_p),
+                ("mean", ctypes.c_void_p),
+                ("type", ctypes.c_int),
+                ("blocks", ctypes.c_int64),
+                ("block", ctypes.c_int64),
+                ("heads", ctypes.c_int64),
+                ("size", ctypes.c_int64),
+                ("key_stride", ctypes.c_int64 * 3),
+                ("value_stride", ctypes.c_int64 * 3),
+                ("mean_stride", ctypes.c_int64 * 2)]
 
 
 _LIB = None
@@ -101,6 +118,14 @@ def _lib():
         lib.comet_beam_select_work.argtypes = [ci, i64, i64, i64, i64, pi64]
         lib.comet_beam_select.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, ctypes.c_int32, i64, vp, vp, vp, vp, i64, vp]
         lib.comet_beam_reorder.argtypes = [vp, i64, i64, i64, i64, i64, i64, i64, i64, vp, vp]
+        lib.comet_cache_map_work.argtypes = [i64, i64, i64, pi64]
+        lib.comet_cache_map.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp]
+        lib.comet_cache_write.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp]
+        lib.comet_block_select_work.argtypes = lib.comet_block_attend_work.argtypes = [vp, i64, i64, i64, i64, i64, pi64]
+        lib.comet_block_select.argtypes = [vp, i64, i64, vp, vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp, i64, vp]
+        lib.comet_block_attend.argtypes = [vp, i64, i64, vp, vp, i64, vp, vp, vp, i64, i64, vp, i64, f64, vp, vp, vp, i64, vp]
+        lib.comet_draft_verify_work.argtypes = [ci, i64, i64, i64, i64, ci, pi64]
+        lib.comet_draft_verify.argtypes = [vp, ci, i64, i64, i64, i64, vp, vp, vp, vp, vp, ci, i64, vp, vp, i64, f64, vp, vp, vp, vp, vp, i64, vp]
         lib.comet_status_string.argtypes = [ci]
         lib.comet_status_string.restype = ctypes.c_char_p
         for n in EXPORTS:
@@ -695,3 +720,207 @@ def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, str
     torch.autograd.graph.increment_version(states)
     for layout, ptrs in layouts:
         _call("comet_beam_reorder", parent.device, stream, (ctypes.c_void_p * len(ptrs))(*ptrs), len(ptrs), B, W, *layout, parent.data_ptr())
+
+
+# ---- a cache in blocks ------------------------------------------------------------------------------------------------------
+def _bytes_of(t: Optional[torch.Tensor], shape, what: str, device) -> Optional[torch.Tensor]:
+    if isinstance(t, torch.Tensor) and t.dtype == torch.bool:
+        t = t.view(torch.uint8)
+    return _given(t, torch.uint8, shape, what, device)
+
+
+def _table(table: torch.Tensor, B: int, device):
+    """(pointer, columns, distance of rows) of the requests' blocks."""
+    if not isinstance(table, torch.Tensor) or not table.is_cuda or table.dtype != torch.int32:
+        raise TypeError("table must be an int32 tensor in device memory")
+    if table.dim() != 2 or table.shape[0] != B or table.device != device:
+        raise ValueError("table must have a row for each of the %d requests, on %s" % (B, device))
+    M, (ld, step) = table.shape[1], table.stride()
+    if (step != 1 and M > 1) or (ld < M and B > 1):
+        raise ValueError("table must have its columns next to each other and rows that do not overlap")
+    return table.data_ptr(), M, ld if B > 1 else M
+
+
+def _vectors(t: torch.Tensor, what: str, dims: int, dtype=None, device=None):
+    """Strides of all dimensions but the last, whose elements lie next to each other; as the kernels' 16-byte loads need them."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a torch tensor in device memory" % what)
+    if t.dtype not in _TYPES or (dtype is not None and t.dtype != dtype):
+        raise TypeError("%s must have dtype %s, got %s" % (what, dtype or "float32, bfloat16 or float16", t.dtype))
+    if t.dim() != dims:
+        raise ValueError("%s must have %d dimensions" % (what, dims))
+    if device is not None and t.device != device:
+        raise ValueError("%s must be on %s" % (what, device))
+    strides = tuple(s if n > 1 else 0 for n, s in zip(t.shape, t.stride()))
+    if strides[-1] > 1 or t.data_ptr() % 16 or any(s * t.element_size() % 16 for s in strides[:-1]):
+        raise ValueError("%s must have the last dimension's elements next to each other, and the others at multiples of 16 bytes" % what)
+    return strides[:-1]
+
+
+def _cache(keys, values, mean, device):
+    """(description, dtype) of a cache: keys and values [blocks, block, heads, size], mean [blocks, heads, size]."""
+    some = mean if keys is None else keys
+    kind = getattr(some, "dtype", None)
+    ks = vs = (0, 0, 0)
+    ms = (0, 0)
+    if keys is not None:
+        ks = _vectors(keys, "K", 4, None, device)
+        vs = _vectors(values, "V", 4, kind, device)
+        if values.shape != keys.shape:
+            raise ValueError("K and V must have one shape")
+    if mean is not None:
+        ms = _vectors(mean, "mean", 3, kind if keys is not None else None, device)
+        if keys is not None and mean.shape != (keys.shape[0], *keys.shape[2:]):
+            raise ValueError("mean must have shape %s, got %s" % ((keys.shape[0], *keys.shape[2:]), tuple(mean.shape)))
+    blocks, heads, size = some.shape[0], some.shape[-2], some.shape[-1]
+    c = _Cache(_ptr(keys), _ptr(values), _ptr(mean), _TYPES[kind], blocks, 16 if keys is None else keys.shape[1], heads, size)
+    c.key_stride[:], c.value_stride[:], c.mean_stride[:] = ks, vs, ms
+    return c, kind
+
+
+def comet_cache_map(add: torch.Tensor, length: torch.Tensor, held: torch.Tensor, table: torch.Tensor, spare: torch.Tensor, count: torch.Tensor, block: int, N: int,
+                    ended: Optional[torch.Tensor] = None, stream=None):
+    """(pos, slot, place) of the next tokens, add[b] of each request, N at most in all; length, held, table, spare and count are brought up to date."""
+    if not isinstance(length, torch.Tensor) or length.dim() != 1:
+        raise ValueError("length must have one dimension")
+    _dev(length, torch.int32, "length")
+    (B,), dev, N = length.shape, length.device, int(N)
+    ptr, M, ldt = _table(table, B, dev)
+    _given(add, torch.int32, (B,), "add", dev)
+    _given(held, torch.int32, (B,), "held", dev)
+    ended = _bytes_of(ended, (B,), "ended", dev)
+    if not isinstance(spare, torch.Tensor) or spare.dim() != 1:
+        raise ValueError("spare must have one dimension")
+    _given(spare, torch.int32, tuple(spare.shape), "spare", dev)
+    _given(count, torch.int32, (1,), "count", dev)
+    if add is None or held is None or count is None:
+        raise ValueError("add, held and count are needed")
+    need = _work_bytes("comet_cache_map", B, M, N)
+    pos = _new(None, torch.int32, (B + 1,), "pos", dev, stream)
+    slot = _new(None, torch.int64, (N,), "slot", dev, stream)
+    place = _new(None, torch.int32, (N,), "place", dev, stream)
+    torch.autograd.graph.increment_version([length, held, table, spare, count])
+    work, wptr = _work(need, dev, stream)
+    _call("comet_cache_map", dev, stream, B, M, int(block), add.data_ptr(), _ptr(ended), length.data_ptr(), held.data_ptr(), ptr, ldt, spare.data_ptr(),
+          spare.shape[0], count.data_ptr(), N, pos.data_ptr(), slot.data_ptr(), place.data_ptr(), wptr, need)
+    return pos, slot, place
+
+
+def comet_cache_write(k: torch.Tensor, v: torch.Tensor, K: torch.Tensor, V: torch.Tensor, slot: torch.Tensor, mean: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    """Rows of k and v, [N, heads, size], into their slots of K and V, [blocks, block, heads, size]; mean, [blocks, heads, size], of the blocks that become whole."""
+    if not isinstance(K, torch.Tensor) or not K.is_cuda:
+        raise TypeError("K must be a torch tensor in device memory")
+    dev = K.device
+    cache, kind = _cache(K, V, mean, dev)
+    ks, vs = _vectors(k, "k", 3, kind, dev), _vectors(v, "v", 3, kind, dev)
+    N = k.shape[0]
+    if k.shape != (N, *K.shape[2:]) or v.shape != k.shape:
+        raise ValueError("k and v must have shape %s" % ((N, *K.shape[2:]),))
+    _given(slot, torch.int64, (N,), "slot", dev)
+    if slot is None:
+        raise ValueError("slot is missing")
+    torch.autograd.graph.increment_version([K, V] if mean is None else [K, V, mean])
+    _call("comet_cache_write", dev, stream, ctypes.byref(cache), N, k.data_ptr(), (ctypes.c_int64 * 2)(*ks), v.data_ptr(), (ctypes.c_int64 * 2)(*vs), slot.data_ptr())
+
+
+def _queries(q, cache, kind, table, pos, length, device):
+    """What the two calls with queries share: (N, Q, B, M) and their arguments."""
+    qs = _vectors(q, "q", 3, kind, device)
+    N, Q, size = q.shape
+    if size != cache.size or Q % cache.heads:
+        raise ValueError("q must have heads of %d elements, a multiple of %d of them" % (cache.size, cache.heads))
+    if not isinstance(length, torch.Tensor) or length.dim() != 1:
+        raise ValueError("length must have one dimension")
+    (B,) = length.shape
+    _given(length, torch.int32, (B,), "length", device)
+    _given(pos, torch.int32, (B + 1,), "pos", device)
+    if pos is None:
+        raise ValueError("pos is missing")
+    ptr, M, ldt = _table(table, B, device)
+    return (N, Q, B, M), (q.data_ptr(), (ctypes.c_int64 * 2)(*qs), B, pos.data_ptr(), length.data_ptr(), ptr, M, ldt)
+
+
+@functools.lru_cache(maxsize=1024)
+def _query_work(call: str, kind: int, block: int, heads: int, size: int, *sizes) -> int:
+    need, cache = ctypes.c_int64(0), _Cache(None, None, None, kind, 0, block, heads, size)
+    _check(getattr(_lib(), call + "_work")(ctypes.byref(cache), *sizes, ctypes.byref(need)), call)
+    return need.value
+
+
+def comet_block_select(q: torch.Tensor, mean: torch.Tensor, table: torch.Tensor, pos: torch.Tensor, length: torch.Tensor, block: int, K: int, first: int = 1,
+                       last: int = 1, sel: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """sel, [N, heads, K]: the K blocks that each query token's heads are to read, ascending, -1 behind them where there are fewer."""
+    if not isinstance(mean, torch.Tensor) or not mean.is_cuda:
+        raise TypeError("mean must be a torch tensor in device memory")
+    dev, K = mean.device, int(K)
+    cache, kind = _cache(None, None, mean, dev)
+    cache.block = int(block)
+    sizes, args = _queries(q, cache, kind, table, pos, length, dev)
+    need = _query_work("comet_block_select", cache.type, cache.block, cache.heads, cache.size, *sizes, K)
+    sel = _new(sel, torch.int32, (sizes[0], cache.heads, K), "sel", dev, stream)
+    work, wptr = _work(need, dev, stream)
+    _call("comet_block_select", dev, stream, ctypes.byref(cache), *sizes[:2], *args, K, int(first), int(last), sel.data_ptr(), wptr, need)
+    return sel
+
+
+def comet_block_attend(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, pos: torch.Tensor, length: torch.Tensor, sel: torch.Tensor,
+                       scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, stream=None):
+    """(out, lse): attention of the query tokens q, [N, heads, size], over the blocks of the cache that sel names; scale is size ** -0.5 unless given."""
+    if not isinstance(K, torch.Tensor) or not K.is_cuda:
+        raise TypeError("K must be a torch tensor in device memory")
+    dev = K.device
+    cache, kind = _cache(K, V, None, dev)
+    sizes, args = _queries(q, cache, kind, table, pos, length, dev)
+    N, Q = sizes[:2]
+    if not isinstance(sel, torch.Tensor) or sel.dim() != 3:
+        raise ValueError("sel must have three dimensions")
+    chosen = sel.shape[2]
+    _given(sel, torch.int32, (N, cache.heads, chosen), "sel", dev)
+    need = _query_work("comet_block_attend", cache.type, cache.block, cache.heads, cache.size, *sizes, chosen)
+    out = _new(out, kind, (N, Q, cache.size), "out", dev, stream)
+    lse = _new(lse, torch.float32, (N, Q), "lse", dev, stream)
+    work, wptr = _work(need, dev, stream)
+    _call("comet_block_attend", dev, stream, ctypes.byref(cache), N, Q, *args, sel.data_ptr(), chosen, float(cache.size ** -0.5 if scale is None else scale),
+          out.data_ptr(), lse.data_ptr(), wptr, need)
+    return out, lse
+
+
+def comet_draft_verify(Z: torch.Tensor, token: torch.Tensor, pos: torch.Tensor, u: torch.Tensor, v: torch.Tensor, draft: Optional[torch.Tensor] = None,
+                       crd: Optional[torch.Tensor] = None, vals: Optional[torch.Tensor] = None, scale=1.0, length: Optional[torch.Tensor] = None, stream=None):
+    """(accepted, next), each [B]: how many of each request's drafted tokens are taken, and the token behind them.  The draft's distribution: logits
+    `draft`, or entries (crd, vals), or neither.  scale: a number, or a float32 tensor with one for each request.  length is brought up to date."""
+    ptr, kind, N, V, ld = _rows(Z)
+    dev = Z.device
+    if not isinstance(pos, torch.Tensor) or pos.dim() != 1 or pos.shape[0] < 1:
+        raise ValueError("pos must have one dimension")
+    B = pos.shape[0] - 1
+    for t, dtype, shape, what in ((pos, torch.int32, (B + 1,), "pos"), (token, torch.int32, (N,), "token"), (u, torch.float32, (N,), "u"), (v, torch.float32, (B,), "v")):
+        if t is None:
+            raise ValueError("%s is missing" % what)
+        _given(t, dtype, shape, what, dev)
+    _given(length, torch.int32, (B,), "length", dev)
+    dptr, dkind, ldd, K, scales = None, COMET_F32, V, 0, None
+    if draft is not None:
+        if crd is not None or vals is not None:
+            raise ValueError("either draft or crd and vals")
+        dptr, dkind, _, _, ldd = _rows(draft, "draft")
+        if draft.shape != Z.shape or draft.device != dev:
+            raise ValueError("draft must have Z's shape and device")
+    elif crd is not None or vals is not None:
+        if not isinstance(crd, torch.Tensor) or crd.dim() != 2 or vals is None:
+            raise ValueError("crd and vals must both be [N, K] matrices")
+        K = crd.shape[1]
+        _given(crd, torch.int32, (N, K), "crd", dev)
+        _given(vals, torch.float32, (N, K), "vals", dev)
+    if isinstance(scale, torch.Tensor):
+        scales, scale = _given(scale, torch.float32, (B,), "scale", dev), 1.0
+    need = _work_bytes("comet_draft_verify", kind, N, V, B, K, 1 if draft is not None else 0)
+    accepted = _new(None, torch.int32, (B,), "accepted", dev, stream)
+    follow = _new(None, torch.int32, (B,), "next", dev, stream)
+    if length is not None:
+        torch.autograd.graph.increment_version(length)
+    work, wptr = _work(need, dev, stream)
+    _call("comet_draft_verify", dev, stream, ptr, kind, N, V, ld, B, pos.data_ptr(), token.data_ptr(), u.data_ptr(), v.data_ptr(), dptr, dkind, ldd, _ptr(crd),
+          _ptr(vals), K, float(scale), _ptr(scales), accepted.data_ptr(), follow.data_ptr(), _ptr(length), wptr, need)
+    return accepted, follow

@@ -1,0 +1,91 @@
+// What the kernels over a cache in blocks share, and their launchers (cache_map.hip, cache_write.hip, block_select.hip, block_attend.hip).
+// Arguments are checked by the entry points (cache_api.hip); every launcher only enqueues work on `st`.
+#pragma once
+
+#include "rows.hpp"
+
+namespace comet {
+
+struct MapArgs {
+    int64_t B, M, block;
+    const int32_t *add;
+    const uint8_t *ended;
+    int32_t *length, *held, *table;
+    int64_t ldt;
+    int32_t *spare;
+    int64_t S;
+    int32_t *count;
+    int64_t N;
+    int32_t *pos;
+    int64_t *slot;
+    int32_t *place;
+};
+int64_t cache_map_work(int64_t B, int64_t M, int64_t N);
+hipError_t cache_map(const MapArgs &a, void *work, hipStream_t st);
+
+hipError_t cache_write(const comet_cache &c, int64_t N, const void *k, const int64_t k_stride[2], const void *v, const int64_t v_stride[2],
+                       const int64_t *slot, hipStream_t st);
+
+// The packed queries of B requests, and where their blocks are.
+struct Queries {
+    const void *q;
+    int64_t N, Q, row, head;             // rows, heads, and their strides in elements
+    int64_t B;
+    const int32_t *pos, *length, *table;
+    int64_t M, ldt;
+};
+int64_t block_select_work(const comet_cache &c, int64_t N, int64_t Q, int64_t B, int64_t M, int64_t K);
+hipError_t block_select(const comet_cache &c, const Queries &q, int64_t K, int64_t first, int64_t last, int32_t *sel, void *work, hipStream_t st);
+
+int64_t block_attend_work(const comet_cache &c, int64_t N, int64_t Q, int64_t B, int64_t M, int64_t K);
+hipError_t block_attend(const comet_cache &c, const Queries &q, const int32_t *sel, int64_t K, double scale, void *out, float *lse, void *work,
+                        hipStream_t st);
+
+// ---- sums over a workgroup, in the order of the threads ------------------------------------------------------------
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {
+    const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int64_t y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+// The sum up to and with each thread's x; `total` becomes that of all.  buf: a place for each wavefront, free again afterwards.
+template <int T> __device__ __forceinline__ int64_t block_scan(int64_t x, int64_t *buf, int64_t &total) {
+    const int64_t up = wave_scan(x);
+    if ((threadIdx.x & (kWave - 1)) == kWave - 1) buf[threadIdx.x / kWave] = up;
+    __syncthreads();
+    int64_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < T / kWave; ++w) {
+        if (w < (int)(threadIdx.x / kWave)) before += buf[w];
+        total += buf[w];
+    }
+    __syncthreads();
+    return before + up;
+}
+
+// ---- requests of packed rows ---------------------------------------------------------------------------------------
+// The request that a row belongs to, or -1: the number of requests that end at it or before it.  By a whole workgroup; count: one place of LDS.
+template <int T> __device__ __forceinline__ int64_t request_of(const int32_t *pos, int64_t B, int64_t row, int *count) {
+    if (threadIdx.x == 0) *count = 0;
+    __syncthreads();
+    int n = 0;
+    for (int64_t b = threadIdx.x; b < B; b += T) n += pos[b + 1] <= row ? 1 : 0;
+    if (n) atomicAdd(count, n);
+    __syncthreads();
+    const int b = *count;
+    __syncthreads();
+    return b < B && row >= pos[b] ? b : -1;
+}
+
+// An unsigned number whose order is that of the double: NaN is lowest, -0 is 0.
+__device__ __forceinline__ uint64_t order_of_double(double x) {
+    if (x != x) return 0;
+    const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
+    return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+}  // namespace comet

@@ -1,4 +1,4 @@
-// Launchers of the operators on dense rows (rows_topk.hip, rows_distill.hip, rows_beam.hip).  Arguments are checked by the
+// Launchers of the operators on dense rows (rows_topk.hip, rows_distill.hip, rows_beam.hip, rows_verify.hip).  Arguments are checked by the
 // entry points (rows_api.hip); every launcher only enqueues work on `st`.
 #pragma once
 
@@ -40,6 +40,11 @@ hipError_t distill_step(const DistillArgs &a, float *loss, void *dZ, int64_t ldd
 int64_t beam_select_work(int type, int64_t B, int64_t W, int64_t V, int64_t n);
 hipError_t beam_select(const void *Z, int type, int64_t B, int64_t W, int64_t V, int64_t ldz, const float *score, const uint8_t *finished,
                        int32_t eos, int64_t n, float *out_score, int32_t *out_parent, int32_t *out_token, void *work, hipStream_t st);
+
+int64_t draft_verify_work(int type, int64_t N, int64_t V, int64_t B, bool with_draft);
+hipError_t draft_verify(const void *Z, int type, int64_t N, int64_t V, int64_t ldz, int64_t B, const int32_t *pos, const int32_t *token, const float *u,
+                        const float *v, const void *draft, int draft_type, int64_t ldd, const int32_t *crd, const float *vals, int64_t K, double scale,
+                        const float *scales, int32_t *accepted, int32_t *next, int32_t *length, void *work, hipStream_t st);
 
 struct StateLayout {
     int64_t B, W, batch_stride, beam_stride, outer, outer_stride, inner;      // strides and inner in bytes
