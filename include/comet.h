@@ -407,7 +407,8 @@ typedef struct comet_cache {
     int64_t mean_stride[2];                        /* of p and h */
 } comet_cache;
 /* A block has a multiple of 16 places, COMET_MAX_BLOCK at most; size is a multiple of 8, 256 at most; pointers and strides are
- * multiples of 16 bytes (COMET_ERR_UNSUPPORTED or COMET_ERR_INVALID_ARG where they are not), strides at most 2^40. */
+ * multiples of 16 bytes (COMET_ERR_UNSUPPORTED or COMET_ERR_INVALID_ARG where they are not), strides at most 2^40; the places of a block lie within
+ * 2^31 bytes. */
 
 /* Tables and slots for the next tokens, from the lengths, on the device: nothing of it has to be known on the host.
  *   add        device, [B]: tokens that each request wants to add (below 0: none).

@@ -11,9 +11,10 @@ Plan plan_of(const comet_cache &c, int64_t N, int64_t Q, int64_t B, int64_t M, i
     Plan p{};
     const int64_t G = Q / c.heads, each = B > 0 ? (N + B - 1) / B : 1;
     p.wide = c.size <= 64 ? 64 : c.size <= 128 ? 128 : 256;
-    // rows of a workgroup: as many tokens as a request has on average, as far as four tiles of 16 go
+    // rows of a workgroup: as many tokens as a request has on average, as far as the registers go
     const int64_t rows = each * G;
     p.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    if (p.mt > attend_tiles(c.type, p.wide)) p.mt = attend_tiles(c.type, p.wide);
     p.chunk = (int)(G < 16 * p.mt ? G : 16 * p.mt);
     p.chunks = (int)((G + p.chunk - 1) / p.chunk);
     int64_t tokens = p.chunks > 1 ? 1 : 16 * p.mt / p.chunk;

@@ -7,11 +7,8 @@
 // joined at the end: nothing is handed from wavefront to wavefront on the way, and no barrier waits.
 //
 // Both products are turned around, S^T = K Q^T and O^T = V^T P^T: then a lane of the first one's result holds four places of one row, which is
-// how the second one wants P, and no element has to move.  V^T's fragments come from rows of V in registers: a lane reads the same 4 or 8
-// elements of its 8 places, and pairs of places are put together 16 bits by 16 bits.
+// how the second one wants P, and no element has to move.  V^T's fragments come from LDS, which turns 16-bit elements around as it is read.
 #pragma once
-
-#include <type_traits>
 
 #include "cache.hpp"
 
@@ -34,20 +31,24 @@ struct AttendArgs {
     float *part;                              // splits > 1: [item x splits x rows x (DT + 2)]
 };
 
-constexpr int kAttend = 256, kWaves = kAttend / kWave;
-
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef __bf16 B8 __attribute__((ext_vector_type(8)));
 typedef _Float16 H8 __attribute__((ext_vector_type(8)));
 typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+typedef short S4 __attribute__((ext_vector_type(4)));
 
-// What the types do differently.  CH: elements of 16 bytes.
+// What the types do differently.  A step of a wavefront takes HALVES times 16 places: of 16 bits 32, which one matrix instruction of the second
+// product adds up, of 32 bits 16.
 template <int TYPE, int DT> struct Shape {
-    static constexpr int CH = Elem<TYPE>::kPer;
-    static constexpr int NK = DT / (4 * CH);                   // vectors of a key in a lane: d = 4 CH kk + CH (lane / 16) + ..
-    static constexpr int U = TYPE == COMET_F32 || DT == 64 ? 4 : 8;      // elements of a value that lie together in a lane: d = 16 U dd + U (lane % 16) + ..
-    static constexpr int NV = DT / (16 * U);
-    static constexpr int VW = U * (TYPE == COMET_F32 ? 4 : 2) / 4;       // ... in 32-bit words
+    static constexpr int CH = Elem<TYPE>::kPer;                // elements of 16 bytes
+    static constexpr int HALVES = TYPE == COMET_F32 ? 1 : 2;
+    static constexpr int CHUNKS = DT / CH;                     // 16-byte pieces of a key
+    static constexpr int NK = CHUNKS / 4;                      // of them in a lane: piece 4 kk + lane / 16
+    static constexpr int TURN = CHUNKS < 16 ? 1 : 0;
+    static constexpr int LINE = CHUNKS * 16, ROWS = kWave / CHUNKS > 0 ? kWave / CHUNKS : 1;      // bytes of a key; keys of one load
+    static constexpr int LOADS = HALVES * 16 * CHUNKS / kWave; // loads of a step's keys
+    static constexpr int STAGE = 2 * HALVES * 16 * LINE;       // bytes of LDS for a step's keys and values
+    static constexpr int OT = DT / 16;                         // tiles of 16 elements of the output
 };
 
 template <int TYPE> __device__ __forceinline__ F4 product(U4 a, U4 b, F4 c) {
@@ -59,6 +60,11 @@ template <int TYPE> __device__ __forceinline__ F4 product(U4 a, U4 b, F4 c) {
         return c;
     }
 }
+
+// Tiles of 16 rows that a wavefront's registers hold, and wavefronts that a SIMD does.
+constexpr int attend_tiles(int type, int wide) { return wide <= 128 ? (type == COMET_F32 ? 2 : 2) : 1; }
+constexpr int attend_waves(int, int, int) { return 4; }
+constexpr int attend_pairs(int type, int wide, int mt) { return wide * mt <= 256 && wide <= 128 ? 2 : 1; }
 
 // Which tokens a workgroup has.
 struct Tile { int64_t b, first; int n; };
@@ -92,31 +98,31 @@ template <int T> __device__ __forceinline__ Tile find_tile(const Queries &q, int
 }
 
 // What a workgroup works at.
-struct Item { int64_t tile; int head, chunk, split; int64_t id; };
+struct Item { int tile, head, chunk, split; int64_t id; };
 __device__ __forceinline__ bool item_of(const AttendArgs &a, Item &i) {
     // neighbouring workgroups go to the eight dies in turn, each of which has a cache of its own: a die gets a stretch of the items
-    const int64_t all = a.tiles * a.heads * a.chunks * a.splits, each = gridDim.x / 8;
-    int64_t x = (blockIdx.x & 7) * each + (blockIdx.x >> 3);
+    const uint32_t hc = a.heads * a.chunks, tiles = (uint32_t)a.tiles, splits = a.splits, all = tiles * hc * splits, each = gridDim.x / 8;
+    uint32_t x = (blockIdx.x & 7) * each + (blockIdx.x >> 3), at;
     if (x >= all) return false;
-    const int hc = a.heads * a.chunks;
-    int at;
     if (a.tokens == 1) {             // heads of one token next to each other: their keys are next to each other in memory
-        at = (int)(x % hc), x /= hc;
-        i.split = (int)(x % a.splits), i.tile = x / a.splits;
+        const uint32_t y = x / hc;
+        at = x - y * hc, i.tile = (int)(y / splits), i.split = (int)(y - i.tile * splits);
     } else {                         // tokens next to each other: they read the same keys
-        i.split = (int)(x % a.splits), x /= a.splits;
-        i.tile = x % a.tiles, at = (int)(x / a.tiles);
+        const uint32_t y = x / splits;
+        i.split = (int)(x - y * splits), at = y / tiles, i.tile = (int)(y - at * tiles);
     }
-    i.head = at / a.chunks, i.chunk = at % a.chunks;
-    i.id = (i.tile * hc + at) * a.splits + i.split;
+    i.head = (int)(at / a.chunks), i.chunk = (int)(at - i.head * a.chunks);
+    i.id = ((int64_t)i.tile * hc + at) * splits + i.split;
     return true;
 }
 
-// The union of the tokens' choices in LDS: entry i is block j[i] of the request, at id[i] in the cache (below 0: it is none), chosen by the tokens of mask[i].
+// The union of the tokens' choices in LDS: entry i is block j[i] of the request, at id[i] in the cache, chosen by the tokens of mask[i] (0 where there is no
+// such block: it counts as the cache's first then, and nobody reads it).
 struct List { int *j, *id; uint32_t *mask; int n; };
+__host__ __device__ inline int behind_list(const AttendArgs &a) { return (3 * a.entries + 3) / 4 * 16; }
 template <int T> __device__ __forceinline__ List make_list(const AttendArgs &a, const Tile &t, int head, int64_t place0, uint32_t *raw, int64_t *buf) {
-    uint32_t *bits = raw, *before = raw + a.words;
-    List l{(int *)(raw + 2 * a.words), (int *)(raw + 2 * a.words) + a.entries, raw + 2 * a.words + 2 * a.entries, 0};
+    uint32_t *bits = raw + behind_list(a) / 4, *before = bits + a.words;          // not needed any more afterwards
+    List l{(int *)raw, (int *)raw + a.entries, raw + 2 * a.entries, 0};
     const auto seen = [&](int64_t place) {
         const int64_t c = place < 0 ? 0 : place / a.block + 1;
         return (int)(c < a.q.M ? c : a.q.M);
@@ -145,6 +151,7 @@ template <int T> __device__ __forceinline__ List make_list(const AttendArgs &a, 
         l.id[i] = id >= 0 && id < a.blocks ? id : -1;
         l.mask[i] = 0;
     }
+    if (a.blocks == 0) l.n = 0;
     __syncthreads();
     for (int e = threadIdx.x; e < t.n * a.K; e += T) {
         const int i = e / a.K, j = a.sel[((t.first + i) * a.heads + head) * a.K + (e - i * a.K)];
@@ -153,6 +160,9 @@ template <int T> __device__ __forceinline__ List make_list(const AttendArgs &a, 
             if (l.id[x] >= 0) atomicOr(&l.mask[x], 1u << i);
         }
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < l.n; i += T)
+        if (l.id[i] < 0) l.id[i] = 0;
     __syncthreads();
     return l;
 }
@@ -164,31 +174,32 @@ __device__ __forceinline__ float xor32(float v) { return __shfl_xor(v, 32); }
 struct Places {
     const char *key, *value;                  // the block's first place, of the head
     int start, last;                          // the first place's number in the block, the last one's that any of the tokens reads
-    int from;                                 // ... and in the request
+    int from;                                 // the first place's number in the request
     uint32_t mask;
 };
 
-template <int TYPE, int DT> struct Data {
-    using S = Shape<TYPE, DT>;
-    U4 k[2][S::NK];
-    uint32_t v[8][S::NV * S::VW];
-};
+typedef __attribute__((address_space(1))) const void Global;
+typedef __attribute__((address_space(3))) void Lds;
+
+// The wavefront's loads into LDS are there; what it has read from LDS is in registers.
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 template <int TYPE, int DT, int MT>
-__global__ void __launch_bounds__(kAttend, MT >= 4 || DT > 128 ? 1 : 2) k_attend(AttendArgs a) {
+__global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pairs(TYPE, DT, MT)) k_attend(AttendArgs a) {
     using S = Shape<TYPE, DT>;
     using E = Elem<TYPE>;
     using T = typename E::T;
-    constexpr int SIZE = (int)sizeof(T), OT = DT / 16, LINE = DT + 4;
+    constexpr int WAVES = attend_waves(TYPE, DT, MT), THREADS = WAVES * kWave, SIZE = (int)sizeof(T), OT = S::OT, LINE = DT + 4, HALVES = S::HALVES;
     extern __shared__ __align__(16) uint32_t raw[];
-    __shared__ int64_t buf[kWaves], where[3];
-    __shared__ float2 ml[kWaves][16];
+    __shared__ int64_t buf[WAVES], where[3];
+    __shared__ float2 ml[WAVES][16];
     Item item;
     if (!item_of(a, item)) return;
-    const Tile t = find_tile<kAttend>(a.q, a.tokens, item.tile, buf, where);
+    const Tile t = find_tile<THREADS>(a.q, a.tokens, item.tile, buf, where);
     if (t.n == 0) return;
     const int64_t place0 = a.q.length[t.b] - ((int64_t)a.q.pos[t.b + 1] - t.first), place1 = place0 + t.n - 1;
-    const List list = make_list<kAttend>(a, t, item.head, place0, raw, buf);
+    const List list = make_list<THREADS>(a, t, item.head, place0, raw, buf);
 
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane & 15, g = lane >> 4;
     const int heads = a.group - item.chunk * a.chunk < a.chunk ? a.group - item.chunk * a.chunk : a.chunk;      // of this chunk
@@ -201,10 +212,8 @@ __global__ void __launch_bounds__(kAttend, MT >= 4 || DT > 128 ? 1 : 2) k_attend
     for (int m = 0; m < MT; ++m) {
         const int r = 16 * m + col, i = r / heads;
         token[m] = i < t.n ? i : t.n - 1;
-        const int i0 = 16 * m / heads, i1 = (16 * m + 15) / heads;
-        of_tile[m] = 0;
-        for (int k = i0; k <= i1 && k < t.n; ++k) of_tile[m] |= 1u << k;
-        of_tile[m] = __builtin_amdgcn_readfirstlane(of_tile[m]);
+        const int i0 = 16 * m / heads, i1 = (16 * m + 15) / heads, most = i1 < t.n ? i1 : t.n - 1;
+        of_tile[m] = i0 > most ? 0 : __builtin_amdgcn_readfirstlane((most == 31 ? ~0u : (2u << most) - 1) & ~((1u << i0) - 1));
         const T *from = (const T *)a.q.q + (t.first + i) * a.q.row + (int64_t)(x0 + r - i * heads) * a.q.head;
 #pragma unroll
         for (int kk = 0; kk < S::NK; ++kk) {
@@ -213,66 +222,47 @@ __global__ void __launch_bounds__(kAttend, MT >= 4 || DT > 128 ? 1 : 2) k_attend
             if (r < rows && d < a.size) q[m][kk] = *(const U4 *)(from + d);
         }
     }
-    const uint32_t everyone = t.n == 32 ? ~0u : (1u << t.n) - 1;
 
-    const int per = a.block / 16;             // sixteens of a block
-    const int sixteens = list.n * per, pairs = (sixteens + 1) / 2;
-    const int begin = (int)((int64_t)pairs * item.split / a.splits), end = (int)((int64_t)pairs * (item.split + 1) / a.splits);
+    // Sixteens of all blocks, as far as anything is read; the last block of the list is the last of the request.
+    const int per = a.block / 16;
+    int sixteens = 0;
+    if (list.n > 0) {
+        const int64_t left = (place1 - (int64_t)list.j[list.n - 1] * a.block) / 16 + 1;
+        sixteens = (list.n - 1) * per + (int)(left < per ? left : per);
+    }
+    const int steps = (sixteens + HALVES - 1) / HALVES;
+    const int begin = (int)((int64_t)steps * item.split / a.splits), end = (int)((int64_t)steps * (item.split + 1) / a.splits);
 
     const auto places = [&](int s) {
-        Places p{nullptr, nullptr, 0, 0, 0, 0};
-        if (s >= sixteens) return p;
+        const bool there = s < sixteens;
+        if (!there) s = sixteens - 1;
+        Places p;
         const int e = s / per, j = __builtin_amdgcn_readfirstlane(list.j[e]), id = __builtin_amdgcn_readfirstlane(list.id[e]);
+        const uint32_t mask = __builtin_amdgcn_readfirstlane(list.mask[e]);
         p.start = (s - e * per) * 16;
         p.from = j * a.block + p.start;
         const int64_t last = place1 - (int64_t)j * a.block;
         p.last = (int)(last < a.block ? last : a.block - 1);
-        p.mask = p.start <= p.last ? __builtin_amdgcn_readfirstlane(list.mask[e]) : 0;
-        if (id < 0) p.mask = 0;
+        p.mask = there ? mask : 0;
         p.key = a.keys + id * a.key_stride[0] + item.head * a.key_stride[2];
         p.value = a.values + id * a.value_stride[0] + item.head * a.value_stride[2];
         return p;
     };
+    // Keys and values go to LDS straight from memory, a row of 16-byte pieces after the other, and from there to the lanes that want them: read by
+    // those lanes themselves, a load would ask for 64 pieces of 16 rows, and take four times as long.  Piece c of row i is at c ^ i, so
+    // that what is read together, of 16 rows, lies in different banks.  Places behind the last one that is read are taken from there:
+    // nothing comes from memory that no token reads.
+    char *const stage = (char *)raw + behind_list(a) + wave * S::STAGE, *const stage_v = stage + S::STAGE / 2;
     const bool ragged = a.size % (4 * S::CH) != 0;
-    // Places behind the last one that is read are taken from there: nothing comes from memory that no token reads.
-    const auto load = [&](const Places &p0, const Places &p1, Data<TYPE, DT> &x) {
+    const int key_line = (int)a.key_stride[1], value_line = (int)a.value_stride[1];
+    const auto load = [&](const Places (&x)[HALVES]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const Places &p = h ? p1 : p0;
-            if (p.mask) {
-                const int i = p.start + col < p.last ? p.start + col : p.last;
-                const char *from = p.key + (int64_t)i * a.key_stride[1];
-#pragma unroll
-                for (int kk = 0; kk < S::NK; ++kk) {
-                    const int d = (4 * kk + g) * S::CH;
-                    x.k[h][kk] = *(const U4 *)(from + (d < a.size ? d * SIZE : 0));
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int iv = p.start + 4 * g + r < p.last ? p.start + 4 * g + r : p.last;
-                    const char *v = p.value + (int64_t)iv * a.value_stride[1];
-#pragma unroll
-                    for (int dd = 0; dd < S::NV; ++dd) {
-                        const int d = 16 * S::U * dd + S::U * col;
-                        const uint32_t *w = (const uint32_t *)(v + (d < a.size ? d * SIZE : 0));
-                        if constexpr (S::VW == 2) {
-                            const uint2 y = *(const uint2 *)w;
-                            x.v[4 * h + r][2 * dd] = y.x, x.v[4 * h + r][2 * dd + 1] = y.y;
-                        } else {
-                            const U4 y = *(const U4 *)w;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) x.v[4 * h + r][4 * dd + e] = y[e];
-                        }
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int kk = 0; kk < S::NK; ++kk) x.k[h][kk] = U4{0, 0, 0, 0};
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int e = 0; e < S::NV * S::VW; ++e) x.v[4 * h + r][e] = 0;
-            }
+        for (int n = 0; n < S::LOADS; ++n) {
+            const Places &p = x[n * HALVES / S::LOADS];
+            const int k = n * kWave / S::CHUNKS % 16 + lane / S::CHUNKS, at = (n * kWave + lane) % S::CHUNKS, c = at ^ (k >> S::TURN & 15 & (S::CHUNKS - 1));
+            const int i = p.start + k < p.last ? p.start + k : p.last, d = c * S::CH < a.size ? c * 16 : 0;
+            __builtin_amdgcn_global_load_lds((Global *)(p.key + (uint32_t)(i * key_line + d)), (Lds *)(stage + n * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((Global *)(p.value + (uint32_t)(i * value_line + d)), (Lds *)(stage_v + n * 1024), 16, 0, 0);
         }
     };
 
@@ -285,95 +275,119 @@ __global__ void __launch_bounds__(kAttend, MT >= 4 || DT > 128 ? 1 : 2) k_attend
         for (int c = 0; c < OT; ++c) o[m][c] = F4{0, 0, 0, 0};
     }
 
-    const auto compute = [&](const Places &p0, const Places &p1, Data<TYPE, DT> &x) {
-        if (ragged) {
+    // The next step's keys and values are on their way while these are computed with.
+    if (begin + wave < end) {
+        Places now[HALVES];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < HALVES; ++h) now[h] = places(HALVES * (begin + wave) + h);
+        load(now);
+        for (int i = begin + wave; i < end; i += WAVES) {
+            U4 key[HALVES][S::NK], value[TYPE == COMET_F32 ? 4 * OT / 4 : OT];
+            loads_done();
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                 for (int kk = 0; kk < S::NK; ++kk)
-                    if ((4 * kk + g) * S::CH >= a.size) x.k[h][kk] = U4{0, 0, 0, 0};
-        }
-        const bool whole = p0.mask == everyone && p1.mask == everyone && p0.from + 15 <= place0 && p1.from + 15 <= place0;
-        float w[MT][8];
+                    key[h][kk] = *(const U4 *)(stage + (16 * h + col) * S::LINE + ((4 * kk + g) ^ (col >> S::TURN & (S::CHUNKS - 1))) * 16);
+            if constexpr (TYPE == COMET_F32) {
+                // a lane: places 4 g + r, elements 64 dd + 4 col + ..: each of the four belongs to an output tile of its own
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            if (!((p0.mask | p1.mask) & of_tile[m])) continue;
-            F4 s[2] = {F4{0, 0, 0, 0}, F4{0, 0, 0, 0}};
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int kk = 0; kk < S::NK; ++kk) {
-                if (4 * kk * S::CH >= a.size) continue;
-                s[0] = product<TYPE>(x.k[0][kk], q[m][kk], s[0]);
-                s[1] = product<TYPE>(x.k[1][kk], q[m][kk], s[1]);
-            }
-            float *z = w[m];
+                    for (int dd = 0; dd < OT / 4; ++dd)
+                        value[r * (OT / 4) + dd] = *(const U4 *)(stage_v + (4 * g + r) * S::LINE + ((16 * dd + col) ^ ((4 * g + r) >> S::TURN & 15)) * 16);
+            } else {
+                // Sixteen lanes read four places' 16 elements, and get an element's four places each: V^T as the matrix instruction wants it.
+                const int row = 4 * g + col / 4, turn = row >> S::TURN & (S::CHUNKS - 1);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = s[i / 4][i & 3] * a.c;
-            if (!whole) {
-                const int64_t mine = place0 + token[m];
-                const int l0 = p0.mask >> token[m] & 1 ? (int)(mine - p0.from) : -1, l1 = p1.mask >> token[m] & 1 ? (int)(mine - p1.from) : -1;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    z[i] = 4 * g + i <= l0 ? z[i] : kNegInf;
-                    z[4 + i] = 4 * g + i <= l1 ? z[4 + i] : kNegInf;
+                for (int c = 0; c < OT; ++c) {
+                    const char *at = stage_v + row * S::LINE + ((2 * c + (col >> 1 & 1)) ^ turn) * 16 + (col & 1) * 8;
+                    const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4 *)at);
+                    const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4 *)(at + 16 * S::LINE));
+                    const uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
+                    value[c] = U4{x.x, x.y, y.x, y.y};
                 }
             }
-            float most = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-            // The maximum follows when a score is 256 times over it, and not before: weights are 256 at most, which costs nothing in floating
-            // point, and the output is seldom scaled anew.
-            if (__ballot(most > top[m] + 8.f)) {
-                most = fmaxf(most, xor16(most));
-                most = fmaxf(most, xor32(most));
-                const float now = fmaxf(top[m], most), back = now == kNegInf ? 1.f : exp2_fast(top[m] - now);
-                top[m] = now;
-                sum[m] *= back;
+            reads_done();
+            Places then[HALVES];
+            if (i + WAVES < end) {
 #pragma unroll
-                for (int c = 0; c < OT; ++c) o[m][c] *= back;
+                for (int h = 0; h < HALVES; ++h) then[h] = places(HALVES * (i + WAVES) + h);
+                load(then);
+            } else {
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) then[h] = now[h];
             }
-            const float shift = top[m] == kNegInf ? 0.f : top[m];
-            float add[2] = {0.f, 0.f};
+            if (ragged) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                z[i] = exp2_fast(z[i] - shift);
-                add[i & 1] += z[i];
+                for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                    for (int kk = 0; kk < S::NK; ++kk)
+                        if ((4 * kk + g) * S::CH >= a.size) key[h][kk] = U4{0, 0, 0, 0};
             }
-            sum[m] += add[0] + add[1];
-        }
-        if constexpr (TYPE == COMET_F32) {
+            uint32_t some = 0, all = ~0u;                      // tokens that read something of it, and those that read all
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int c = 0; c < OT; ++c)
-#pragma unroll
-                    for (int m = 0; m < MT; ++m)
-                        if ((p0.mask | p1.mask) & of_tile[m])
-                            o[m][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][c]), w[m][i], o[m][c], 0, 0, 0);
-        } else {
-            // Weights are rounded to the type: half a step each, of as many that their errors cancel; a product in 32 bits would take 16 times as long.
-            U4 p[MT];
+            for (int h = 0; h < HALVES; ++h) some |= now[h].mask, all &= now[h].from + 15 <= place0 ? now[h].mask : 0;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const uint4 y = E::narrow(w[m]);
-                p[m] = U4{y.x, y.y, y.z, y.w};
+                if (!(some & of_tile[m])) continue;
+                float z[4 * HALVES];
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) {
+                    F4 s = F4{0, 0, 0, 0};
+#pragma unroll
+                    for (int kk = 0; kk < S::NK; ++kk) s = product<TYPE>(key[h][kk], q[m][kk], s);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[4 * h + r] = s[r];
+                }
+                if (of_tile[m] & ~all) {
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) {
+                        const int last = now[h].mask >> token[m] & 1 ? (int)(place0 + token[m] - now[h].from) : -1;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) z[4 * h + r] = 4 * g + r <= last ? z[4 * h + r] : kNegInf;
+                    }
+                }
+                float most = z[0];
+#pragma unroll
+                for (int r = 1; r < 4 * HALVES; ++r) most = fmaxf(most, z[r]);
+                most *= a.c;
+                // The maximum follows when a score is 256 times over it, and not before: weights are 256 at most, which costs nothing in floating
+                // point, and the output is seldom scaled anew.
+                if (__ballot(most > top[m] + 8.f)) {
+                    most = fmaxf(most, xor16(most));
+                    most = fmaxf(most, xor32(most));
+                    const float high = fmaxf(top[m], most), back = high == kNegInf ? 1.f : exp2_fast(top[m] - high);
+                    top[m] = high;
+                    sum[m] *= back;
+#pragma unroll
+                    for (int c = 0; c < OT; ++c) o[m][c] *= back;
+                }
+                const float shift = top[m] == kNegInf ? 0.f : top[m];
+                float add = 0.f;
+#pragma unroll
+                for (int r = 0; r < 4 * HALVES; ++r) {
+                    z[r] = exp2_fast(__builtin_fmaf(z[r], a.c, -shift));
+                    add += z[r];
+                }
+                sum[m] += add;
+                if constexpr (TYPE == COMET_F32) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int c = 0; c < OT; ++c)
+                            o[m][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(value[r * (OT / 4) + c / 4][c & 3]), z[r], o[m][c], 0, 0, 0);
+                } else {
+                    // Weights are rounded to the type: half a step each, of as many that their errors cancel; a product in 32 bits would take 16 times as long.
+                    const uint4 y = E::narrow(z);
+                    const U4 p = U4{y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int c = 0; c < OT; ++c) o[m][c] = product<TYPE>(value[c], p, o[m][c]);
+                }
             }
 #pragma unroll
-            for (int c = 0; c < OT; ++c) {
-                const int at = c / 2;
-                U4 v;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][at], x.v[2 * i][at], c & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-                    if ((p0.mask | p1.mask) & of_tile[m]) o[m][c] = product<TYPE>(v, p[m], o[m][c]);
-            }
+            for (int h = 0; h < HALVES; ++h) now[h] = then[h];
         }
-    };
-
-    for (int i = begin + wave; i < end; i += kWaves) {
-        const Places p0 = places(2 * i), p1 = places(2 * i + 1);
-        if (!(p0.mask | p1.mask)) continue;
-        Data<TYPE, DT> x;
-        load(p0, p1, x);
-        compute(p0, p1, x);
     }
 
     // ---- the wavefronts' parts together, one tile of rows after the other
@@ -388,7 +402,7 @@ __global__ void __launch_bounds__(kAttend, MT >= 4 || DT > 128 ? 1 : 2) k_attend
         sum[m] += xor16(sum[m]);
         sum[m] += xor32(sum[m]);
     }
-    float *line = (float *)raw + wave * 16 * LINE;
+    float *const lines = (float *)raw + behind_list(a) / 4, *const line = lines + wave * 16 * LINE;      // where the keys were
     // A row that came out as NaN once more, by itself: what it does not read weighs 0 in the products above, but 0 times a NaN or an infinity of
     // another row's is a NaN.  One place after the other, its own ones only.
     const auto alone = [&](int m, int n) {
@@ -397,12 +411,12 @@ __global__ void __launch_bounds__(kAttend, MT >= 4 || DT > 128 ? 1 : 2) k_attend
         const int i = r / heads;
         const T *from = (const T *)a.q.q + (t.first + i) * a.q.row + (int64_t)(x0 + r - i * heads) * a.q.head;
         float high = kNegInf, total = 0.f, out[DT / kWave] = {};
-        for (int pair = begin + wave; pair < end; pair += kWaves)
-            for (int h = 0; h < 2; ++h) {
-                const int s = 2 * pair + h;
+        for (int step = begin + wave; step < end; step += WAVES)
+            for (int h = 0; h < HALVES; ++h) {
+                const int s = HALVES * step + h;
                 if (s >= sixteens) break;
                 const int e = s / per, id = list.id[e];
-                if (id < 0 || !(list.mask[e] >> i & 1)) continue;
+                if (!(list.mask[e] >> i & 1)) continue;
                 for (int k = 0; k < 16; ++k) {
                     const int in = (s - e * per) * 16 + k;
                     if ((int64_t)list.j[e] * a.block + in > place0 + i) break;
@@ -434,61 +448,57 @@ __global__ void __launch_bounds__(kAttend, MT >= 4 || DT > 128 ? 1 : 2) k_attend
 #pragma unroll
         for (int u = 0; u < DT / kWave; ++u) line[n * LINE + u * kWave + lane] = out[u];
     };
-    __syncthreads();                           // the list is not needed any more, unless a row is done again
-    const bool again = __syncthreads_or(
-        [&] { uint32_t b = 0;
-#pragma unroll
-              for (int m = 0; m < MT; ++m) b |= bad[m];
-              return b != 0; }());
-    if (again) line += 2 * a.words + 3 * a.entries;
-    float *lines = (float *)raw + (again ? 2 * a.words + 3 * a.entries : 0);
+    __syncthreads();
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
         if (16 * m >= rows) break;
 #pragma unroll
-        for (int dd = 0; dd < S::NV; ++dd)
+        for (int c = 0; c < OT; ++c) {
+            float *to = line + col * LINE;
+            if constexpr (TYPE == COMET_F32) {
+                if (c % 4 == 0)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float *to = line + col * LINE + 16 * S::U * dd + S::U * (4 * g + r);
-#pragma unroll
-                for (int e = 0; e < S::U; e += 4)
-                    *(F4 *)(to + e) = F4{o[m][dd * S::U + e][r], o[m][dd * S::U + e + 1][r], o[m][dd * S::U + e + 2][r], o[m][dd * S::U + e + 3][r]};
+                    for (int r = 0; r < 4; ++r) *(F4 *)(to + 16 * c + 4 * (4 * g + r)) = F4{o[m][c][r], o[m][c + 1][r], o[m][c + 2][r], o[m][c + 3][r]};
+            } else {
+                *(F4 *)(to + 16 * c + 4 * g) = o[m][c];
             }
+        }
         if (g == 0) ml[wave][col] = make_float2(top[m], sum[m]);
         if (bad[m]) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             for (uint32_t left = bad[m]; left; left &= left - 1) alone(m, __builtin_ctz(left));
         }
         __syncthreads();
-        // sixteen threads a row, OT elements each
-        const int n = threadIdx.x / 16, d0 = (threadIdx.x & 15) * OT, r = 16 * m + n;
+        // some threads a row, a few elements each
+        constexpr int EACH = 16 * DT / THREADS, OVER = DT / EACH;
+        const int n = threadIdx.x / OVER, d0 = threadIdx.x % OVER * EACH, r = 16 * m + n;
         if (r < rows) {
-            float high = kNegInf, total = 0.f, part[kWaves], out[OT] = {};
+            float high = kNegInf, total = 0.f, part[WAVES], out[EACH] = {};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) high = fmaxf(high, ml[w][n].x);
+            for (int w = 0; w < WAVES; ++w) high = fmaxf(high, ml[w][n].x);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float2 y = ml[w][n];
                 part[w] = y.x == high || y.x != y.x ? 1.f : y.x == kNegInf ? 0.f : exp2_fast(y.x - high);
                 total += y.y * part[w];
             }
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w)
+            for (int w = 0; w < WAVES; ++w)
                 if (part[w] != 0.f)
 #pragma unroll
-                    for (int e = 0; e < OT; ++e) out[e] = __builtin_fmaf(lines[(w * 16 + n) * LINE + d0 + e], part[w], out[e]);
+                    for (int e = 0; e < EACH; ++e) out[e] = __builtin_fmaf(lines[(w * 16 + n) * LINE + d0 + e], part[w], out[e]);
             if (a.splits > 1) {
                 float *to = a.part + (item.id * (16 * MT) + r) * (DT + 4);
                 if (d0 == 0) to[DT] = high, to[DT + 1] = total;
 #pragma unroll
-                for (int e = 0; e < OT; e += 4) *(F4 *)(to + d0 + e) = F4{out[e], out[e + 1], out[e + 2], out[e + 3]};
+                for (int e = 0; e < EACH; e += 4) *(F4 *)(to + d0 + e) = F4{out[e], out[e + 1], out[e + 2], out[e + 3]};
             } else {
                 const int i = r / heads;
                 const int64_t row = (t.first + i) * a.q.Q + x0 + r - i * heads;
                 const float by = total == 0.f ? 0.f : 1.f / total;
                 T *to = (T *)a.out + row * a.size + d0;
 #pragma unroll
-                for (int e = 0; e < OT; ++e)
+                for (int e = 0; e < EACH; ++e)
                     if (d0 + e < a.size) to[e] = (T)E::bits(total == 0.f ? 0.f : out[e] * by);
                 if (d0 == 0 && a.lse) a.lse[row] = total == 0.f ? kNegInf : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
             }
@@ -499,8 +509,9 @@ __global__ void __launch_bounds__(kAttend, MT >= 4 || DT > 128 ? 1 : 2) k_attend
 
 // The parts of a tile that several workgroups share: one workgroup a tile and head, a wavefront a row.
 template <int TYPE, int DT, int MT>
-__global__ void __launch_bounds__(kAttend) k_attend_join(AttendArgs a) {
+__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
     using E = Elem<TYPE>;
+    constexpr int kAttend = 256, kWaves = kAttend / kWave;
     __shared__ int64_t buf[kWaves], where[3];
     const int hc = a.heads * a.chunks;
     const int64_t tile = blockIdx.x / hc;
@@ -532,26 +543,29 @@ __global__ void __launch_bounds__(kAttend) k_attend_join(AttendArgs a) {
 }
 
 template <int TYPE, int DT, int MT> hipError_t attend_run(const AttendArgs &a, hipStream_t st) {
+    constexpr int WAVES = attend_waves(TYPE, DT, MT);
     const int64_t items = a.tiles * a.heads * a.chunks * a.splits;
-    const size_t list = (size_t)(2 * a.words + 3 * a.entries) * 4, lds = list + (size_t)kWaves * 16 * (DT + 4) * 4;
+    size_t lds = (size_t)WAVES * Shape<TYPE, DT>::STAGE;
+    for (const size_t other : {(size_t)WAVES * 16 * (DT + 4) * 4, (size_t)a.words * 8}) lds = other > lds ? other : lds;
+    lds += behind_list(a);
     hipError_t e = hipSuccess;
     if (lds > 65536) e = hipFuncSetAttribute((const void *)k_attend<TYPE, DT, MT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_attend<TYPE, DT, MT>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(kAttend), lds, st, a);
+    hipLaunchKernelGGL((k_attend<TYPE, DT, MT>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(WAVES * kWave), lds, st, a);
     e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    hipLaunchKernelGGL((k_attend_join<TYPE, DT, MT>), dim3((unsigned)(a.tiles * a.heads * a.chunks)), dim3(kAttend), 0, st, a);
+    hipLaunchKernelGGL((k_attend_join<TYPE, DT, MT>), dim3((unsigned)(a.tiles * a.heads * a.chunks)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
+template <int TYPE, int DT> hipError_t attend_wide(const AttendArgs &a, int mt, hipStream_t st) {
+    constexpr int MOST = attend_tiles(TYPE, DT);
+    if constexpr (MOST >= 4) if (mt == 4) return attend_run<TYPE, DT, 4>(a, st);
+    if constexpr (MOST >= 2) if (mt == 2) return attend_run<TYPE, DT, 2>(a, st);
+    return attend_run<TYPE, DT, 1>(a, st);
+}
 template <int TYPE> hipError_t attend_type(const AttendArgs &a, int wide, int mt, hipStream_t st) {
-    const auto with = [&](auto d) {
-        constexpr int DT = decltype(d)::value;
-        return mt == 1 ? attend_run<TYPE, DT, 1>(a, st) : mt == 2 ? attend_run<TYPE, DT, 2>(a, st) : attend_run<TYPE, DT, 4>(a, st);
-    };
-    if (wide == 64) return with(std::integral_constant<int, 64>());
-    if (wide == 128) return with(std::integral_constant<int, 128>());
-    return with(std::integral_constant<int, 256>());
+    return wide == 64 ? attend_wide<TYPE, 64>(a, mt, st) : wide == 128 ? attend_wide<TYPE, 128>(a, mt, st) : attend_wide<TYPE, 256>(a, mt, st);
 }
 hipError_t attend_f32(const AttendArgs &a, int wide, int mt, hipStream_t st);
 hipError_t attend_bf16(const AttendArgs &a, int wide, int mt, hipStream_t st);

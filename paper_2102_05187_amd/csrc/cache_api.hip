@@ -38,6 +38,9 @@ comet_status check_cache(const comet_cache *c, bool data, bool mean) {
         if (s != COMET_OK) return s;
         if (c->blocks > 0 && (!c->keys || !c->values)) return COMET_ERR_INVALID_ARG;
         if (!aligned(c->keys, 16) || !aligned(c->values, 16)) return COMET_ERR_INVALID_ARG;
+        // a place's distance from its block's first is computed in 32 bits
+        for (const int64_t line : {c->key_stride[1], c->value_stride[1]})
+            if (line * element_size(c->type) * c->block >= kLim - 1024) return COMET_ERR_UNSUPPORTED;
     }
     if (mean || c->mean) {
         s = check_strides(c->mean_stride, 2, c->type);
