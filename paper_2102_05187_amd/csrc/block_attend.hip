@@ -19,7 +19,7 @@ Plan plan_of(const comet_cache &c, int64_t N, int64_t Q, int64_t B, int64_t M, i
     p.chunks = (int)((G + p.chunk - 1) / p.chunk);
     int64_t tokens = p.chunks > 1 ? 1 : 16 * p.mt / p.chunk;
     if (tokens > 32) tokens = 32;
-    if (tokens * K > 2048) tokens = 2048 / K;
+    if (tokens * K > kMostEntries) tokens = kMostEntries / K;
     if (tokens > each) tokens = each;
     p.tokens = (int)tokens;
     p.tiles = N / tokens + (B < N ? B : N);

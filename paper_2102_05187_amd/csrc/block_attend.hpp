@@ -66,34 +66,68 @@ constexpr int attend_tiles(int type, int wide) { return wide <= 128 ? (type == C
 constexpr int attend_waves(int, int, int) { return 4; }
 constexpr int attend_pairs(int type, int wide, int mt) { return wide * mt <= 256 && wide <= 128 ? 2 : 1; }
 
-// Which tokens a workgroup has.
-struct Tile { int64_t b, first; int n; };
+// Which tokens a workgroup has, and the first one's place in its request.
+struct Tile { int64_t b, first; int n; int64_t place; };
+
+// The sum over the lanes up to and with each.
+__device__ __forceinline__ int lanes_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
 
 // Tile `tile` of those that cut every request's tokens into pieces of `tokens`; n = 0 where there are not as many.
-template <int T> __device__ __forceinline__ Tile find_tile(const Queries &q, int tokens, int64_t tile, int64_t *buf, int64_t *where) {
+template <int T> __device__ __forceinline__ Tile find_tile(const Queries &q, int tokens, int tile, int64_t *buf, int64_t *where) {
+    Tile t{0, 0, 0, 0};
+    const auto cut = [&](int64_t b, int begin, int end, int length, int number) {
+        const int n = end - begin, i = number * tokens;
+        t.b = b, t.first = (int64_t)begin + i, t.n = n - i < tokens ? n - i : tokens, t.place = (int64_t)length - n + i;
+        if (t.first + t.n > q.N) t.n = t.first < q.N ? (int)(q.N - t.first) : 0;
+    };
+    if (q.B <= 4 * kWave) {
+        // every wavefront by itself: a request a lane, all that is needed of it with one wait
+        const int lane = threadIdx.x & (kWave - 1);
+        int begin[4], end[4], length[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = i * kWave + lane;
+            begin[i] = end[i] = length[i] = 0;
+            if (b < q.B) begin[i] = q.pos[b], end[i] = q.pos[b + 1], length[i] = q.length[b];
+        }
+        int before = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i * kWave >= q.B) break;
+            const int mine = end[i] > begin[i] ? (end[i] - begin[i] + tokens - 1) / tokens : 0, upto = before + lanes_scan(mine);
+            const uint64_t hit = __ballot(tile < upto);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                cut(i * kWave + l, __builtin_amdgcn_readlane(begin[i], l), __builtin_amdgcn_readlane(end[i], l), __builtin_amdgcn_readlane(length[i], l),
+                    tile - __builtin_amdgcn_readlane(upto - mine, l));
+                return t;
+            }
+            before = __builtin_amdgcn_readlane(upto, kWave - 1);
+        }
+        return t;
+    }
     if (threadIdx.x == 0) where[0] = -1;
     const int64_t each = (q.B + T - 1) / T, b0 = threadIdx.x * each, b1 = b0 + each < q.B ? b0 + each : q.B;
     int64_t mine = 0, total;
-    for (int64_t b = b0; b < b1; ++b) {
-        const int n = q.pos[b + 1] - q.pos[b];
-        mine += n > 0 ? (n + tokens - 1) / tokens : 0;
-    }
+    const auto pieces = [&](int64_t b) { return q.pos[b + 1] > q.pos[b] ? (q.pos[b + 1] - q.pos[b] + tokens - 1) / tokens : 0; };
+    for (int64_t b = b0; b < b1; ++b) mine += pieces(b);
     const int64_t upto = block_scan<T>(mine, buf, total);
     if (tile >= upto - mine && tile < upto) {
-        int64_t left = tile - (upto - mine);
-        for (int64_t b = b0; b < b1; ++b) {
-            const int n = q.pos[b + 1] - q.pos[b], pieces = n > 0 ? (n + tokens - 1) / tokens : 0;
-            if (left < pieces) {
-                where[0] = b, where[1] = q.pos[b] + left * tokens, where[2] = n - left * tokens < tokens ? n - left * tokens : tokens;
-                break;
-            }
-            left -= pieces;
-        }
+        int64_t left = tile - (upto - mine), b = b0;
+        for (; left >= pieces(b); ++b) left -= pieces(b);
+        where[0] = b, where[1] = left;
     }
     __syncthreads();
-    Tile t{where[0], where[0] < 0 ? 0 : where[1], where[0] < 0 ? 0 : (int)where[2]};
-    if (t.first + t.n > q.N) t.n = t.first < q.N ? (int)(q.N - t.first) : 0;
-    __syncthreads();
+    const int64_t b = where[0];
+    if (b >= 0) cut(b, q.pos[b], q.pos[b + 1], q.length[b], (int)where[1]);
     return t;
 }
 
@@ -120,49 +154,91 @@ __device__ __forceinline__ bool item_of(const AttendArgs &a, Item &i) {
 // such block: it counts as the cache's first then, and nobody reads it).
 struct List { int *j, *id; uint32_t *mask; int n; };
 __host__ __device__ inline int behind_list(const AttendArgs &a) { return (3 * a.entries + 3) / 4 * 16; }
-template <int T> __device__ __forceinline__ List make_list(const AttendArgs &a, const Tile &t, int head, int64_t place0, uint32_t *raw, int64_t *buf) {
+constexpr int kMostEntries = 2048;           // tokens times their choices
+template <int T> __device__ __forceinline__ List make_list(const AttendArgs &a, const Tile &t, int head, uint32_t *raw, int64_t *buf) {
     uint32_t *bits = raw + behind_list(a) / 4, *before = bits + a.words;          // not needed any more afterwards
     List l{(int *)raw, (int *)raw + a.entries, raw + 2 * a.entries, 0};
     const auto seen = [&](int64_t place) {
         const int64_t c = place < 0 ? 0 : place / a.block + 1;
         return (int)(c < a.q.M ? c : a.q.M);
     };
-    const int words = (seen(place0 + t.n - 1) + 31) / 32;
-    for (int w = threadIdx.x; w < words; w += T) bits[w] = 0;
-    __syncthreads();
-    for (int e = threadIdx.x; e < t.n * a.K; e += T) {
-        const int i = e / a.K, j = a.sel[((t.first + i) * a.heads + head) * a.K + (e - i * a.K)];
-        if (j >= 0 && j < seen(place0 + i)) atomicOr(&bits[j >> 5], 1u << (j & 31));
+    const int32_t *table = a.q.table + t.b * a.q.ldt, *sel = a.sel + (t.first * a.heads + head) * a.K;
+    const int last = seen(t.place + t.n - 1), all = t.n * a.K;
+    const auto id_of = [&](int j) {
+        const int id = table[j];
+        return id >= 0 && id < a.blocks ? id : -1;
+    };
+    if (a.blocks == 0 || last == 0) return l;
+    constexpr int MOST = kMostEntries / T;
+    int j[MOST];                                // the thread's choices, -1 where they are none
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) {
+        j[k] = -1;
+        if (k * T >= all) continue;
+        const int e = k * T + threadIdx.x;
+        if (e >= all) continue;
+        const int i = t.n == 1 ? 0 : e / a.K, x = sel[(int64_t)i * a.heads * a.K + (e - i * a.K)];
+        j[k] = x >= 0 && x < seen(t.place + i) ? x : -1;
     }
-    __syncthreads();
-    const int each = (words + T - 1) / T, w0 = threadIdx.x * each, w1 = w0 + each < words ? w0 + each : words;
-    int64_t mine = 0, total;
-    for (int w = w0; w < w1; ++w) mine += __builtin_popcount(bits[w]);
-    int at = (int)(block_scan<T>(mine, buf, total) - mine);
-    for (int w = w0; w < w1; ++w) {
-        before[w] = at;
-        for (uint32_t left = bits[w]; left; left &= left - 1) l.j[at++] = w * 32 + __builtin_ctz(left);
-    }
-    l.n = (int)total;
-    __syncthreads();
-    const int32_t *table = a.q.table + t.b * a.q.ldt;
-    for (int i = threadIdx.x; i < l.n; i += T) {
-        const int id = table[l.j[i]];
-        l.id[i] = id >= 0 && id < a.blocks ? id : -1;
-        l.mask[i] = 0;
-    }
-    if (a.blocks == 0) l.n = 0;
-    __syncthreads();
-    for (int e = threadIdx.x; e < t.n * a.K; e += T) {
-        const int i = e / a.K, j = a.sel[((t.first + i) * a.heads + head) * a.K + (e - i * a.K)];
-        if (j >= 0 && j < seen(place0 + i)) {
-            const int x = (int)before[j >> 5] + __builtin_popcount(bits[j >> 5] & ((1u << (j & 31)) - 1));
-            if (l.id[x] >= 0) atomicOr(&l.mask[x], 1u << i);
+    if (t.n == 1 && all <= T) {
+        // one token: its choices as they are, where they ascend, and behind them there is none
+        const int e = threadIdx.x;
+        int id = -1;
+        if (j[0] >= 0) id = id_of(j[0]);
+        if (e < all) l.j[e] = j[0];
+        __syncthreads();
+        const bool mixed = e < all && e > 0 && (j[0] >= 0 ? l.j[e - 1] >= j[0] || l.j[e - 1] < 0 : false);
+        const int some = __syncthreads_count(j[0] >= 0);
+        if (!__syncthreads_or(mixed)) {
+            if (e < some) l.id[e] = id < 0 ? 0 : id, l.mask[e] = id < 0 ? 0 : 1;
+            l.n = some;
+            __syncthreads();
+            return l;
         }
     }
+    const int words = (last + 31) / 32;
+    for (int w = threadIdx.x; w < words; w += T) bits[w] = 0;
+    for (int i = threadIdx.x; i < a.entries; i += T) l.mask[i] = 0;
+    int id[MOST];
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) {
+        id[k] = -1;
+        if (j[k] >= 0) id[k] = id_of(j[k]);
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < l.n; i += T)
-        if (l.id[i] < 0) l.id[i] = 0;
+#pragma unroll
+    for (int k = 0; k < MOST; ++k)
+        if (j[k] >= 0) atomicOr(&bits[j[k] >> 5], 1u << (j[k] & 31));
+    __syncthreads();
+    if (words <= kWave) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const uint32_t mine = lane < words ? bits[lane] : 0;
+        const int upto = lanes_scan(__builtin_popcount(mine));
+        int at = upto - __builtin_popcount(mine);
+        l.n = __builtin_amdgcn_readlane(upto, kWave - 1);
+        if (threadIdx.x < words) {
+            before[lane] = at;
+            for (uint32_t left = mine; left; left &= left - 1) l.j[at++] = lane * 32 + __builtin_ctz(left);
+        }
+    } else {
+        const int each = (words + T - 1) / T, w0 = threadIdx.x * each, w1 = w0 + each < words ? w0 + each : words;
+        int64_t mine = 0, total;
+        for (int w = w0; w < w1; ++w) mine += __builtin_popcount(bits[w]);
+        int at = (int)(block_scan<T>(mine, buf, total) - mine);
+        for (int w = w0; w < w1; ++w) {
+            before[w] = at;
+            for (uint32_t left = bits[w]; left; left &= left - 1) l.j[at++] = w * 32 + __builtin_ctz(left);
+        }
+        l.n = (int)total;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < MOST; ++k)
+        if (j[k] >= 0) {
+            const int e = k * T + threadIdx.x, x = (int)before[j[k] >> 5] + __builtin_popcount(bits[j[k] >> 5] & ((1u << (j[k] & 31)) - 1));
+            l.id[x] = id[k] < 0 ? 0 : id[k];
+            if (id[k] >= 0) atomicOr(&l.mask[x], 1u << (t.n == 1 ? 0 : e / a.K));
+        }
     __syncthreads();
     return l;
 }
@@ -198,8 +274,7 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
     if (!item_of(a, item)) return;
     const Tile t = find_tile<THREADS>(a.q, a.tokens, item.tile, buf, where);
     if (t.n == 0) return;
-    const int64_t place0 = a.q.length[t.b] - ((int64_t)a.q.pos[t.b + 1] - t.first), place1 = place0 + t.n - 1;
-    const List list = make_list<THREADS>(a, t, item.head, place0, raw, buf);
+    const int64_t place0 = t.place, place1 = place0 + t.n - 1;
 
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane & 15, g = lane >> 4;
     const int heads = a.group - item.chunk * a.chunk < a.chunk ? a.group - item.chunk * a.chunk : a.chunk;      // of this chunk
@@ -223,6 +298,8 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
         }
     }
 
+    const List list = make_list<THREADS>(a, t, item.head, raw, buf);
+
     // Sixteens of all blocks, as far as anything is read; the last block of the list is the last of the request.
     const int per = a.block / 16;
     int sixteens = 0;
@@ -233,20 +310,38 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
     const int steps = (sixteens + HALVES - 1) / HALVES;
     const int begin = (int)((int64_t)steps * item.split / a.splits), end = (int)((int64_t)steps * (item.split + 1) / a.splits);
 
-    const auto places = [&](int s) {
-        const bool there = s < sixteens;
-        if (!there) s = sixteens - 1;
+    // Sixteen `r` of entry e.  Those behind the last one are the last one's, and read by nobody.
+    const char *const keys = a.keys + item.head * a.key_stride[2], *const values = a.values + item.head * a.value_stride[2];
+    const auto places = [&](int e, int r) {
+        const bool there = e * per + r < sixteens;
+        if (!there) e = list.n - 1, r = 0;
         Places p;
-        const int e = s / per, j = __builtin_amdgcn_readfirstlane(list.j[e]), id = __builtin_amdgcn_readfirstlane(list.id[e]);
+        const int j = __builtin_amdgcn_readfirstlane(list.j[e]), id = __builtin_amdgcn_readfirstlane(list.id[e]);
         const uint32_t mask = __builtin_amdgcn_readfirstlane(list.mask[e]);
-        p.start = (s - e * per) * 16;
+        p.start = r * 16;
         p.from = j * a.block + p.start;
-        const int64_t last = place1 - (int64_t)j * a.block;
-        p.last = (int)(last < a.block ? last : a.block - 1);
+        const int last = (int)place1 - j * a.block;
+        p.last = last < a.block ? last : a.block - 1;
         p.mask = there ? mask : 0;
-        p.key = a.keys + id * a.key_stride[0] + item.head * a.key_stride[2];
-        p.value = a.values + id * a.value_stride[0] + item.head * a.value_stride[2];
+        p.key = keys + id * a.key_stride[0];
+        p.value = values + id * a.value_stride[0];
         return p;
+    };
+    // The places of a step, from where it begins; then where the wavefront's next step begins.
+    int entry = HALVES * (begin + wave) / per, sixteen = HALVES * (begin + wave) - entry * per;
+    const int skip = HALVES * WAVES / per, more = HALVES * WAVES - skip * per;
+    const auto step = [&](Places (&x)[HALVES]) {
+        x[0] = places(entry, sixteen);
+        if constexpr (HALVES == 2) {
+            if (sixteen + 1 < per && entry * per + sixteen + 1 < sixteens) {
+                x[1] = x[0];
+                x[1].start += 16, x[1].from += 16;
+            } else {
+                x[1] = sixteen + 1 < per ? places(entry, sixteen + 1) : places(entry + 1, 0);
+            }
+        }
+        entry += skip, sixteen += more;
+        if (sixteen >= per) sixteen -= per, ++entry;
     };
     // Keys and values go to LDS straight from memory, a row of 16-byte pieces after the other, and from there to the lanes that want them: read by
     // those lanes themselves, a load would ask for 64 pieces of 16 rows, and take four times as long.  Piece c of row i is at c ^ i, so
@@ -255,14 +350,33 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
     char *const stage = (char *)raw + behind_list(a) + wave * S::STAGE, *const stage_v = stage + S::STAGE / 2;
     const bool ragged = a.size % (4 * S::CH) != 0;
     const int key_line = (int)a.key_stride[1], value_line = (int)a.value_stride[1];
+    int key_at[S::LOADS], value_at[S::LOADS];
+#pragma unroll
+    for (int n = 0; n < S::LOADS; ++n) {
+        const int k = n * kWave / S::CHUNKS % 16 + lane / S::CHUNKS, at = (n * kWave + lane) % S::CHUNKS, c = at ^ (k >> S::TURN & 15 & (S::CHUNKS - 1));
+        const int d = c * S::CH < a.size ? c * 16 : 0;
+        key_at[n] = k * key_line + d, value_at[n] = k * value_line + d;
+    }
     const auto load = [&](const Places (&x)[HALVES]) {
 #pragma unroll
-        for (int n = 0; n < S::LOADS; ++n) {
-            const Places &p = x[n * HALVES / S::LOADS];
-            const int k = n * kWave / S::CHUNKS % 16 + lane / S::CHUNKS, at = (n * kWave + lane) % S::CHUNKS, c = at ^ (k >> S::TURN & 15 & (S::CHUNKS - 1));
-            const int i = p.start + k < p.last ? p.start + k : p.last, d = c * S::CH < a.size ? c * 16 : 0;
-            __builtin_amdgcn_global_load_lds((Global *)(p.key + (uint32_t)(i * key_line + d)), (Lds *)(stage + n * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((Global *)(p.value + (uint32_t)(i * value_line + d)), (Lds *)(stage_v + n * 1024), 16, 0, 0);
+        for (int h = 0; h < HALVES; ++h) {
+            const Places &p = x[h];
+            constexpr int EACH = S::LOADS / HALVES;
+            if (p.start + 15 <= p.last) {
+                const char *key = p.key + (uint32_t)(p.start * key_line), *value = p.value + (uint32_t)(p.start * value_line);
+#pragma unroll
+                for (int n = h * EACH; n < (h + 1) * EACH; ++n) {
+                    __builtin_amdgcn_global_load_lds((Global *)(key + (uint32_t)key_at[n]), (Lds *)(stage + n * 1024), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((Global *)(value + (uint32_t)value_at[n]), (Lds *)(stage_v + n * 1024), 16, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int n = h * EACH; n < (h + 1) * EACH; ++n) {
+                    const int k = n * kWave / S::CHUNKS % 16 + lane / S::CHUNKS, i = p.start + k < p.last ? p.start + k : p.last;
+                    __builtin_amdgcn_global_load_lds((Global *)(p.key + (uint32_t)(key_at[n] + (i - k) * key_line)), (Lds *)(stage + n * 1024), 16, 0, 0);
+                    __builtin_amdgcn_global_load_lds((Global *)(p.value + (uint32_t)(value_at[n] + (i - k) * value_line)), (Lds *)(stage_v + n * 1024), 16, 0, 0);
+                }
+            }
         }
     };
 
@@ -278,8 +392,7 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
     // The next step's keys and values are on their way while these are computed with.
     if (begin + wave < end) {
         Places now[HALVES];
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) now[h] = places(HALVES * (begin + wave) + h);
+        step(now);
         load(now);
         for (int i = begin + wave; i < end; i += WAVES) {
             U4 key[HALVES][S::NK], value[TYPE == COMET_F32 ? 4 * OT / 4 : OT];
@@ -310,14 +423,8 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
             }
             reads_done();
             Places then[HALVES];
-            if (i + WAVES < end) {
-#pragma unroll
-                for (int h = 0; h < HALVES; ++h) then[h] = places(HALVES * (i + WAVES) + h);
-                load(then);
-            } else {
-#pragma unroll
-                for (int h = 0; h < HALVES; ++h) then[h] = now[h];
-            }
+            step(then);
+            if (i + WAVES < end) load(then);
             if (ragged) {
 #pragma unroll
                 for (int h = 0; h < HALVES; ++h)
@@ -327,7 +434,7 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
             }
             uint32_t some = 0, all = ~0u;                      // tokens that read something of it, and those that read all
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h) some |= now[h].mask, all &= now[h].from + 15 <= place0 ? now[h].mask : 0;
+            for (int h = 0; h < HALVES; ++h) some |= now[h].mask, all &= now[h].from + 15 <= (int)place0 ? now[h].mask : 0;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 if (!(some & of_tile[m])) continue;
@@ -343,7 +450,7 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
                 if (of_tile[m] & ~all) {
 #pragma unroll
                     for (int h = 0; h < HALVES; ++h) {
-                        const int last = now[h].mask >> token[m] & 1 ? (int)(place0 + token[m] - now[h].from) : -1;
+                        const int last = now[h].mask >> token[m] & 1 ? (int)place0 + token[m] - now[h].from : -1;
 #pragma unroll
                         for (int r = 0; r < 4; ++r) z[4 * h + r] = 4 * g + r <= last ? z[4 * h + r] : kNegInf;
                     }
@@ -516,7 +623,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
     const int hc = a.heads * a.chunks;
     const int64_t tile = blockIdx.x / hc;
     const int at = (int)(blockIdx.x % hc), head = at / a.chunks, chunk = at % a.chunks;
-    const Tile t = find_tile<kAttend>(a.q, a.tokens, tile, buf, where);
+    const Tile t = find_tile<kAttend>(a.q, a.tokens, (int)tile, buf, where);
     const int heads = a.group - chunk * a.chunk < a.chunk ? a.group - chunk * a.chunk : a.chunk, x0 = head * a.group + chunk * a.chunk;
     const int lane = threadIdx.x & (kWave - 1);
     const float *from = a.part + (int64_t)blockIdx.x * a.splits * (16 * MT) * (DT + 4);
