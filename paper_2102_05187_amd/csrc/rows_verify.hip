@@ -9,34 +9,34 @@ namespace {
 // How the draft's distribution is known: not at all (the token has all of it), by some of its logits, by all of them.
 enum { kPoint = 0, kEntries = 1, kDense = 2 };
 
-constexpr int kRow = 256;
-constexpr int kVectors = 8;                   // 16-byte vectors of a thread: a piece of a row is 2048 vectors
+constexpr int kRow = 256, kWavesRow = kRow / kWave;
+constexpr int kParts = 32;                    // parts of a piece whose weights are kept: of a wavefront's vectors that lie next to each other
 
-int64_t pieces_of(int type, int64_t V) {
-    const int64_t n = kRow * kVectors * (type == COMET_F32 ? 4 : 8);
+// A thread has VEC 16-byte vectors of a piece, a piece VEC * kRow.  Long rows, or many, are cut into pieces of 2048 vectors, few short ones into
+// pieces of 512: 8 rows of 32000 32-bit logits take 24 us in 16 pieces each, and 38 in 4.
+int vectors_of(int64_t N, int64_t V) { return N * V < int64_t(1) << 20 ? 2 : 8; }
+int64_t pieces_of(int type, int64_t N, int64_t V) {
+    const int64_t n = kRow * vectors_of(N, V) * (type == COMET_F32 ? 4 : 8);
     return V > n ? (V + n - 1) / n : 1;
 }
 
-// exp2 in 64 bits for arguments of at most 0, to about 2^-49: the nearest whole number taken off, a Taylor polynomial of exp(f ln 2) for |f| <= 1/2
-// (the first term that is left out is 4e-18 of the sum at most, the roundings of its steps are more).
-__device__ __forceinline__ double exp2_wide(double x) {
-    if (!(x > -1000.0)) return x != x ? x : 0.0;
-    const double n = __builtin_rint(x), f = (x - n) * 0.6931471805599453094;
-    double r = 1.0 / 6227020800.0;
-    r = __builtin_fma(r, f, 1.0 / 479001600.0);
-    r = __builtin_fma(r, f, 1.0 / 39916800.0);
-    r = __builtin_fma(r, f, 1.0 / 3628800.0);
-    r = __builtin_fma(r, f, 1.0 / 362880.0);
-    r = __builtin_fma(r, f, 1.0 / 40320.0);
-    r = __builtin_fma(r, f, 1.0 / 5040.0);
-    r = __builtin_fma(r, f, 1.0 / 720.0);
-    r = __builtin_fma(r, f, 1.0 / 120.0);
-    r = __builtin_fma(r, f, 1.0 / 24.0);
-    r = __builtin_fma(r, f, 1.0 / 6.0);
-    r = __builtin_fma(r, f, 0.5);
-    r = __builtin_fma(r, f, 1.0);
-    r = __builtin_fma(r, f, 1.0);
-    return __builtin_amdgcn_ldexp(r, (int)n);
+// exp2 in 64 bits for arguments of at most 0: the nearest whole number taken off, by adding 1.5 2^52, and a polynomial for |f| <= 1/2, which goes
+// through 2^f at the ten zeros of a Chebyshev polynomial (off by 2e-14 at most).  Below -1000 it is 2^-1000, or 0 where ZERO.  A NaN is not kept.
+// Bound by the issue of 64-bit instructions: sixteen of them, and the sums of 320 rows of 131072 take 42 million such exponentials.
+template <bool ZERO> __device__ __forceinline__ double exp2_wide(double x) {
+    const double low = __builtin_fmax(x, -1000.0), big = low + 0x1.8p52, f = low - (big - 0x1.8p52);
+    double r = 0x1.b6557c7da8ca4p-24;
+    r = __builtin_fma(r, f, 0x1.63efd536dcb25p-20);
+    r = __builtin_fma(r, f, 0x1.ffcb7a04d3b13p-17);
+    r = __builtin_fma(r, f, 0x1.43088df6dd4a7p-13);
+    r = __builtin_fma(r, f, 0x1.5d87fe8e6c4b1p-10);
+    r = __builtin_fma(r, f, 0x1.3b2ab72b2b245p-7);
+    r = __builtin_fma(r, f, 0x1.c6b08d7045e60p-5);
+    r = __builtin_fma(r, f, 0x1.ebfbdff814945p-3);
+    r = __builtin_fma(r, f, 0x1.62e42fefa39e9p-1);
+    r = __builtin_fma(r, f, 0x1.000000000003dp+0);
+    const double y = __hiloint2double(__double2hiint(r) + (__double2loint(big) << 20), __double2loint(r));
+    return ZERO && !(x > -1000.0) ? 0.0 : y;
 }
 
 // The sum of exp2((z - m) c) over a part of a row, m its largest logit: of nothing, m is -inf; with a NaN or +inf in it, s is a NaN.
@@ -45,25 +45,22 @@ struct Sum {
     double m;
     __device__ __forceinline__ bool good() const { return s > 0; }
 };
-__device__ __forceinline__ Sum join(Sum a, Sum b, double c) {
-    Sum r;
-    r.m = a.m > b.m ? a.m : b.m;
-    r.s = (a.m == r.m ? a.s : a.s == 0 ? 0 : a.s * exp2_wide((a.m - r.m) * c)) + (b.m == r.m ? b.s : b.s == 0 ? 0 : b.s * exp2_wide((b.m - r.m) * c));
-    return r;
-}
-__device__ __forceinline__ Sum wave_join(Sum a, double c) {
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const Sum b{__shfl_xor(a.s, d), __shfl_xor(a.m, d)};
-        a = join(a, b, c);
+// What a part's sum is relative to a larger maximum.
+__device__ __forceinline__ double onto(Sum a, double m, double c) { return a.m == m || a.s == 0 || a.s != a.s ? a.s : a.s * exp2_wide<true>((a.m - m) * c); }
+// Over groups of `over` lanes, a power of two.
+__device__ __forceinline__ Sum group_join(Sum a, int over, double c) {
+    double m = a.m;
+    for (int d = 1; d < over; d *= 2) {
+        const double y = __shfl_xor(m, d);
+        m = y > m ? y : m;
     }
-    return a;
+    double s = onto(a, m, c);
+    for (int d = 1; d < over; d *= 2) s += __shfl_xor(s, d);
+    return Sum{s, m};
 }
-// Of a whole row, from its pieces' sums; by a wavefront, the same in all lanes.
-__device__ __forceinline__ Sum row_sum(const Sum *piece, int64_t pieces, double c) {
-    Sum a{0, kNegInfD};
-    for (int64_t i = threadIdx.x & (kWave - 1); i < pieces; i += kWave) a = join(a, piece[i], c);
-    return wave_join(a, c);
+__device__ __forceinline__ Sum two(Sum a, Sum b, double c) {
+    const double m = a.m > b.m ? a.m : b.m;
+    return Sum{onto(a, m, c) + onto(b, m, c), m};
 }
 
 struct VerifyArgs {
@@ -80,28 +77,42 @@ struct VerifyArgs {
     const float *scales;
     int32_t *accepted, *next, *length;
     Sum *target, *drafted;                    // [N x pieces], [N x draft_pieces]
-    double *weight;                           // [B x pieces]: what is drawn from, piece by piece
+    double *weight;                           // [B x pieces x kParts]: what is drawn from
     int32_t *arrived;                         // [B]
-    int64_t pieces, draft_pieces;
+    int32_t pieces, draft_pieces;
 
     // scale log2 e of a request; NaN where it is no scale, +inf where the largest logit is taken
     __device__ __forceinline__ double of(int64_t b) const {
         const double s = scales ? (double)scales[b] : scale;
         return s > 0 ? s * 1.4426950408889634 : __builtin_nan("");
     }
+    // the request of a row, by every wavefront for itself where there are no more than 256
+    __device__ __forceinline__ int64_t request(int64_t row, int *count) const {
+        if (B > 4 * kWave) return request_of<kRow>(pos, B, row, count);
+        int32_t end[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = i * kWave + (int)(threadIdx.x & (kWave - 1));
+            end[i] = b < B ? pos[b + 1] : 0x7fffffff;
+        }
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += __builtin_popcountll(__ballot(end[i] <= row));
+        return n < B && row >= pos[n] ? n : -1;
+    }
 };
 
 // One piece of one row.
-template <int TYPE>
-__device__ void piece_sum(const void *base, int64_t row, int64_t ld, int64_t V, int64_t piece, double c, Sum *out) {
+template <int TYPE, int VEC>
+__device__ __forceinline__ void piece_sum(const void *base, int64_t row, int64_t ld, int64_t V, int64_t piece, double c, Sum *out) {
     using E = Elem<TYPE>;
-    __shared__ float top[kRow / kWave];
-    __shared__ double part[kRow / kWave];
+    __shared__ float top[kWavesRow];
+    __shared__ double part[kWavesRow];
     const Row<TYPE> r(base, row, ld, V);
-    const int64_t v0 = piece * (kRow * kVectors);
-    uint4 x[kVectors];
+    const int64_t v0 = piece * (kRow * VEC);
+    uint4 x[VEC];
 #pragma unroll
-    for (int j = 0; j < kVectors; ++j) {
+    for (int j = 0; j < VEC; ++j) {
         const int64_t i = v0 + j * kRow + threadIdx.x;
         if (r.whole(i)) {
             x[j] = r.raw(i);
@@ -111,52 +122,65 @@ __device__ void piece_sum(const void *base, int64_t row, int64_t ld, int64_t V, 
             x[j] = E::narrow(f);
         }
     }
+    const auto larger = [](float a, float b) { return __builtin_elementwise_maximum(a, b); };      // a NaN stays
     float m = kNegInf;
 #pragma unroll
-    for (int j = 0; j < kVectors; ++j) {
+    for (int j = 0; j < VEC; ++j) {
         float f[E::kPer];
         E::widen(x[j], f);
 #pragma unroll
-        for (int e = 0; e < E::kPer; ++e) m = fmaxf(m, f[e]);
+        for (int e = 0; e < E::kPer; ++e) m = larger(m, f[e]);
     }
-    m = wave_reduce(m, kNegInf, Larger());
+    m = wave_reduce(m, kNegInf, larger);
     if ((threadIdx.x & (kWave - 1)) == 0) top[threadIdx.x / kWave] = m;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kRow / kWave; ++w) m = fmaxf(m, top[w]);
+    for (int w = 0; w < kWavesRow; ++w) m = larger(m, top[w]);
     double s = 0;
-    const double big = m == kNegInf ? 0 : m;                    // exp2 of -inf is 0
-    const bool largest = c == __builtin_huge_val();
-    for (int j = 0; j < kVectors; ++j) {
-        float f[E::kPer];
-        E::widen(x[j], f);
+    if (c == __builtin_huge_val()) {
 #pragma unroll
-        for (int e = 0; e < E::kPer; ++e) s += largest ? (f[e] != f[e] ? f[e] : f[e] == m ? 1.0 : 0.0) : exp2_wide(((double)f[e] - big) * c);
+        for (int j = 0; j < VEC; ++j) {
+            float f[E::kPer];
+            E::widen(x[j], f);
+#pragma unroll
+            for (int e = 0; e < E::kPer; ++e) s += f[e] == m ? 1.0 : 0.0;
+        }
+    } else {
+        const double big = m;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            float f[E::kPer];
+            E::widen(again(x[j]), f);
+#pragma unroll
+            for (int e = 0; e < E::kPer; ++e) s += exp2_wide<false>(((double)f[e] - big) * c);
+        }
     }
     s = wave_reduce(s, 0.0, Add());
     if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kRow / kWave; ++w) s += part[w];
-        *out = Sum{s, m};
+        for (int w = 1; w < kWavesRow; ++w) s += part[w];
+        if (m == kNegInf) s = 0;
+        if (!(m < -kNegInf) || c != c) s = __builtin_nan("");
+        *out = Sum{s, m != m ? kNegInfD : (double)m};
     }
 }
 
 // Sums of all pieces of all rows that are judged by or drawn from.
-template <int TYPE, int DRAFT>
+template <int TYPE, int DRAFT, int VEC>
 __global__ void __launch_bounds__(kRow) k_verify_sums(VerifyArgs a) {
     __shared__ int count;
-    const int64_t all = a.pieces + a.draft_pieces, row = blockIdx.x / all;
-    int64_t piece = blockIdx.x - row * all;
+    const int all = a.pieces + a.draft_pieces, row = (int)(blockIdx.x / (unsigned)all);
+    int piece = (int)blockIdx.x - row * all;
     for (int64_t b = (int64_t)blockIdx.x * kRow + threadIdx.x; b < a.B; b += (int64_t)gridDim.x * kRow) a.arrived[b] = 0;
-    const int64_t b = request_of<kRow>(a.pos, a.B, row, &count);
+    const int64_t b = a.request(row, &count);
     if (b < 0) return;
     const double c = a.of(b);
     if (piece < a.pieces) {
-        piece_sum<TYPE>(a.Z, row, a.ldz, a.V, piece, c, a.target + row * a.pieces + piece);
+        piece_sum<TYPE, VEC>(a.Z, row, a.ldz, a.V, piece, c, a.target + (int64_t)row * a.pieces + piece);
     } else if (row + 1 < a.pos[b + 1]) {
         piece -= a.pieces;
-        piece_sum<DRAFT>(a.draft, row, a.ldd, a.V, piece, c, a.drafted + row * a.draft_pieces + piece);
+        piece_sum<DRAFT, VEC>(a.draft, row, a.ldd, a.V, piece, c, a.drafted + (int64_t)row * a.draft_pieces + piece);
     }
 }
 
@@ -170,31 +194,43 @@ template <int TYPE, int DRAFT, int MODE> struct Left {
     int64_t d;
     const uint16_t *at;                       // kEntries: 1 + the entry of a place of the piece, 0: none
     const double *chance;                     //           and the entries' probabilities
-    // weights of vector i, `in` its number in the piece
-    __device__ __forceinline__ void weights(int64_t i, int in, double *w) const {
-        constexpr int PER = Elem<TYPE>::kPer;
-        float f[PER], g[PER];
-        z.load(i, f);
-        if (MODE == kDense && rejected) {
+    // the logits of vector i
+    static constexpr int PER = Elem<TYPE>::kPer;
+    struct Logits { float f[PER], g[MODE == kDense ? PER : 1]; };
+    __device__ __forceinline__ Logits logits(int64_t i) const {
+        Logits v;
+        z.load(i, v.f);
+        if constexpr (MODE == kDense) {
+            if (!rejected) return v;
             if constexpr (Elem<DRAFT>::kPer == PER) {
-                x.load(i, g);
+                x.load(i, v.g);
             } else if constexpr (Elem<DRAFT>::kPer < PER) {
-                x.load(2 * i, g), x.load(2 * i + 1, g + Elem<DRAFT>::kPer);
+                x.load(2 * i, v.g), x.load(2 * i + 1, v.g + Elem<DRAFT>::kPer);
             } else {
                 float both[Elem<DRAFT>::kPer];
                 x.load(i / 2, both);
 #pragma unroll
-                for (int e = 0; e < PER; ++e) g[e] = both[(i & 1) * PER + e];
+                for (int e = 0; e < PER; ++e) v.g[e] = both[(i & 1) * PER + e];
             }
         }
+        return v;
+    }
+    // its weights; `in` its number in the piece
+    __device__ __forceinline__ void weights(int64_t i, int in, const Logits &v, double *w) const {
+        const float *f = v.f;
+        if (largest) {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) w[e] = (double)f[e] == p.m ? 1 : 0;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < PER; ++e) w[e] = exp2_wide<true>(((double)f[e] - p.m) * c) * p_part;
+        if (!rejected) return;
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
-            if (largest) { w[e] = (double)f[e] == p.m ? 1 : 0; continue; }
-            w[e] = exp2_wide(((double)f[e] - p.m) * c) * p_part;
-            if (!rejected) continue;
             double off = 0;
             if (MODE == kPoint) off = z.first(i) + e == d ? 1 : 0;
-            if (MODE == kDense) off = q_part > 0 ? exp2_wide(((double)g[e] - q.m) * c) * q_part : 0;
+            if constexpr (MODE == kDense) off = exp2_wide<true>(((double)v.g[e] - q.m) * c) * q_part;
             if (MODE == kEntries) {
                 const int k = at[in * PER + e];
                 off = k ? chance[k - 1] : 0;
@@ -205,14 +241,17 @@ template <int TYPE, int DRAFT, int MODE> struct Left {
 };
 
 // One piece of the row that a request's next token is drawn from.  Each workgroup finds for itself how far the drafted tokens are taken; the one that
-// is done last has all pieces' weights, and draws.
-template <int TYPE, int DRAFT, int MODE>
+// is done last has all parts' weights, and draws.  Bound by the latency of its steps: requests, tokens, sums, logits, weights, and what the last one
+// has to read again, each a read from memory that the one before it names.
+template <int TYPE, int DRAFT, int MODE, int VEC>
 __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
-    constexpr int PER = Elem<TYPE>::kPer, kPiece = kRow * kVectors;
-    __shared__ int first, hit, final_one;
-    __shared__ double part[kRow / kWave], chance[MODE == kEntries ? COMET_MAX_TOP : 1];
+    constexpr int PER = Elem<TYPE>::kPer, kPiece = kRow * VEC;
+    static_assert(VEC * kWavesRow <= kParts, "a part for each wavefront's vectors next to each other");
+    __shared__ int first, final_one, chosen_part, behind;
+    __shared__ double part[kWavesRow], sums[kParts], chance[MODE == kEntries ? COMET_MAX_TOP : 1], before_part, goal_;
     __shared__ uint16_t at[MODE == kEntries ? kPiece * PER : 1];
-    const int64_t b = blockIdx.x / a.pieces, piece = blockIdx.x - b * a.pieces;
+    __shared__ Sum known[2][kRow / 8];
+    const int b = (int)(blockIdx.x / (unsigned)a.pieces), piece = (int)blockIdx.x - b * a.pieces;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int64_t r0 = a.pos[b], n = (a.pos[b + 1] < a.N ? a.pos[b + 1] : a.N) - r0;
     if (n <= 0) {
@@ -221,66 +260,74 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     }
     const double c = a.of(b);
     const bool largest = c == __builtin_huge_val();
-    // the sum of a row's entries; by a wavefront
-    const auto entries = [&](int64_t row) {
-        Sum s{0, kNegInfD};
-        for (int64_t k = lane; k < a.K; k += kWave) {
-            const int64_t col = a.crd[row * a.K + k];
-            if (col < 0 || col >= a.V) continue;
-            const double t = a.vals[row * a.K + k];
-            s = join(s, Sum{t == kNegInfD ? 0.0 : t - t == 0 ? 1.0 : __builtin_nan(""), t == t ? t : kNegInfD}, c);
-        }
-        return wave_join(s, c);
+    const auto usable = [&](const Sum &p) { return largest ? p.m > kNegInfD && p.m < -kNegInfD && p.s == p.s : p.good(); };
+    // rows in groups of lanes: 8 lanes a row, or a wavefront where there are entries or many pieces
+    const int over = MODE == kEntries || a.pieces > 64 || a.draft_pieces > 64 ? kWave : 8, at_once = kRow / over, group = threadIdx.x / over, l = threadIdx.x % over;
+    const auto row_sum = [&](const Sum *s, int pieces) {
+        Sum x{0, kNegInfD};
+        for (int i = l; i < pieces; i += over) x = two(x, s[i], c);
+        return group_join(x, over, c);
     };
     if (threadIdx.x == 0) first = (int)(n - 1);
     __syncthreads();
-    for (int64_t i = wave; i < n - 1; i += kRow / kWave) {
-        if (i > first) break;
-        const int64_t row = r0 + i, d = a.token[row + 1];
-        bool take = false;
-        if (d >= 0 && d < a.V) {
-            const Sum p = row_sum(a.target + row * a.pieces, a.pieces, c);
-            const double z = Elem<TYPE>::one(((const typename Elem<TYPE>::T *)a.Z)[row * a.ldz + d]);
-            if (largest) {
-                take = p.m == z && p.m > kNegInfD && p.m < -kNegInfD && p.s == p.s;
-            } else if (p.good()) {
-                double q = 1;
-                if (MODE == kDense) {
-                    const Sum s = row_sum(a.drafted + row * a.draft_pieces, a.draft_pieces, c);
-                    q = s.good() ? exp2_wide(((double)Elem<DRAFT>::one(((const typename Elem<DRAFT>::T *)a.draft)[row * a.ldd + d]) - s.m) * c) / s.s : 0;
-                }
-                if (MODE == kEntries) {
-                    const Sum s = entries(row);
-                    q = 0;
-                    if (s.good())
-                        for (int64_t k = lane; k < a.K; k += kWave)
-                            if (a.crd[row * a.K + k] == d) q = exp2_wide(((double)a.vals[row * a.K + k] - s.m) * c) / s.s;
-                    q = wave_reduce(q, 0.0, Add());
-                }
-                take = (double)a.u[row] * q < exp2_wide((z - p.m) * c) / p.s;
-            }
+    int took = 0, slot = 0;
+    for (int64_t i0 = 0; i0 < n; i0 += at_once) {
+        const int64_t i = i0 + group, row = r0 + (i < n ? i : n - 1);
+        const bool judged = i < n - 1;
+        const int64_t d = judged ? a.token[row + 1] : -1;
+        const bool real = d >= 0 && d < a.V;
+        float z = 0, x = 0, u = 0;
+        if (judged) u = a.u[row];
+        if (real) z = Elem<TYPE>::one(((const typename Elem<TYPE>::T *)a.Z)[row * a.ldz + d]);
+        if (MODE == kDense && real) x = Elem<DRAFT>::one(((const typename Elem<DRAFT>::T *)a.draft)[row * a.ldd + d]);
+        const Sum p = row_sum(a.target + row * a.pieces, a.pieces);
+        Sum s{0, kNegInfD};
+        double q = 1;
+        if (MODE == kDense && judged) {
+            s = row_sum(a.drafted + row * a.draft_pieces, a.draft_pieces);
+            q = s.good() ? exp2_wide<true>(((double)x - s.m) * c) / s.s : 0;
         }
-        if (!take && lane == 0) atomicMin(&first, (int)i);
+        if (MODE == kEntries) {
+            double mine = 0;
+            for (int64_t k = l; k < a.K && judged; k += over) {
+                const int64_t col = a.crd[row * a.K + k];
+                const double t = a.vals[row * a.K + k];
+                if (col < 0 || col >= a.V || t == kNegInfD) continue;
+                const Sum one{t - t == 0 ? 1.0 : __builtin_nan(""), t == t ? t : kNegInfD};
+                s = k < over ? one : two(s, one, c);
+            }
+            s = group_join(s, over, c);
+            for (int64_t k = l; k < a.K && judged; k += over)
+                if (a.crd[row * a.K + k] == d) mine += exp2_wide<true>(((double)a.vals[row * a.K + k] - s.m) * c);
+            for (int e = 1; e < over; e *= 2) mine += __shfl_xor(mine, e);
+            q = s.good() ? mine / s.s : 0;
+        }
+        bool take = false;
+        if (real && usable(p)) take = largest ? p.m == (double)z : (double)u * q < exp2_wide<true>(((double)z - p.m) * c) / p.s;
+        if (l == 0) {
+            known[0][group] = p, known[1][group] = s;
+            if (judged && !take) atomicMin(&first, (int)i);
+        }
+        __syncthreads();
+        took = first;
+        slot = (int)(took - i0);
+        if (took < i0 + at_once) break;
+        __syncthreads();
     }
-    __syncthreads();
-    const int64_t took = first, row = r0 + took;
+    const int64_t row = r0 + took;
     if (piece == 0 && threadIdx.x == 0) {
-        a.accepted[b] = (int32_t)took;
+        a.accepted[b] = took;
         if (a.length) a.length[b] -= (int32_t)(n - 1 - took);
     }
-    Left<TYPE, DRAFT, MODE> left{Row<TYPE>(a.Z, row, a.ldz, a.V), Row<DRAFT>(a.draft, MODE == kDense ? row : 0, a.ldd, a.V), row_sum(a.target + row * a.pieces, a.pieces, c),
-                                 Sum{0, 0}, c, 0, 0, took < n - 1 && !largest, largest, took < n - 1 ? a.token[row + 1] : -1, at, chance};
-    const bool any = largest ? left.p.m > kNegInfD && left.p.m < -kNegInfD && left.p.s == left.p.s : left.p.good();
-    if (!any) {
+    Left<TYPE, DRAFT, MODE> left{Row<TYPE>(a.Z, row, a.ldz, a.V), Row<DRAFT>(a.draft, MODE == kDense ? row : 0, a.ldd, a.V), known[0][slot], known[1][slot], c, 0, 0,
+                                 took < n - 1 && !largest, largest, took < n - 1 ? a.token[row + 1] : -1, at, chance};
+    if (!usable(left.p)) {
         if (piece == 0 && threadIdx.x == 0) a.next[b] = -1;
         return;
     }
-    if (left.rejected) {
-        if (MODE == kDense) left.q = row_sum(a.drafted + row * a.draft_pieces, a.draft_pieces, c);
-        if (MODE == kEntries) left.q = entries(row);
-        left.q_part = left.q.good() ? 1 / left.q.s : 0;
-    }
     left.p_part = 1 / left.p.s;
+    left.q_part = left.q.good() ? 1 / left.q.s : 0;
+    if (MODE == kDense && !left.q.good()) left.q.m = 0;
     // the entries that lie in a piece, by place
     const auto lay_out = [&](int64_t of) {
         if (MODE != kEntries || !left.rejected) return;
@@ -290,81 +337,54 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
         if (left.q_part > 0)
             for (int64_t k = threadIdx.x; k < a.K; k += kRow) {
                 const int64_t col = a.crd[row * a.K + k], to = col - of * kPiece * PER;
-                chance[k] = exp2_wide(((double)a.vals[row * a.K + k] - left.q.m) * c) * left.q_part;
+                chance[k] = exp2_wide<true>(((double)a.vals[row * a.K + k] - left.q.m) * c) * left.q_part;
                 if (col >= 0 && col < a.V && to >= 0 && to < kPiece * PER) at[to] = (uint16_t)(k + 1);
             }
         __syncthreads();
     };
-    const auto total = [&](double s) {
-        s = wave_reduce(s, 0.0, Add());
-        if (lane == 0) part[wave] = s;
-        __syncthreads();
-        s = 0;
-        for (int w = 0; w < kRow / kWave; ++w) s += part[w];
-        __syncthreads();
-        return s;
-    };
-    const auto piece_weight = [&](int64_t of) {
-        double s = 0;
-        for (int j = 0; j < kVectors; ++j) {
-            double w[PER];
-            left.weights(of * kPiece + j * kRow + threadIdx.x, j * kRow + threadIdx.x, w);
+    // the weights of a piece's parts: part j * 4 + w are the vectors of wavefront w at j, in the order of the row
+    const auto piece_parts = [&](int64_t of, auto put) {
+        typename Left<TYPE, DRAFT, MODE>::Logits ahead = left.logits(of * kPiece + threadIdx.x);
+#pragma unroll 1
+        for (int j = 0; j < VEC; ++j) {
+            double w[PER], s = 0;
+            const auto v = ahead;
+            if (j + 1 < VEC) ahead = left.logits(of * kPiece + (j + 1) * kRow + threadIdx.x);
+            left.weights(of * kPiece + j * kRow + threadIdx.x, j * kRow + threadIdx.x, v, w);
 #pragma unroll
             for (int e = 0; e < PER; ++e) s += w[e];
+            s = wave_reduce(s, 0.0, Add());
+            if (lane == 0) put(j * kWavesRow + wave, s);
         }
-        return total(s);
     };
     lay_out(piece);
-    const double mine = piece_weight(piece);
-    double *weight = a.weight + b * a.pieces;
-    if (a.pieces > 1) {
-        if (threadIdx.x == 0) {
-            __hip_atomic_store(weight + piece, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            final_one = __hip_atomic_fetch_add(a.arrived + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)a.pieces - 1;
-        }
-        __syncthreads();
-        if (!final_one) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-    }
-    const auto of_piece = [&](int64_t i) { return a.pieces > 1 ? __hip_atomic_load(weight + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : mine; };
-    double sum = 0;
-    for (int64_t i = 0; i < a.pieces; ++i) sum += of_piece(i);
-    const bool nothing = !(sum > 0);                             // p <= q throughout: p itself, of which the pieces are known
-    if (nothing) left.rejected = false;
-    const auto now = [&](int64_t i) {
-        if (!nothing) return of_piece(i);
-        const Sum s = a.target[row * a.pieces + i];
-        return s.s > 0 ? s.s * exp2_wide((s.m - left.p.m) * c) / left.p.s : 0.0;
-    };
-    if (nothing) {
-        sum = 0;
-        for (int64_t i = 0; i < a.pieces; ++i) sum += now(i);
-    }
-    const double v = largest || !(a.v[b] > 0) ? 0 : (double)a.v[b];
-    double goal = v * sum, upto = 0;
-    int64_t chosen = -1, last = 0;
-    for (int64_t i = 0; i < a.pieces && chosen < 0; ++i) {
-        const double w = now(i);
-        if (w > 0) last = i;
-        if (upto + w > goal) chosen = i;
-        else upto += w;
-    }
-    if (chosen < 0) chosen = last, goal = -kNegInfD;              // v rounds to all of the sum: the last place that has a weight
-    if (chosen != piece && left.rejected) lay_out(chosen);
-    if (threadIdx.x == 0) hit = -1;
+    double *weight = a.weight + (int64_t)b * a.pieces * kParts;
+    piece_parts(piece, [&](int i, double s) { __hip_atomic_store(weight + piece * kParts + i, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
     __syncthreads();
-    int behind = -1;                                             // the last place with a weight so far
-    for (int j = 0; j < kVectors; ++j) {
-        const int in = j * kRow + threadIdx.x;
-        double w[PER], s = 0;
-        left.weights(chosen * kPiece + in, in, w);
-        int at_last = -1;
+    if (threadIdx.x == 0) final_one = __hip_atomic_fetch_add(a.arrived + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
+    __syncthreads();
+    if (!final_one) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+
+    // Of `count` weights in order the first at which their running sum, from `upto` on, is beyond the goal: chosen_part, and the sum before it.  Where there is
+    // none, the last one that has a weight.  The goal is v times the sum of all where v is given (0 and above).
+    constexpr int kParts_ = VEC * kWavesRow;
+    const auto choose = [&](int count, auto get, double v, double goal) {
+        if (threadIdx.x == 0) chosen_part = 0x7fffffff, behind = -1;
+        const int each = (count + kRow - 1) / kRow, i0 = threadIdx.x * each, i1 = i0 + each < count ? i0 + each : count;
+        double mine = 0, kept[4];
+        if (each <= 4) {
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            s += w[e];
-            if (w[e] > 0) at_last = in * PER + e;
+            for (int k = 0; k < 4; ++k) {
+                kept[k] = 0;
+                if (i0 + k < i1) kept[k] = get(i0 + k);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mine += kept[k];
+        } else {
+            for (int i = i0; i < i1; ++i) mine += get(i);
         }
-        double run = s;
+        double run = mine;
 #pragma unroll
         for (int step = 1; step < kWave; step *= 2) {
             const double y = __shfl_up(run, step);
@@ -372,62 +392,113 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
         }
         if (lane == kWave - 1) part[wave] = run;
         __syncthreads();
-        double before = upto;
-        for (int w2 = 0; w2 < wave; ++w2) before += part[w2];
-        const double end = before + run;
-        if (at_last >= 0) behind = at_last;
-        const uint64_t over = __ballot(end > goal && s > 0);
-        if (over && lane == __builtin_ctzll(over)) {
-            double x = end - s;
-            int place = at_last;
-            for (int e = PER - 1; e >= 0; --e) {
-                double y = x;
-                for (int g = 0; g <= e; ++g) y += w[g];
-                if (w[e] > 0 && y > goal) place = in * PER + e;
-            }
-            atomicMin((unsigned *)&hit, (unsigned)place);
+        double upto = run - mine, all = 0;
+        for (int w = 0; w < kWavesRow; ++w) {
+            if (w < wave) upto += part[w];
+            all += part[w];
         }
-        for (int w2 = 0; w2 < kRow / kWave; ++w2) upto += part[w2];
+        if (v >= 0) goal = v * all;
+        int last = -1, hit = -1;
+        double x = upto, before = 0;
+        const auto take = [&](int i, double w) {
+            if (w > 0) last = i;
+            if (hit < 0 && x + w > goal) hit = i, before = x;
+            x += w;
+        };
+        if (each <= 4) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i0 + k < i1) take(i0 + k, kept[k]);
+        } else {
+            for (int i = i0; i < i1; ++i) take(i, get(i));
+        }
+        if (hit >= 0) atomicMin(&chosen_part, hit);
+        if (last >= 0) atomicMax(&behind, last);
         __syncthreads();
-        if (hit >= 0) break;
+        if (hit >= 0 && hit == chosen_part) before_part = before;
+        if (threadIdx.x == 0) {
+            goal_ = goal;
+            if (chosen_part == 0x7fffffff) chosen_part = behind, goal_ = __builtin_huge_val(), before_part = 0;         // v rounds to all of the sum
+        }
         __syncthreads();
+        return all;
+    };
+    const double v = largest || !(a.v[b] > 0) ? 0 : (double)a.v[b];
+    const double sum = choose(a.pieces * kParts_, [&](int i) {
+        return __hip_atomic_load(weight + i / kParts_ * kParts + i % kParts_, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }, v, 0);
+    int64_t of = chosen_part / kParts_;
+    int in = chosen_part % kParts_;
+    if (!(sum > 0)) {
+        // p <= q throughout: p itself is drawn from, first a piece of it, then a part of that
+        left.rejected = false;
+        __syncthreads();
+        choose(a.pieces, [&](int i) { return onto(a.target[row * a.pieces + i], left.p.m, c) * left.p_part; }, v, 0);
+        of = chosen_part;
+        const double goal = goal_ - before_part;
+        piece_parts(of, [&](int i, double s) { sums[i] = s; });
+        __syncthreads();
+        choose(kParts_, [&](int i) { return sums[i]; }, -1, goal);
+        in = chosen_part;
     }
-    if (hit < 0) {
-        if (threadIdx.x == 0) first = -1;
-        __syncthreads();
-        if (behind >= 0) atomicMax(&first, behind);
-        __syncthreads();
-        if (threadIdx.x == 0) hit = first;
-        __syncthreads();
+    if (of != piece) lay_out(of);
+    if (wave != 0) return;
+    // the part's vectors, one a lane
+    const int vec = (in / kWavesRow) * kRow + (in % kWavesRow) * kWave + lane;
+    double w[PER], s = 0;
+    left.weights(of * kPiece + vec, vec, left.logits(of * kPiece + vec), w);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) s += w[e];
+    double run = s;
+#pragma unroll
+    for (int step = 1; step < kWave; step *= 2) {
+        const double y = __shfl_up(run, step);
+        if (lane >= step) run += y;
     }
-    if (threadIdx.x == 0) a.next[b] = hit < 0 ? -1 : (int32_t)(chosen * kPiece * PER + hit);
+    int place = -1, last = -1;
+    double x = before_part + (run - s);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        x += w[e];
+        if (w[e] > 0) {
+            last = e;
+            if (place < 0 && x > goal_) place = e;
+        }
+    }
+    const uint64_t over_it = __ballot(place >= 0), some = __ballot(last >= 0);
+    const int who = over_it ? __builtin_ctzll(over_it) : some ? 63 - __builtin_clzll(some) : 0;
+    const int e = __builtin_amdgcn_readlane(over_it ? place : last, who);
+    if (lane == 0) a.next[b] = e < 0 ? -1 : (int32_t)((of * kPiece + vec + who) * PER + e);
 }
 
-template <int TYPE, int DRAFT, int MODE> hipError_t launch(const VerifyArgs &a, hipStream_t st) {
+template <int TYPE, int DRAFT, int MODE, int VEC> hipError_t launch(const VerifyArgs &a, hipStream_t st) {
     if (a.N > 0) {
-        hipLaunchKernelGGL((k_verify_sums<TYPE, DRAFT>), dim3((unsigned)(a.N * (a.pieces + a.draft_pieces))), dim3(kRow), 0, st, a);
+        hipLaunchKernelGGL((k_verify_sums<TYPE, DRAFT, VEC>), dim3((unsigned)(a.N * (a.pieces + a.draft_pieces))), dim3(kRow), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL((k_verify_draw<TYPE, DRAFT, MODE>), dim3((unsigned)(a.B * a.pieces)), dim3(kRow), 0, st, a);
+    hipLaunchKernelGGL((k_verify_draw<TYPE, DRAFT, MODE, VEC>), dim3((unsigned)(a.B * a.pieces)), dim3(kRow), 0, st, a);
     return hipGetLastError();
 }
-template <int TYPE> hipError_t launch(const VerifyArgs &a, int draft_type, hipStream_t st) {
+template <int TYPE, int VEC> hipError_t launch(const VerifyArgs &a, int draft_type, hipStream_t st) {
     if (a.draft) {
-        if (draft_type == COMET_F32) return launch<TYPE, COMET_F32, kDense>(a, st);
-        if (draft_type == COMET_BF16) return launch<TYPE, COMET_BF16, kDense>(a, st);
-        return launch<TYPE, COMET_F16, kDense>(a, st);
+        if (draft_type == COMET_F32) return launch<TYPE, COMET_F32, kDense, VEC>(a, st);
+        if (draft_type == COMET_BF16) return launch<TYPE, COMET_BF16, kDense, VEC>(a, st);
+        return launch<TYPE, COMET_F16, kDense, VEC>(a, st);
     }
-    return a.K > 0 ? launch<TYPE, TYPE, kEntries>(a, st) : launch<TYPE, TYPE, kPoint>(a, st);
+    return a.K > 0 ? launch<TYPE, TYPE, kEntries, VEC>(a, st) : launch<TYPE, TYPE, kPoint, VEC>(a, st);
+}
+template <int TYPE> hipError_t launch(const VerifyArgs &a, int draft_type, hipStream_t st) {
+    return vectors_of(a.N, a.V) == 2 ? launch<TYPE, 2>(a, draft_type, st) : launch<TYPE, 8>(a, draft_type, st);
 }
 
 struct Layout { int64_t target, drafted, weight, arrived, bytes; };
 Layout layout(int type, int64_t N, int64_t V, int64_t B, int draft_type, bool with_draft) {
     Layout l{};
     l.target = 0;
-    l.drafted = l.target + N * pieces_of(type, V) * (int64_t)sizeof(Sum);
-    l.weight = l.drafted + (with_draft ? N * pieces_of(draft_type, V) * (int64_t)sizeof(Sum) : 0);
-    l.arrived = l.weight + B * pieces_of(type, V) * 8;
+    l.drafted = l.target + N * pieces_of(type, N, V) * (int64_t)sizeof(Sum);
+    l.weight = l.drafted + (with_draft ? N * pieces_of(draft_type, N, V) * (int64_t)sizeof(Sum) : 0);
+    l.arrived = l.weight + B * pieces_of(type, N, V) * kParts * 8;
     l.bytes = l.arrived + B * 4;
     return l;
 }
@@ -442,7 +513,8 @@ hipError_t draft_verify(const void *Z, int type, int64_t N, int64_t V, int64_t l
     const Layout l = layout(type, N, V, B, draft_type, draft != nullptr);
     char *w = (char *)work;
     const VerifyArgs a{Z, N, V, ldz, B, pos, token, u, v, draft, ldd, crd, vals, K, scale, scales, accepted, next, length, (Sum *)(w + l.target),
-                       (Sum *)(w + l.drafted), (double *)(w + l.weight), (int32_t *)(w + l.arrived), pieces_of(type, V), draft ? pieces_of(draft_type, V) : 0};
+                       (Sum *)(w + l.drafted), (double *)(w + l.weight), (int32_t *)(w + l.arrived), (int32_t)pieces_of(type, N, V),
+                       draft ? (int32_t)pieces_of(draft_type, N, V) : 0};
     if (type == COMET_F32) return launch<COMET_F32>(a, draft_type, st);
     if (type == COMET_BF16) return launch<COMET_BF16>(a, draft_type, st);
     return launch<COMET_F16>(a, draft_type, st);
