@@ -723,15 +723,33 @@ def comet_beam_reorder(states: Sequence[torch.Tensor], parent: torch.Tensor, str
 
 
 # ---- a cache in blocks ------------------------------------------------------------------------------------------------------
+# The smallest of these calls take 3 to 10 us on the device: what depends on layouts alone is looked up, and the arrays of strides that the
+# library reads are made once for a layout.
 def _bytes_of(t: Optional[torch.Tensor], shape, what: str, device) -> Optional[torch.Tensor]:
     if isinstance(t, torch.Tensor) and t.dtype == torch.bool:
         t = t.view(torch.uint8)
     return _given(t, torch.uint8, shape, what, device)
 
 
+def _needed(t: torch.Tensor, dtype, shape, what: str, device) -> int:
+    """The address of an operand that has to be there."""
+    if t is None:
+        raise ValueError("%s is missing" % what)
+    return _given(t, dtype, shape, what, device).data_ptr()
+
+
+def _numbers(t: torch.Tensor, what: str) -> int:
+    """The length of an int32 vector."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("%s must be a torch tensor in device memory" % what)
+    if t.dim() != 1:
+        raise ValueError("%s must have one dimension" % what)
+    return t.shape[0]
+
+
 def _table(table: torch.Tensor, B: int, device):
     """(pointer, columns, distance of rows) of the requests' blocks."""
-    if not isinstance(table, torch.Tensor) or not table.is_cuda or table.dtype != torch.int32:
+    if not isinstance(table, torch.Tensor) or not table.is_cuda or table.dtype is not torch.int32:
         raise TypeError("table must be an int32 tensor in device memory")
     if table.dim() != 2 or table.shape[0] != B or table.device != device:
         raise ValueError("table must have a row for each of the %d requests, on %s" % (B, device))
@@ -741,68 +759,78 @@ def _table(table: torch.Tensor, B: int, device):
     return table.data_ptr(), M, ld if B > 1 else M
 
 
+@functools.lru_cache(maxsize=1024)
+def _lines(shape, stride, size):
+    """Strides of all dimensions but the last, of one that does not count 0, as numbers and as the library reads them; None where they are not what
+    its 16-byte loads need."""
+    strides = tuple(s if n > 1 else 0 for n, s in zip(shape, stride))
+    if strides[-1] > 1 or any(s * size % 16 for s in strides[:-1]):
+        return None
+    return strides[:-1], (ctypes.c_int64 * (len(shape) - 1))(*strides[:-1])
+
+
 def _vectors(t: torch.Tensor, what: str, dims: int, dtype=None, device=None):
-    """Strides of all dimensions but the last, whose elements lie next to each other; as the kernels' 16-byte loads need them."""
+    """(address, strides, strides as the library reads them) of a tensor whose last dimension's elements lie next to each other."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError("%s must be a torch tensor in device memory" % what)
-    if t.dtype not in _TYPES or (dtype is not None and t.dtype != dtype):
+    if t.dtype not in _TYPES or (dtype is not None and t.dtype is not dtype):
         raise TypeError("%s must have dtype %s, got %s" % (what, dtype or "float32, bfloat16 or float16", t.dtype))
-    if t.dim() != dims:
+    shape = t.shape
+    if len(shape) != dims:
         raise ValueError("%s must have %d dimensions" % (what, dims))
     if device is not None and t.device != device:
         raise ValueError("%s must be on %s" % (what, device))
-    strides = tuple(s if n > 1 else 0 for n, s in zip(t.shape, t.stride()))
-    if strides[-1] > 1 or t.data_ptr() % 16 or any(s * t.element_size() % 16 for s in strides[:-1]):
+    lines, at = _lines(shape, t.stride(), t.itemsize), t.data_ptr()
+    if lines is None or at & 15:
         raise ValueError("%s must have the last dimension's elements next to each other, and the others at multiples of 16 bytes" % what)
-    return strides[:-1]
+    return at, *lines
 
 
-def _cache(keys, values, mean, device):
+@functools.lru_cache(maxsize=256)
+def _cache_layout(kind, shape, key_stride, value_stride, mean_stride):
+    c = _Cache(None, None, None, kind, *shape)
+    c.key_stride[:], c.value_stride[:], c.mean_stride[:] = key_stride, value_stride, mean_stride
+    return c
+
+
+def _cache(keys, values, mean, device, block=None):
     """(description, dtype) of a cache: keys and values [blocks, block, heads, size], mean [blocks, heads, size]."""
-    some = mean if keys is None else keys
-    kind = getattr(some, "dtype", None)
+    k = v = m = None
     ks = vs = (0, 0, 0)
     ms = (0, 0)
     if keys is not None:
-        ks = _vectors(keys, "K", 4, None, device)
-        vs = _vectors(values, "V", 4, kind, device)
-        if values.shape != keys.shape:
+        kind, shape = keys.dtype, keys.shape
+        k, ks, _ = _vectors(keys, "K", 4, None, device)
+        v, vs, _ = _vectors(values, "V", 4, kind, device)
+        if values.shape != shape:
             raise ValueError("K and V must have one shape")
+        if mean is not None and mean.shape != (shape[0], *shape[2:]):
+            raise ValueError("mean must have shape %s, got %s" % ((shape[0], *shape[2:]), tuple(mean.shape)))
     if mean is not None:
-        ms = _vectors(mean, "mean", 3, kind if keys is not None else None, device)
-        if keys is not None and mean.shape != (keys.shape[0], *keys.shape[2:]):
-            raise ValueError("mean must have shape %s, got %s" % ((keys.shape[0], *keys.shape[2:]), tuple(mean.shape)))
-    blocks, heads, size = some.shape[0], some.shape[-2], some.shape[-1]
-    c = _Cache(_ptr(keys), _ptr(values), _ptr(mean), _TYPES[kind], blocks, 16 if keys is None else keys.shape[1], heads, size)
-    c.key_stride[:], c.value_stride[:], c.mean_stride[:] = ks, vs, ms
+        m, ms, _ = _vectors(mean, "mean", 3, None if keys is None else kind, device)
+        if keys is None:
+            kind, shape = mean.dtype, (mean.shape[0], block, *mean.shape[1:])
+    c = _Cache.from_buffer_copy(_cache_layout(_TYPES[kind], tuple(shape), ks, vs, ms))
+    c.keys, c.values, c.mean = k, v, m
     return c, kind
 
 
 def comet_cache_map(add: torch.Tensor, length: torch.Tensor, held: torch.Tensor, table: torch.Tensor, spare: torch.Tensor, count: torch.Tensor, block: int, N: int,
                     ended: Optional[torch.Tensor] = None, stream=None):
     """(pos, slot, place) of the next tokens, add[b] of each request, N at most in all; length, held, table, spare and count are brought up to date."""
-    if not isinstance(length, torch.Tensor) or length.dim() != 1:
-        raise ValueError("length must have one dimension")
-    _dev(length, torch.int32, "length")
-    (B,), dev, N = length.shape, length.device, int(N)
+    B, S, dev, N = _numbers(length, "length"), _numbers(spare, "spare"), length.device, int(N)
     ptr, M, ldt = _table(table, B, dev)
-    _given(add, torch.int32, (B,), "add", dev)
-    _given(held, torch.int32, (B,), "held", dev)
-    ended = _bytes_of(ended, (B,), "ended", dev)
-    if not isinstance(spare, torch.Tensor) or spare.dim() != 1:
-        raise ValueError("spare must have one dimension")
-    _given(spare, torch.int32, tuple(spare.shape), "spare", dev)
-    _given(count, torch.int32, (1,), "count", dev)
-    if add is None or held is None or count is None:
-        raise ValueError("add, held and count are needed")
+    each = (B,)
+    args = (_needed(add, torch.int32, each, "add", dev), None if ended is None else _bytes_of(ended, each, "ended", dev).data_ptr(),
+            _needed(length, torch.int32, each, "length", dev), _needed(held, torch.int32, each, "held", dev), ptr, ldt, _needed(spare, torch.int32, (S,), "spare", dev), S,
+            _needed(count, torch.int32, (1,), "count", dev), N)
     need = _work_bytes("comet_cache_map", B, M, N)
     pos = _new(None, torch.int32, (B + 1,), "pos", dev, stream)
     slot = _new(None, torch.int64, (N,), "slot", dev, stream)
     place = _new(None, torch.int32, (N,), "place", dev, stream)
-    torch.autograd.graph.increment_version([length, held, table, spare, count])
+    torch.autograd.graph.increment_version((length, held, table, spare, count))
     work, wptr = _work(need, dev, stream)
-    _call("comet_cache_map", dev, stream, B, M, int(block), add.data_ptr(), _ptr(ended), length.data_ptr(), held.data_ptr(), ptr, ldt, spare.data_ptr(),
-          spare.shape[0], count.data_ptr(), N, pos.data_ptr(), slot.data_ptr(), place.data_ptr(), wptr, need)
+    _call("comet_cache_map", dev, stream, B, M, int(block), *args, pos.data_ptr(), slot.data_ptr(), place.data_ptr(), wptr, need)
     return pos, slot, place
 
 
@@ -813,32 +841,24 @@ def comet_cache_write(k: torch.Tensor, v: torch.Tensor, K: torch.Tensor, V: torc
         raise TypeError("K must be a torch tensor in device memory")
     dev = K.device
     cache, kind = _cache(K, V, mean, dev)
-    ks, vs = _vectors(k, "k", 3, kind, dev), _vectors(v, "v", 3, kind, dev)
-    N = k.shape[0]
-    if k.shape != (N, *K.shape[2:]) or v.shape != k.shape:
-        raise ValueError("k and v must have shape %s" % ((N, *K.shape[2:]),))
-    _given(slot, torch.int64, (N,), "slot", dev)
-    if slot is None:
-        raise ValueError("slot is missing")
-    torch.autograd.graph.increment_version([K, V] if mean is None else [K, V, mean])
-    _call("comet_cache_write", dev, stream, ctypes.byref(cache), N, k.data_ptr(), (ctypes.c_int64 * 2)(*ks), v.data_ptr(), (ctypes.c_int64 * 2)(*vs), slot.data_ptr())
+    (kptr, _, ks), (vptr, _, vs) = _vectors(k, "k", 3, kind, dev), _vectors(v, "v", 3, kind, dev)
+    N, heads, size = k.shape
+    if v.shape != k.shape or heads != cache.heads or size != cache.size:
+        raise ValueError("k and v must have shape [N, %d, %d]" % (cache.heads, cache.size))
+    slots = _needed(slot, torch.int64, (N,), "slot", dev)
+    torch.autograd.graph.increment_version((K, V) if mean is None else (K, V, mean))
+    _call("comet_cache_write", dev, stream, ctypes.byref(cache), N, kptr, ks, vptr, vs, slots)
 
 
 def _queries(q, cache, kind, table, pos, length, device):
     """What the two calls with queries share: (N, Q, B, M) and their arguments."""
-    qs = _vectors(q, "q", 3, kind, device)
+    qptr, _, qs = _vectors(q, "q", 3, kind, device)
     N, Q, size = q.shape
     if size != cache.size or Q % cache.heads:
         raise ValueError("q must have heads of %d elements, a multiple of %d of them" % (cache.size, cache.heads))
-    if not isinstance(length, torch.Tensor) or length.dim() != 1:
-        raise ValueError("length must have one dimension")
-    (B,) = length.shape
-    _given(length, torch.int32, (B,), "length", device)
-    _given(pos, torch.int32, (B + 1,), "pos", device)
-    if pos is None:
-        raise ValueError("pos is missing")
+    B = _numbers(length, "length")
     ptr, M, ldt = _table(table, B, device)
-    return (N, Q, B, M), (q.data_ptr(), (ctypes.c_int64 * 2)(*qs), B, pos.data_ptr(), length.data_ptr(), ptr, M, ldt)
+    return (N, Q, B, M), (qptr, qs, B, _needed(pos, torch.int32, (B + 1,), "pos", device), _needed(length, torch.int32, (B,), "length", device), ptr, M, ldt)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -853,14 +873,14 @@ def comet_block_select(q: torch.Tensor, mean: torch.Tensor, table: torch.Tensor,
     """sel, [N, heads, K]: the K blocks that each query token's heads are to read, ascending, -1 behind them where there are fewer."""
     if not isinstance(mean, torch.Tensor) or not mean.is_cuda:
         raise TypeError("mean must be a torch tensor in device memory")
-    dev, K = mean.device, int(K)
-    cache, kind = _cache(None, None, mean, dev)
-    cache.block = int(block)
+    dev, K, block = mean.device, int(K), int(block)
+    cache, kind = _cache(None, None, mean, dev, block)
     sizes, args = _queries(q, cache, kind, table, pos, length, dev)
-    need = _query_work("comet_block_select", cache.type, cache.block, cache.heads, cache.size, *sizes, K)
-    sel = _new(sel, torch.int32, (sizes[0], cache.heads, K), "sel", dev, stream)
+    heads = cache.heads
+    need = _query_work("comet_block_select", cache.type, block, heads, cache.size, *sizes, K)
+    sel = _new(sel, torch.int32, (sizes[0], heads, K), "sel", dev, stream)
     work, wptr = _work(need, dev, stream)
-    _call("comet_block_select", dev, stream, ctypes.byref(cache), *sizes[:2], *args, K, int(first), int(last), sel.data_ptr(), wptr, need)
+    _call("comet_block_select", dev, stream, ctypes.byref(cache), sizes[0], sizes[1], *args, K, int(first), int(last), sel.data_ptr(), wptr, need)
     return sel
 
 
@@ -872,17 +892,17 @@ def comet_block_attend(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, table:
     dev = K.device
     cache, kind = _cache(K, V, None, dev)
     sizes, args = _queries(q, cache, kind, table, pos, length, dev)
-    N, Q = sizes[:2]
+    N, Q, heads, size = sizes[0], sizes[1], cache.heads, cache.size
     if not isinstance(sel, torch.Tensor) or sel.dim() != 3:
         raise ValueError("sel must have three dimensions")
     chosen = sel.shape[2]
-    _given(sel, torch.int32, (N, cache.heads, chosen), "sel", dev)
-    need = _query_work("comet_block_attend", cache.type, cache.block, cache.heads, cache.size, *sizes, chosen)
-    out = _new(out, kind, (N, Q, cache.size), "out", dev, stream)
+    sptr = _needed(sel, torch.int32, (N, heads, chosen), "sel", dev)
+    need = _query_work("comet_block_attend", cache.type, cache.block, heads, size, *sizes, chosen)
+    out = _new(out, kind, (N, Q, size), "out", dev, stream)
     lse = _new(lse, torch.float32, (N, Q), "lse", dev, stream)
     work, wptr = _work(need, dev, stream)
-    _call("comet_block_attend", dev, stream, ctypes.byref(cache), N, Q, *args, sel.data_ptr(), chosen, float(cache.size ** -0.5 if scale is None else scale),
-          out.data_ptr(), lse.data_ptr(), wptr, need)
+    _call("comet_block_attend", dev, stream, ctypes.byref(cache), N, Q, *args, sptr, chosen, size ** -0.5 if scale is None else float(scale), out.data_ptr(),
+          lse.data_ptr(), wptr, need)
     return out, lse
 
 
@@ -891,16 +911,13 @@ def comet_draft_verify(Z: torch.Tensor, token: torch.Tensor, pos: torch.Tensor, 
     """(accepted, next), each [B]: how many of each request's drafted tokens are taken, and the token behind them.  The draft's distribution: logits
     `draft`, or entries (crd, vals), or neither.  scale: a number, or a float32 tensor with one for each request.  length is brought up to date."""
     ptr, kind, N, V, ld = _rows(Z)
-    dev = Z.device
-    if not isinstance(pos, torch.Tensor) or pos.dim() != 1 or pos.shape[0] < 1:
-        raise ValueError("pos must have one dimension")
-    B = pos.shape[0] - 1
-    for t, dtype, shape, what in ((pos, torch.int32, (B + 1,), "pos"), (token, torch.int32, (N,), "token"), (u, torch.float32, (N,), "u"), (v, torch.float32, (B,), "v")):
-        if t is None:
-            raise ValueError("%s is missing" % what)
-        _given(t, dtype, shape, what, dev)
-    _given(length, torch.int32, (B,), "length", dev)
-    dptr, dkind, ldd, K, scales = None, COMET_F32, V, 0, None
+    dev, B = Z.device, _numbers(pos, "pos") - 1
+    if B < 0:
+        raise ValueError("pos must have at least one element")
+    each, rows = (B,), (N,)
+    at = (_needed(pos, torch.int32, (B + 1,), "pos", dev), _needed(token, torch.int32, rows, "token", dev), _needed(u, torch.float32, rows, "u", dev),
+          _needed(v, torch.float32, each, "v", dev))
+    dptr, dkind, ldd, K, cptr, tptr, scales = None, COMET_F32, V, 0, None, None, None
     if draft is not None:
         if crd is not None or vals is not None:
             raise ValueError("either draft or crd and vals")
@@ -911,16 +928,17 @@ def comet_draft_verify(Z: torch.Tensor, token: torch.Tensor, pos: torch.Tensor, 
         if not isinstance(crd, torch.Tensor) or crd.dim() != 2 or vals is None:
             raise ValueError("crd and vals must both be [N, K] matrices")
         K = crd.shape[1]
-        _given(crd, torch.int32, (N, K), "crd", dev)
-        _given(vals, torch.float32, (N, K), "vals", dev)
+        cptr, tptr = _needed(crd, torch.int32, (N, K), "crd", dev), _needed(vals, torch.float32, (N, K), "vals", dev)
     if isinstance(scale, torch.Tensor):
-        scales, scale = _given(scale, torch.float32, (B,), "scale", dev), 1.0
+        scales, scale = _needed(scale, torch.float32, each, "scale", dev), 1.0
     need = _work_bytes("comet_draft_verify", kind, N, V, B, K, 1 if draft is not None else 0)
-    accepted = _new(None, torch.int32, (B,), "accepted", dev, stream)
-    follow = _new(None, torch.int32, (B,), "next", dev, stream)
+    accepted = _new(None, torch.int32, each, "accepted", dev, stream)
+    follow = _new(None, torch.int32, each, "next", dev, stream)
+    lptr = None
     if length is not None:
+        lptr = _given(length, torch.int32, each, "length", dev).data_ptr()
         torch.autograd.graph.increment_version(length)
     work, wptr = _work(need, dev, stream)
-    _call("comet_draft_verify", dev, stream, ptr, kind, N, V, ld, B, pos.data_ptr(), token.data_ptr(), u.data_ptr(), v.data_ptr(), dptr, dkind, ldd, _ptr(crd),
-          _ptr(vals), K, float(scale), _ptr(scales), accepted.data_ptr(), follow.data_ptr(), _ptr(length), wptr, need)
+    _call("comet_draft_verify", dev, stream, ptr, kind, N, V, ld, B, *at, dptr, dkind, ldd, cptr, tptr, K, float(scale), scales, accepted.data_ptr(),
+          follow.data_ptr(), lptr, wptr, need)
     return accepted, follow
