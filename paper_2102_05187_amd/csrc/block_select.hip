@@ -12,87 +12,207 @@ struct SelectArgs {
     int block, heads, size, group;
     int K, first, last;
     int32_t *sel;
+    int tokens, candidates;                  // tokens of a workgroup at most; room for a token's keys
 };
 
-constexpr int kSelect = 256;
 constexpr uint64_t kAlways = ~0ull;          // above the order of every double
+constexpr int kHeld = 16;                    // candidates of a lane, where a wavefront chooses
 
-// One workgroup a token and head.  Scores in 64 bits: products of 16-bit elements are exact there, and a sum of a few hundred of
-// them is off by 1e-14, so that it is the exact scores' order that decides.
-template <int TYPE>
-__global__ void __launch_bounds__(kSelect) k_select_one(SelectArgs a) {
-    using E = Elem<TYPE>;
-    extern __shared__ __align__(16) char raw[];
-    uint64_t *key = (uint64_t *)raw;
-    __shared__ double q[256];
-    __shared__ int count[64 + 1];
-    __shared__ int64_t scan[kSelect / kWave];
-    const int64_t n = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
-    const int64_t b = request_of<kSelect>(a.q.pos, a.q.B, n, count);
-    if (b < 0) return;
-    int32_t *sel = a.sel + (n * a.heads + h) * a.K;
-    const int64_t place = a.q.length[b] - ((int64_t)a.q.pos[b + 1] - n);
-    const int64_t seen = place < 0 ? 0 : place / a.block + 1;
-    const int C = (int)(seen < a.q.M ? seen : a.q.M);
-    if (C <= a.K) {
-        for (int i = threadIdx.x; i < a.K; i += kSelect) sel[i] = i < C ? i : -1;
-        return;
+struct Choice { int32_t *sel; int C; };      // where a token's blocks go, and how many it sees
+
+// What a token sees, of which it takes the K with the largest keys, equal ones by their number: by a wavefront, the keys in registers.
+// The K-th largest is found bit by bit, from the highest on, until as many as are wanted reach it.
+__device__ __forceinline__ void choose_held(const uint64_t *key, const Choice &t, int K) {
+    const int lane = threadIdx.x & (kWave - 1);
+    uint64_t x[kHeld];
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+        x[r] = 0;
+        if (r * kWave + lane < t.C) x[r] = key[r * kWave + lane];
     }
-    for (int d = threadIdx.x; d < a.size; d += kSelect) {
-        double s = 0;
-        for (int g = 0; g < a.group; ++g) s += (double)E::one(((const typename E::T *)a.q.q)[n * a.q.row + (h * a.group + g) * a.q.head + d]);
-        q[d] = s;
+    const auto there = [&](int r) { return r * kWave + lane < t.C; };
+    uint64_t bar = 0;
+    int reach = t.C;
+    for (int bit = 63; bit >= 0 && reach != K; --bit) {
+        const uint64_t y = bar | 1ull << bit;
+        int n = 0;
+#pragma unroll
+        for (int r = 0; r < kHeld; ++r)
+            if (r * kWave < t.C) n += __builtin_popcountll(__ballot(x[r] >= y));
+        if (n >= K) bar = y, reach = n;
     }
+    int over = 0;
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r)
+        if (r * kWave < t.C) over += __builtin_popcountll(__ballot(there(r) && x[r] > bar));
+    const uint64_t below = (1ull << lane) - 1;
+    int at = 0, equal = K - over;                        // of those at the bar, the lowest
+#pragma unroll
+    for (int r = 0; r < kHeld; ++r) {
+        if (r * kWave >= t.C) break;
+        const uint64_t ties = __ballot(there(r) && x[r] == bar);
+        const bool in = there(r) && (x[r] > bar || (x[r] == bar && __builtin_popcountll(ties & below) < equal));
+        const uint64_t taken = __ballot(in);
+        if (in) t.sel[at + __builtin_popcountll(taken & below)] = r * kWave + lane;
+        at += __builtin_popcountll(taken);
+        const int n = __builtin_popcountll(ties);
+        equal -= n < equal ? n : equal;
+    }
+}
+
+// The same by a workgroup of T threads, the keys in LDS.
+template <int T> __device__ __forceinline__ void choose_all(const uint64_t *key, const Choice &t, int K, int *count, int64_t *scan) {
     if (threadIdx.x < 65) count[threadIdx.x] = 0;
     __syncthreads();
-    const int32_t *table = a.q.table + b * a.q.ldt;
-    for (int j = threadIdx.x; j < C; j += kSelect) {
-        uint64_t k = kAlways;
-        if (j >= a.first && j < C - a.last) {
-            const int64_t p = table[j];
-            k = 0;
-            if (p >= 0 && p < a.blocks) {
-                const typename E::T *m = (const typename E::T *)a.mean + p * a.mean_block + h * a.mean_head;
-                double s = 0;
-                for (int d = 0; d < a.size; d += E::kPer) {
-                    float f[E::kPer];
-                    E::widen(*(const uint4 *)(m + d), f);
-#pragma unroll
-                    for (int e = 0; e < E::kPer; ++e) s = __builtin_fma(q[d + e], (double)f[e], s);
-                }
-                k = order_of_double(s);
-            }
-        }
-        key[j] = k;
-    }
-    __syncthreads();
-    // the K-th largest key: bits from the highest on, each kept where K keys reach it
     uint64_t bar = 0;
     for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t t = bar | 1ull << bit;
+        const uint64_t y = bar | 1ull << bit;
         int c = 0;
-        for (int j = threadIdx.x; j < C; j += kSelect) c += key[j] >= t ? 1 : 0;
+        for (int j = threadIdx.x; j < t.C; j += T) c += key[j] >= y ? 1 : 0;
         if (c) atomicAdd(&count[bit], c);
         __syncthreads();
-        if (count[bit] >= a.K) bar = t;
-        if (count[bit] == a.K) break;
+        if (count[bit] >= K) bar = y;
+        if (count[bit] == K) break;
     }
     int more = 0;
-    for (int j = threadIdx.x; j < C; j += kSelect) more += key[j] > bar ? 1 : 0;
+    for (int j = threadIdx.x; j < t.C; j += T) more += key[j] > bar ? 1 : 0;
     if (more) atomicAdd(&count[64], more);
     __syncthreads();
-    const int equal = a.K - count[64];                       // of those that are at the bar, the lowest j
+    const int equal = K - count[64];
     int64_t before = 0, ties = 0, all;
-    for (int j0 = 0; j0 < C; j0 += kSelect) {
+    for (int j0 = 0; j0 < t.C; j0 += T) {
         const int j = j0 + threadIdx.x;
-        const uint64_t k = j < C ? key[j] : 0;
-        const int64_t tie = ties + block_scan<kSelect>(j < C && k == bar ? 1 : 0, scan, all);
+        const uint64_t k = j < t.C ? key[j] : 0;
+        const int64_t tie = ties + block_scan<T>(j < t.C && k == bar ? 1 : 0, scan, all);
         ties += all;
-        const bool in = j < C && (k > bar || (k == bar && tie <= equal));
-        const int64_t at = before + block_scan<kSelect>(in ? 1 : 0, scan, all);
+        const bool in = j < t.C && (k > bar || (k == bar && tie <= equal));
+        const int64_t at = before + block_scan<T>(in ? 1 : 0, scan, all);
         before += all;
-        if (in) sel[at - 1] = j;
+        if (in) t.sel[at - 1] = j;
     }
+}
+
+typedef double D4 __attribute__((ext_vector_type(4)));
+
+// One workgroup a head and TOKENS tokens of a request that follow each other.  Scores in 64 bits: products of 16-bit elements are exact there, and a sum
+// of a few hundred of them is off by 1e-14, so that it is the exact scores' order that decides.  Sixteen blocks at a time, a lane a block and a quarter
+// of its 16-byte pieces: the fragment of a 64-bit matrix instruction whose columns are 16 tokens' sums over their heads; a single token's
+// products are added up by the lanes themselves, which takes half the time.
+template <int TYPE, int WIDE, int TOKENS, int WAVES>
+__global__ void __launch_bounds__(WAVES * kWave) k_select(SelectArgs a) {
+    using E = Elem<TYPE>;
+    using T = typename E::T;
+    constexpr int THREADS = WAVES * kWave, CH = E::kPer, NK = WIDE / (4 * CH);
+    extern __shared__ __align__(16) uint64_t keys[];
+    __shared__ int64_t buf[WAVES], where[2];
+    __shared__ int count[65];
+    const int tile = (int)(blockIdx.x / (unsigned)a.heads), h = (int)(blockIdx.x - (unsigned)tile * a.heads);
+    const Tile t = find_tile<THREADS>(a.q, a.tokens, tile, buf, where);
+    if (t.n == 0) return;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, col = lane & 15, g = lane >> 4;
+    const auto seen = [&](int i) {
+        const int64_t place = t.place + i, c = place < 0 ? 0 : (int64_t)((uint32_t)place / (uint32_t)a.block) + 1;
+        return (int)(c < a.q.M ? c : a.q.M);
+    };
+    const auto choice = [&](int i) { return Choice{a.sel + ((t.first + i) * a.heads + h) * a.K, seen(i)}; };
+    const int most = seen(t.n - 1), stride = a.candidates;
+    const bool scored = most > a.K;                                // else there is nothing to choose
+    if (scored) {
+        const int32_t *table = a.q.table + t.b * a.q.ldt;
+        double q[NK][CH];
+        const int token = TOKENS == 1 || col >= t.n ? 0 : col;
+        const T *from = (const T *)a.q.q + (t.first + token) * a.q.row + (int64_t)h * a.group * a.q.head;
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+#pragma unroll
+            for (int e = 0; e < CH; ++e) q[k][e] = 0;
+            const int d = (4 * k + g) * CH;
+            if (d < a.size)
+                for (int x = 0; x < a.group; ++x) {
+                    float f[CH];
+                    E::widen(*(const uint4 *)(from + x * a.q.head + d), f);
+#pragma unroll
+                    for (int e = 0; e < CH; ++e) q[k][e] += (double)f[e];
+                }
+        }
+        for (int j0 = wave * 16; j0 < most; j0 += THREADS / 4) {
+            const int j = j0 + col;
+            const int64_t p = j < most ? table[j] : -1;
+            const bool real = p >= 0 && p < a.blocks;
+            const T *m = (const T *)a.mean + (real ? p : 0) * a.mean_block + h * a.mean_head;
+            uint4 v[NK];
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                const int d = (4 * k + g) * CH;
+                v[k] = make_uint4(0, 0, 0, 0);
+                if (real && d < a.size) v[k] = *(const uint4 *)(m + d);
+            }
+            // a block's key for a token; blocks of the table that are none have NaN's
+            const auto put = [&](int i, int block, double s, bool is) {
+                if (i < t.n && block < most) {
+                    const int C = seen(i);
+                    keys[i * stride + block] = block < a.first || block >= C - a.last ? kAlways : is ? order_of_double(s) : 0;
+                }
+            };
+            if constexpr (TOKENS == 1) {
+                double s = 0;
+#pragma unroll
+                for (int k = 0; k < NK; ++k) {
+                    float f[CH];
+                    E::widen(v[k], f);
+#pragma unroll
+                    for (int e = 0; e < CH; ++e) s = __builtin_fma(q[k][e], (double)f[e], s);
+                }
+                s += __shfl_xor(s, 16);
+                s += __shfl_xor(s, 32);
+                if (g == 0) put(0, j, s, real);
+            } else {
+                D4 s = {0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < NK; ++k) {
+                    if (4 * k * CH >= a.size) continue;
+                    float f[CH];
+                    E::widen(v[k], f);
+#pragma unroll
+                    for (int e = 0; e < CH; ++e) s = __builtin_amdgcn_mfma_f64_16x16x4f64((double)f[e], q[k][e], s, 0, 0, 0);
+                }
+                const uint32_t is = (uint32_t)(__ballot(real) & 0xffff);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) put(col, j0 + 4 * r + g, s[r], is >> (4 * r + g) & 1);
+            }
+        }
+        __syncthreads();
+    }
+    for (int i = TOKENS == 1 ? 0 : wave; i < t.n; i += TOKENS == 1 ? 1 : WAVES) {
+        const Choice c = choice(i);
+        if (c.C <= a.K) {
+            for (int k = TOKENS == 1 ? threadIdx.x : lane; k < a.K; k += TOKENS == 1 ? THREADS : kWave) c.sel[k] = k < c.C ? k : -1;
+        } else if (TOKENS > 1 || a.q.M <= kHeld * kWave) {
+            if (TOKENS > 1 || wave == 0) choose_held(keys + i * stride, c, a.K);
+        } else if constexpr (TOKENS == 1) {
+            choose_all<THREADS>(keys, c, a.K, count, buf);
+        }
+    }
+}
+
+template <int TYPE, int WIDE> hipError_t launch(SelectArgs a, hipStream_t st) {
+    // Sixteen tokens share their blocks' means where requests have as many, and a wavefront's registers hold a token's candidates.
+    const int64_t B = a.q.B < a.q.N ? a.q.B : a.q.N, each = (a.q.N + B - 1) / B;
+    const bool many = each >= 4 && a.q.M <= kHeld * kWave;
+    const auto kernel = many ? k_select<TYPE, WIDE, 16, 4> : k_select<TYPE, WIDE, 1, 8>;
+    a.tokens = many ? 16 : 1;
+    int64_t tiles = a.q.N / a.tokens + B;
+    if (tiles > a.q.N) tiles = a.q.N;
+    const size_t lds = (size_t)a.candidates * 8 * a.tokens;
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * a.heads)), dim3(many ? 256 : 512), lds, st, a);
+    return hipGetLastError();
+}
+template <int TYPE> hipError_t launch(const SelectArgs &a, hipStream_t st) {
+    return a.size <= 64 ? launch<TYPE, 64>(a, st) : a.size <= 128 ? launch<TYPE, 128>(a, st) : launch<TYPE, 256>(a, st);
 }
 
 }  // namespace
@@ -100,17 +220,10 @@ __global__ void __launch_bounds__(kSelect) k_select_one(SelectArgs a) {
 int64_t block_select_work(const comet_cache &, int64_t, int64_t, int64_t, int64_t, int64_t) { return 0; }
 
 hipError_t block_select(const comet_cache &c, const Queries &q, int64_t K, int64_t first, int64_t last, int32_t *sel, void *, hipStream_t st) {
+    // a token's keys lie 16 bytes off those of the one before it: 16 tokens' writes meet in few banks
     const SelectArgs a{q, c.mean, c.blocks, c.mean_stride[0], c.mean_stride[1], (int)c.block, (int)c.heads, (int)c.size, (int)(q.Q / c.heads),
-                       (int)K, (int)first, (int)last, sel};
-    const dim3 grid((unsigned)(q.N * c.heads));
-    const size_t lds = (size_t)q.M * 8;
-    const auto kernel = c.type == COMET_F32 ? k_select_one<COMET_F32> : c.type == COMET_BF16 ? k_select_one<COMET_BF16> : k_select_one<COMET_F16>;
-    if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL(kernel, grid, dim3(kSelect), lds, st, a);
-    return hipGetLastError();
+                       (int)K, (int)first, (int)last, sel, 0, (int)((q.M + 15) / 16 * 16 + 2)};
+    return c.type == COMET_F32 ? launch<COMET_F32>(a, st) : c.type == COMET_BF16 ? launch<COMET_BF16>(a, st) : launch<COMET_F16>(a, st);
 }
 
 }  // namespace comet

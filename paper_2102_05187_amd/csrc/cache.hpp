@@ -81,6 +81,71 @@ template <int T> __device__ __forceinline__ int64_t request_of(const int32_t *po
     return b < B && row >= pos[b] ? b : -1;
 }
 
+// Which tokens a workgroup has, and the first one's place in its request.
+struct Tile { int64_t b, first; int n; int64_t place; };
+
+// The sum over the lanes up to and with each.
+__device__ __forceinline__ int lanes_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
+// Tile `tile` of those that cut every request's tokens into pieces of `tokens`; n = 0 where there are not as many.
+template <int T> __device__ __forceinline__ Tile find_tile(const Queries &q, int tokens, int tile, int64_t *buf, int64_t *where) {
+    Tile t{0, 0, 0, 0};
+    const auto cut = [&](int64_t b, int begin, int end, int length, int number) {
+        const int n = end - begin, i = number * tokens;
+        t.b = b, t.first = (int64_t)begin + i, t.n = n - i < tokens ? n - i : tokens, t.place = (int64_t)length - n + i;
+        if (t.first + t.n > q.N) t.n = t.first < q.N ? (int)(q.N - t.first) : 0;
+    };
+    if (q.B <= 4 * kWave) {
+        // every wavefront by itself: a request a lane, all that is needed of it with one wait
+        const int lane = threadIdx.x & (kWave - 1);
+        int begin[4], end[4], length[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = i * kWave + lane;
+            begin[i] = end[i] = length[i] = 0;
+            if (b < q.B) begin[i] = q.pos[b], end[i] = q.pos[b + 1], length[i] = q.length[b];
+        }
+        int before = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i * kWave >= q.B) break;
+            const int mine = end[i] > begin[i] ? (end[i] - begin[i] + tokens - 1) / tokens : 0, upto = before + lanes_scan(mine);
+            const uint64_t hit = __ballot(tile < upto);
+            if (hit) {
+                const int l = __builtin_ctzll(hit);
+                cut(i * kWave + l, __builtin_amdgcn_readlane(begin[i], l), __builtin_amdgcn_readlane(end[i], l), __builtin_amdgcn_readlane(length[i], l),
+                    tile - __builtin_amdgcn_readlane(upto - mine, l));
+                return t;
+            }
+            before = __builtin_amdgcn_readlane(upto, kWave - 1);
+        }
+        return t;
+    }
+    if (threadIdx.x == 0) where[0] = -1;
+    const int64_t each = (q.B + T - 1) / T, b0 = threadIdx.x * each, b1 = b0 + each < q.B ? b0 + each : q.B;
+    int64_t mine = 0, total;
+    const auto pieces = [&](int64_t b) { return q.pos[b + 1] > q.pos[b] ? (q.pos[b + 1] - q.pos[b] + tokens - 1) / tokens : 0; };
+    for (int64_t b = b0; b < b1; ++b) mine += pieces(b);
+    const int64_t upto = block_scan<T>(mine, buf, total);
+    if (tile >= upto - mine && tile < upto) {
+        int64_t left = tile - (upto - mine), b = b0;
+        for (; left >= pieces(b); ++b) left -= pieces(b);
+        where[0] = b, where[1] = left;
+    }
+    __syncthreads();
+    const int64_t b = where[0];
+    if (b >= 0) cut(b, q.pos[b], q.pos[b + 1], q.length[b], (int)where[1]);
+    return t;
+}
+
 // An unsigned number whose order is that of the double: NaN is lowest, -0 is 0.
 __device__ __forceinline__ uint64_t order_of_double(double x) {
     if (x != x) return 0;

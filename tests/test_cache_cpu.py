@@ -34,7 +34,7 @@ def cache_map(lib, B=2, M=4, block=16, add=P, ended=None, length=P, held=P, tabl
 
 def test_map(lib):
     need = ctypes.c_int64(-1)
-    assert lib.comet_cache_map_work(2, 4, 5, ctypes.byref(need)) == OK and need.value > 0
+    assert lib.comet_cache_map_work(2, 4, 5000, ctypes.byref(need)) == OK and need.value > 0
     assert lib.comet_cache_map_work(2, 4, 5, None) == INVALID
     for kw, status in ((dict(B=-1), INVALID), (dict(M=-1), INVALID), (dict(N=-1), INVALID), (dict(S=-1), INVALID), (dict(block=0), INVALID), (dict(block=1025), UNSUPPORTED),
                        (dict(ldt=3), SHAPE), (dict(ldt=1 << 41), UNSUPPORTED), (dict(B=(1 << 20) + 1), UNSUPPORTED), (dict(M=1 << 31, ldt=1 << 31), UNSUPPORTED),
@@ -42,7 +42,7 @@ def test_map(lib):
                        (dict(B=1 << 20, M=1 << 20, ldt=1 << 20), UNSUPPORTED), (dict(add=None), INVALID), (dict(length=None), INVALID), (dict(held=None), INVALID),
                        (dict(table=None), INVALID), (dict(spare=None), INVALID), (dict(count=None), INVALID), (dict(pos=None), INVALID), (dict(slot=None), INVALID),
                        (dict(place=None), INVALID), (dict(add=ODD4), INVALID), (dict(slot=ctypes.c_void_p(4100)), INVALID), (dict(table=ODD4), INVALID),
-                       (dict(work=None), INVALID), (dict(size=need.value - 1), INVALID), (dict(work=ctypes.c_void_p(4104)), INVALID)):
+                       (dict(N=5000, work=None), INVALID), (dict(N=5000, size=need.value - 1), INVALID), (dict(N=5000, work=ctypes.c_void_p(4104)), INVALID)):
         assert cache_map(lib, **kw) == status, kw
 
 
