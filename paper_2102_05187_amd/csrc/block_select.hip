@@ -20,36 +20,44 @@ constexpr int kHeld = 16;                    // candidates of a lane, where a wa
 
 struct Choice { int32_t *sel; int C; };      // where a token's blocks go, and how many it sees
 
-// What a token sees, of which it takes the K with the largest keys, equal ones by their number: by a wavefront, the keys in registers.
-// The K-th largest is found bit by bit, from the highest on, until as many as are wanted reach it.
-__device__ __forceinline__ void choose_held(const uint64_t *key, const Choice &t, int K) {
+// What a token sees, of which it takes the K with the largest keys, equal ones by their number: by a wavefront, the keys in registers, HELD a lane.
+// The K-th largest is found bit by bit, from the highest on, until as many as are wanted reach it: about 25 bits, of which the upper 32 are
+// compared by themselves.  One count is a few instructions a register; the number of registers is fixed so that there is nothing else.
+template <int HELD> __device__ __forceinline__ void choose_held(const uint64_t *key, const Choice &t, int K) {
     const int lane = threadIdx.x & (kWave - 1);
-    uint64_t x[kHeld];
+    uint64_t x[HELD];
+    uint32_t high[HELD];
 #pragma unroll
-    for (int r = 0; r < kHeld; ++r) {
+    for (int r = 0; r < HELD; ++r) {
         x[r] = 0;
         if (r * kWave + lane < t.C) x[r] = key[r * kWave + lane];
+        high[r] = (uint32_t)(x[r] >> 32);
     }
     const auto there = [&](int r) { return r * kWave + lane < t.C; };
-    uint64_t bar = 0;
+    uint32_t bar_high = 0, bar_low = 0;
     int reach = t.C;
-    for (int bit = 63; bit >= 0 && reach != K; --bit) {
-        const uint64_t y = bar | 1ull << bit;
+    for (int bit = 31; bit >= 0 && reach != K; --bit) {
+        const uint32_t y = bar_high | 1u << bit;
         int n = 0;
 #pragma unroll
-        for (int r = 0; r < kHeld; ++r)
-            if (r * kWave < t.C) n += __builtin_popcountll(__ballot(x[r] >= y));
-        if (n >= K) bar = y, reach = n;
+        for (int r = 0; r < HELD; ++r) n += __builtin_popcountll(__ballot(high[r] >= y));
+        if (n >= K) bar_high = y, reach = n;
     }
+    for (int bit = 31; bit >= 0 && reach != K; --bit) {
+        const uint64_t y = (uint64_t)bar_high << 32 | bar_low | 1u << bit;
+        int n = 0;
+#pragma unroll
+        for (int r = 0; r < HELD; ++r) n += __builtin_popcountll(__ballot(x[r] >= y));
+        if (n >= K) bar_low |= 1u << bit, reach = n;
+    }
+    const uint64_t bar = (uint64_t)bar_high << 32 | bar_low;
     int over = 0;
 #pragma unroll
-    for (int r = 0; r < kHeld; ++r)
-        if (r * kWave < t.C) over += __builtin_popcountll(__ballot(there(r) && x[r] > bar));
+    for (int r = 0; r < HELD; ++r) over += __builtin_popcountll(__ballot(there(r) && x[r] > bar));
     const uint64_t below = (1ull << lane) - 1;
     int at = 0, equal = K - over;                        // of those at the bar, the lowest
 #pragma unroll
-    for (int r = 0; r < kHeld; ++r) {
-        if (r * kWave >= t.C) break;
+    for (int r = 0; r < HELD; ++r) {
         const uint64_t ties = __ballot(there(r) && x[r] == bar);
         const bool in = there(r) && (x[r] > bar || (x[r] == bar && __builtin_popcountll(ties & below) < equal));
         const uint64_t taken = __ballot(in);
@@ -58,6 +66,12 @@ __device__ __forceinline__ void choose_held(const uint64_t *key, const Choice &t
         const int n = __builtin_popcountll(ties);
         equal -= n < equal ? n : equal;
     }
+}
+__device__ __forceinline__ void choose_held(const uint64_t *key, const Choice &t, int K) {
+    if (t.C <= 2 * kWave) choose_held<2>(key, t, K);
+    else if (t.C <= 4 * kWave) choose_held<4>(key, t, K);
+    else if (t.C <= 8 * kWave) choose_held<8>(key, t, K);
+    else choose_held<kHeld>(key, t, K);
 }
 
 // The same by a workgroup of T threads, the keys in LDS.
@@ -119,53 +133,73 @@ __global__ void __launch_bounds__(WAVES * kWave) k_select(SelectArgs a) {
     const bool scored = most > a.K;                                // else there is nothing to choose
     if (scored) {
         const int32_t *table = a.q.table + t.b * a.q.ldt;
-        double q[NK][CH];
-        const int token = TOKENS == 1 || col >= t.n ? 0 : col;
-        const T *from = (const T *)a.q.q + (t.first + token) * a.q.row + (int64_t)h * a.group * a.q.head;
-#pragma unroll
-        for (int k = 0; k < NK; ++k) {
-#pragma unroll
-            for (int e = 0; e < CH; ++e) q[k][e] = 0;
-            const int d = (4 * k + g) * CH;
-            if (d < a.size)
-                for (int x = 0; x < a.group; ++x) {
+        // the heads' sums, a thread a token and 16-byte piece, to where each lane finds its own
+        constexpr int PIECES = 4 * NK, LINE = WIDE + 2;
+        double *const sums = (double *)(keys + TOKENS * stride);
+        for (int x = threadIdx.x; x < TOKENS * PIECES; x += THREADS) {
+            const int i = x / PIECES, d = x % PIECES * CH;
+            double s[CH] = {};
+            if (i < t.n && d < a.size) {
+                const T *from = (const T *)a.q.q + (t.first + i) * a.q.row + (int64_t)h * a.group * a.q.head + d;
+#pragma unroll 4
+                for (int y = 0; y < a.group; ++y) {
                     float f[CH];
-                    E::widen(*(const uint4 *)(from + x * a.q.head + d), f);
+                    E::widen(*(const uint4 *)(from + y * a.q.head), f);
 #pragma unroll
-                    for (int e = 0; e < CH; ++e) q[k][e] += (double)f[e];
+                    for (int e = 0; e < CH; ++e) s[e] += (double)f[e];
                 }
+            }
+#pragma unroll
+            for (int e = 0; e < CH; ++e) sums[i * LINE + d + e] = s[e];
         }
-        for (int j0 = wave * 16; j0 < most; j0 += THREADS / 4) {
-            const int j = j0 + col;
-            const int64_t p = j < most ? table[j] : -1;
-            const bool real = p >= 0 && p < a.blocks;
-            const T *m = (const T *)a.mean + (real ? p : 0) * a.mean_block + h * a.mean_head;
-            uint4 v[NK];
+        __syncthreads();
+        double q[NK][CH];
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int e = 0; e < CH; ++e) q[k][e] = sums[(TOKENS == 1 ? 0 : col) * LINE + (4 * k + g) * CH + e];
+        const int mine = TOKENS == 1 ? most : col < t.n ? seen(col) : 0;          // blocks that the lane's token sees
+        // A step's numbers of the table are asked for while the steps before it are computed; where a wavefront has the SIMD to itself, its means too.
+        constexpr int STEP = THREADS / 4;
+        const auto number = [&](int j0) {
+            int p = -1;
+            if (j0 + col < most) p = table[j0 + col];
+            return p >= 0 && p < a.blocks ? p : -1;
+        };
+        const auto read = [&](int p, uint4 (&v)[NK]) {
+            const T *m = (const T *)a.mean + (int64_t)(p < 0 ? 0 : p) * a.mean_block + h * a.mean_head;
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
                 const int d = (4 * k + g) * CH;
                 v[k] = make_uint4(0, 0, 0, 0);
-                if (real && d < a.size) v[k] = *(const uint4 *)(m + d);
+                if (p >= 0 && d < a.size) v[k] = *(const uint4 *)(m + d);
             }
-            // a block's key for a token; blocks of the table that are none have NaN's
-            const auto put = [&](int i, int block, double s, bool is) {
-                if (i < t.n && block < most) {
-                    const int C = seen(i);
-                    keys[i * stride + block] = block < a.first || block >= C - a.last ? kAlways : is ? order_of_double(s) : 0;
-                }
-            };
+        };
+        // a block's key for a token; blocks of the table that are none have NaN's
+        const auto put = [&](int i, int block, double s, bool is) {
+            if (block < mine) keys[i * stride + block] = block < a.first || block >= mine - a.last ? kAlways : is ? order_of_double(s) : 0;
+        };
+        int now = number(wave * 16), then = number(wave * 16 + STEP);
+        uint4 v[NK];
+        if (TOKENS == 1) read(now, v);
+        for (int j0 = wave * 16; j0 < most; j0 += STEP) {
+            const int later = number(j0 + 2 * STEP);
+            uint4 w[NK];
+            if (TOKENS == 1) read(then, w);
+            else read(now, v);
             if constexpr (TOKENS == 1) {
-                double s = 0;
+                double s = 0, s2 = 0;
 #pragma unroll
                 for (int k = 0; k < NK; ++k) {
                     float f[CH];
                     E::widen(v[k], f);
 #pragma unroll
-                    for (int e = 0; e < CH; ++e) s = __builtin_fma(q[k][e], (double)f[e], s);
+                    for (int e = 0; e < CH; e += 2) s = __builtin_fma(q[k][e], (double)f[e], s), s2 = __builtin_fma(q[k][e + 1], (double)f[e + 1], s2);
                 }
+                s += s2;
                 s += __shfl_xor(s, 16);
                 s += __shfl_xor(s, 32);
-                if (g == 0) put(0, j, s, real);
+                if (g == 0) put(0, j0 + col, s, now >= 0);
             } else {
                 D4 s = {0, 0, 0, 0};
 #pragma unroll
@@ -176,10 +210,14 @@ __global__ void __launch_bounds__(WAVES * kWave) k_select(SelectArgs a) {
 #pragma unroll
                     for (int e = 0; e < CH; ++e) s = __builtin_amdgcn_mfma_f64_16x16x4f64((double)f[e], q[k][e], s, 0, 0, 0);
                 }
-                const uint32_t is = (uint32_t)(__ballot(real) & 0xffff);
+                const uint32_t is = (uint32_t)(__ballot(now >= 0) & 0xffff);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) put(col, j0 + 4 * r + g, s[r], is >> (4 * r + g) & 1);
             }
+            now = then, then = later;
+            if (TOKENS == 1)
+#pragma unroll
+                for (int k = 0; k < NK; ++k) v[k] = w[k];
         }
         __syncthreads();
     }
@@ -203,7 +241,7 @@ template <int TYPE, int WIDE> hipError_t launch(SelectArgs a, hipStream_t st) {
     a.tokens = many ? 16 : 1;
     int64_t tiles = a.q.N / a.tokens + B;
     if (tiles > a.q.N) tiles = a.q.N;
-    const size_t lds = (size_t)a.candidates * 8 * a.tokens;
+    const size_t lds = (size_t)(a.candidates + WIDE + 2) * 8 * a.tokens;
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
