@@ -5,41 +5,81 @@ namespace comet {
 
 namespace {
 
+typedef uint32_t V4 __attribute__((ext_vector_type(4)));
+
 struct WriteArgs {
     const char *k, *v;
     char *keys, *values, *mean;
     int64_t N, slots;
     int block, heads, per_head;                  // per_head: 16-byte vectors of a head
     int64_t k_row, k_head, v_row, v_head;        // all in bytes
-    int64_t key_stride[3], value_stride[3], mean_stride[2];
+    int64_t key_block, key_place, key_head, value_block, value_place, value_head, mean_block, mean_head;
     const int64_t *slot;
 };
 
-constexpr int kWrite = 256;
+constexpr int kWrite = 256, kSlice = 32;      // threads of a workgroup; columns of one that takes means
 
-template <int TYPE>
-__global__ void __launch_bounds__(kWrite) k_cache_write(WriteArgs a, int rows) {
-    using E = Elem<TYPE>;
-    __shared__ float part[kWrite * E::kPer];
-    __shared__ int run;
-    const int columns = a.heads * a.per_head;
-    const int64_t i0 = (int64_t)blockIdx.x * rows;
-    const int64_t here = a.N - i0 < rows ? a.N - i0 : rows;
-    for (int64_t x = threadIdx.x; x < here * columns * 2; x += kWrite) {
-        const int64_t r = x / (2 * columns);
-        int c = (int)(x - r * 2 * columns);
-        const bool value = c >= columns;
-        if (value) c -= columns;
-        const int64_t s = a.slot[i0 + r];
-        if (s < 0 || s >= a.slots) continue;
-        const int64_t p = s / a.block, in = s - p * a.block, h = c / a.per_head, d = (int64_t)(c - h * a.per_head) * 16;
-        if (value) *(uint4 *)(a.values + p * a.value_stride[0] + in * a.value_stride[1] + h * a.value_stride[2] + d) = *(const uint4 *)(a.v + (i0 + r) * a.v_row + h * a.v_head + d);
-        else *(uint4 *)(a.keys + p * a.key_stride[0] + in * a.key_stride[1] + h * a.key_stride[2] + d) = *(const uint4 *)(a.k + (i0 + r) * a.k_row + h * a.k_head + d);
+// Block and place of a slot; false where it is none.  In 32 bits where the cache has fewer slots.
+template <class I> __device__ __forceinline__ bool find(const WriteArgs &a, int64_t s, int64_t &p, int &in) {
+    if (s < 0 || s >= a.slots) return false;
+    const I b = (I)s / (I)a.block;
+    p = b, in = (int)((I)s - b * (I)a.block);
+    return true;
+}
+
+// Rows i0 .. i0 + here - 1 to their slots: a thread a 16-byte column of the keys or the values, four rows under way.
+template <class I> __device__ __forceinline__ void copy_rows(const WriteArgs &a, int64_t i0, int here) {
+    const int columns = a.heads * a.per_head, both = 2 * columns;
+    const auto column = [&](int x, int r0, int step) {
+        const bool value = x >= columns;
+        const int c = value ? x - columns : x, h = c / a.per_head, d = (c - h * a.per_head) * 16;
+        const char *from = (value ? a.v : a.k) + h * (value ? a.v_head : a.k_head) + d;
+        char *to = (value ? a.values : a.keys) + h * (value ? a.value_head : a.key_head) + d;
+        const int64_t line = value ? a.v_row : a.k_row, block = value ? a.value_block : a.key_block, place = value ? a.value_place : a.key_place;
+        for (int r = r0; r < here; r += 4 * step) {
+            V4 y[4];
+            int64_t s[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t i = i0 + (r + u * step < here ? r + u * step : here - 1);
+                y[u] = *(const V4 *)(from + i * line);
+                s[u] = a.slot[i];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                int64_t p;
+                int in;
+                if (r + u * step < here && find<I>(a, s[u], p, in)) *(V4 *)(to + p * block + in * place) = y[u];
+            }
+        }
+    };
+    if (both >= kWrite) {
+        for (int x = threadIdx.x; x < both; x += kWrite) column(x, 0, 1);        // the rows' slots are the same for all threads
+    } else {
+        const int step = kWrite / both, r0 = threadIdx.x / both;
+        if (r0 < step) column(threadIdx.x - r0 * both, r0, step);
     }
-    if (!a.mean) return;
-    for (int64_t i = i0; i < i0 + here; ++i) {
-        const int64_t s = a.slot[i];
-        if (s < 0 || s >= a.slots || s % a.block != a.block - 1) continue;           // the same for all threads
+}
+
+// The means of the blocks whose last place is that of one of `here` rows from i0 on, at 16-byte columns c0 .. c0 + kSlice - 1.  Eight threads a column, which
+// add up every eighth place.
+template <int TYPE, class I> __device__ __forceinline__ void means(const WriteArgs &a, int64_t i0, int here, int c0) {
+    using E = Elem<TYPE>;
+    constexpr int GROUPS = kWrite / kSlice;
+    __shared__ float part[kWrite * E::kPer];
+    __shared__ int ends[COMET_MAX_BLOCK], count, run;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    for (int r = threadIdx.x; r < here; r += kWrite) {
+        int64_t p;
+        int in;
+        if (find<I>(a, a.slot[i0 + r], p, in) && in == a.block - 1) ends[atomicAdd(&count, 1)] = r;
+    }
+    __syncthreads();
+    const int some = count, g = threadIdx.x / kSlice, c = c0 + threadIdx.x % kSlice, columns = a.heads * a.per_head;
+    const int64_t h = c / a.per_head, d = (int64_t)(c - h * a.per_head) * 16;
+    for (int n = 0; n < some; ++n) {
+        const int64_t i = i0 + ends[n], s = a.slot[i];
         // how many rows before this one fill the places before its own: those are read from k, where another workgroup may be copying them
         if (threadIdx.x == 0) run = a.block;
         __syncthreads();
@@ -47,38 +87,57 @@ __global__ void __launch_bounds__(kWrite) k_cache_write(WriteArgs a, int rows) {
             if (j > i || a.slot[i - j] != s - j) atomicMin(&run, j);
         __syncthreads();
         const int old = a.block - run;                                                // places that the cache has already
-        const int64_t p = s / a.block;
-        // columns side by side, places in groups: each thread adds up a column's places o, o + groups, ..
-        for (int c0 = 0; c0 < columns; c0 += kWrite) {
-            const int width = columns - c0 < kWrite ? columns - c0 : kWrite, groups = kWrite / width;
-            const int g = threadIdx.x / width, c = c0 + threadIdx.x - g * width;
-            const int64_t h = c / a.per_head, d = (int64_t)(c - h * a.per_head) * 16;
-            float sum[E::kPer] = {};
-            if (g < groups) {
-#pragma unroll 4
-                for (int o = g; o < a.block; o += groups) {
-                    const char *from = o < old ? a.keys + p * a.key_stride[0] + o * a.key_stride[1] + h * a.key_stride[2] + d
-                                               : a.k + (i - (a.block - 1 - o)) * a.k_row + h * a.k_head + d;
-                    float f[E::kPer];
-                    E::widen(*(const uint4 *)from, f);
+        int64_t p;
+        int in;
+        find<I>(a, s, p, in);
+        float sum[E::kPer] = {};
+        if (c < columns) {
+            const char *key = a.keys + p * a.key_block + h * a.key_head + d, *row = a.k + (i - a.block + 1) * a.k_row + h * a.k_head + d;
+#pragma unroll 8
+            for (int o = g; o < a.block; o += GROUPS) {
+                const V4 y = *(const V4 *)(o < old ? key + o * a.key_place : row + o * a.k_row);
+                float f[E::kPer];
+                E::widen(make_uint4(y.x, y.y, y.z, y.w), f);
 #pragma unroll
-                    for (int e = 0; e < E::kPer; ++e) sum[e] += f[e];
-                }
+                for (int e = 0; e < E::kPer; ++e) sum[e] += f[e];
             }
-#pragma unroll
-            for (int e = 0; e < E::kPer; ++e) part[threadIdx.x * E::kPer + e] = sum[e];
-            __syncthreads();
-            if (g == 0) {
-                for (int o = 1; o < groups; ++o)
-#pragma unroll
-                    for (int e = 0; e < E::kPer; ++e) sum[e] += part[(o * width + threadIdx.x) * E::kPer + e];
-#pragma unroll
-                for (int e = 0; e < E::kPer; ++e) sum[e] /= (float)a.block;
-                *(uint4 *)(a.mean + p * a.mean_stride[0] + h * a.mean_stride[1] + d) = E::narrow(sum);
-            }
-            __syncthreads();
         }
+#pragma unroll
+        for (int e = 0; e < E::kPer; ++e) part[e * kWrite + threadIdx.x] = sum[e];
+        __syncthreads();
+        if (g == 0 && c < columns) {
+            for (int o = 1; o < GROUPS; ++o)
+#pragma unroll
+                for (int e = 0; e < E::kPer; ++e) sum[e] += part[e * kWrite + o * kSlice + threadIdx.x];
+#pragma unroll
+            for (int e = 0; e < E::kPer; ++e) sum[e] /= (float)a.block;
+            *(uint4 *)(a.mean + p * a.mean_block + h * a.mean_head + d) = E::narrow(sum);
+        }
+        __syncthreads();
     }
+}
+
+// The first workgroups take means, of `block` rows and a slice of the columns each, the others copy.  Bound by memory where rows are many (8191 rows of
+// 2 x 2 KB: 16 us, 13 without means, and two copies of half the size 20), by one read after the other where they are few.  Means taken by the
+// workgroups that copy the blocks' last rows, behind the copy, were 26.
+template <int TYPE, class I>
+__global__ void __launch_bounds__(kWrite) k_cache_write(WriteArgs a, int rows, unsigned slices, unsigned for_means) {
+    if (blockIdx.x < for_means) {
+        const int64_t i0 = (int64_t)(blockIdx.x / slices) * a.block;
+        means<TYPE, I>(a, i0, (int)(a.N - i0 < a.block ? a.N - i0 : a.block), (int)(blockIdx.x % slices) * kSlice);
+    } else {
+        const int64_t i0 = (int64_t)(blockIdx.x - for_means) * rows;
+        copy_rows<I>(a, i0, (int)(a.N - i0 < rows ? a.N - i0 : rows));
+    }
+}
+
+template <int TYPE, class I> hipError_t launch(const WriteArgs &a, hipStream_t st) {
+    const int64_t rows = a.N > 2048 ? 4 : 1, slices = (a.heads * a.per_head + kSlice - 1) / kSlice, for_means = a.mean ? (a.N + a.block - 1) / a.block * slices : 0;
+    hipLaunchKernelGGL((k_cache_write<TYPE, I>), dim3((unsigned)(for_means + (a.N + rows - 1) / rows)), dim3(kWrite), 0, st, a, (int)rows, (unsigned)slices, (unsigned)for_means);
+    return hipGetLastError();
+}
+template <int TYPE> hipError_t launch(const WriteArgs &a, hipStream_t st) {
+    return a.slots < (int64_t(1) << 31) ? launch<TYPE, uint32_t>(a, st) : launch<TYPE, int64_t>(a, st);
 }
 
 }  // namespace
@@ -86,16 +145,11 @@ __global__ void __launch_bounds__(kWrite) k_cache_write(WriteArgs a, int rows) {
 hipError_t cache_write(const comet_cache &c, int64_t N, const void *k, const int64_t k_stride[2], const void *v, const int64_t v_stride[2],
                        const int64_t *slot, hipStream_t st) {
     const int64_t e = c.type == COMET_F32 ? 4 : 2;
-    WriteArgs a{(const char *)k, (const char *)v, (char *)c.keys, (char *)c.values, (char *)c.mean, N, c.blocks * c.block, (int)c.block, (int)c.heads,
-                (int)(c.size * e / 16), k_stride[0] * e, k_stride[1] * e, v_stride[0] * e, v_stride[1] * e, {}, {}, {}, slot};
-    for (int i = 0; i < 3; ++i) a.key_stride[i] = c.key_stride[i] * e, a.value_stride[i] = c.value_stride[i] * e;
-    for (int i = 0; i < 2; ++i) a.mean_stride[i] = c.mean_stride[i] * e;
-    const int rows = N > 4096 ? 8 : 1;
-    const dim3 grid((unsigned)((N + rows - 1) / rows));
-    if (c.type == COMET_F32) hipLaunchKernelGGL(k_cache_write<COMET_F32>, grid, dim3(kWrite), 0, st, a, rows);
-    else if (c.type == COMET_BF16) hipLaunchKernelGGL(k_cache_write<COMET_BF16>, grid, dim3(kWrite), 0, st, a, rows);
-    else hipLaunchKernelGGL(k_cache_write<COMET_F16>, grid, dim3(kWrite), 0, st, a, rows);
-    return hipGetLastError();
+    const WriteArgs a{(const char *)k, (const char *)v, (char *)c.keys, (char *)c.values, (char *)c.mean, N, c.blocks * c.block, (int)c.block, (int)c.heads,
+                      (int)(c.size * e / 16), k_stride[0] * e, k_stride[1] * e, v_stride[0] * e, v_stride[1] * e,
+                      c.key_stride[0] * e, c.key_stride[1] * e, c.key_stride[2] * e, c.value_stride[0] * e, c.value_stride[1] * e, c.value_stride[2] * e,
+                      c.mean_stride[0] * e, c.mean_stride[1] * e, slot};
+    return c.type == COMET_F32 ? launch<COMET_F32>(a, st) : c.type == COMET_BF16 ? launch<COMET_BF16>(a, st) : launch<COMET_F16>(a, st);
 }
 
 }  // namespace comet
