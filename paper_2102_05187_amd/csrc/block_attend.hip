@@ -30,7 +30,7 @@ Plan plan_of(const comet_cache &c, int64_t N, int64_t Q, int64_t B, int64_t M, i
     const int64_t items = p.tiles * c.heads * p.chunks, most = K * c.block / 256;
     int64_t splits = items > 0 ? 512 / items : 1;
     if (splits > most) splits = most;
-    if (splits > 64) splits = 64;
+    if (splits > kSplits) splits = kSplits;
     p.splits = (int)(splits < 1 ? 1 : splits);
     p.bytes = p.splits > 1 ? items * p.splits * 16 * p.mt * (p.wide + 4) * 4 : 0;
     return p;

@@ -549,38 +549,47 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
     }
 }
 
-// The parts of a tile that several workgroups share: one workgroup a tile and head, a wavefront a row.
+// The parts of a tile that several workgroups share: one workgroup a tile and head, a thread four elements of a row.  Bound by two waits, for the
+// requests and for the parts.
+constexpr int kSplits = 16;
 template <int TYPE, int DT, int MT>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
     using E = Elem<TYPE>;
-    constexpr int kAttend = 256, kWaves = kAttend / kWave;
-    __shared__ int64_t buf[kWaves], where[3];
-    const int hc = a.heads * a.chunks;
-    const int64_t tile = blockIdx.x / hc;
-    const int at = (int)(blockIdx.x % hc), head = at / a.chunks, chunk = at % a.chunks;
-    const Tile t = find_tile<kAttend>(a.q, a.tokens, (int)tile, buf, where);
+    using T = typename E::T;
+    constexpr int THREADS = 256, EACH = DT / 4;
+    __shared__ int64_t buf[THREADS / kWave], where[2];
+    const uint32_t hc = a.heads * a.chunks, tile = blockIdx.x / hc, at = blockIdx.x - tile * hc;
+    const int head = (int)(at / a.chunks), chunk = (int)(at - head * a.chunks);
+    const Tile t = find_tile<THREADS>(a.q, a.tokens, (int)tile, buf, where);
     const int heads = a.group - chunk * a.chunk < a.chunk ? a.group - chunk * a.chunk : a.chunk, x0 = head * a.group + chunk * a.chunk;
-    const int lane = threadIdx.x & (kWave - 1);
     const float *from = a.part + (int64_t)blockIdx.x * a.splits * (16 * MT) * (DT + 4);
-    for (int r = threadIdx.x / kWave; r < t.n * heads; r += kWaves) {
-        float high = kNegInf, total = 0.f, out[DT / kWave] = {};
-        for (int s = 0; s < a.splits; ++s) {
-            const float *p = from + (s * 16 * MT + r) * (DT + 4);
-            const float m = p[DT], sum = p[DT + 1], now = fmaxf(high, m);
-            const float old = high == now ? 1.f : high == kNegInf ? 0.f : exp2_fast(high - now), add = m == now || m != m ? 1.f : m == kNegInf ? 0.f : exp2_fast(m - now);
-            total = total * old + sum * add;
+    for (int x = threadIdx.x; x < t.n * heads * EACH; x += THREADS) {
+        const int r = x / EACH, d0 = x % EACH * 4;
+        float high[kSplits], sum[kSplits], top = kNegInf, total = 0.f;
+        F4 part[kSplits], out = F4{0, 0, 0, 0};
 #pragma unroll
-            for (int u = 0; u < DT / kWave; ++u) out[u] = out[u] * old + (add == 0.f ? 0.f : p[u * kWave + lane] * add);
-            high = now;
+        for (int s = 0; s < kSplits; ++s) {
+            high[s] = kNegInf, sum[s] = 0.f, part[s] = F4{0, 0, 0, 0};
+            if (s >= a.splits) continue;
+            const float *p = from + (s * 16 * MT + r) * (DT + 4);
+            high[s] = p[DT], sum[s] = p[DT + 1], part[s] = *(const F4 *)(p + d0);
+        }
+#pragma unroll
+        for (int s = 0; s < kSplits; ++s) top = fmaxf(top, high[s]);
+#pragma unroll
+        for (int s = 0; s < kSplits; ++s) {
+            const float weight = high[s] == top || high[s] != high[s] ? 1.f : high[s] == kNegInf ? 0.f : exp2_fast(high[s] - top);
+            total += sum[s] * weight;
+            if (weight != 0.f) out += part[s] * weight;
         }
         const int i = r / heads;
         const int64_t row = (t.first + i) * a.q.Q + x0 + r - i * heads;
+        const float by = total == 0.f ? 0.f : 1.f / total;
+        T *to = (T *)a.out + row * a.size + d0;
+        if (d0 < a.size)                       // of 8 elements, as sizes are
 #pragma unroll
-        for (int u = 0; u < DT / kWave; ++u) {
-            const int d = u * kWave + lane;
-            if (d < a.size) ((typename E::T *)a.out)[row * a.size + d] = (typename E::T)E::bits(total == 0.f ? 0.f : out[u] / total);
-        }
-        if (lane == 0 && a.lse) a.lse[row] = total == 0.f ? kNegInf : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+            for (int e = 0; e < 4; ++e) to[e] = (T)E::bits(total == 0.f ? 0.f : out[e] * by);
+        if (d0 == 0 && a.lse) a.lse[row] = total == 0.f ? kNegInf : (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
     }
 }
 
