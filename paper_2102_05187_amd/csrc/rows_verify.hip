@@ -39,6 +39,59 @@ template <bool ZERO> __device__ __forceinline__ double exp2_wide(double x) {
     return ZERO && !(x > -1000.0) ? 0.0 : y;
 }
 
+// exp2(z c - R) for the logits of a row, or of a piece of one, R the whole number next to m c, m the largest of them.  With t = 16 z c and n the whole
+// number next to it, which is found by one multiply-add with 1.5 2^52 - 16 R, it is 2^(n / 16 - R) 2^((t - n) / 16): a sixteenth root of 2 from LDS with its
+// exponent, times a polynomial (through 2^(f / 16) at the six zeros of a Chebyshev polynomial, off by 1e-14 at most).  t - n is one multiply-add,
+// and exact: no difference of z and m is rounded, and the 64-bit instructions, which take twice as long as those of 32 bits, are ten
+// (with exp2_wide of (z - m) c they were 17: the sums of 320 rows of 131072 took 45 us).  Below 2^-1000 it is 2^-1000, or 0 where ZERO.
+struct Powers {
+    double c, m, c16, magic, unit;            // unit: what makes it exp2((z - m) c)
+    float low;                                // the logit whose power is 2^-1000
+    bool plain;                               // m c is not so large that whole numbers are lost
+    const double *root;                       // LDS, [16]
+    __device__ __forceinline__ Powers(double m, double c, const double *root) : c(c), m(m), root(root) {
+        const double R = __builtin_rint(m * c);
+        c16 = 16 * c, magic = 0x1.8p52 - 16 * R;
+        low = (float)((R - 1000) / c);
+        plain = fabs(m * c) < 0x1p40 && c < 0x1p100 && low > kNegInf;
+        unit = plain ? exp2_wide<false>(__builtin_fma(-m, c, R)) : 1;
+    }
+    // the scaled root, and the polynomial that goes with it
+    __device__ __forceinline__ double parts(float z, double &poly) const {
+        const double x = z > low ? z : low, big = __builtin_fma(x, c16, magic), f = __builtin_fma(x, c16, magic - big);
+        const int n = __double2loint(big);
+        const double t = root[n & 15];
+        double r = 0x1.5d8b6e76d3913p-30;
+        r = __builtin_fma(r, f, 0x1.3b2c9c307f552p-23);
+        r = __builtin_fma(r, f, 0x1.c6b08d6b1d71bp-17);
+        r = __builtin_fma(r, f, 0x1.ebfbdff5547dcp-11);
+        r = __builtin_fma(r, f, 0x1.62e42fefa3a3dp-5);
+        poly = __builtin_fma(r, f, 0x1.0000000000015p+0);
+        return __hiloint2double(__double2hiint(t) + (n >> 4 << 20), __double2loint(t));
+    }
+    // N of them, added up; PLAIN as it is above
+    template <bool PLAIN, int N> __device__ __forceinline__ double sum(const float *z, double s) const {
+        double t[N], poly[N], s2 = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if (PLAIN) t[e] = parts(z[e], poly[e]);
+            else t[e] = exp2_wide<false>(((double)z[e] - m) * c), poly[e] = 1;
+        }
+#pragma unroll
+        for (int e = 0; e < N; e += 2) s = __builtin_fma(t[e], poly[e], s), s2 = __builtin_fma(t[e + 1], poly[e + 1], s2);
+        return s + s2;
+    }
+    template <bool PLAIN> __device__ __forceinline__ double one(float z) const {
+        if (!PLAIN) return exp2_wide<true>(((double)z - m) * c);
+        double poly;
+        const double t = parts(z, poly);
+        return z > low ? t * poly : 0;
+    }
+};
+__device__ __forceinline__ void make_roots(double *root) {
+    if (threadIdx.x < 16) root[threadIdx.x] = exp2_wide<false>(threadIdx.x / 16.0);
+}
+
 // The sum of exp2((z - m) c) over a part of a row, m its largest logit: of nothing, m is -inf; with a NaN or +inf in it, s is a NaN.
 struct Sum {
     double s;
@@ -107,7 +160,8 @@ template <int TYPE, int VEC>
 __device__ __forceinline__ void piece_sum(const void *base, int64_t row, int64_t ld, int64_t V, int64_t piece, double c, Sum *out) {
     using E = Elem<TYPE>;
     __shared__ float top[kWavesRow];
-    __shared__ double part[kWavesRow];
+    __shared__ double part[kWavesRow], root[16];
+    make_roots(root);
     const Row<TYPE> r(base, row, ld, V);
     const int64_t v0 = piece * (kRow * VEC);
     uint4 x[VEC];
@@ -146,14 +200,26 @@ __device__ __forceinline__ void piece_sum(const void *base, int64_t row, int64_t
             for (int e = 0; e < E::kPer; ++e) s += f[e] == m ? 1.0 : 0.0;
         }
     } else {
-        const double big = m;
+        const Powers power(m, c, root);
+        if (power.plain)
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            float f[E::kPer];
-            E::widen(again(x[j]), f);
+            for (int j = 0; j < VEC; ++j) {
+                float f[E::kPer];
+                E::widen(x[j], f);
 #pragma unroll
-            for (int e = 0; e < E::kPer; ++e) s += exp2_wide<false>(((double)f[e] - big) * c);
-        }
+                for (int e = 0; e < E::kPer; e += 4) {
+                    s = power.sum<true, 4>(f + e, s);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        else
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                float f[E::kPer];
+                E::widen(again(x[j]), f);
+                s = power.sum<false, E::kPer>(f, s);
+            }
+        s *= power.unit;
     }
     s = wave_reduce(s, 0.0, Add());
     if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = s;
@@ -189,48 +255,62 @@ template <int TYPE, int DRAFT, int MODE> struct Left {
     Row<TYPE> z;
     Row<DRAFT> x;
     Sum p, q;
-    double c, p_part, q_part;                 // 1 / p.s, and 1 / q.s or 0
+    Powers of_p, of_q;
+    double p_part, q_part;                    // what makes a power a probability; the second one 0 where there is none
     bool rejected, largest;                   // something of the draft is taken off; only the largest logit counts
     int64_t d;
     const uint16_t *at;                       // kEntries: 1 + the entry of a place of the piece, 0: none
     const double *chance;                     //           and the entries' probabilities
-    // the logits of vector i
-    static constexpr int PER = Elem<TYPE>::kPer;
-    struct Logits { float f[PER], g[MODE == kDense ? PER : 1]; };
+    static constexpr int PER = Elem<TYPE>::kPer, DRAFT_PER = Elem<DRAFT>::kPer, MORE = DRAFT_PER < PER ? 2 : 1;
+    // the logits of vector i, as they are in memory: the target's, and of the draft as many or, where its vectors are longer, those around them
+    struct Logits { uint4 z, x[MODE == kDense ? MORE : 1]; };
+    template <int K> static __device__ __forceinline__ uint4 vector(const Row<K> &row, int64_t i) {
+        if (row.whole(i)) return row.raw(i);
+        float f[Elem<K>::kPer];
+        row.load(i, f);
+        return Elem<K>::narrow(f);
+    }
     __device__ __forceinline__ Logits logits(int64_t i) const {
         Logits v;
-        z.load(i, v.f);
+        v.z = vector<TYPE>(z, i);
         if constexpr (MODE == kDense) {
-            if (!rejected) return v;
-            if constexpr (Elem<DRAFT>::kPer == PER) {
-                x.load(i, v.g);
-            } else if constexpr (Elem<DRAFT>::kPer < PER) {
-                x.load(2 * i, v.g), x.load(2 * i + 1, v.g + Elem<DRAFT>::kPer);
-            } else {
-                float both[Elem<DRAFT>::kPer];
-                x.load(i / 2, both);
 #pragma unroll
-                for (int e = 0; e < PER; ++e) v.g[e] = both[(i & 1) * PER + e];
+            for (int k = 0; k < MORE; ++k) {
+                v.x[k] = make_uint4(0, 0, 0, 0);
+                if (rejected) v.x[k] = vector<DRAFT>(x, DRAFT_PER > PER ? i / 2 : MORE * i + k);
             }
         }
         return v;
     }
     // its weights; `in` its number in the piece
     __device__ __forceinline__ void weights(int64_t i, int in, const Logits &v, double *w) const {
-        const float *f = v.f;
+        if (of_p.plain && (MODE != kDense || of_q.plain)) weights_as<true>(i, in, v, w);
+        else weights_as<false>(i, in, v, w);
+    }
+    template <bool PLAIN> __device__ __forceinline__ void weights_as(int64_t i, int in, const Logits &v, double *w) const {
+        float f[PER], g[MODE == kDense ? (DRAFT_PER > PER ? DRAFT_PER : PER) : 1];
+        Elem<TYPE>::widen(v.z, f);
+        if constexpr (MODE == kDense) {
+#pragma unroll
+            for (int k = 0; k < MORE; ++k) Elem<DRAFT>::widen(v.x[k], g + k * DRAFT_PER);
+            if constexpr (DRAFT_PER > PER) {
+#pragma unroll
+                for (int e = 0; e < PER; ++e) g[e] = i & 1 ? g[PER + e] : g[e];
+            }
+        }
         if (largest) {
 #pragma unroll
             for (int e = 0; e < PER; ++e) w[e] = (double)f[e] == p.m ? 1 : 0;
             return;
         }
 #pragma unroll
-        for (int e = 0; e < PER; ++e) w[e] = exp2_wide<true>(((double)f[e] - p.m) * c) * p_part;
+        for (int e = 0; e < PER; ++e) w[e] = of_p.template one<PLAIN>(f[e]) * p_part;
         if (!rejected) return;
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
             double off = 0;
             if (MODE == kPoint) off = z.first(i) + e == d ? 1 : 0;
-            if constexpr (MODE == kDense) off = exp2_wide<true>(((double)v.g[e] - q.m) * c) * q_part;
+            if constexpr (MODE == kDense) off = of_q.template one<PLAIN>(g[e]) * q_part;
             if (MODE == kEntries) {
                 const int k = at[in * PER + e];
                 off = k ? chance[k - 1] : 0;
@@ -246,10 +326,13 @@ template <int TYPE, int DRAFT, int MODE> struct Left {
 template <int TYPE, int DRAFT, int MODE, int VEC>
 __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     constexpr int PER = Elem<TYPE>::kPer, kPiece = kRow * VEC;
-    static_assert(VEC * kWavesRow <= kParts, "a part for each wavefront's vectors next to each other");
+    constexpr int kMine = VEC * kWavesRow;       // a part for each wavefront's vectors next to each other
+    static_assert(kMine <= kParts && kMine <= kWave, "one wavefront writes them");
     __shared__ int first, final_one, chosen_part, behind;
     __shared__ double part[kWavesRow], sums[kParts], chance[MODE == kEntries ? COMET_MAX_TOP : 1], before_part, goal_;
+    __shared__ double root[16];
     __shared__ uint16_t at[MODE == kEntries ? kPiece * PER : 1];
+    make_roots(root);
     __shared__ Sum known[2][kRow / 8];
     const int b = (int)(blockIdx.x / (unsigned)a.pieces), piece = (int)blockIdx.x - b * a.pieces;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -319,15 +402,15 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
         a.accepted[b] = took;
         if (a.length) a.length[b] -= (int32_t)(n - 1 - took);
     }
-    Left<TYPE, DRAFT, MODE> left{Row<TYPE>(a.Z, row, a.ldz, a.V), Row<DRAFT>(a.draft, MODE == kDense ? row : 0, a.ldd, a.V), known[0][slot], known[1][slot], c, 0, 0,
+    Left<TYPE, DRAFT, MODE> left{Row<TYPE>(a.Z, row, a.ldz, a.V), Row<DRAFT>(a.draft, MODE == kDense ? row : 0, a.ldd, a.V), known[0][slot], known[1][slot], Powers(known[0][slot].m, c, root),
+                                 Powers(MODE == kDense && known[1][slot].good() ? known[1][slot].m : 0, c, root), 0, 0,
                                  took < n - 1 && !largest, largest, took < n - 1 ? a.token[row + 1] : -1, at, chance};
     if (!usable(left.p)) {
         if (piece == 0 && threadIdx.x == 0) a.next[b] = -1;
         return;
     }
-    left.p_part = 1 / left.p.s;
-    left.q_part = left.q.good() ? 1 / left.q.s : 0;
-    if (MODE == kDense && !left.q.good()) left.q.m = 0;
+    left.p_part = left.of_p.unit / left.p.s;
+    left.q_part = left.q.good() ? (MODE == kDense ? left.of_q.unit : 1) / left.q.s : 0;
     // the entries that lie in a piece, by place
     const auto lay_out = [&](int64_t of) {
         if (MODE != kEntries || !left.rejected) return;
@@ -344,13 +427,14 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     };
     // the weights of a piece's parts: part j * 4 + w are the vectors of wavefront w at j, in the order of the row
     const auto piece_parts = [&](int64_t of, auto put) {
-        typename Left<TYPE, DRAFT, MODE>::Logits ahead = left.logits(of * kPiece + threadIdx.x);
-#pragma unroll 1
+        // all are asked for before the first is waited for: one after the other, with the next one under way, took 24 us for eight
+        typename Left<TYPE, DRAFT, MODE>::Logits v[VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) v[j] = left.logits(of * kPiece + j * kRow + threadIdx.x);
+#pragma unroll
         for (int j = 0; j < VEC; ++j) {
             double w[PER], s = 0;
-            const auto v = ahead;
-            if (j + 1 < VEC) ahead = left.logits(of * kPiece + (j + 1) * kRow + threadIdx.x);
-            left.weights(of * kPiece + j * kRow + threadIdx.x, j * kRow + threadIdx.x, v, w);
+            left.weights(of * kPiece + j * kRow + threadIdx.x, j * kRow + threadIdx.x, v[j], w);
 #pragma unroll
             for (int e = 0; e < PER; ++e) s += w[e];
             s = wave_reduce(s, 0.0, Add());
@@ -359,8 +443,9 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     };
     lay_out(piece);
     double *weight = a.weight + (int64_t)b * a.pieces * kParts;
-    piece_parts(piece, [&](int i, double s) { __hip_atomic_store(weight + piece * kParts + i, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); });
+    piece_parts(piece, [&](int i, double s) { sums[i] = s; });
     __syncthreads();
+    if (threadIdx.x < kMine) __hip_atomic_store(weight + piece * kParts + threadIdx.x, sums[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (threadIdx.x == 0) final_one = __hip_atomic_fetch_add(a.arrived + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
     __syncthreads();
     if (!final_one) return;
@@ -368,7 +453,6 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
 
     // Of `count` weights in order the first at which their running sum, from `upto` on, is beyond the goal: chosen_part, and the sum before it.  Where there is
     // none, the last one that has a weight.  The goal is v times the sum of all where v is given (0 and above).
-    constexpr int kParts_ = VEC * kWavesRow;
     const auto choose = [&](int count, auto get, double v, double goal) {
         if (threadIdx.x == 0) chosen_part = 0x7fffffff, behind = -1;
         const int each = (count + kRow - 1) / kRow, i0 = threadIdx.x * each, i1 = i0 + each < count ? i0 + each : count;
@@ -402,7 +486,7 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
         double x = upto, before = 0;
         const auto take = [&](int i, double w) {
             if (w > 0) last = i;
-            if (hit < 0 && x + w > goal) hit = i, before = x;
+            if (hit < 0 && w > 0 && x + w > goal) hit = i, before = x;          // a running sum of another rounding may be beyond it already
             x += w;
         };
         if (each <= 4) {
@@ -424,21 +508,21 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
         return all;
     };
     const double v = largest || !(a.v[b] > 0) ? 0 : (double)a.v[b];
-    const double sum = choose(a.pieces * kParts_, [&](int i) {
-        return __hip_atomic_load(weight + i / kParts_ * kParts + i % kParts_, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const double sum = choose(a.pieces * kMine, [&](int i) {
+        return __hip_atomic_load(weight + i / kMine * kParts + i % kMine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }, v, 0);
-    int64_t of = chosen_part / kParts_;
-    int in = chosen_part % kParts_;
+    int64_t of = chosen_part / kMine;
+    int in = chosen_part % kMine;
     if (!(sum > 0)) {
         // p <= q throughout: p itself is drawn from, first a piece of it, then a part of that
         left.rejected = false;
         __syncthreads();
-        choose(a.pieces, [&](int i) { return onto(a.target[row * a.pieces + i], left.p.m, c) * left.p_part; }, v, 0);
+        choose(a.pieces, [&](int i) { return onto(a.target[row * a.pieces + i], left.p.m, c) / left.p.s; }, v, 0);
         of = chosen_part;
         const double goal = goal_ - before_part;
         piece_parts(of, [&](int i, double s) { sums[i] = s; });
         __syncthreads();
-        choose(kParts_, [&](int i) { return sums[i]; }, -1, goal);
+        choose(kMine, [&](int i) { return sums[i]; }, -1, goal);
         in = chosen_part;
     }
     if (of != piece) lay_out(of);
