@@ -178,6 +178,22 @@ template <int T> __device__ __forceinline__ List make_list(const AttendArgs &a, 
     return l;
 }
 
+// N elements of a row of the output, at a multiple of N from its start, of which `left` are left: 8 bytes or 16 at a time.
+template <int TYPE, int N> __device__ __forceinline__ void put_elements(typename Elem<TYPE>::T *to, const float *f, int left) {
+    using E = Elem<TYPE>;
+    if constexpr (N < E::kPer) {
+        float g[E::kPer] = {};
+#pragma unroll
+        for (int e = 0; e < N; ++e) g[e] = f[e];
+        const uint4 y = E::narrow(g);
+        if (left > 0) *(uint2 *)to = make_uint2(y.x, y.y);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; e += E::kPer)
+            if (left > e) *(uint4 *)(to + e) = E::narrow(f + e);
+    }
+}
+
 __device__ __forceinline__ float xor16(float v) { return __shfl_xor(v, 16); }
 __device__ __forceinline__ float xor32(float v) { return __shfl_xor(v, 32); }
 
@@ -538,10 +554,9 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
                 const int i = r / heads;
                 const int64_t row = (t.first + i) * a.q.Q + x0 + r - i * heads;
                 const float by = total == 0.f ? 0.f : 1.f / total;
-                T *to = (T *)a.out + row * a.size + d0;
 #pragma unroll
-                for (int e = 0; e < EACH; ++e)
-                    if (d0 + e < a.size) to[e] = (T)E::bits(total == 0.f ? 0.f : out[e] * by);
+                for (int e = 0; e < EACH; ++e) out[e] = total == 0.f ? 0.f : out[e] * by;
+                put_elements<TYPE, EACH>((T *)a.out + row * a.size + d0, out, a.size - d0);
                 if (d0 == 0 && a.lse) a.lse[row] = total == 0.f ? kNegInf : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
             }
         }
@@ -585,10 +600,10 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
         const int i = r / heads;
         const int64_t row = (t.first + i) * a.q.Q + x0 + r - i * heads;
         const float by = total == 0.f ? 0.f : 1.f / total;
-        T *to = (T *)a.out + row * a.size + d0;
-        if (d0 < a.size)                       // of 8 elements, as sizes are
+        float f[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) to[e] = (T)E::bits(total == 0.f ? 0.f : out[e] * by);
+        for (int e = 0; e < 4; ++e) f[e] = total == 0.f ? 0.f : out[e] * by;
+        put_elements<TYPE, 4>((T *)a.out + row * a.size + d0, f, a.size - d0);
         if (d0 == 0 && a.lse) a.lse[row] = total == 0.f ? kNegInf : (top + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
     }
 }

@@ -133,9 +133,9 @@ __global__ void __launch_bounds__(WAVES * kWave) k_select(SelectArgs a) {
     const bool scored = most > a.K;                                // else there is nothing to choose
     if (scored) {
         const int32_t *table = a.q.table + t.b * a.q.ldt;
-        // the heads' sums, a thread a token and 16-byte piece, to where each lane finds its own
+        // the heads' sums, a thread a token and 16-byte piece, to where each lane finds its own, and the keys go afterwards
         constexpr int PIECES = 4 * NK, LINE = WIDE + 2;
-        double *const sums = (double *)(keys + TOKENS * stride);
+        double *const sums = (double *)keys;
         for (int x = threadIdx.x; x < TOKENS * PIECES; x += THREADS) {
             const int i = x / PIECES, d = x % PIECES * CH;
             double s[CH] = {};
@@ -158,6 +158,7 @@ __global__ void __launch_bounds__(WAVES * kWave) k_select(SelectArgs a) {
         for (int k = 0; k < NK; ++k)
 #pragma unroll
             for (int e = 0; e < CH; ++e) q[k][e] = sums[(TOKENS == 1 ? 0 : col) * LINE + (4 * k + g) * CH + e];
+        __syncthreads();
         const int mine = TOKENS == 1 ? most : col < t.n ? seen(col) : 0;          // blocks that the lane's token sees
         // A step's numbers of the table are asked for while the steps before it are computed; where a wavefront has the SIMD to itself, its means too.
         constexpr int STEP = THREADS / 4;
@@ -241,7 +242,7 @@ template <int TYPE, int WIDE> hipError_t launch(SelectArgs a, hipStream_t st) {
     a.tokens = many ? 16 : 1;
     int64_t tiles = a.q.N / a.tokens + B;
     if (tiles > a.q.N) tiles = a.q.N;
-    const size_t lds = (size_t)(a.candidates + WIDE + 2) * 8 * a.tokens;
+    const size_t lds = (size_t)(a.candidates > WIDE + 2 ? a.candidates : WIDE + 2) * 8 * a.tokens;
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;

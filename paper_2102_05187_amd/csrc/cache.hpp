@@ -100,9 +100,29 @@ template <int T> __device__ __forceinline__ Tile find_tile(const Queries &q, int
     Tile t{0, 0, 0, 0};
     const auto cut = [&](int64_t b, int begin, int end, int length, int number) {
         const int n = end - begin, i = number * tokens;
+        if (begin < 0) return;
         t.b = b, t.first = (int64_t)begin + i, t.n = n - i < tokens ? n - i : tokens, t.place = (int64_t)length - n + i;
         if (t.first + t.n > q.N) t.n = t.first < q.N ? (int)(q.N - t.first) : 0;
     };
+    // One token a request, as decoding has them, or few requests: what is needed comes by scalar loads, which do not wait behind other workgroups' data.
+    if (tokens == 1 && tile < q.B && q.pos[tile] == tile && q.pos[tile + 1] == tile + 1) {
+        cut(tile, tile, tile + 1, q.length[tile], 0);
+        return t;
+    }
+    if (q.B <= 4) {
+        int at[5], length[4], left = tile;
+#pragma unroll
+        for (int b = 0; b < 5; ++b) at[b] = q.pos[b < q.B ? b : q.B];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) length[b] = q.length[b < q.B ? b : 0];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int pieces = at[b + 1] > at[b] ? (at[b + 1] - at[b] + tokens - 1) / tokens : 0;
+            if (left >= 0 && left < pieces) cut(b, at[b], at[b + 1], length[b], left);
+            left -= pieces;
+        }
+        return t;
+    }
     if (q.B <= 4 * kWave) {
         // every wavefront by itself: a request a lane, all that is needed of it with one wait
         const int lane = threadIdx.x & (kWave - 1);

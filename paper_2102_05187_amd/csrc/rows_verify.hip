@@ -337,7 +337,7 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     const int b = (int)(blockIdx.x / (unsigned)a.pieces), piece = (int)blockIdx.x - b * a.pieces;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int64_t r0 = a.pos[b], n = (a.pos[b + 1] < a.N ? a.pos[b + 1] : a.N) - r0;
-    if (n <= 0) {
+    if (n <= 0 || r0 < 0) {
         if (piece == 0 && threadIdx.x == 0) a.accepted[b] = 0, a.next[b] = -1;
         return;
     }

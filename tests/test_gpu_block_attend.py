@@ -174,9 +174,31 @@ def test_a_cache_of_more_than_4_gib():
     check(dict(q=q, K=K[ids].contiguous(), V=V[ids].contiguous(), table=near, pos=pos, length=length, sel=sel))
 
 
-def test_captured_and_replayed_on_another_stream():
+def test_a_table_as_wide_as_it_may_be():
+    """The list of chosen blocks takes the most room then, next to keys and values of the largest size."""
+    for dtype, D in ((torch.float16, 256), (torch.float32, 256), (torch.bfloat16, 128)):
+        s = make([1, 9], [300, 200], 1, 3, D, 16, dtype, seed=10, K=6)
+        want = check(s)
+        wide = torch.full((2, 262144), -1, dtype=torch.int32, device="cuda")
+        wide[:, :s["table"].shape[1]] = s["table"]
+        sel = torch.full((10, 1, 1000), -1, dtype=torch.int32, device="cuda")
+        sel[:, :, 3:9] = s["sel"]
+        got = _comet().comet_block_attend(s["q"], s["K"], s["V"], wide, s["pos"], s["length"], sel)
+        unit = ref.UNIT[dtype]
+        # the places are shared out in another way: weights rounded to the type, sums in another order
+        assert bool(((got[0].double() - want[0].double()).abs() <= 8 * unit * (1 + want[0].double().abs())).all())
+
+
+def test_in_inference_mode():
     comet = _comet()
-    s = make([1] * 8 + [40], [200 + i for i in range(8)] + [600], 2, 2, 64, 16, torch.bfloat16, seed=8, K=5)
+    with torch.inference_mode():
+        check(make([2, 9], [100, 200], 2, 2, 64, 16, torch.bfloat16, seed=11, K=4))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_captured_and_replayed_on_another_stream(D):
+    comet = _comet()
+    s = make([1] * 8 + [40], [200 + i for i in range(8)] + [600], 2, 2, D, 16, torch.bfloat16, seed=8, K=5)
     side = torch.cuda.Stream()
     call = lambda stream=None: comet.comet_block_attend(s["q"], s["K"], s["V"], s["table"], s["pos"], s["length"], s["sel"], stream=stream)
     want = call()

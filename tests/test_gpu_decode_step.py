@@ -72,3 +72,19 @@ def test_tokens_read_one_by_one_or_together():
                 assert bool(((mine - want[b][read[b]:read[b] + add[b]]).abs() <= 2.0 ** -24 * 1024 * size).all())
                 read[b] += add[b]
         assert read == length and cache.length.tolist() == length
+
+
+def test_a_step_in_inference_mode():
+    example = _example()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    with torch.inference_mode():
+        model = example.Model(101, 128, g, torch.float32)
+        cache = example.Cache(2, 16, 8, torch.float32)
+        for add in ([40, 3], [1, 1]):
+            tokens = torch.zeros(sum(add), dtype=torch.int32, device="cuda")
+            pos, _, logits = example.step(model, cache, tokens, torch.tensor(add, dtype=torch.int32).cuda(), None, 4)
+        comet = example.comet
+        u = torch.rand(2, device="cuda")
+        accepted, follow = comet.comet_draft_verify(logits, tokens, pos, u, u, length=cache.length)
+    assert cache.length.tolist() == [41, 4] and accepted.tolist() == [0, 0] and bool(((follow >= 0) & (follow < 101)).all())
