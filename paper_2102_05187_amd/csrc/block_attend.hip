@@ -44,8 +44,10 @@ int64_t block_attend_work(const comet_cache &c, int64_t N, int64_t Q, int64_t B,
 hipError_t block_attend(const comet_cache &c, const Queries &q, const int32_t *sel, int64_t K, double scale, void *out, float *lse, void *work, hipStream_t st) {
     const Plan p = plan_of(c, q.N, q.Q, q.B, q.M, K);
     const int e = c.type == COMET_F32 ? 4 : 2;
+    // 256 MB and more (64 tokens, 537 MB: 91 us past the last cache, 102 through it); the next token reads much of the same again, and less stays there
+    const bool once = q.N * c.heads * K * c.block * c.size * 2 * e >= int64_t(256) << 20;
     AttendArgs a{q, (const char *)c.keys, (const char *)c.values, c.blocks, (int)c.block, (int)c.heads, (int)c.size, (int)(q.Q / c.heads), {}, {}, sel, (int)K,
-                 (float)(scale * 1.4426950408889634), out, lse, p.tokens, p.chunk, p.chunks, p.tiles, p.splits, p.words, p.entries, (float *)work};
+                 (float)(scale * 1.4426950408889634), out, lse, p.tokens, p.chunk, p.chunks, p.tiles, p.splits, p.words, p.entries, once, (float *)work};
     for (int i = 0; i < 3; ++i) a.key_stride[i] = c.key_stride[i] * e, a.value_stride[i] = c.value_stride[i] * e;
     if (c.type == COMET_F32) return attend_f32(a, p.wide, p.mt, st);
     if (c.type == COMET_BF16) return attend_bf16(a, p.wide, p.mt, st);

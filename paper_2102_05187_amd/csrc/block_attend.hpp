@@ -28,6 +28,7 @@ struct AttendArgs {
     int tokens, chunk, chunks;                // of a workgroup: tokens at most, query heads; chunks of them in a group
     int64_t tiles;                            // at most
     int splits, words, entries;               // workgroups that share a tile's places; sizes of the list
+    bool once;                                // what is read does not stay in the last cache: it is read past it
     float *part;                              // splits > 1: [item x splits x rows x (DT + 2)]
 };
 
@@ -317,8 +318,13 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
                 const char *key = p.key + (uint32_t)(p.start * key_line), *value = p.value + (uint32_t)(p.start * value_line);
 #pragma unroll
                 for (int n = h * EACH; n < (h + 1) * EACH; ++n) {
-                    __builtin_amdgcn_global_load_lds((Global *)(key + (uint32_t)key_at[n]), (Lds *)(stage + n * 1024), 16, 0, 0);
-                    __builtin_amdgcn_global_load_lds((Global *)(value + (uint32_t)value_at[n]), (Lds *)(stage_v + n * 1024), 16, 0, 0);
+                    if (MT == 1 && a.once) {
+                        __builtin_amdgcn_global_load_lds((Global *)(key + (uint32_t)key_at[n]), (Lds *)(stage + n * 1024), 16, 0, 2);
+                        __builtin_amdgcn_global_load_lds((Global *)(value + (uint32_t)value_at[n]), (Lds *)(stage_v + n * 1024), 16, 0, 2);
+                    } else {
+                        __builtin_amdgcn_global_load_lds((Global *)(key + (uint32_t)key_at[n]), (Lds *)(stage + n * 1024), 16, 0, 0);
+                        __builtin_amdgcn_global_load_lds((Global *)(value + (uint32_t)value_at[n]), (Lds *)(stage_v + n * 1024), 16, 0, 0);
+                    }
                 }
             } else {
 #pragma unroll

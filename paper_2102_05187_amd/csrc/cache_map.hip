@@ -5,13 +5,13 @@ namespace comet {
 
 namespace {
 
-// What the steps tell each other about a request: its length and blocks before the call adds to them, what it adds, the running number of its
-// first new block, and, where it has ended, how many blocks come back and where among all that do.
+// What the steps tell each other about a request: its length and blocks before the call adds to them, what it adds, and the running number of its
+// first new block.
 struct Plan {
-    int32_t length, held, fresh, gone;
-    int64_t first, back;
+    int32_t length, held, fresh, add;
+    int64_t first;
 };
-struct Head { int64_t before, count; };      // spare blocks before the call, and with the ended requests' among them
+struct Head { int64_t count, left; };         // spare blocks with the ended requests' among them, and those that are left
 
 constexpr int kPlan = 1024, kPos = 4096;      // requests whose places among the tokens a workgroup keeps in LDS
 
@@ -62,10 +62,8 @@ template <class I, int T> __device__ __forceinline__ void plan(const MapArgs &a,
     if (a.ended)
         for (int64_t b0 = 0; b0 < a.B; b0 += T) {
             const int64_t b = b0 + t;
-            const I n = b < a.B && a.ended[b] ? (I)within(a.held[b], a.M) : 0;
-            I upto = n, none = 0;
-            sums(upto, none, all, more);
-            if (b < a.B) p[b].gone = (int32_t)n, p[b].back = back + upto - n;
+            I n = b < a.B && a.ended[b] ? (I)within(a.held[b], a.M) : 0, none = 0;
+            sums(n, none, all, more);
             back += all;
         }
     const int64_t count = within(before + back, a.S);
@@ -90,9 +88,7 @@ template <class I, int T> __device__ __forceinline__ void plan(const MapArgs &a,
         rows += all, taken += more;
         if (on) {
             Plan &x = p[b];
-            x.length = (int32_t)length, x.held = (int32_t)held, x.fresh = (int32_t)fresh, x.first = block_no - want;
-            a.length[b] = (int32_t)(length + add);
-            a.held[b] = (int32_t)(held + fresh);
+            x.length = (int32_t)length, x.held = (int32_t)held, x.fresh = (int32_t)fresh, x.add = (int32_t)add, x.first = block_no - want;
             a.pos[b + 1] = (int32_t)row;
             if (at) at[b + 1] = (int32_t)row;
         }
@@ -100,18 +96,39 @@ template <class I, int T> __device__ __forceinline__ void plan(const MapArgs &a,
     if (t == 0) {
         a.pos[0] = 0;
         if (at) at[0] = 0;
-        head->before = before, head->count = count;
-        *a.count = (int32_t)(count - taken);
+        head->count = count, head->left = count - taken;
     }
 }
 
-// The blocks of ended requests b, b + step, ..: behind the spare ones, as far as there is room.
-__device__ __forceinline__ void give_back(const MapArgs &a, const Plan *p, const Head *head, int64_t b, int64_t step) {
-    for (; b < a.B; b += step) {
-        if (!a.ended[b]) continue;
-        const int64_t n = p[b].gone, to = head->before + p[b].back;
-        for (int64_t j = threadIdx.x; j < n && to + j < a.S; j += blockDim.x) a.spare[to + j] = a.table[b * a.ldt + j];
+// The blocks of ended requests: behind the spare ones, as far as there is room.  Every one of `groups` workgroups runs through all requests for where their
+// blocks go, and moves those of some.
+template <class I, int T> __device__ __forceinline__ void give_back(const MapArgs &a, int group, int groups) {
+    __shared__ I buf[2][2][T / kWave];
+    __shared__ I number[T], where[T];
+    Sums<I, T> sums{buf};
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const int64_t before = within(*a.count, a.S);
+    I back = 0, all, more;
+    for (int64_t b0 = 0; b0 < a.B; b0 += T) {
+        const int64_t b = b0 + threadIdx.x;
+        const I n = b < a.B && a.ended[b] ? (I)within(a.held[b], a.M) : 0;
+        I upto = n, none = 0;
+        sums(upto, none, all, more);
+        number[threadIdx.x] = n, where[threadIdx.x] = back + upto - n;
+        back += all;
+        __syncthreads();
+        for (int i = group * (T / kWave) + wave; i < T; i += groups * (T / kWave)) {
+            const int64_t to = before + where[i];
+            for (I j = lane; j < number[i] && to + j < a.S; j += kWave) a.spare[to + j] = a.table[(b0 + i) * a.ldt + j];
+        }
+        __syncthreads();
     }
+}
+
+// The requests' new lengths and blocks, once nobody reads the old ones any more.
+__device__ __forceinline__ void bring_up_to_date(const MapArgs &a, const Plan *p, const Head *head, int64_t t, int64_t threads) {
+    for (int64_t b = t; b < a.B; b += threads) a.length[b] = p[b].length + p[b].add, a.held[b] = p[b].held + p[b].fresh;
+    if (t == 0) *a.count = (int32_t)head->left;
 }
 
 // Token i: its request by halving (pos is in LDS where there is room), its block from the table or, where that is new, from the spare ones.  A new
@@ -149,16 +166,18 @@ template <int T> __global__ void __launch_bounds__(T) k_map_all(MapArgs a) {
     __shared__ Head head;
     __shared__ int32_t pos[kSmall + 1];
     plan<int32_t, T>(a, p, &head, pos);
+    if (a.ended) give_back<int32_t, T>(a, 0, 1);
     __syncthreads();
-    if (a.ended) {
-        give_back(a, p, &head, 0, 1);
-        __syncthreads();
-    }
+    bring_up_to_date(a, p, &head, threadIdx.x, T);
     for (int64_t i = threadIdx.x; i < a.N; i += T) token(a, p, &head, pos, i);
 }
-template <class I> __global__ void __launch_bounds__(kPlan) k_map_plan(MapArgs a, Plan *p, Head *head) { plan<I, kPlan>(a, p, head, nullptr); }
-__global__ void __launch_bounds__(256) k_map_back(MapArgs a, const Plan *p, const Head *head) { give_back(a, p, head, blockIdx.x, gridDim.x); }
+// The first workgroup plans; where requests have ended the others give their blocks back.
+template <class I> __global__ void __launch_bounds__(kPlan) k_map_plan(MapArgs a, Plan *p, Head *head) {
+    if (blockIdx.x == 0) plan<I, kPlan>(a, p, head, nullptr);
+    else give_back<I, kPlan>(a, (int)blockIdx.x - 1, (int)gridDim.x - 1);
+}
 __global__ void __launch_bounds__(256) k_map_tokens(MapArgs a, const Plan *p, const Head *head) {
+    bring_up_to_date(a, p, head, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
     __shared__ int32_t pos[kPos + 1];
     const bool near = a.B <= kPos;
     if (near) {
@@ -184,19 +203,14 @@ hipError_t cache_map(const MapArgs &a, void *work, hipStream_t st) {
     Head *head = (Head *)work;
     Plan *p = (Plan *)(head + 1);
     // no sum is over all places of all requests
-    if (a.B * a.M < (int64_t(1) << 31) / a.block) hipLaunchKernelGGL(k_map_plan<int32_t>, dim3(1), dim3(kPlan), 0, st, a, p, head);
-    else hipLaunchKernelGGL(k_map_plan<int64_t>, dim3(1), dim3(kPlan), 0, st, a, p, head);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.ended && a.B > 0) {
-        hipLaunchKernelGGL(k_map_back, dim3((unsigned)(a.B < 4096 ? a.B : 4096)), dim3(256), 0, st, a, p, head);
-        e = hipGetLastError();
-    }
-    if (e == hipSuccess && a.N > 0) {
-        const int64_t groups = (a.N + 1023) / 1024;
-        hipLaunchKernelGGL(k_map_tokens, dim3((unsigned)(groups < 65536 ? groups : 65536)), dim3(256), 0, st, a, p, head);
-        e = hipGetLastError();
-    }
-    return e;
+    const int64_t backs = !a.ended ? 0 : a.B < 16 * 64 ? (a.B + 15) / 16 : 64;
+    if (a.B * a.M < (int64_t(1) << 31) / a.block) hipLaunchKernelGGL(k_map_plan<int32_t>, dim3((unsigned)(1 + backs)), dim3(kPlan), 0, st, a, p, head);
+    else hipLaunchKernelGGL(k_map_plan<int64_t>, dim3((unsigned)(1 + backs)), dim3(kPlan), 0, st, a, p, head);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t groups = (a.N + 1023) / 1024;
+    hipLaunchKernelGGL(k_map_tokens, dim3((unsigned)(groups < 1 ? 1 : groups < 65536 ? groups : 65536)), dim3(256), 0, st, a, p, head);
+    return hipGetLastError();
 }
 
 }  // namespace comet

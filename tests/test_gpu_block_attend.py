@@ -174,6 +174,30 @@ def test_a_cache_of_more_than_4_gib():
     check(dict(q=q, K=K[ids].contiguous(), V=V[ids].contiguous(), table=near, pos=pos, length=length, sel=sel))
 
 
+def test_more_than_the_last_cache_holds():
+    """From 256 MB of chosen keys and values on they are read past it; every token reads all of its request's 2560 places."""
+    B, H, G, D, block, blocks = 16, 8, 4, 128, 64, 40
+    L = block * blocks - 5
+    g = torch.Generator(device="cuda")
+    g.manual_seed(12)
+    K, V = (torch.randn((B * blocks, block, H, D), device="cuda", generator=g).bfloat16() for _ in range(2))
+    q = torch.randn((B, H * G, D), device="cuda", generator=g).bfloat16()
+    table = torch.arange(B * blocks, dtype=torch.int32, device="cuda").view(B, blocks)
+    pos, length = torch.arange(B + 1, dtype=torch.int32, device="cuda"), torch.full((B,), L, dtype=torch.int32, device="cuda")
+    sel = torch.arange(blocks, dtype=torch.int32, device="cuda").expand(B, H, blocks).contiguous()
+    out, lse = _comet().comet_block_attend(q, K, V, table, pos, length, sel)
+    for b in range(B):
+        k, v = (t[b * blocks:(b + 1) * blocks].flatten(0, 1)[:L].transpose(0, 1).double() for t in (K, V))          # H, L, D
+        z = torch.matmul(q[b].view(H, G, D).double(), k.transpose(1, 2).contiguous()) * D ** -0.5
+        w = torch.softmax(z, 2)
+        want = torch.matmul(w, v.contiguous()).view(H * G, D)
+        mass = torch.matmul(w, v.abs().contiguous()).view(H * G, D)
+        # weights and the result are rounded to 8 bits; scores of 128 terms and sums of 2560 in 32 bits
+        bound = (2.0 ** -8 + 2.0 ** -24 * 4096) * mass + 2.0 ** -8 * want.abs()
+        assert bool(((out[b].double() - want).abs() <= bound).all())
+        assert bool(((lse[b].double() - torch.logsumexp(z, 2).view(-1)).abs() <= 2.0 ** -24 * 4096).all())
+
+
 def test_a_table_as_wide_as_it_may_be():
     """The list of chosen blocks takes the most room then, next to keys and values of the largest size."""
     for dtype, D in ((torch.float16, 256), (torch.float32, 256), (torch.bfloat16, 128)):

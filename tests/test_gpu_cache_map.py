@@ -69,6 +69,16 @@ def test_ended_requests_make_room(B, M, N, ends):
     check(s, add, 16, N, ended=ended)
 
 
+def test_sums_that_pass_32_bits():
+    """All places of all requests are more than 2^31: running sums are held in 64 bits."""
+    s = state(1500, 2000, 1024, seed=4, most=3000, S=5000)
+    g = torch.Generator().manual_seed(7)
+    add = torch.randint(0, 1500, (1500,), generator=g).tolist()
+    add[700] = add[701] = 2000 * 1024 - 3000
+    ended = (torch.rand(1500, generator=g) < 0.1).tolist()
+    check(s, add, 1024, 100000, ended=ended)
+
+
 @pytest.mark.parametrize("S", [0, 1, 7, 40])
 def test_too_few_spare_blocks(S):
     s = state(40, 9, 16, seed=S, S=S, held_more=False, most=100)
