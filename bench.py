@@ -124,12 +124,13 @@ _TRAFFIC = None
 
 def kernel_sources_digest():
     """sha256 over the HIP sources of the library (file names and contents, sorted): which kernels a figure belongs to.  The
-    kernels over dense rows (rows*) share nothing with those of this benchmark and are left out."""
+    kernels over dense rows (rows*) and over a cache in blocks (cache*, block*) share nothing with those of this benchmark and are
+    left out."""
     import hashlib
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2102_05187_amd", "csrc")
     for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".hpp")) and not name.startswith("rows"):
+        if name.endswith((".hip", ".hpp")) and not name.startswith(("rows", "cache", "block")):
             h.update(name.encode())
             with open(os.path.join(d, name), "rb") as f:
                 h.update(f.read())

@@ -25,7 +25,7 @@ Plan plan_of(const comet_cache &c, int64_t N, int64_t Q, int64_t B, int64_t M, i
     p.tiles = N / tokens + (B < N ? B : N);
     if (p.tiles > N) p.tiles = N;
     p.words = (int)((M + 31) / 32);
-    p.entries = (int)(tokens * K < M ? tokens * K : M);
+    p.entries = (int)(tokens * K < M ? tokens * K : M > K ? M : K);           // a single token's choices are kept as they are
     // places are shared out where there are few tiles: to 512 workgroups, 64 KB of keys and values each or more (1 token, 2 x 64 KB: 14 us in two
     // workgroups, 18 in four and joined; 71 tokens, 141 x 410 KB: 44 us in 141, 38 in 423)
     const int64_t items = p.tiles * c.heads * p.chunks, most = K * c.block * c.size * (c.type == COMET_F32 ? 8 : 4) / 65536;
