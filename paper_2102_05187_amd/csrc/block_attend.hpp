@@ -8,6 +8,10 @@
 //
 // Both products are turned around, S^T = K Q^T and O^T = V^T P^T: then a lane of the first one's result holds four places of one row, which is
 // how the second one wants P, and no element has to move.  V^T's fragments come from LDS, which turns 16-bit elements around as it is read.
+//
+// Bound by memory where tokens are single (64 tokens, 8 heads, 2048 places each, 537 MB: 92 us, 5.9 TB/s; the same loads alone 6.6 to 7.0), by the dies'
+// caches where they are neighbours (4093 tokens, 4 heads, 1024 places each: 310 us, 222 TFLOP/s; keys and values are read by every fourth
+// token, 5.8 GB, at 19 TB/s of 31).  More tokens a workgroup would read less, but leave registers for one wavefront a SIMD: 547 us with eight.
 #pragma once
 
 #include "cache.hpp"
@@ -295,8 +299,8 @@ __global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pai
         entry += skip, sixteen += more;
         if (sixteen >= per) sixteen -= per, ++entry;
     };
-    // Keys and values go to LDS straight from memory, a row of 16-byte pieces after the other, and from there to the lanes that want them: read by
-    // those lanes themselves, a load would ask for 64 pieces of 16 rows, and take four times as long.  Piece c of row i is at c ^ i, so
+    // Keys and values go to LDS straight from memory, a row of 16-byte pieces after the other, and from there to the lanes that want them.  Read by
+    // those lanes themselves, a load asks for 64 pieces of 16 rows (4093 tokens: 783 us with values by way of registers, 346 so).  Piece c of row i is at c ^ i, so
     // that what is read together, of 16 rows, lies in different banks.  Places behind the last one that is read are taken from there:
     // nothing comes from memory that no token reads.
     char *const stage = (char *)raw + behind_list(a) + wave * S::STAGE, *const stage_v = stage + S::STAGE / 2;

@@ -13,7 +13,7 @@ constexpr int kRow = 256, kWavesRow = kRow / kWave;
 constexpr int kParts = 32;                    // parts of a piece whose weights are kept: of a wavefront's vectors that lie next to each other
 
 // A thread has VEC 16-byte vectors of a piece, a piece VEC * kRow.  Long rows, or many, are cut into pieces of 2048 vectors, few short ones into
-// pieces of 512: 8 rows of 32000 32-bit logits take 24 us in 16 pieces each, and 38 in 4.
+// pieces of 512, so that there are more workgroups, whose latency is what such calls take (8 rows of 32000 32-bit logits: 18 us, 21 in pieces of 2048).
 int vectors_of(int64_t N, int64_t V) { return N * V < int64_t(1) << 20 ? 2 : 8; }
 int64_t pieces_of(int type, int64_t N, int64_t V) {
     const int64_t n = kRow * vectors_of(N, V) * (type == COMET_F32 ? 4 : 8);
@@ -22,7 +22,6 @@ int64_t pieces_of(int type, int64_t N, int64_t V) {
 
 // exp2 in 64 bits for arguments of at most 0: the nearest whole number taken off, by adding 1.5 2^52, and a polynomial for |f| <= 1/2, which goes
 // through 2^f at the ten zeros of a Chebyshev polynomial (off by 2e-14 at most).  Below -1000 it is 2^-1000, or 0 where ZERO.  A NaN is not kept.
-// Bound by the issue of 64-bit instructions: sixteen of them, and the sums of 320 rows of 131072 take 42 million such exponentials.
 template <bool ZERO> __device__ __forceinline__ double exp2_wide(double x) {
     const double low = __builtin_fmax(x, -1000.0), big = low + 0x1.8p52, f = low - (big - 0x1.8p52);
     double r = 0x1.b6557c7da8ca4p-24;
@@ -42,8 +41,9 @@ template <bool ZERO> __device__ __forceinline__ double exp2_wide(double x) {
 // exp2(z c - R) for the logits of a row, or of a piece of one, R the whole number next to m c, m the largest of them.  With t = 16 z c and n the whole
 // number next to it, which is found by one multiply-add with 1.5 2^52 - 16 R, it is 2^(n / 16 - R) 2^((t - n) / 16): a sixteenth root of 2 from LDS with its
 // exponent, times a polynomial (through 2^(f / 16) at the six zeros of a Chebyshev polynomial, off by 1e-14 at most).  t - n is one multiply-add,
-// and exact: no difference of z and m is rounded, and the 64-bit instructions, which take twice as long as those of 32 bits, are ten
-// (with exp2_wide of (z - m) c they were 17: the sums of 320 rows of 131072 took 45 us).  Below 2^-1000 it is 2^-1000, or 0 where ZERO.
+// and exact: no difference of z and m is rounded, and the 64-bit instructions, which take twice as long as those of 32 bits, are ten (17 with exp2_wide of
+// (z - m) c).  They bound the sums and the draw all the same: 42 million powers of 320 rows of 131072 44 us (46 with 17), where reading the rows takes 12.
+// Sums in 32 bits would take half of it, but not say which token a number draws: a token of the tail has 1e-8 of the whole.
 struct Powers {
     double c, m, c16, magic, unit;            // unit: what makes it exp2((z - m) c)
     float low;                                // the logit whose power is 2^-1000
@@ -321,8 +321,9 @@ template <int TYPE, int DRAFT, int MODE> struct Left {
 };
 
 // One piece of the row that a request's next token is drawn from.  Each workgroup finds for itself how far the drafted tokens are taken; the one that
-// is done last has all parts' weights, and draws.  Bound by the latency of its steps: requests, tokens, sums, logits, weights, and what the last one
-// has to read again, each a read from memory that the one before it names.
+// is done last has all parts' weights, and draws.  Bound by 64-bit instructions where rows are long (64 requests, 131072 logits and the draft's: 39 us, of which the
+// weights 20), else by the latency of its steps: requests, tokens, sums, logits, weights, and what the last one has to read again, each a read
+// from memory that the one before it names (2 requests, 32000 logits: 16 us, of which 4 until it is known how far they are taken, and 6 for choosing a part).
 template <int TYPE, int DRAFT, int MODE, int VEC>
 __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     constexpr int PER = Elem<TYPE>::kPer, kPiece = kRow * VEC;
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     };
     // the weights of a piece's parts: part j * 4 + w are the vectors of wavefront w at j, in the order of the row
     const auto piece_parts = [&](int64_t of, auto put) {
-        // all are asked for before the first is waited for: one after the other, with the next one under way, took 24 us for eight
+        // all are asked for before the first is waited for: eight vectors and the draft's take 44 thousand clocks, 52 with the next one under way only
         typename Left<TYPE, DRAFT, MODE>::Logits v[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) v[j] = left.logits(of * kPiece + j * kRow + threadIdx.x);
