@@ -13,8 +13,7 @@ Plan plan_of(const comet_cache &c, int64_t N, int64_t Q, int64_t B, int64_t M, i
     p.wide = c.size <= 64 ? 64 : c.size <= 128 ? 128 : 256;
     // rows of a workgroup: as many tokens as a request has on average, as far as the registers go
     const int64_t rows = each * G;
-    p.mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    if (p.mt > attend_tiles(c.type, p.wide)) p.mt = attend_tiles(c.type, p.wide);
+    p.mt = rows <= 16 ? 1 : attend_tiles(p.wide);
     p.chunk = (int)(G < 16 * p.mt ? G : 16 * p.mt);
     p.chunks = (int)((G + p.chunk - 1) / p.chunk);
     int64_t tokens = p.chunks > 1 ? 1 : 16 * p.mt / p.chunk;

@@ -66,10 +66,9 @@ template <int TYPE> __device__ __forceinline__ F4 product(U4 a, U4 b, F4 c) {
     }
 }
 
-// Tiles of 16 rows that a wavefront's registers hold, and wavefronts that a SIMD does.
-constexpr int attend_tiles(int type, int wide) { return wide <= 128 ? (type == COMET_F32 ? 2 : 2) : 1; }
-constexpr int attend_waves(int, int, int) { return 4; }
-constexpr int attend_pairs(int type, int wide, int mt) { return wide * mt <= 256 && wide <= 128 ? 2 : 1; }
+// Tiles of 16 rows that a wavefront's registers hold with two wavefronts a SIMD (one where keys are of more than 128 elements).
+constexpr int attend_tiles(int wide) { return wide <= 128 ? 2 : 1; }
+constexpr int kWaves = 4;
 
 // What a workgroup works at.
 struct Item { int tile, head, chunk, split; int64_t id; };
@@ -218,11 +217,11 @@ __device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)"
 __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 template <int TYPE, int DT, int MT>
-__global__ void __launch_bounds__(attend_waves(TYPE, DT, MT) * kWave, attend_pairs(TYPE, DT, MT)) k_attend(AttendArgs a) {
+__global__ void __launch_bounds__(kWaves * kWave, DT <= 128 ? 2 : 1) k_attend(AttendArgs a) {
     using S = Shape<TYPE, DT>;
     using E = Elem<TYPE>;
     using T = typename E::T;
-    constexpr int WAVES = attend_waves(TYPE, DT, MT), THREADS = WAVES * kWave, SIZE = (int)sizeof(T), OT = S::OT, LINE = DT + 4, HALVES = S::HALVES;
+    constexpr int WAVES = kWaves, THREADS = WAVES * kWave, SIZE = (int)sizeof(T), OT = S::OT, LINE = DT + 4, HALVES = S::HALVES;
     extern __shared__ __align__(16) uint32_t raw[];
     __shared__ int64_t buf[WAVES], where[3];
     __shared__ float2 ml[WAVES][16];
@@ -619,7 +618,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
 }
 
 template <int TYPE, int DT, int MT> hipError_t attend_run(const AttendArgs &a, hipStream_t st) {
-    constexpr int WAVES = attend_waves(TYPE, DT, MT);
+    constexpr int WAVES = kWaves;
     const int64_t items = a.tiles * a.heads * a.chunks * a.splits;
     size_t lds = (size_t)WAVES * Shape<TYPE, DT>::STAGE;
     for (const size_t other : {(size_t)WAVES * 16 * (DT + 4) * 4, (size_t)a.words * 8}) lds = other > lds ? other : lds;
@@ -635,9 +634,7 @@ template <int TYPE, int DT, int MT> hipError_t attend_run(const AttendArgs &a, h
 }
 
 template <int TYPE, int DT> hipError_t attend_wide(const AttendArgs &a, int mt, hipStream_t st) {
-    constexpr int MOST = attend_tiles(TYPE, DT);
-    if constexpr (MOST >= 4) if (mt == 4) return attend_run<TYPE, DT, 4>(a, st);
-    if constexpr (MOST >= 2) if (mt == 2) return attend_run<TYPE, DT, 2>(a, st);
+    if constexpr (attend_tiles(DT) >= 2) if (mt == 2) return attend_run<TYPE, DT, 2>(a, st);
     return attend_run<TYPE, DT, 1>(a, st);
 }
 template <int TYPE> hipError_t attend_type(const AttendArgs &a, int wide, int mt, hipStream_t st) {

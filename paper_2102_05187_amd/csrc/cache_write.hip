@@ -117,9 +117,9 @@ template <int TYPE, class I> __device__ __forceinline__ void means(const WriteAr
     }
 }
 
-// The first workgroups take means, of `block` rows and a slice of the columns each, the others copy.  Bound by memory where rows are many (8191 rows of
-// 2 x 2 KB: 16 us, 13 without means, and two copies of half the size 20), by one read after the other where they are few.  Means taken by the
-// workgroups that copy the blocks' last rows, behind the copy, were 26.
+// The first workgroups take means, of `block` rows and a slice of the columns each, the others copy four rows.  Bound by memory where rows are many (8191 rows of
+// 2 x 2 KB: 14 to 16 us, 13 without means, and two copies of half the size 20; a row a workgroup 18), by one read after the other where they are few.  Means
+// taken by the workgroups that copy the blocks' last rows, behind the copy, were 26.
 template <int TYPE, class I>
 __global__ void __launch_bounds__(kWrite) k_cache_write(WriteArgs a, int rows, unsigned slices, unsigned for_means) {
     if (blockIdx.x < for_means) {
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(kWrite) k_cache_write(WriteArgs a, int rows, u
 }
 
 template <int TYPE, class I> hipError_t launch(const WriteArgs &a, hipStream_t st) {
-    const int64_t rows = a.N > 2048 ? 4 : 1, slices = (a.heads * a.per_head + kSlice - 1) / kSlice, for_means = a.mean ? (a.N + a.block - 1) / a.block * slices : 0;
+    const int64_t rows = 4, slices = (a.heads * a.per_head + kSlice - 1) / kSlice, for_means = a.mean ? (a.N + a.block - 1) / a.block * slices : 0;
     hipLaunchKernelGGL((k_cache_write<TYPE, I>), dim3((unsigned)(for_means + (a.N + rows - 1) / rows)), dim3(kWrite), 0, st, a, (int)rows, (unsigned)slices, (unsigned)for_means);
     return hipGetLastError();
 }
