@@ -396,7 +396,9 @@ comet_status comet_beam_reorder(void *const *states, int64_t nstates, int64_t B,
  * b = 0 .. B-1 have length[b] tokens each, and row b of the table [B x M] (rows at b * ldt, ldt >= M) names the block
  * that holds the places j * block .. j * block + block - 1 in its element j.  The tokens of one step are packed: request b has the
  * rows pos[b] .. pos[b+1]-1 (pos: device, [B + 1], from 0 upwards), the newest ones that it has, so that row pos[b] + i is its token at
- * place length[b] - (pos[b+1] - pos[b]) + i.  Rows from pos[B] on belong to no request: results for them are left as they were. */
+ * place length[b] - (pos[b+1] - pos[b]) + i.  Rows from pos[B] on belong to no request: results for them are left as they were.
+ * As above, work is scratch of the bytes that the matching _work call states for the same sizes, no call allocates or synchronises, all can be captured into
+ * a HIP graph, and their errors are those listed there (COMET_ERR_SHAPE also where Q is no multiple of the cache's heads). */
 #define COMET_MAX_BLOCK 1024
 typedef struct comet_cache {
     void *keys, *values;               /* device, element (p, i, h, d) at p * stride[0] + i * stride[1] + h * stride[2] + d */
@@ -434,7 +436,8 @@ comet_status comet_cache_map(int64_t B, int64_t M, int64_t block, const int32_t 
 /* New keys and values into their slots.  Row i of k and v (element (i, h, d) at i * stride[0] + h * stride[1] + d, of the cache's type)
  * goes to slot[i]; a slot outside of [0, blocks * block) is left out.  Where a block's last place is written its mean (if
  * the cache has one) becomes the mean of the keys of all its places, added in 32 bits and rounded once: of those that this call
- * writes in the rows right before with the slots right before, and of what the cache holds for the places before them.
+ * writes in the rows right before with the slots right before, as comet_cache_map lists them (of rows in another order a mean is not defined), and of what
+ * the cache holds for the places before them.
  * No two rows may have the same slot.   N < 2^31. */
 comet_status comet_cache_write(const comet_cache *cache, int64_t N, const void *k, const int64_t k_stride[2], const void *v,
                                const int64_t v_stride[2], const int64_t *slot, void *stream);

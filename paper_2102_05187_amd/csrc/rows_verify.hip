@@ -447,6 +447,7 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     piece_parts(piece, [&](int i, double s) { sums[i] = s; });
     __syncthreads();
     if (threadIdx.x < kMine) __hip_atomic_store(weight + piece * kParts + threadIdx.x, sums[threadIdx.x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();                             // thread 0 makes known what all of them have stored
     if (threadIdx.x == 0) final_one = __hip_atomic_fetch_add(a.arrived + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == a.pieces - 1;
     __syncthreads();
     if (!final_one) return;
