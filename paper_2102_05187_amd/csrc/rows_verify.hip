@@ -257,6 +257,7 @@ template <int TYPE, int DRAFT, int MODE> struct Left {
     Sum p, q;
     Powers of_p, of_q;
     double p_part, q_part;                    // what makes a power a probability; the second one 0 where there is none
+    bool plain;                               // how the powers are computed: both rows' in one way
     bool rejected, largest;                   // something of the draft is taken off; only the largest logit counts
     int64_t d;
     const uint16_t *at;                       // kEntries: 1 + the entry of a place of the piece, 0: none
@@ -284,7 +285,7 @@ template <int TYPE, int DRAFT, int MODE> struct Left {
     }
     // its weights; `in` its number in the piece
     __device__ __forceinline__ void weights(int64_t i, int in, const Logits &v, double *w) const {
-        if (of_p.plain && (MODE != kDense || of_q.plain)) weights_as<true>(i, in, v, w);
+        if (plain) weights_as<true>(i, in, v, w);
         else weights_as<false>(i, in, v, w);
     }
     template <bool PLAIN> __device__ __forceinline__ void weights_as(int64_t i, int in, const Logits &v, double *w) const {
@@ -404,14 +405,15 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
         if (a.length) a.length[b] -= (int32_t)(n - 1 - took);
     }
     Left<TYPE, DRAFT, MODE> left{Row<TYPE>(a.Z, row, a.ldz, a.V), Row<DRAFT>(a.draft, MODE == kDense ? row : 0, a.ldd, a.V), known[0][slot], known[1][slot], Powers(known[0][slot].m, c, root),
-                                 Powers(MODE == kDense && known[1][slot].good() ? known[1][slot].m : 0, c, root), 0, 0,
+                                 Powers(MODE == kDense && known[1][slot].good() ? known[1][slot].m : 0, c, root), 0, 0, false,
                                  took < n - 1 && !largest, largest, took < n - 1 ? a.token[row + 1] : -1, at, chance};
     if (!usable(left.p)) {
         if (piece == 0 && threadIdx.x == 0) a.next[b] = -1;
         return;
     }
-    left.p_part = left.of_p.unit / left.p.s;
-    left.q_part = left.q.good() ? (MODE == kDense ? left.of_q.unit : 1) / left.q.s : 0;
+    left.plain = left.of_p.plain && (MODE != kDense || left.of_q.plain);
+    left.p_part = (left.plain ? left.of_p.unit : 1) / left.p.s;
+    left.q_part = left.q.good() ? (MODE == kDense && left.plain ? left.of_q.unit : 1) / left.q.s : 0;
     // the entries that lie in a piece, by place
     const auto lay_out = [&](int64_t of) {
         if (MODE != kEntries || !left.rejected) return;
