@@ -414,6 +414,8 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     left.plain = left.of_p.plain && (MODE != kDense || left.of_q.plain);
     left.p_part = (left.plain ? left.of_p.unit : 1) / left.p.s;
     left.q_part = left.q.good() ? (MODE == kDense && left.plain ? left.of_q.unit : 1) / left.q.s : 0;
+    // a draft row without probabilities takes nothing off, whatever its logits: 0 times the power of +inf would be a NaN
+    if (MODE != kPoint && !left.q.good()) left.rejected = false;
     // the entries that lie in a piece, by place
     const auto lay_out = [&](int64_t of) {
         if (MODE != kEntries || !left.rejected) return;
