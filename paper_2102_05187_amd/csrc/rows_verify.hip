@@ -46,14 +46,16 @@ template <bool ZERO> __device__ __forceinline__ double exp2_wide(double x) {
 // Sums in 32 bits would take half of it, but not say which token a number draws: a token of the tail has 1e-8 of the whole.
 struct Powers {
     double c, m, c16, magic, unit;            // unit: what makes it exp2((z - m) c)
-    float low;                                // the logit whose power is 2^-1000
-    bool plain;                               // m c is not so large that whole numbers are lost
+    float low;                                // the logit whose power is about 2^-1000: logits are raised to it
+    // m c is below 2^26.  low, which is rounded to 32 bits, is off by half a step then, 2^-24 of its size: four exponents at most, so that its power is
+    // one that 64 bits hold.  At 2^28 it is sixteen, from about 2^29 on the exponent wraps into the sign, and from 2^34 on low can be m itself.
+    bool plain;
     const double *root;                       // LDS, [16]
     __device__ __forceinline__ Powers(double m, double c, const double *root) : c(c), m(m), root(root) {
         const double R = __builtin_rint(m * c);
         c16 = 16 * c, magic = 0x1.8p52 - 16 * R;
         low = (float)((R - 1000) / c);
-        plain = fabs(m * c) < 0x1p40 && c < 0x1p100 && low > kNegInf;
+        plain = fabs(m * c) < 0x1p26 && c < 0x1p100 && low > kNegInf;
         unit = plain ? exp2_wide<false>(__builtin_fma(-m, c, R)) : 1;
     }
     // the scaled root, and the polynomial that goes with it
@@ -523,13 +525,21 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
         // p <= q throughout: p itself is drawn from, first a piece of it, then a part of that
         left.rejected = false;
         __syncthreads();
-        choose(a.pieces, [&](int i) { return onto(a.target[row * a.pieces + i], left.p.m, c) / left.p.s; }, v, 0);
-        of = chosen_part;
+        // pieces whose powers may all be taken as 0, being below 2^-996 of the largest, are left out
+        choose(a.pieces, [&](int i) {
+            const double w = onto(a.target[row * a.pieces + i], left.p.m, c) / left.p.s;
+            return w > 0x1p-900 ? w : 0;
+        }, v, 0);
+        of = chosen_part < 0 ? piece : chosen_part;
         const double goal = goal_ - before_part;
         piece_parts(of, [&](int i, double s) { sums[i] = s; });
         __syncthreads();
         choose(kMine, [&](int i) { return sums[i]; }, -1, goal);
         in = chosen_part;
+    }
+    if (in < 0) {                                // nothing has a weight: no place is read
+        if (threadIdx.x == 0) a.next[b] = -1;
+        return;
     }
     if (of != piece) lay_out(of);
     if (wave != 0) return;
