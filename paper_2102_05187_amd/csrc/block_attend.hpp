@@ -69,6 +69,9 @@ template <int TYPE> __device__ __forceinline__ F4 product(U4 a, U4 b, F4 c) {
 // Tiles of 16 rows that a wavefront's registers hold with two wavefronts a SIMD (one where keys are of more than 128 elements).
 constexpr int attend_tiles(int wide) { return wide <= 128 ? 2 : 1; }
 constexpr int kWaves = 4;
+// Weights are relative to 2^-kRaise of the maximum.  16-bit floats have 15 exponents above 1, which are of no use otherwise: 2^13 is the largest weight
+// then (what rounding a maximum beyond 2^24 to 32 bits adds to that is at most 2^2 below 2^26; a row that comes out infinite is done again by itself).
+template <int TYPE> constexpr float kRaise = TYPE == COMET_F16 ? 5.f : 0.f;
 
 // What a workgroup works at.
 struct Item { int tile, head, chunk, split; int64_t id; };
@@ -419,12 +422,12 @@ __global__ void __launch_bounds__(kWaves * kWave, DT <= 128 ? 2 : 1) k_attend(At
 #pragma unroll
                 for (int r = 1; r < 4 * HALVES; ++r) most = fmaxf(most, z[r]);
                 most *= a.c;
-                // The maximum follows when a score is 256 times over it, and not before: weights are 256 at most, which costs nothing in floating
-                // point, and the output is seldom scaled anew.
-                if (__ballot(most > top[m] + 8.f)) {
+                // The maximum follows when a score is 256 times over it, and not before: weights are 256 at most (above 2^kRaise), which costs nothing in
+                // floating point, and the output is seldom scaled anew.
+                if (__ballot(most > top[m] + (8.f + kRaise<TYPE>))) {
                     most = fmaxf(most, xor16(most));
                     most = fmaxf(most, xor32(most));
-                    const float high = fmaxf(top[m], most), back = high == kNegInf ? 1.f : exp2_fast(top[m] - high);
+                    const float high = fmaxf(top[m], most - kRaise<TYPE>), back = high == kNegInf ? 1.f : exp2_fast(top[m] - high);
                     top[m] = high;
                     sum[m] *= back;
 #pragma unroll
@@ -450,6 +453,25 @@ __global__ void __launch_bounds__(kWaves * kWave, DT <= 128 ? 2 : 1) k_attend(At
                     const U4 p = U4{y.x, y.y, y.z, y.w};
 #pragma unroll
                     for (int c = 0; c < OT; ++c) o[m][c] = product<TYPE>(value[c], p, o[m][c]);
+                    if constexpr (TYPE == COMET_F16) {
+                        // Below 2^-14 these have fewer bits, and what is missing of such weights goes by a product of its own, 2^24 times as large: what is
+                        // taken off in the end is half a step down to 2^-43 of the row's largest weight, and 2^-54 of that below.
+                        constexpr uint32_t kLeast = (127u - 49) << 23, kNormal = (127u - 14) << 23;      // bits of 2^-49, 2^-14
+                        uint32_t least = ~0u;
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            const uint32_t bits = __float_as_uint(z[r]) - kLeast;        // what is below is large
+                            least = bits < least ? bits : least;
+                        }
+                        if (__ballot(least < kNormal - kLeast)) {
+#pragma unroll
+                            for (int r = 0; r < 8; ++r) z[r] = z[r] < 0x1p-14f ? (z[r] - (float)(_Float16)z[r]) * 0x1p24f : 0.f;
+                            const uint4 y = E::narrow(z);
+                            const U4 p = U4{y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int c = 0; c < OT; ++c) o[m][c] = product<TYPE>(value[c], p, o[m][c] * 0x1p24f) * 0x1p-24f;
+                        }
+                    }
                 }
             }
 #pragma unroll
