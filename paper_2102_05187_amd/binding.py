@@ -764,7 +764,7 @@ def _lines(shape, stride, size):
     """Strides of all dimensions but the last, of one that does not count 0, as numbers and as the library reads them; None where they are not what
     its 16-byte loads need."""
     strides = tuple(s if n > 1 else 0 for n, s in zip(shape, stride))
-    if strides[-1] > 1 or any(s * size % 16 for s in strides[:-1]):
+    if (stride[-1] != 1 and shape[-1] > 1) or any(s * size % 16 for s in strides[:-1]):
         return None
     return strides[:-1], (ctypes.c_int64 * (len(shape) - 1))(*strides[:-1])
 
