@@ -438,7 +438,8 @@ comet_status comet_cache_map(int64_t B, int64_t M, int64_t block, const int32_t 
  * the cache has one) becomes the mean of the keys of all its places, added in 32 bits and rounded once: of those that this call
  * writes in the rows right before with the slots right before, as comet_cache_map lists them (of rows in another order a mean is not defined), and of what
  * the cache holds for the places before them.
- * No two rows may have the same slot.   N < 2^31. */
+ * No two rows may have the same slot, and no two elements of the cache lie at the same place (COMET_ERR_INVALID_ARG where the stride of a dimension with more
+ * than one element is below `size`).   N < 2^31. */
 comet_status comet_cache_write(const comet_cache *cache, int64_t N, const void *k, const int64_t k_stride[2], const void *v,
                                const int64_t v_stride[2], const int64_t *slot, void *stream);
 

@@ -769,6 +769,12 @@ def _lines(shape, stride, size):
     return strides[:-1], (ctypes.c_int64 * (len(shape) - 1))(*strides[:-1])
 
 
+@functools.lru_cache(maxsize=1024)
+def _apart(shape, stride):
+    """Whether neighbours in every dimension lie apart."""
+    return all(n <= 1 or s >= shape[-1] for n, s in zip(shape[:-1], stride[:-1]))
+
+
 def _vectors(t: torch.Tensor, what: str, dims: int, dtype=None, device=None):
     """(address, strides, strides as the library reads them) of a tensor whose last dimension's elements lie next to each other."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
@@ -842,6 +848,9 @@ def comet_cache_write(k: torch.Tensor, v: torch.Tensor, K: torch.Tensor, V: torc
     dev = K.device
     cache, kind = _cache(K, V, mean, dev)
     (kptr, _, ks), (vptr, _, vs) = _vectors(k, "k", 3, kind, dev), _vectors(v, "v", 3, kind, dev)
+    for t, what in ((K, "K"), (V, "V"), (mean, "mean")):
+        if t is not None and not _apart(t.shape, t.stride()):
+            raise ValueError("%s is written: its elements must not share memory" % what)
     N, heads, size = k.shape
     if v.shape != k.shape or heads != cache.heads or size != cache.size:
         raise ValueError("k and v must have shape [N, %d, %d]" % (cache.heads, cache.size))

@@ -1,5 +1,6 @@
 // C ABI of the operators over a cache in blocks: argument checks, then the launchers of cache.hpp and rows_kernels.hpp.
 #include <cmath>
+#include <initializer_list>
 
 #include "cache.hpp"
 #include "rows_kernels.hpp"
@@ -48,6 +49,15 @@ comet_status check_cache(const comet_cache *c, bool data, bool mean) {
         if ((mean && c->blocks > 0 && !c->mean) || !aligned(c->mean, 16)) return COMET_ERR_INVALID_ARG;
     }
     return COMET_OK;
+}
+
+// Whether what is written lies apart: neighbours in each dimension of more than one element at least.
+bool apart(const int64_t *stride, std::initializer_list<int64_t> sizes, int64_t length) {
+    for (const int64_t n : sizes) {
+        if (n > 1 && *stride < length) return false;
+        ++stride;
+    }
+    return true;
 }
 
 comet_status check_sizes(const comet_cache *c, int64_t N, int64_t Q, int64_t B, int64_t M, int64_t K, int64_t most) {
@@ -120,6 +130,10 @@ comet_status comet_cache_write(const comet_cache *cache, int64_t N, const void *
     if (s == COMET_OK) s = check_strides(v_stride, 2, cache->type);
     if (s != COMET_OK) return s;
     if (N < 0) return COMET_ERR_INVALID_ARG;
+    if (!apart(cache->key_stride, {cache->blocks, cache->block, cache->heads}, cache->size) ||
+        !apart(cache->value_stride, {cache->blocks, cache->block, cache->heads}, cache->size) ||
+        (cache->mean && !apart(cache->mean_stride, {cache->blocks, cache->heads}, cache->size)))
+        return COMET_ERR_INVALID_ARG;
     // a workgroup for some rows, and for every 512 bytes of a block's mean
     if (N >= kLim || N + (N / cache->block + 1) * (cache->heads * cache->size * element_size(cache->type) / 512 + 1) >= kLim) return COMET_ERR_UNSUPPORTED;
     if (N == 0) return COMET_OK;

@@ -49,3 +49,39 @@ def test_queries_that_share_memory_are_read():
     for a, b in zip(comet.comet_block_attend(q, s["K"], s["V"], s["table"], s["pos"], s["length"], s["sel"]),
                     comet.comet_block_attend(q.contiguous(), s["K"], s["V"], s["table"], s["pos"], s["length"], s["sel"])):
         assert torch.equal(a, b)
+
+
+def test_a_cache_that_is_written_lies_apart():
+    import ctypes
+    from paper_2102_05187_amd import binding, build
+    build.build_if_missing()
+    two, p, invalid = ctypes.c_int64 * 2, ctypes.c_void_p(4096), 1
+
+    def write(ks=(2048, 128, 64), vs=(2048, 128, 64), ms=(128, 64), mean=4096, blocks=10, block=16, heads=2, N=3):
+        c = binding._Cache(4096, 4096, mean, 1, blocks, block, heads, 64)
+        c.key_stride[:], c.value_stride[:], c.mean_stride[:] = ks, vs, ms
+        return binding._lib().comet_cache_write(ctypes.byref(c), N, p, two(128, 64), p, two(128, 64), p, None)
+
+    for kw in (dict(ks=(0, 128, 64)), dict(ks=(2048, 0, 64)), dict(ks=(2048, 128, 0)), dict(ks=(2048, 128, 56)), dict(vs=(0, 128, 64)), dict(vs=(2048, 8, 64)),
+               dict(vs=(2048, 128, 0)), dict(ms=(0, 64)), dict(ms=(128, 0)), dict(ms=(128, 32))):
+        assert write(**kw) == invalid, kw
+    # of one element, or without means: nothing to lie apart
+    assert write(ks=(0, 64, 0), vs=(0, 64, 0), ms=(0, 0), blocks=1, heads=1, N=0) == 0
+    assert write(ms=(0, 0), mean=None, N=0) == 0
+    apart = lambda t: binding._apart(t.shape, t.stride())
+    x = torch.zeros((4, 16, 2, 64))
+    assert apart(x) and apart(x.transpose(1, 2)) and apart(x[..., :8]) and apart(x[:1].expand(1, 16, 2, 64)) and apart(x[:0])
+    assert not apart(x[:1].expand(4, 16, 2, 64)) and not apart(x[:, :1].expand(4, 16, 2, 64)) and not apart(x[:, :, :1].expand(4, 16, 2, 64))
+
+
+@gpu
+@pytest.mark.parametrize("which", ["K", "V", "mean"])
+def test_a_cache_of_one_block_many_times_is_not_written(which):
+    import paper_2102_05187_amd as comet
+    from cache_util import make
+    s = make([2, 3], [100, 90], 2, 2, 64, 16, torch.bfloat16)
+    s["slot"] = torch.arange(5, device="cuda")
+    k, v = (torch.zeros((5, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    s[which] = s[which][:1].expand(s[which].shape)
+    with pytest.raises(ValueError):
+        comet.comet_cache_write(k, v, s["K"], s["V"], s["slot"], s["mean"])
