@@ -115,14 +115,15 @@ typedef double D4 __attribute__((ext_vector_type(4)));
 // of which the matrix instructions are 10, the rest counts and waits; a token at a time, a thread a block, took 159.  16 tokens of 8 heads, up to
 // 512 blocks: 12 us, all of it latency (25 that way).
 template <int TYPE, int WIDE, int TOKENS, int WAVES>
-__global__ void __launch_bounds__(WAVES * kWave) k_select(SelectArgs a) {
+__global__ void __launch_bounds__(WAVES * kWave) k_select(SelectArgs a, uint32_t from) {
     using E = Elem<TYPE>;
     using T = typename E::T;
     constexpr int THREADS = WAVES * kWave, CH = E::kPer, NK = WIDE / (4 * CH);
     extern __shared__ __align__(16) uint64_t keys[];
     __shared__ int64_t buf[WAVES], where[2];
     __shared__ int count[65];
-    const int tile = (int)(blockIdx.x / (unsigned)a.heads), h = (int)(blockIdx.x - (unsigned)tile * a.heads);
+    const uint32_t item = from + blockIdx.x;
+    const int tile = (int)(item / (unsigned)a.heads), h = (int)(item - (unsigned)tile * a.heads);
     const Tile t = find_tile<THREADS>(a.q, a.tokens, tile, buf, where);
     if (t.n == 0) return;
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, col = lane & 15, g = lane >> 4;
@@ -250,8 +251,8 @@ template <int TYPE, int WIDE> hipError_t launch(SelectArgs a, hipStream_t st) {
         const hipError_t e = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * a.heads)), dim3(many ? 256 : 512), lds, st, a);
-    return hipGetLastError();
+    const int threads = many ? 256 : 512;
+    return in_launches(tiles * a.heads, threads, [&](uint32_t from, unsigned n) { hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), lds, st, a, from); });
 }
 template <int TYPE> hipError_t launch(const SelectArgs &a, hipStream_t st) {
     return a.size <= 64 ? launch<TYPE, 64>(a, st) : a.size <= 128 ? launch<TYPE, 128>(a, st) : launch<TYPE, 256>(a, st);

@@ -41,6 +41,18 @@ int64_t block_attend_work(const comet_cache &c, int64_t N, int64_t Q, int64_t B,
 hipError_t block_attend(const comet_cache &c, const Queries &q, const int32_t *sel, int64_t K, double scale, void *out, float *lse, void *work,
                         hipStream_t st);
 
+// ---- many workgroups -------------------------------------------------------------------------------------------------
+// A launch has fewer than 2^32 threads.  More workgroups are enqueued in several, launch(first, count) each: a multiple of 8, so that the eight dies get as many.
+template <class F> hipError_t in_launches(int64_t groups, int threads, F launch) {
+    const int64_t most = (int64_t(1) << 32) / threads - 8;
+    for (int64_t first = 0; first < groups; first += most) {
+        launch((uint32_t)first, (unsigned)(groups - first < most ? groups - first : most));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // ---- sums over a workgroup, in the order of the threads ------------------------------------------------------------
 __device__ __forceinline__ int64_t wave_scan(int64_t x) {
     const int lane = threadIdx.x & (kWave - 1);

@@ -134,8 +134,7 @@ comet_status comet_cache_write(const comet_cache *cache, int64_t N, const void *
         !apart(cache->value_stride, {cache->blocks, cache->block, cache->heads}, cache->size) ||
         (cache->mean && !apart(cache->mean_stride, {cache->blocks, cache->heads}, cache->size)))
         return COMET_ERR_INVALID_ARG;
-    // a workgroup for some rows, and for every 512 bytes of a block's mean
-    if (N >= kLim || N + (N / cache->block + 1) * (cache->heads * cache->size * element_size(cache->type) / 512 + 1) >= kLim) return COMET_ERR_UNSUPPORTED;
+    if (N >= kLim) return COMET_ERR_UNSUPPORTED;
     if (N == 0) return COMET_OK;
     if (!k || !v || !slot || !aligned(k, 16) || !aligned(v, 16) || !aligned(slot, 8)) return COMET_ERR_INVALID_ARG;
     return done(comet::cache_write(*cache, N, k, k_stride, v, v_stride, slot, (hipStream_t)stream));

@@ -121,20 +121,28 @@ template <int TYPE, class I> __device__ __forceinline__ void means(const WriteAr
 // 2 x 2 KB: 14 to 16 us, 13 without means, and two copies of half the size 20; a row a workgroup 18), by one read after the other where they are few.  Means
 // taken by the workgroups that copy the blocks' last rows, behind the copy, were 26.
 template <int TYPE, class I>
-__global__ void __launch_bounds__(kWrite) k_cache_write(WriteArgs a, int rows, unsigned slices, unsigned for_means) {
+__global__ void __launch_bounds__(kWrite) k_cache_write(WriteArgs a, int64_t from, int rows, unsigned slices, unsigned for_means) {
     if (blockIdx.x < for_means) {
-        const int64_t i0 = (int64_t)(blockIdx.x / slices) * a.block;
+        const int64_t i0 = from + (int64_t)(blockIdx.x / slices) * a.block;
         means<TYPE, I>(a, i0, (int)(a.N - i0 < a.block ? a.N - i0 : a.block), (int)(blockIdx.x % slices) * kSlice);
     } else {
-        const int64_t i0 = (int64_t)(blockIdx.x - for_means) * rows;
+        const int64_t i0 = from + (int64_t)(blockIdx.x - for_means) * rows;
         copy_rows<I>(a, i0, (int)(a.N - i0 < rows ? a.N - i0 : rows));
     }
 }
 
 template <int TYPE, class I> hipError_t launch(const WriteArgs &a, hipStream_t st) {
-    const int64_t rows = 4, slices = (a.heads * a.per_head + kSlice - 1) / kSlice, for_means = a.mean ? (a.N + a.block - 1) / a.block * slices : 0;
-    hipLaunchKernelGGL((k_cache_write<TYPE, I>), dim3((unsigned)(for_means + (a.N + rows - 1) / rows)), dim3(kWrite), 0, st, a, (int)rows, (unsigned)slices, (unsigned)for_means);
-    return hipGetLastError();
+    const int64_t rows = 4, slices = (a.heads * a.per_head + kSlice - 1) / kSlice;
+    // as many rows, of whole blocks' number, as a launch has threads for: fewer than 2^32
+    const int64_t most = ((int64_t(1) << 32) / kWrite - 1) / (a.block / rows + slices) * a.block;
+    for (int64_t from = 0; from < a.N; from += most) {
+        const int64_t n = a.N - from < most ? a.N - from : most, for_means = a.mean ? (n + a.block - 1) / a.block * slices : 0;
+        hipLaunchKernelGGL((k_cache_write<TYPE, I>), dim3((unsigned)(for_means + (n + rows - 1) / rows)), dim3(kWrite), 0, st, a, from, (int)rows, (unsigned)slices,
+                           (unsigned)for_means);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 template <int TYPE> hipError_t launch(const WriteArgs &a, hipStream_t st) {
     return a.slots < (int64_t(1) << 31) ? launch<TYPE, uint32_t>(a, st) : launch<TYPE, int64_t>(a, st);

@@ -236,10 +236,11 @@ __device__ __forceinline__ void piece_sum(const void *base, int64_t row, int64_t
 
 // Sums of all pieces of all rows that are judged by or drawn from.
 template <int TYPE, int DRAFT, int VEC>
-__global__ void __launch_bounds__(kRow) k_verify_sums(VerifyArgs a) {
+__global__ void __launch_bounds__(kRow) k_verify_sums(VerifyArgs a, uint32_t from) {
     __shared__ int count;
-    const int all = a.pieces + a.draft_pieces, row = (int)(blockIdx.x / (unsigned)all);
-    int piece = (int)blockIdx.x - row * all;
+    const uint32_t item = from + blockIdx.x, all = a.pieces + a.draft_pieces;
+    const int row = (int)(item / all);
+    int piece = (int)(item - row * all);
     for (int64_t b = (int64_t)blockIdx.x * kRow + threadIdx.x; b < a.B; b += (int64_t)gridDim.x * kRow) a.arrived[b] = 0;
     const int64_t b = a.request(row, &count);
     if (b < 0) return;
@@ -328,7 +329,7 @@ template <int TYPE, int DRAFT, int MODE> struct Left {
 // weights 20), else by the latency of its steps: requests, tokens, sums, logits, weights, and what the last one has to read again, each a read
 // from memory that the one before it names (2 requests, 32000 logits: 16 us, of which 4 until it is known how far they are taken, and 6 for choosing a part).
 template <int TYPE, int DRAFT, int MODE, int VEC>
-__global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
+__global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a, uint32_t from) {
     constexpr int PER = Elem<TYPE>::kPer, kPiece = kRow * VEC;
     constexpr int kMine = VEC * kWavesRow;       // a part for each wavefront's vectors next to each other
     static_assert(kMine <= kParts && kMine <= kWave, "one wavefront writes them");
@@ -338,7 +339,8 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
     __shared__ uint16_t at[MODE == kEntries ? kPiece * PER : 1];
     make_roots(root);
     __shared__ Sum known[2][kRow / 8];
-    const int b = (int)(blockIdx.x / (unsigned)a.pieces), piece = (int)blockIdx.x - b * a.pieces;
+    const uint32_t item = from + blockIdx.x;
+    const int b = (int)(item / (unsigned)a.pieces), piece = (int)(item - (uint32_t)b * a.pieces);
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     const int64_t r0 = a.pos[b], n = (a.pos[b + 1] < a.N ? a.pos[b + 1] : a.N) - r0;
     if (n <= 0 || r0 < 0) {
@@ -572,13 +574,13 @@ __global__ void __launch_bounds__(kRow) k_verify_draw(VerifyArgs a) {
 }
 
 template <int TYPE, int DRAFT, int MODE, int VEC> hipError_t launch(const VerifyArgs &a, hipStream_t st) {
-    if (a.N > 0) {
-        hipLaunchKernelGGL((k_verify_sums<TYPE, DRAFT, VEC>), dim3((unsigned)(a.N * (a.pieces + a.draft_pieces))), dim3(kRow), 0, st, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    hipLaunchKernelGGL((k_verify_draw<TYPE, DRAFT, MODE, VEC>), dim3((unsigned)(a.B * a.pieces)), dim3(kRow), 0, st, a);
-    return hipGetLastError();
+    const hipError_t e = in_launches(a.N * (a.pieces + a.draft_pieces), kRow, [&](uint32_t from, unsigned n) {
+        hipLaunchKernelGGL((k_verify_sums<TYPE, DRAFT, VEC>), dim3(n), dim3(kRow), 0, st, a, from);
+    });
+    if (e != hipSuccess) return e;
+    return in_launches(a.B * a.pieces, kRow, [&](uint32_t from, unsigned n) {
+        hipLaunchKernelGGL((k_verify_draw<TYPE, DRAFT, MODE, VEC>), dim3(n), dim3(kRow), 0, st, a, from);
+    });
 }
 template <int TYPE, int VEC> hipError_t launch(const VerifyArgs &a, int draft_type, hipStream_t st) {
     if (a.draft) {
