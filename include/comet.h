@@ -448,10 +448,13 @@ comet_status comet_cache_write(const comet_cache *cache, int64_t N, const void *
  * token and h, K of them are chosen, or all where there are no more: the first `first`, the last `last` (its own block is
  * the very last), and of the others those with the largest score
  *     s_j = sum over the G heads and d of q[n, x, d] * mean[table[b, j], h, d],
- * of equal ones the lower j; NaN comes last.  Scores are computed and compared in 64 bits: the choice is that of the exact numbers.
+ * of equal ones the lower j; NaN comes last.  Scores are computed and compared in 64 bits, in an order of additions that is not the same for few tokens and for
+ * many: they are off by (size + G) * 2^-53 times the sum of the products' sizes at most, and blocks whose exact scores lie closer together than that may be
+ * taken for each other.  Blocks with the same mean have the same score.
  *   sel        device, [N x heads x K]: the chosen j, ascending, and -1 behind them.
  *   first >= 0, last >= 1, first + last <= K <= COMET_MAX_CHOSEN, M <= COMET_MAX_CANDIDATES.
- * A block whose number in the table is outside of [0, blocks) has the score NaN. */
+ * A block whose number in the table is outside of [0, blocks) has the score NaN.  Tokens are scored together where M is 1024 at most, and time and LDS go by M,
+ * not by what the tokens see: a wide table is best handed over with M cut to the longest request and its own ldt. */
 #define COMET_MAX_CHOSEN 1024
 #define COMET_MAX_CANDIDATES 16384
 comet_status comet_block_select_work(const comet_cache *cache, int64_t N, int64_t Q, int64_t B, int64_t M, int64_t K, int64_t *bytes /* host */);
@@ -464,8 +467,9 @@ comet_status comet_block_select(const comet_cache *cache, int64_t N, int64_t Q, 
  * a number outside of [0, M), a block behind the token's own and one whose number in the table is outside of [0, blocks) are none.
  *   out        device, [N x Q x size] without gaps, of the cache's type, 16-byte aligned.
  *   lse        device, [N x Q], or NULL: ln sum exp(scale * (q . key)).
- * A token that has no place to read gets out 0 and lse -inf.  What a token does not read does not reach it, NaN included.
- *   M <= COMET_MAX_TABLE. */
+ * A token that has no place to read gets out 0 and lse -inf.  What a token does not read does not reach it, NaN included.  Weights of 16-bit types are rounded to
+ * the type before they meet the values; scores, weights' sums and outputs are held in 32 bits.
+ *   scale > 0 and finite, also as a float and times log2 e (COMET_ERR_INVALID_ARG).  M <= COMET_MAX_TABLE. */
 #define COMET_MAX_TABLE 262144
 comet_status comet_block_attend_work(const comet_cache *cache, int64_t N, int64_t Q, int64_t B, int64_t M, int64_t K, int64_t *bytes /* host */);
 comet_status comet_block_attend(const comet_cache *cache, int64_t N, int64_t Q, const void *q, const int64_t q_stride[2], int64_t B,
@@ -477,6 +481,8 @@ comet_status comet_block_attend(const comet_cache *cache, int64_t N, int64_t Q, 
  * d = token[r+1].  With p = softmax(scale z_r) and q the distribution that d was drawn from, d is taken where u_r q_d < p_d.  At the
  * first that is not, the next token is drawn from what is left of p, max(p - q, 0); where all are taken, from p of the
  * last row: the first j whose running sum of these weights is larger than v_b times their sum.  So the tokens are distributed as p.
+ * All rows of a request but the last are judges: in a step that reads prompts too they would judge the prompts' tokens.  Such a step hands over the rows of
+ * the drafts, and each prompt's last one, with a pos of their own.
  *   draft      device, rows of type draft_type and length V at r * ldd: q = softmax(scale draft_r).  Or NULL, and then
  *   crd, vals  device, [N x K] coordinates (distinct in a row) and logits: q = softmax(scale vals) over a row's entries, 0 elsewhere; an
  *              entry whose coordinate is outside of [0, V) is none.  With K = 0: q is 1 at d (the draft was no draw).

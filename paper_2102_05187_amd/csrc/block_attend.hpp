@@ -11,7 +11,8 @@
 //
 // Bound by memory where tokens are single (64 tokens, 8 heads, 2048 places each, 537 MB: 92 us, 5.9 TB/s; the same loads alone 6.6 to 7.0), by the dies'
 // caches where they are neighbours (4093 tokens, 4 heads, 1024 places each: 310 us, 222 TFLOP/s; keys and values are read by every fourth
-// token, 5.8 GB, at 19 TB/s of 31).  More tokens a workgroup would read less, but leave registers for one wavefront a SIMD: 547 us with eight.
+// token, 5.8 GB, at 19 TB/s of 31).  Every wavefront holds all of the workgroup's rows.  Four tiles of them in a wavefront would read less, but leave registers for
+// one wavefront a SIMD: 547 us with eight tokens.  Rows spread over the wavefronts, all of which would read one tile of keys, have not been measured.
 #pragma once
 
 #include "cache.hpp"
@@ -50,7 +51,7 @@ template <int TYPE, int DT> struct Shape {
     static constexpr int CHUNKS = DT / CH;                     // 16-byte pieces of a key
     static constexpr int NK = CHUNKS / 4;                      // of them in a lane: piece 4 kk + lane / 16
     static constexpr int TURN = CHUNKS < 16 ? 1 : 0;
-    static constexpr int LINE = CHUNKS * 16, ROWS = kWave / CHUNKS > 0 ? kWave / CHUNKS : 1;      // bytes of a key; keys of one load
+    static constexpr int LINE = CHUNKS * 16;                   // bytes of a key
     static constexpr int LOADS = HALVES * 16 * CHUNKS / kWave; // loads of a step's keys
     static constexpr int STAGE = 2 * HALVES * 16 * LINE;       // bytes of LDS for a step's keys and values
     static constexpr int OT = DT / 16;                         // tiles of 16 elements of the output

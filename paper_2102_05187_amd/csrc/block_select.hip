@@ -108,8 +108,9 @@ template <int T> __device__ __forceinline__ void choose_all(const uint64_t *key,
 
 typedef double D4 __attribute__((ext_vector_type(4)));
 
-// One workgroup a head and TOKENS tokens of a request that follow each other.  Scores in 64 bits: products of 16-bit elements are exact there, and a sum
-// of a few hundred of them is off by 1e-14, so that it is the exact scores' order that decides.  Sixteen blocks at a time, a lane a block and a quarter
+// One workgroup a head and TOKENS tokens of a request that follow each other.  Scores in 64 bits: off by (size + G) 2^-53
+// times the sum of the products' sizes at most (products of 16-bit elements are exact), so that the exact scores' order decides but for blocks that are closer; the
+// lanes and the matrix instructions add in different orders.  Sixteen blocks at a time, a lane a block and a quarter
 // of its 16-byte pieces: the fragment of a 64-bit matrix instruction whose columns are 16 tokens' sums over their heads; a single token's
 // products are added up by the lanes themselves, which is less work than columns that are not used.  4093 tokens of 4 heads, contexts of up to 256 blocks: 43 us,
 // of which the matrix instructions are 10, the rest counts and waits; a token at a time, a thread a block, took 159.  16 tokens of 8 heads, up to
@@ -241,6 +242,7 @@ template <int TYPE, int WIDE> hipError_t launch(SelectArgs a, hipStream_t st) {
     // Tokens share their blocks' means where requests have four of them or more, and a wavefront's registers hold a token's candidates.  64 requests of 3, 4, 8
     // and 16 tokens, 4 heads, up to 250 blocks: 16.7, 16.8, 19.3 and 25.7 us together, 16.5, 18.2, 32.3 and 60.2 one by one.
     const int64_t B = a.q.B < a.q.N ? a.q.B : a.q.N, each = (a.q.N + B - 1) / B;
+    // Where the table has more columns than a wavefront holds, every token goes by itself, however few blocks it sees.
     const bool many = each >= 4 && a.q.M <= kHeld * kWave;
     const auto kernel = many ? k_select<TYPE, WIDE, 16, 4> : k_select<TYPE, WIDE, 1, 8>;
     a.tokens = many ? 16 : 1;

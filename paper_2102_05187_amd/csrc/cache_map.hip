@@ -19,15 +19,7 @@ __device__ __forceinline__ int64_t within(int64_t x, int64_t hi) { return x < 0 
 
 // Two running sums over the workgroup at once, in 32 bits (data-parallel moves) or 64: x and y become the sums up to and with each thread's, all_x and
 // all_y those of all.  buf is used in turn, so that one barrier is enough.
-__device__ __forceinline__ int32_t wave_upto(int32_t x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-    return x;
-}
+__device__ __forceinline__ int32_t wave_upto(int32_t x) { return lanes_scan(x); }
 __device__ __forceinline__ int64_t wave_upto(int64_t x) { return wave_scan(x); }
 template <class I, int T> struct Sums {
     I (*buf)[2][T / kWave];
