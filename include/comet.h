@@ -467,8 +467,8 @@ comet_status comet_block_select(const comet_cache *cache, int64_t N, int64_t Q, 
  * a number outside of [0, M), a block behind the token's own and one whose number in the table is outside of [0, blocks) are none.
  *   out        device, [N x Q x size] without gaps, of the cache's type, 16-byte aligned.
  *   lse        device, [N x Q], or NULL: ln sum exp(scale * (q . key)).
- * A token that has no place to read gets out 0 and lse -inf.  What a token does not read does not reach it, NaN included.  Weights of 16-bit types are rounded to
- * the type before they meet the values; scores, weights' sums and outputs are held in 32 bits.
+ * A token that has no place to read gets out 0 and lse -inf.  What a token does not read does not reach it, NaN included.  Weights meet 16-bit values
+ * as the sum of two numbers of their type (2^-16 of a weight is lost with bfloat16); scores, weights' sums and outputs are held in 32 bits, and outputs rounded once.
  *   scale > 0 and finite, also as a float and times log2 e (COMET_ERR_INVALID_ARG).  M <= COMET_MAX_TABLE. */
 #define COMET_MAX_TABLE 262144
 comet_status comet_block_attend_work(const comet_cache *cache, int64_t N, int64_t Q, int64_t B, int64_t M, int64_t K, int64_t *bytes /* host */);

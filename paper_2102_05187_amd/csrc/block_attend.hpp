@@ -10,7 +10,7 @@
 // how the second one wants P, and no element has to move.  V^T's fragments come from LDS, which turns 16-bit elements around as it is read.
 //
 // Bound by memory where tokens are single (64 tokens, 8 heads, 2048 places each, 537 MB: 92 us, 5.9 TB/s; the same loads alone 6.6 to 7.0), by the dies'
-// caches where they are neighbours (4093 tokens, 4 heads, 1024 places each: 310 us, 222 TFLOP/s; keys and values are read by every fourth
+// caches where they are neighbours (4093 tokens, 4 heads, 1024 places each: 318 us, 216 TFLOP/s; keys and values are read by every fourth
 // token, 5.8 GB, at 19 TB/s of 31).  Every wavefront holds all of the workgroup's rows.  Four tiles of them in a wavefront would read less, but leave registers for
 // one wavefront a SIMD: 547 us with eight tokens.  Rows spread over the wavefronts, all of which would read one tile of keys, have not been measured.
 #pragma once
@@ -449,14 +449,25 @@ __global__ void __launch_bounds__(kWaves * kWave, DT <= 128 ? 2 : 1) k_attend(At
                         for (int c = 0; c < OT; ++c)
                             o[m][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(value[r * (OT / 4) + c / 4][c & 3]), z[r], o[m][c], 0, 0, 0);
                 } else {
-                    // Weights are rounded to the type: half a step each, of as many that their errors cancel; a product in 32 bits would take 16 times as long.
+                    // Weights are rounded to the type, and what that takes off goes by a second product: 2^-16 of a weight is lost (bfloat16), 2^-22 and 2^-30 of the
+                    // row's largest (16-bit float).  With the first one alone results are off by 0.0022 of their size for 0.0017, all of which is their own
+                    // rounding; 4093 tokens take 307 us for 318, 64 single ones 92 for 92.  A product in 32 bits would take 16 times as long.
                     const uint4 y = E::narrow(z);
                     const U4 p = U4{y.x, y.y, y.z, y.w};
+                    float rest[8];
+                    E::widen(y, rest);
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) rest[r] = z[r] - rest[r];
+                    const uint4 y2 = E::narrow(rest);
+                    const U4 p2 = U4{y2.x, y2.y, y2.z, y2.w};
 #pragma unroll
                     for (int c = 0; c < OT; ++c) o[m][c] = product<TYPE>(value[c], p, o[m][c]);
+#pragma unroll
+                    for (int c = 0; c < OT; ++c) o[m][c] = product<TYPE>(value[c], p2, o[m][c]);
                     if constexpr (TYPE == COMET_F16) {
-                        // Below 2^-14 these have fewer bits, and what is missing of such weights goes by a product of its own, 2^24 times as large: what is
-                        // taken off in the end is half a step down to 2^-43 of the row's largest weight, and 2^-54 of that below.  4093 tokens: 315 us for 308.
+                        // Both together do not hold a weight below 2^-14 to half a step, and none below 2^-25.  What is missing of these goes by a third product, 2^24 times
+                        // as large: half a step is lost down to 2^-43 of the row's largest weight, and 2^-54 of that below.  4093 tokens, some of whose
+                        // weights are such: 325 us for 318.
                         constexpr uint32_t kLeast = (127u - 49) << 23, kNormal = (127u - 14) << 23;      // bits of 2^-49, 2^-14
                         uint32_t least = ~0u;
 #pragma unroll
